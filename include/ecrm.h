@@ -222,6 +222,75 @@ int ecrm_recovery_state(ecrm_ctx *ctx, void *hip_stream, uint32_t *active, uint3
 int ecrm_recovery_read(ecrm_ctx *ctx, const uint64_t *keys, uint64_t n, float *out_E, float *out_A,
                        void *hip_stream);
 
+/* Training a model on the table: the tokens of a batch are looked up in the activations' type, and the gradient of the
+ * looked-up rows comes back as one fp32 gradient for each distinct token, which ecrm_update takes.
+ *
+ * ecrm_embed            out[i][0..D) = scale * entry keys[i], rounded to `type`; a row of zeros where keys[i] == padding.  The
+ *                       product is formed in fp32 first.  `stride` elements lie between rows of out.  `lost_server`: as in
+ *                       ecrm_degraded_read, whose semantics this call has also during a recovery (waiting updates are not
+ *                       seen); its rows are decoded, rounded to fp32, then scaled.  Keys >= rows other than the padding raise
+ *                       the sticky EKEYRANGE status and leave their rows unwritten.  Any n.
+ * ecrm_embed_grad       d_out[i][0..D): gradient of the row that ecrm_embed gave for keys[i], `stride` elements between rows.
+ *                       out_keys[0..u) receives the u distinct keys of the batch in ascending order, out_grads[j][0..D) =
+ *                       scale * (sum of d_out[i] over the i with keys[i] == out_keys[j]), and *count = u.  The padding key
+ *                       counts for nothing, whatever its rows of d_out hold.  out_keys and out_grads have room for n;
+ *                       out_keys[u..n) receives ECRM_NO_KEY, the rows of out_grads behind u are left alone.  Sums are carried
+ *                       in fp64 in an order that follows from the keys alone, and rounded once.  A batch with a key >= rows
+ *                       other than the padding is rejected: sticky EKEYRANGE, *count = 0, every out_keys ECRM_NO_KEY,
+ *                       out_grads left alone.  n = 0 gives *count = 0.
+ * ecrm_embed_grad_dense the same sums as a table dE[R][D] of its own: with accumulate = 0 rows without a token become zero, with
+ *                       accumulate = 1 the sums are added to dE (one rounding) and other rows are left alone.  A rejected batch
+ *                       leaves dE alone.
+ *
+ * d_out and out: device memory aligned to four elements, stride >= D and a multiple of 4; out_grads and dE: 16 bytes; count:
+ * 8 bytes, memory the device can write.  padding: any value, a row of the table or not (-1, -100); ECRM_NO_PADDING (2^63):
+ * there is none.  scale has to be finite.  The
+ * gradient calls use the scratch buffer (call them on the update stream; n <= max_batch, else EBATCH) but no table, and leave
+ * what ecrm_batch_stats reports; the lookup uses none.  All only enqueue. */
+enum { ECRM_F32 = 0, ECRM_BF16 = 1, ECRM_F16 = 2 };
+#define ECRM_NO_KEY 0xFFFFFFFFFFFFFFFFull
+#define ECRM_NO_PADDING 0x8000000000000000ull
+int ecrm_embed(ecrm_ctx *ctx, const uint64_t *keys, uint64_t n, uint64_t padding, float scale, uint32_t lost_server,
+               void *out, uint32_t type, uint64_t stride, void *hip_stream);
+int ecrm_embed_grad(ecrm_ctx *ctx, const uint64_t *keys, const void *d_out, uint32_t type, uint64_t stride, uint64_t n,
+                    uint64_t padding, float scale, uint64_t *out_keys, float *out_grads, uint64_t *count, void *hip_stream);
+int ecrm_embed_grad_dense(ecrm_ctx *ctx, const uint64_t *keys, const void *d_out, uint32_t type, uint64_t stride, uint64_t n,
+                          uint64_t padding, float scale, float *dE, int accumulate, void *hip_stream);
+
+/* The global norm of a step's gradients and clipping, over a list of tensors of any sizes and of mixed types.  Needs no
+ * ecrm_ctx: the list may hold the gradients of a model beside the rows of ecrm_embed_grad.
+ *
+ * ecrm_grads_create  copies the list into a host-side handle (destroy it with ecrm_grads_destroy; NULL is allowed).  Tensors are
+ *                    contiguous device memory aligned to their element.  rows != NULL: only the first *rows * row_elements
+ *                    elements are there, *rows read on the device when a call runs (the count of ecrm_embed_grad); elements is
+ *                    then what there is room for, a multiple of row_elements.  EINVAL for a bad tensor.
+ * ecrm_grads_bytes   size of the device memory that ecrm_grads_bind needs.
+ * ecrm_grads_bind    hands it over (256-byte aligned, else ESCRATCH) and enqueues the writing of the list into it.  It is
+ *                    private to the library while bound, and used by every call on the handle: calls that overlap in time race;
+ *                    order them, and the streams they are on, as for a context.
+ * ecrm_grads_norm    *norm (device) = square root of the sum of the squares of all elements, summed in fp64 in an order that
+ *                    follows from the list alone, rounded once.  Not finite if an element is not, or the norm is beyond fp32.
+ * ecrm_grads_clip    out[t][e] = list[t][e] * min(1, max_norm / (*norm + 1e-6)), rounded to the type of out[t]; out = NULL:
+ *                    in place, where nothing is written when the factor is 1.  *norm is read on the device: what
+ *                    ecrm_grads_norm left, or what a job of several devices made of theirs.  An infinite norm gives the factor 0,
+ *                    one that is not a number a factor that is none.  out: a bound list of as many tensors with as many elements
+ *                    each (its rows are not looked at); a tensor of out is the list's own memory, of the same type, or overlaps
+ *                    none of it.  max_norm has to be finite and not negative. */
+typedef struct {
+    void *data;
+    uint64_t elements;
+    const uint64_t *rows;
+    uint32_t row_elements;
+    uint32_t type; /* ECRM_F32, ECRM_BF16, ECRM_F16 */
+} ecrm_tensor;
+typedef struct ecrm_grads ecrm_grads;
+int ecrm_grads_create(const ecrm_tensor *tensors, uint32_t count, ecrm_grads **out);
+void ecrm_grads_destroy(ecrm_grads *grads);
+size_t ecrm_grads_bytes(const ecrm_grads *grads);
+int ecrm_grads_bind(ecrm_grads *grads, void *table, size_t table_bytes, void *hip_stream);
+int ecrm_grads_norm(ecrm_grads *grads, float *norm, void *hip_stream);
+int ecrm_grads_clip(ecrm_grads *grads, const ecrm_grads *out, const float *norm, float max_norm, void *hip_stream);
+
 /* Waits for the stream, then returns ECRM_OK, or EKEYRANGE if any batch since the last
  * ecrm_clear_status (or bind) carried a bad key, EBUFFER if one overflowed the recovery buffer, or
  * EHIP if the runtime reports an error. */

@@ -22,13 +22,20 @@ SYMBOLS = ["ecrm_create", "ecrm_destroy", "ecrm_data_bytes", "ecrm_parity_bytes"
            "ecrm_tune", "ecrm_probe_row_traffic", "ecrm_profile", "ecrm_profile_read", "ecrm_batch_stats", "ecrm_host_placement", "ecrm_strerror",
            "ecrm_fail_server", "ecrm_recover_server", "ecrm_degraded_read",
            "ecrm_recovery_begin", "ecrm_recovery_lock", "ecrm_recovery_decode", "ecrm_recovery_unlock",
-           "ecrm_recovery_state", "ecrm_recovery_read"]
+           "ecrm_recovery_state", "ecrm_recovery_read",
+           "ecrm_embed", "ecrm_embed_grad", "ecrm_embed_grad_dense",
+           "ecrm_grads_create", "ecrm_grads_destroy", "ecrm_grads_bytes", "ecrm_grads_bind", "ecrm_grads_norm", "ecrm_grads_clip"]
 
 
 class EcrmConfig(C.Structure):
     _fields_ = [("rows", C.c_uint64), ("dim", C.c_uint32), ("k", C.c_uint32), ("servers", C.c_uint32),
                 ("optimizer", C.c_uint32), ("lr", C.c_float), ("eps", C.c_float), ("max_batch", C.c_uint64),
                 ("momentum", C.c_float), ("combine", C.c_uint32), ("propagation", C.c_uint32)]
+
+
+class EcrmTensor(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("elements", C.c_uint64), ("rows", C.c_void_p), ("row_elements", C.c_uint32),
+                ("type", C.c_uint32)]
 
 
 class EcrmError(RuntimeError):
@@ -79,6 +86,18 @@ def load_library():
         lib.ecrm_batch_stats.argtypes = [vp, vp, C.POINTER(C.c_uint64)]
         lib.ecrm_host_placement.argtypes = [vp, C.c_uint64, C.c_uint32, C.c_uint32, C.c_uint32, C.c_uint32,
                                             C.POINTER(C.c_uint32)]
+        u64, u32, f32 = C.c_uint64, C.c_uint32, C.c_float
+        lib.ecrm_embed.argtypes = [vp, u64p, u64, u64, f32, u32, vp, u32, u64, vp]
+        lib.ecrm_embed_grad.argtypes = [vp, u64p, vp, u32, u64, u64, u64, f32, u64p, f32p, u64p, vp]
+        lib.ecrm_embed_grad_dense.argtypes = [vp, u64p, vp, u32, u64, u64, u64, f32, f32p, C.c_int, vp]
+        lib.ecrm_grads_create.argtypes = [C.POINTER(EcrmTensor), u32, C.POINTER(C.c_void_p)]
+        lib.ecrm_grads_destroy.argtypes = [vp]
+        lib.ecrm_grads_destroy.restype = None
+        lib.ecrm_grads_bytes.argtypes = [vp]
+        lib.ecrm_grads_bytes.restype = C.c_size_t
+        lib.ecrm_grads_bind.argtypes = [vp, vp, C.c_size_t, vp]
+        lib.ecrm_grads_norm.argtypes = [vp, f32p, vp]
+        lib.ecrm_grads_clip.argtypes = [vp, vp, f32p, f32, vp]
         lib.ecrm_strerror.argtypes = [C.c_int]
         lib.ecrm_strerror.restype = C.c_char_p
         _lib = lib
@@ -106,6 +125,84 @@ def probe_row_traffic(table_a, table_b, table_rows, rows, write, sink, stream=No
                                                _stream(stream))
     if rc != ECRM_OK:
         raise EcrmError(rc, "ecrm_probe_row_traffic")
+
+
+_NO_PADDING = 1 << 63
+_types = {}
+
+
+def _type(t):
+    """ECRM_F32, ECRM_BF16 or ECRM_F16 of a tensor."""
+    if not _types:
+        import torch
+        _types.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    return _types[t.dtype]
+
+
+def _key(padding):
+    """A padding token as the library takes it: negative ones as the unsigned value with the same bits."""
+    return _NO_PADDING if padding is None else padding & 0xFFFFFFFFFFFFFFFF
+
+
+def _row(t):
+    """Elements from one row to the next; of a single row torch may say anything."""
+    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 4) * 4
+
+
+class Grads:
+    """A list of gradient tensors: their global norm, and clipping (ecrm_grads_<name>).  An item is a contiguous tensor, or a
+    pair (rows of a gradient [n, D], device tensor with the number of rows that count).  The tensors are kept alive, and
+    have to stay where they are; make a new list when they move."""
+
+    def __init__(self, tensors, stream=None):
+        import torch
+        self._lib = load_library()
+        self._grads = C.c_void_p(0)
+        items = [t if isinstance(t, (tuple, list)) else (t, None) for t in tensors]
+        assert items, "a list of at least one tensor"
+        table = (EcrmTensor * len(items))()
+        for to, (t, rows) in zip(table, items):
+            assert t.is_cuda and t.is_contiguous()
+            to.data, to.elements, to.type = t.data_ptr(), t.numel(), _type(t)
+            if rows is not None:
+                assert rows.is_cuda and rows.dtype in (torch.int64, torch.uint64) and rows.numel() == 1 and t.dim() == 2
+                to.rows, to.row_elements = rows.data_ptr(), t.shape[1]
+        rc = self._lib.ecrm_grads_create(table, C.c_uint32(len(items)), C.byref(self._grads))
+        if rc != ECRM_OK:
+            raise EcrmError(rc, "ecrm_grads_create")
+        size = self._lib.ecrm_grads_bytes(self._grads)
+        self._keep = (items, torch.empty(size, dtype=torch.uint8, device=items[0][0].device))
+        rc = self._lib.ecrm_grads_bind(self._grads, _ptr(self._keep[1]), C.c_size_t(size), _stream(stream))
+        if rc != ECRM_OK:
+            raise EcrmError(rc, "ecrm_grads_bind")
+
+    def destroy(self):
+        if self._grads:
+            self._lib.ecrm_grads_destroy(self._grads)
+            self._grads = C.c_void_p(0)
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+    def norm(self, norm, stream=None, check=True):
+        """norm: device tensor of one fp32 value."""
+        assert norm.is_cuda and norm.dtype.is_floating_point and norm.element_size() == 4 and norm.numel() == 1
+        rc = self._lib.ecrm_grads_norm(self._grads, _ptr(norm), _stream(stream))
+        if check and rc != ECRM_OK:
+            raise EcrmError(rc, "ecrm_grads_norm")
+        return rc
+
+    def clip(self, norm, max_norm, out=None, stream=None, check=True):
+        """In place, or into the tensors of `out`, another list."""
+        assert norm.is_cuda and norm.dtype.is_floating_point and norm.element_size() == 4 and norm.numel() == 1
+        rc = self._lib.ecrm_grads_clip(self._grads, out._grads if out is not None else None, _ptr(norm), max_norm,
+                                       _stream(stream))
+        if check and rc != ECRM_OK:
+            raise EcrmError(rc, "ecrm_grads_clip")
+        return rc
 
 
 class Ecrm:
@@ -251,6 +348,49 @@ class Ecrm:
         if rc != ECRM_OK:
             raise EcrmError(rc, "ecrm_recovery_state")
         return dict(active=bool(a.value), next_chunk=int(nx.value), chunks=int(ch.value), buffered=int(bf.value))
+
+    def embed(self, keys, out, scale=1.0, padding=None, lost_server=None, stream=None, check=True):
+        """out: [n, D] of fp32, bf16 or fp16, rows at any multiple of 4 elements from each other."""
+        n = keys.numel()
+        assert keys.is_cuda and keys.element_size() == 8 and keys.is_contiguous()
+        assert out.is_cuda and out.dim() == 2 and out.shape[0] == n and out.shape[1] == self.cfg.dim and (n == 0 or out.stride(1) == 1)
+        rc = self._lib.ecrm_embed(self._ctx, keys.data_ptr(), n, _key(padding), scale,
+                                  0xFFFFFFFF if lost_server is None else lost_server, out.data_ptr(), _type(out), _row(out),
+                                  _stream(stream))
+        if check and rc != ECRM_OK:
+            raise EcrmError(rc, "ecrm_embed")
+        return rc
+
+    def _check_grad(self, keys, d_out):
+        n = keys.numel()
+        assert keys.is_cuda and keys.element_size() == 8 and keys.is_contiguous()
+        assert d_out.is_cuda and d_out.dim() == 2 and d_out.shape[0] == n and d_out.shape[1] == self.cfg.dim
+        assert n == 0 or d_out.stride(1) == 1
+        return n
+
+    def embed_grad(self, keys, d_out, out_keys, out_grads, count, scale=1.0, padding=None, stream=None, check=True):
+        """d_out: [n, D] of fp32, bf16 or fp16; out_keys [n] and out_grads [n, D] have room for as many distinct keys."""
+        import torch
+        n = self._check_grad(keys, d_out)
+        assert out_keys.is_cuda and out_keys.element_size() == 8 and out_keys.is_contiguous() and out_keys.numel() >= n
+        assert out_grads.is_cuda and out_grads.dtype == torch.float32 and out_grads.is_contiguous()
+        assert out_grads.numel() >= n * self.cfg.dim and count.element_size() == 8 and count.numel() == 1
+        rc = self._lib.ecrm_embed_grad(self._ctx, keys.data_ptr(), d_out.data_ptr(), _type(d_out), _row(d_out), n, _key(padding),
+                                       scale, out_keys.data_ptr(), out_grads.data_ptr(), count.data_ptr(), _stream(stream))
+        if check and rc != ECRM_OK:
+            raise EcrmError(rc, "ecrm_embed_grad")
+        return rc
+
+    def embed_grad_dense(self, keys, d_out, out, scale=1.0, padding=None, accumulate=False, stream=None, check=True):
+        """out: [R, D] fp32."""
+        import torch
+        n = self._check_grad(keys, d_out)
+        assert out.is_cuda and out.dtype == torch.float32 and out.is_contiguous() and tuple(out.shape) == (self.cfg.rows, self.cfg.dim)
+        rc = self._lib.ecrm_embed_grad_dense(self._ctx, keys.data_ptr(), d_out.data_ptr(), _type(d_out), _row(d_out), n,
+                                             _key(padding), scale, out.data_ptr(), 1 if accumulate else 0, _stream(stream))
+        if check and rc != ECRM_OK:
+            raise EcrmError(rc, "ecrm_embed_grad_dense")
+        return rc
 
     def status(self, stream=None):
         return self._lib.ecrm_status(self._ctx, _stream(stream))

@@ -5,7 +5,7 @@
 #include <new>
 #include <string.h>
 
-#include "ecrm_internal.h"
+#include "types.h"
 
 using namespace ecrm;
 
@@ -31,6 +31,7 @@ struct ecrm_ctx {
     int key_bits;
     Layout lay;               // of the scratch buffer the caller binds (sized by cfg.max_batch)
     Layout slay;              // of the library's own fixed scratch array (ecrm_update_static)
+    EmbedGradLayout elay;     // of a gradient call's arrays in the scratch buffer, over those of an update behind the sort's buffers
     bool has_partial2;
     // bound state
     bool bound, need_init;
@@ -238,6 +239,8 @@ int ecrm_create(const ecrm_config *cfg, ecrm_ctx **out)
     c->has_partial2 = cfg->optimizer == ECRM_OPT_MOMENTUM && !cfg->combine;
     c->lay = make_layout((uint32_t)cfg->max_batch, cfg->dim, cfg->k, cfg->servers, c->has_partial2);
     c->slay = make_layout(ECRM_STATIC_MAX_BATCH, cfg->dim, cfg->k, cfg->servers, c->has_partial2);
+    c->elay = embed_grad_layout(c->lay.off_long_slot, (uint32_t)cfg->max_batch, cfg->dim);
+    if (c->elay.end > c->lay.bytes) c->lay.bytes = c->elay.end;
     *out = c;
     return ECRM_OK;
 }
@@ -660,6 +663,59 @@ int ecrm_degraded_read(ecrm_ctx *c, const uint64_t *keys, uint64_t n, uint32_t l
     launch_degraded_read(c->s, c->geo, c->t.E, c->t.A, c->t.PE, c->t.PA, keys, n, lost_server, out_E, out_A,
                          c->cus, (hipStream_t)stream);
     return check_launch();
+}
+
+// rows of `type` elements: four of them are loaded at once
+static bool rows_ok(const ecrm_ctx *c, const void *p, uint32_t type, uint64_t stride)
+{
+    return type <= ECRM_F16 && stride >= c->cfg.dim && stride % 4 == 0 && aligned(p, 4 * type_bytes(type));
+}
+
+int ecrm_embed(ecrm_ctx *c, const uint64_t *keys, uint64_t n, uint64_t padding, float scale, uint32_t lost_server, void *out,
+               uint32_t type, uint64_t stride, void *stream)
+{
+    if (!c) return ECRM_EINVAL;
+    if (!c->bound) return ECRM_ENOTBOUND;
+    if (lost_server != ECRM_NO_SERVER && lost_server >= c->geo.S) return ECRM_EINVAL;
+    if (!isfinite(scale)) return ECRM_EINVAL;
+    if (n == 0) return ECRM_OK;
+    if (!aligned(keys, 8) || !rows_ok(c, out, type, stride)) return ECRM_EINVAL;
+    init_if_needed(c, (hipStream_t)stream);
+    launch_embed(c->s, c->geo, c->t.E, c->t.PE, keys, n, padding, scale, lost_server, out, type, stride, c->cus, (hipStream_t)stream);
+    return check_launch();
+}
+
+static int run_embed_grad(ecrm_ctx *c, const uint64_t *keys, const void *d, uint32_t type, uint64_t stride, uint64_t n,
+                          uint64_t padding, float scale, uint64_t *out_keys, float *out, uint64_t *count, bool accumulate,
+                          void *stream)
+{
+    if (n > c->lay.max_batch) return ECRM_EBATCH;
+    if (!isfinite(scale)) return ECRM_EINVAL;
+    if (n && (!aligned(keys, 8) || !rows_ok(c, d, type, stride))) return ECRM_EINVAL;
+    init_if_needed(c, (hipStream_t)stream);
+    int key_bits = c->key_bits;                // one value more than there are rows, for the padding token
+    while (key_bits < 32 && (1ull << key_bits) <= c->cfg.rows) ++key_bits;
+    launch_embed_grad(c->s, c->elay, c->geo, key_bits, keys, d, type, stride, (uint32_t)n, padding, scale, out_keys, out, count,
+                      accumulate, c->cus, (hipStream_t)stream);
+    return check_launch();
+}
+
+int ecrm_embed_grad(ecrm_ctx *c, const uint64_t *keys, const void *d_out, uint32_t type, uint64_t stride, uint64_t n,
+                    uint64_t padding, float scale, uint64_t *out_keys, float *out_grads, uint64_t *count, void *stream)
+{
+    if (!c) return ECRM_EINVAL;
+    if (!c->bound) return ECRM_ENOTBOUND;
+    if (!aligned(count, 8) || (n && (!aligned(out_keys, 8) || !aligned(out_grads, 16)))) return ECRM_EINVAL;
+    return run_embed_grad(c, keys, d_out, type, stride, n, padding, scale, out_keys, out_grads, count, false, stream);
+}
+
+int ecrm_embed_grad_dense(ecrm_ctx *c, const uint64_t *keys, const void *d_out, uint32_t type, uint64_t stride, uint64_t n,
+                          uint64_t padding, float scale, float *dE, int accumulate, void *stream)
+{
+    if (!c) return ECRM_EINVAL;
+    if (!c->bound) return ECRM_ENOTBOUND;
+    if (!aligned(dE, 16)) return ECRM_EINVAL;
+    return run_embed_grad(c, keys, d_out, type, stride, n, padding, scale, nullptr, dE, nullptr, accumulate != 0, stream);
 }
 
 int ecrm_status(ecrm_ctx *c, void *stream)

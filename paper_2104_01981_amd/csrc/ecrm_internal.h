@@ -239,6 +239,8 @@ void launch_sort(const Scratch &s, const Geometry &g, const RecoveryView &rv, co
 constexpr uint32_t kListSortMax = 1u << 18;
 void launch_sort_list(const Scratch &s, const Geometry &g, const uint64_t *list, uint32_t cap, const uint32_t *n_dev, int key_bits,
                       uint32_t *leader, uint32_t **sorted_keys, uint32_t **sorted_vals, hipStream_t st);
+void launch_sort_pairs(const Scratch &s, const Geometry &g, uint32_t n, int key_bits, uint32_t **sorted_keys, uint32_t **sorted_vals,
+                       hipStream_t st);
 // tile_count: scratch for the tiles' counts
 void launch_hold_back(Header *hdr, uint32_t *tile_count, const Geometry &g, const RecoveryView &rv, const uint64_t *keys,
                       const float *grads, uint32_t n, BatchSource src, const HoldBuffer &hb, uint32_t cur, hipStream_t st);
@@ -280,6 +282,21 @@ void launch_recover_server(const Geometry &g, float *E, float *A, float *PE, flo
 void launch_degraded_read(const Scratch &s, const Geometry &g, const float *E, const float *A, const float *PE,
                           const float *PA, const uint64_t *keys, uint64_t n, uint32_t lost, float *out_E,
                           float *out_A, int cus, hipStream_t st);
+
+void launch_embed(const Scratch &s, const Geometry &g, const float *E, const float *PE, const uint64_t *keys, uint64_t n,
+                  uint64_t padding, float scale, uint32_t lost, void *out, uint32_t type, uint64_t stride, int cus,
+                  hipStream_t st);
+// The arrays of a gradient call, from byte `off` of the scratch buffer on.
+struct TokenControl {
+    uint32_t bad;                  // the batch has a key out of range
+    uint32_t distinct;             // distinct rows in it
+};
+struct EmbedGradLayout { size_t off_ctl, off_first, off_state, off_dest, off_part, end; };
+EmbedGradLayout embed_grad_layout(size_t off, uint32_t max_batch, uint32_t D);
+// out_keys null: the dense form
+void launch_embed_grad(const Scratch &s, const EmbedGradLayout &l, const Geometry &g, int key_bits, const uint64_t *keys,
+                       const void *d, uint32_t type, uint64_t stride, uint32_t n, uint64_t padding, float scale,
+                       uint64_t *out_keys, float *out, uint64_t *count, bool accumulate, int cus, hipStream_t st);
 
 // What a batch that was held back in part, or a replay, leaves of the recovery buffer (one thread, after everything of the
 // batch has been appended or released).

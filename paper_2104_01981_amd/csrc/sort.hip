@@ -405,6 +405,28 @@ void launch_sort(const Scratch &s, const Geometry &g, const RecoveryView &rv, co
     *sorted_vals = s.vals[cur];
 }
 
+// Pairs (row id, index) that lie in the second pair of buffers.
+void launch_sort_pairs(const Scratch &s, const Geometry &g, uint32_t n, int key_bits, uint32_t **sorted_keys, uint32_t **sorted_vals,
+                       hipStream_t st)
+{
+    const RecoveryView none{};
+    const int passes = sort_passes(key_bits);
+    int shift = 0, cur = 1;
+    for (int p = 0; p < passes; ++p) {
+        const int bits = digit_bits(key_bits - shift, passes - p), out = cur ^ 1;
+        if (n <= kSmallSortBatch)
+            launch_sort_pass<kSmallSortIpt>(s, g, none, false, s.keys[cur], s.vals[cur], s.keys[out], s.vals[out], n, nullptr, shift, bits,
+                                            0u, 0u, 0u, st);
+        else
+            launch_sort_pass<kSortIpt>(s, g, none, false, s.keys[cur], s.vals[cur], s.keys[out], s.vals[out], n, nullptr, shift, bits,
+                                       0u, 0u, 0u, st);
+        cur = out;
+        shift += bits;
+    }
+    *sorted_keys = s.keys[cur];
+    *sorted_vals = s.vals[cur];
+}
+
 // The waiting updates of a recovery, for a read: two launches to a digit instead of three, and the read's leaders and its list
 // of long runs are cleared on the way.  A read of a few requests is these launches more than anything else: of 64, few updates
 // waiting of up to 1024, 4096, 16 384, 65 536, 262 144, us a call with three to a digit and
