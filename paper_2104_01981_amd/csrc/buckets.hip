@@ -980,13 +980,6 @@ struct HeavyShared {
 // us a call, D = 128, one workgroup to a run and 16 columns / cut up: all of 2^14, 2^16, 2^18 updates on one row 92 / 35, 304 / 54,
 // 1169 / 170; half of 2^18 706 / 222; 2^16 on 16 rows 104 / 65.
 
-// What workgroups of one launch leave each other is written and read by relaxed atomics of device scope: they pass by the
-// caches that the XCDs do not share.  published() waits until a wave's are done, so that a flag or a count written next is
-// seen after them.  (Fences of device scope would write back and invalidate those caches as a whole, for every segment:
-// 2^19 updates on 2^7 rows took 800 us with them.)
-__device__ __forceinline__ double shared_load(const double *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ void shared_store(double *p, double v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ void published() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // Folds the sums (ROWS = 1) or the sums and steps (2) of segments first .. first + count - 1, columns cg * 16 ..: kFoldParts
 // threads per column take kFoldLength segments each and leave theirs in sh.part, with the decay in sh.dec.  The last

@@ -318,6 +318,14 @@ __device__ __forceinline__ void hold_commit(Header *hdr, bool replay)
 __device__ __forceinline__ float4 load4(const float *p) { return *(const float4 *)p; }      // p aligned to 16 bytes
 __device__ __forceinline__ uint32_t lane_id() { return threadIdx.x & (kWave - 1); }
 
+// What workgroups of one launch leave each other is written and read by relaxed atomics of device scope: they pass by the
+// caches that the XCDs do not share.  published() waits until a wave's are done, so that a flag or a count written next is
+// seen after them.  (Fences of device scope would write back and invalidate those caches as a whole, for every segment:
+// 2^19 updates on 2^7 rows took 800 us with them.)
+__device__ __forceinline__ double shared_load(const double *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void shared_store(double *p, double v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void published() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // One Adagrad step of the printed rule on one parameter, carried in fp64:
 //   G += g^2 ; acc += lr * g / sqrt(G + eps)
 // 1/sqrt comes from the fp32 hardware estimate refined by one Newton step in fp64 (relative error
