@@ -240,7 +240,7 @@ int ecrm_recovery_read(ecrm_ctx *ctx, const uint64_t *keys, uint64_t n, float *o
  *                       out_grads left alone.  n = 0 gives *count = 0.
  * ecrm_embed_grad_dense the same sums as a table dE[R][D] of its own: with accumulate = 0 rows without a token become zero, with
  *                       accumulate = 1 the sums are added to dE (one rounding) and other rows are left alone.  A rejected batch
- *                       leaves dE alone.
+ *                       has no tokens: dE becomes zero, or is left alone.
  *
  * d_out and out: device memory aligned to four elements, stride >= D and a multiple of 4; out_grads and dE: 16 bytes; count:
  * 8 bytes, memory the device can write.  padding: any value, a row of the table or not (-1, -100); ECRM_NO_PADDING (2^63):

@@ -239,7 +239,7 @@ int ecrm_create(const ecrm_config *cfg, ecrm_ctx **out)
     c->has_partial2 = cfg->optimizer == ECRM_OPT_MOMENTUM && !cfg->combine;
     c->lay = make_layout((uint32_t)cfg->max_batch, cfg->dim, cfg->k, cfg->servers, c->has_partial2);
     c->slay = make_layout(ECRM_STATIC_MAX_BATCH, cfg->dim, cfg->k, cfg->servers, c->has_partial2);
-    c->elay = embed_grad_layout(c->lay.off_long_slot, (uint32_t)cfg->max_batch, cfg->dim);
+    c->elay = embed_grad_layout(c->lay.off_hist, (uint32_t)cfg->max_batch, cfg->dim, c->key_bits);
     if (c->elay.end > c->lay.bytes) c->lay.bytes = c->elay.end;
     *out = c;
     return ECRM_OK;
@@ -693,9 +693,7 @@ static int run_embed_grad(ecrm_ctx *c, const uint64_t *keys, const void *d, uint
     if (!isfinite(scale)) return ECRM_EINVAL;
     if (n && (!aligned(keys, 8) || !rows_ok(c, d, type, stride))) return ECRM_EINVAL;
     init_if_needed(c, (hipStream_t)stream);
-    int key_bits = c->key_bits;                // one value more than there are rows, for the padding token
-    while (key_bits < 32 && (1ull << key_bits) <= c->cfg.rows) ++key_bits;
-    launch_embed_grad(c->s, c->elay, c->geo, key_bits, keys, d, type, stride, (uint32_t)n, padding, scale, out_keys, out, count,
+    launch_embed_grad(c->s, c->elay, c->geo, c->key_bits, keys, d, type, stride, (uint32_t)n, padding, scale, out_keys, out, count,
                       accumulate, c->cus, (hipStream_t)stream);
     return check_launch();
 }

@@ -239,8 +239,6 @@ void launch_sort(const Scratch &s, const Geometry &g, const RecoveryView &rv, co
 constexpr uint32_t kListSortMax = 1u << 18;
 void launch_sort_list(const Scratch &s, const Geometry &g, const uint64_t *list, uint32_t cap, const uint32_t *n_dev, int key_bits,
                       uint32_t *leader, uint32_t **sorted_keys, uint32_t **sorted_vals, hipStream_t st);
-void launch_sort_pairs(const Scratch &s, const Geometry &g, uint32_t n, int key_bits, uint32_t **sorted_keys, uint32_t **sorted_vals,
-                       hipStream_t st);
 // tile_count: scratch for the tiles' counts
 void launch_hold_back(Header *hdr, uint32_t *tile_count, const Geometry &g, const RecoveryView &rv, const uint64_t *keys,
                       const float *grads, uint32_t n, BatchSource src, const HoldBuffer &hb, uint32_t cur, hipStream_t st);
@@ -286,13 +284,31 @@ void launch_degraded_read(const Scratch &s, const Geometry &g, const float *E, c
 void launch_embed(const Scratch &s, const Geometry &g, const float *E, const float *PE, const uint64_t *keys, uint64_t n,
                   uint64_t padding, float scale, uint32_t lost, void *out, uint32_t type, uint64_t stride, int cus,
                   hipStream_t st);
-// The arrays of a gradient call, from byte `off` of the scratch buffer on.
+// What the kernels of a gradient call tell each other.
 struct TokenControl {
-    uint32_t bad;                  // the batch has a key out of range
-    uint32_t distinct;             // distinct rows in it
+    uint32_t bad;                  // the batch has a key out of range: nothing of it counts
+    uint32_t valid;                // tokens that are rows; they are what the sort leaves
+    uint32_t distinct;             // distinct rows among them, where one kernel counts them for all
+    uint32_t joins[2];             // runs that go over several workgroups, and over many
 };
-struct EmbedGradLayout { size_t off_ctl, off_first, off_state, off_dest, off_part, end; };
-EmbedGradLayout embed_grad_layout(size_t off, uint32_t max_batch, uint32_t D);
+// Grouping of a batch's tokens (token_sort.hip): its arrays in the scratch buffer, from byte `off` on, and what a call makes of them.
+struct TokenSortLayout { size_t off_ctl, off_flags, off_table, off_groups, end; };
+struct TokenSort {
+    TokenControl *ctl;
+    const uint32_t *sk, *si;       // [valid] rows in ascending order, and the indices of their tokens, ascending for a row
+};
+// Memory to be cleared beside the sort, which leaves most of the memory's rate unused; to null: none.
+struct ClearJob { void *to; uint64_t sixteens; };
+TokenSortLayout token_sort_layout(size_t off, uint32_t max_batch, int key_bits);
+TokenSort launch_token_sort(const Scratch &s, const TokenSortLayout &l, const uint64_t *keys, uint32_t n, uint64_t padding, uint32_t rows,
+                            int key_bits, ClearJob clear, int cus, hipStream_t st);
+constexpr uint32_t kRankMost = 8192;   // tokens of a batch that is sorted in one launch
+// The arrays of a gradient call.
+struct EmbedGradLayout {
+    TokenSortLayout sort;
+    size_t off_first, off_state, off_join, off_part, end;
+};
+EmbedGradLayout embed_grad_layout(size_t off, uint32_t max_batch, uint32_t D, int key_bits);
 // out_keys null: the dense form
 void launch_embed_grad(const Scratch &s, const EmbedGradLayout &l, const Geometry &g, int key_bits, const uint64_t *keys,
                        const void *d, uint32_t type, uint64_t stride, uint32_t n, uint64_t padding, float scale,
@@ -317,6 +333,23 @@ __device__ __forceinline__ void hold_commit(Header *hdr, bool replay)
 // ---- small device helpers ------------------------------------------------------------------------
 __device__ __forceinline__ float4 load4(const float *p) { return *(const float4 *)p; }      // p aligned to 16 bytes
 __device__ __forceinline__ uint32_t lane_id() { return threadIdx.x & (kWave - 1); }
+
+// Tile a block works on.  Workgroups go to the 8 XCDs (each with its own L2) round-robin by block id;
+// with this map every XCD gets a contiguous range of tiles, so the short runs that neighbouring
+// tiles write next to each other in a digit's output range meet in one L2 instead of in memory.
+#ifndef ECRM_XCD_TILES
+#define ECRM_XCD_TILES 1
+#endif
+__device__ __forceinline__ uint32_t tile_of_block(uint32_t b, uint32_t nblocks)
+{
+#if ECRM_XCD_TILES
+    constexpr uint32_t X = 8;
+    const uint32_t q = nblocks / X, r = nblocks % X, xcd = b % X, i = b / X;
+    return xcd < r ? xcd * (q + 1u) + i : r * (q + 1u) + (xcd - r) * q + i;
+#else
+    return b;
+#endif
+}
 
 // What workgroups of one launch leave each other is written and read by relaxed atomics of device scope: they pass by the
 // caches that the XCDs do not share.  published() waits until a wave's are done, so that a flag or a count written next is

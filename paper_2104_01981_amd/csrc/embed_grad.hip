@@ -10,103 +10,124 @@
 namespace ecrm {
 
 constexpr int kSumThreads = 256;
-constexpr uint32_t kSumMost = 1024;       // sorted positions of a workgroup, at most
+constexpr uint32_t kSumMost = 2048;       // sorted positions of a workgroup, at most
+constexpr uint32_t kOneBlock = 2048;      // batches of so many tokens are cut by columns, not by positions: nothing is left to join
+constexpr uint32_t kOneUnits = 4;         // of four columns, of a workgroup there
 constexpr uint32_t kSumBlocks = 2048;     // workgroups, unless that would be more positions to one than there is room for
+constexpr uint32_t kScanBlocks = 4096;    // from more on their counts are added up by a launch of its own
 constexpr uint32_t kChunkMin = 4, kChunkMax = 128;
-constexpr int kTokenThreads = 256, kTokenTile = 1024;
+constexpr uint32_t kJoinUnits = 16;       // of four columns, of a job
+constexpr uint32_t kLongJoin = 16;        // workgroups from which on a run is a long one
 
 // What a workgroup has of a run that goes on before it (and maybe behind it) and of one that begins in it and goes on behind it.
 enum { kPartHead = 1, kPartThrough = 2, kPartTail = 4 };
+// Where the number of distinct rows before a workgroup's positions comes from.
+enum { kCountKeys = 0, kAddCounts = 1, kScanned = 2, kAllHere = 3 };
 
 struct SumArgs {
-    const uint32_t *sk, *si;         // sorted: row (`rows` for the padding token), index of the gradient
-    uint32_t n, rows, D;
-    Divider d4;                      // by D / 4
+    const uint32_t *sk, *si;         // sorted: row, index of the gradient
+    uint32_t n, D;
+    uint32_t quads;                  // D / 4
+    Divider units;                   // by the quads of a workgroup: all, or, where one workgroup has all positions, a few
     uint32_t teams, chunk, per;      // teams of a workgroup, positions of a chunk, of a workgroup
     uint32_t blocks;
+    uint32_t counting;
     const void *d;                   // [n][stride] gradients of the looked-up rows
     uint64_t stride;
     double scale;
     uint32_t accumulate;             // dense: add to what is there
     TokenControl *ctl;
-    uint32_t *first;                 // [blocks] distinct rows that begin before the workgroup's positions
+    uint32_t *first;                 // [blocks] distinct rows that begin in the workgroup's positions; scanned: before them
     uint32_t *state;                 // [blocks] kPart*
-    uint32_t *dest;                  // [blocks] row of the output that a kPartTail belongs to
+    uint2 *join;                     // [2][blocks] workgroups with a kPartTail and the rows of the output that it belongs to, in any
+                                     // order: of runs over up to kLongJoin workgroups, and of longer ones
     double *part;                    // [blocks][2][D]: head, tail
     uint64_t *out_keys;              // rows form
     float *out;
     uint64_t *count;
 };
 
-__global__ void token_begin_kernel(TokenControl *ctl)
+// sum of v over the workgroup, to all
+__device__ __forceinline__ uint32_t block_total(uint32_t v, uint32_t *s_wave)
 {
-    if (threadIdx.x == 0) ctl->bad = 0;
-}
-
-// row ids and indices for the sort; the padding token sorts behind every row
-__global__ __launch_bounds__(kTokenThreads) void token_keys_kernel(const uint64_t *keys, uint32_t n, uint64_t padding,
-                                                                   uint32_t rows, uint32_t *k, uint32_t *v, Header *hdr,
-                                                                   TokenControl *ctl)
-{
-    const uint32_t end = min(n - blockIdx.x * kTokenTile, (uint32_t)kTokenTile) + blockIdx.x * kTokenTile;
-    bool bad = false;
-    for (uint32_t i = blockIdx.x * kTokenTile + threadIdx.x; i < end; i += kTokenThreads) {
-        const uint64_t key = keys[i];
-        const bool pad = key == padding && key != ECRM_NO_PADDING;
-        bad |= !pad && key >= (uint64_t)rows;
-        k[i] = pad ? rows : (uint32_t)key;
-        v[i] = i;
-    }
-    if (__ballot(bad) && lane_id() == 0) {
-        atomicOr(&ctl->bad, 1u);
-        atomicOr(&hdr->err_sticky, 1u);
-    }
-}
-
-// is sorted position p the first of a row?
-__device__ __forceinline__ bool run_head(const uint32_t *sk, uint32_t p, uint32_t rows)
-{
-    const uint32_t key = sk[p];
-    return key < rows && (p == 0 || sk[p - 1] != key);
+#pragma unroll
+    for (int by = 1; by < kWave; by <<= 1) v += (uint32_t)__shfl_xor((int)v, by, kWave);
+    if (lane_id() == 0) s_wave[threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = 0;
+#pragma unroll
+    for (int w = 0; w < kSumThreads / kWave; ++w) v += s_wave[w];
+    __syncthreads();
+    return v;
 }
 
 __global__ __launch_bounds__(kSumThreads) void count_heads_kernel(SumArgs a)
 {
-    __shared__ uint32_t s_count;
-    if (threadIdx.x == 0) s_count = 0;
-    __syncthreads();
-    const uint64_t pos0 = (uint64_t)blockIdx.x * a.per;
-    const uint32_t cnt = (uint32_t)min((uint64_t)a.per, a.n - pos0);
-    for (uint32_t i0 = 0; i0 < cnt; i0 += kSumThreads) {
-        const uint32_t i = i0 + threadIdx.x;
-        const unsigned long long m = __ballot(i < cnt && run_head(a.sk, (uint32_t)pos0 + i, a.rows));
-        if (lane_id() == 0 && m) atomicAdd(&s_count, (uint32_t)__popcll(m));
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) a.first[blockIdx.x] = s_count;
+    __shared__ uint32_t s_wave[kSumThreads / kWave];
+    const uint32_t valid = a.ctl->valid, pos0 = blockIdx.x * a.per, end = min(pos0 + a.per, valid);
+    uint32_t heads = 0;
+    for (uint32_t p = pos0 + threadIdx.x; p < end; p += kSumThreads) heads += p == 0 || a.sk[p - 1] != a.sk[p] ? 1u : 0u;
+    heads = block_total(heads, s_wave);
+    if (threadIdx.x == 0) a.first[blockIdx.x] = heads;
 }
 
 // exclusive sums of the workgroups' counts in place; their total is the number of distinct rows
-__global__ __launch_bounds__(kSumThreads) void scan_heads_kernel(SumArgs a)
+__global__ __launch_bounds__(1024) void scan_heads_kernel(SumArgs a)
 {
-    __shared__ uint32_t s_sum[kSumThreads];
-    const uint32_t tid = threadIdx.x, each = (a.blocks + kSumThreads - 1) / kSumThreads;
-    const uint32_t lo = min(tid * each, a.blocks), hi = min(lo + each, a.blocks);
-    uint32_t sum = 0;
-    for (uint32_t i = lo; i < hi; ++i) sum += a.first[i];
-    s_sum[tid] = sum;
-    __syncthreads();
-    uint32_t before = 0;
-    for (uint32_t t = 0; t < tid; ++t) before += s_sum[t];
-    for (uint32_t i = lo; i < hi; ++i) {
-        const uint32_t c = a.first[i];
-        a.first[i] = before;
-        before += c;
+    __shared__ uint32_t s_wave[16];
+    uint32_t carry = 0;
+    for (uint32_t b0 = 0; b0 < a.blocks; b0 += 1024u) {
+        const uint32_t i = b0 + threadIdx.x, v = i < a.blocks ? a.first[i] : 0u;
+        uint32_t incl = v;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const uint32_t t = (uint32_t)__shfl_up((int)incl, d, kWave);
+            if (lane_id() >= (uint32_t)d) incl += t;
+        }
+        if (lane_id() == kWave - 1) s_wave[threadIdx.x / kWave] = incl;
+        __syncthreads();
+        uint32_t before = carry;
+        for (uint32_t w = 0; w < 16u; ++w) {
+            if (w < threadIdx.x / kWave) before += s_wave[w];
+            carry += s_wave[w];
+        }
+        if (i < a.blocks) a.first[i] = before + incl - v;
+        __syncthreads();
     }
-    if (tid == kSumThreads - 1) {
-        a.ctl->distinct = a.ctl->bad ? 0u : before;
-        if (a.count) *a.count = a.ctl->bad ? 0u : before;
+    if (threadIdx.x == 0) a.ctl->distinct = carry;
+}
+
+// The distinct rows before sorted position pos0, and (valid, not SCANNED) in all.
+__device__ __forceinline__ uint32_t distinct_before(const SumArgs &a, uint32_t pos0, uint32_t valid, uint32_t *s_wave, uint32_t &distinct)
+{
+    if (a.counting == kScanned) {
+        distinct = a.ctl->distinct;
+        return a.first[blockIdx.x];
     }
+    const uint32_t tid = threadIdx.x;
+    uint32_t before = 0, all = 0;
+    if (a.counting == kAddCounts) {
+#pragma unroll 4
+        for (uint32_t b = tid; b < a.blocks; b += kSumThreads) {
+            const uint32_t c = a.first[b];
+            all += c;
+            before += b < blockIdx.x ? c : 0u;
+        }
+    } else {
+#pragma unroll 2
+        for (uint32_t p = tid * 4u; p < valid; p += 4u * kSumThreads) {
+            const uint4 k = *(const uint4 *)(a.sk + p);        // room for a multiple of four
+            const uint32_t last = p ? a.sk[p - 1u] : kNoKey;
+            const uint32_t h[4] = {k.x != last ? 1u : 0u, k.y != k.x ? 1u : 0u, k.z != k.y ? 1u : 0u, k.w != k.z ? 1u : 0u};
+#pragma unroll
+            for (uint32_t q = 0; q < 4u; ++q) {
+                all += p + q < valid ? h[q] : 0u;
+                before += p + q < valid && p + q < pos0 ? h[q] : 0u;
+            }
+        }
+    }
+    distinct = block_total(all, s_wave);
+    return block_total(before, s_wave);
 }
 
 __device__ __forceinline__ void write_sum(const SumArgs &a, uint32_t row, uint32_t c, const double (&v)[4])
@@ -133,67 +154,84 @@ __global__ __launch_bounds__(kSumThreads) void sum_runs_kernel(SumArgs a)
     __shared__ uint32_t s_key[kSumMost + 2];             // position i's at i + 1
     __shared__ uint32_t s_idx[kSumMost];
     __shared__ unsigned long long s_head[kSumMost / kWave];
-    __shared__ uint32_t s_rank[kSumMost / kWave];        // of the heads in it and before
-    __shared__ uint32_t s_state[kSumThreads], s_all, s_dest;
+    __shared__ uint32_t s_rank[kSumMost / kWave];        // of the heads before it
+    __shared__ uint32_t s_state[kSumThreads], s_all, s_dest, s_key_of_tail, s_wave[kSumThreads / kWave];
     __shared__ double s_part[2][kSumThreads][4];
     const uint32_t tid = threadIdx.x, b = blockIdx.x;
-    const uint32_t pos0 = b * a.per, cnt = min(a.per, a.n - pos0);
-    const uint32_t distinct = a.ctl->distinct;
-    if (a.ctl->bad) {
-        if (!DENSE)
-            for (uint32_t i = tid; i < cnt; i += kSumThreads) a.out_keys[pos0 + i] = ECRM_NO_KEY;
-        if (tid == 0) a.state[b] = 0;
-        return;
-    }
-    for (uint32_t i = tid; i < cnt + 2u; i += kSumThreads) {
-        const bool in = pos0 + i >= 1u && pos0 + i - 1u < a.n;
-        s_key[i] = in ? a.sk[pos0 + i - 1u] : kNoKey;
-        if (i < cnt) s_idx[i] = a.si[pos0 + i];
+    const uint32_t pos0 = b * a.per, room = min(a.per, a.n - pos0);
+    const bool lists = !DENSE && blockIdx.y == 0;        // the keys are written once, not for every slice of columns
+    for (uint32_t i = tid; i < room + 2u; i += kSumThreads) {          // behind `valid` the buffers hold anything
+        s_key[i] = pos0 + i >= 1u && pos0 + i - 1u < a.n ? a.sk[pos0 + i - 1u] : kNoKey;
+        if (i < room) s_idx[i] = a.si[pos0 + i];
     }
     s_state[tid] = 0;
     if (tid == 0) s_all = 0;
+    const uint32_t valid = a.ctl->bad ? 0u : a.ctl->valid, cnt = pos0 < valid ? min(room, valid - pos0) : 0u;
     __syncthreads();
-    for (uint32_t i0 = 0; i0 < cnt; i0 += kSumThreads) {
-        const uint32_t i = i0 + tid;
-        const bool head = i < cnt && s_key[i + 1] < a.rows && s_key[i + 1] != s_key[i];
-        const unsigned long long m = __ballot(head);
-        if (lane_id() == 0 && i < cnt) s_head[i / kWave] = m;
+    if (cnt < room || pos0 + room == valid) {
+        if (tid == 0) s_key[cnt + 1u] = kNoKey;
+        __syncthreads();
     }
-    __syncthreads();
-    if (tid < (cnt + kWave - 1) / kWave) {
-        uint32_t before = a.first[b];
-        for (uint32_t w = 0; w < tid; ++w) before += (uint32_t)__popcll(s_head[w]);
-        s_rank[tid] = before;
+
+    // the first rows are on their way while the heads are counted
+    const uint32_t team = a.units.div(tid), mine = tid - team * a.units.d, unit = blockIdx.y * a.units.d + mine, c = unit * 4u;
+    const uint32_t lo = min(team * a.chunk, cnt), hi = min(lo + a.chunk, cnt);
+    const bool live = team < a.teams && unit < a.quads;
+    const T *d = (const T *)a.d + c;
+    Four v[U];
+    auto load = [&](uint32_t i0) {
+#pragma unroll
+        for (uint32_t q = 0; q < U; ++q) v[q] = *(const Four *)(d + (size_t)s_idx[min(i0 + q, hi - 1u)] * a.stride);
+    };
+    if (live && lo < hi) load(lo);
+    if (!DENSE) {
+        for (uint32_t i0 = 0; i0 < cnt; i0 += kSumThreads) {
+            const uint32_t i = i0 + tid;
+            const unsigned long long m = __ballot(i < cnt && s_key[min(i, cnt) + 1u] != s_key[min(i, cnt)]);
+            if (lane_id() == 0 && i < cnt) s_head[i / kWave] = m;
+        }
+        uint32_t distinct = 0, first = 0;
+        if (a.counting != kAllHere) first = distinct_before(a, pos0, valid, s_wave, distinct);
+        __syncthreads();
+        if (tid < kWave) {                               // at most 32 words
+            const uint32_t words = (cnt + kWave - 1) / kWave, heads = tid < words ? (uint32_t)__popcll(s_head[tid]) : 0u;
+            uint32_t incl = heads;
+#pragma unroll
+            for (int by = 1; by < kWave / 2; by <<= 1) {
+                const uint32_t t = (uint32_t)__shfl_up((int)incl, by, kWave);
+                if (tid >= (uint32_t)by) incl += t;
+            }
+            if (tid < words) s_rank[tid] = first + incl - heads;
+            if (tid == kWave / 2 - 1) s_wave[0] = incl;
+        }
+        __syncthreads();
+        if (a.counting == kAllHere) distinct = s_wave[0];
+        if (valid == 0) distinct = 0;
+        if (lists) {
+            if (b == 0 && tid == 0) *a.count = distinct;
+            for (uint32_t i = tid; i < room; i += kSumThreads)
+                if (pos0 + i >= distinct) a.out_keys[pos0 + i] = ECRM_NO_KEY;
+        }
     }
-    __syncthreads();
     // the how-manieth distinct row position i has
     auto rank = [&](uint32_t i) {
         return s_rank[i / kWave] + (uint32_t)__popcll(s_head[i / kWave] & (~0ull >> (kWave - 1u - i % kWave))) - 1u;
     };
-    if (!DENSE)
-        for (uint32_t i = tid; i < cnt; i += kSumThreads) {
-            if (s_key[i + 1] < a.rows && s_key[i + 1] != s_key[i]) a.out_keys[rank(i)] = s_key[i + 1];
-            if (pos0 + i >= distinct) a.out_keys[pos0 + i] = ECRM_NO_KEY;
-        }
+    if (lists)
+        for (uint32_t i = tid; i < cnt; i += kSumThreads)
+            if (s_key[i + 1] != s_key[i]) a.out_keys[rank(i)] = s_key[i + 1];
 
-    const uint32_t team = a.d4.div(tid), unit = tid - team * a.d4.d, c = unit * 4u;
-    const bool live = team < a.teams;
-    const T *d = (const T *)a.d + c;
     uint32_t tail_at = 0;
     if (live) {
-        const uint32_t lo = team * a.chunk, hi = min(lo + a.chunk, cnt);
         uint32_t state = 0;
         double acc[4] = {0, 0, 0, 0};
         bool before = lo < hi && s_key[lo] == s_key[lo + 1], open = false;     // the run begins before the chunk; is not at its end
         for (uint32_t i0 = lo; i0 < hi; i0 += U) {
-            if (s_key[i0 + 1] >= a.rows) break;
-            Four v[U];
-#pragma unroll
-            for (uint32_t q = 0; q < U; ++q) v[q] = *(const Four *)(d + (size_t)s_idx[min(i0 + q, hi - 1u)] * a.stride);
+            if (i0 != lo) load(i0);
 #pragma unroll
             for (uint32_t q = 0; q < U; ++q) {
                 const uint32_t i = i0 + q;
-                if (i >= hi || s_key[i + 1] >= a.rows) break;
+                if (i >= hi) break;
                 const f32x4 g = widen4<T>(v[q]);
                 acc[0] += (double)g.x;
                 acc[1] += (double)g.y;
@@ -219,7 +257,7 @@ __global__ __launch_bounds__(kSumThreads) void sum_runs_kernel(SumArgs a)
             state |= before ? kPartHead | kPartThrough : kPartTail;
             tail_at = hi - 1u;
         }
-        if (unit == 0) s_state[team] = state;
+        if (mine == 0) s_state[team] = state;
     }
     __syncthreads();
     if (live) {
@@ -227,7 +265,7 @@ __global__ __launch_bounds__(kSumThreads) void sum_runs_kernel(SumArgs a)
         auto join = [&](uint32_t t, double (&acc)[4], bool through) {       // the run goes on behind team t
             while (through && ++t < a.teams) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[j] += s_part[0][t * a.d4.d + unit][j];
+                for (int j = 0; j < 4; ++j) acc[j] += s_part[0][t * a.units.d + mine][j];
                 through = (s_state[t] & kPartThrough) != 0;
             }
             return through;
@@ -240,7 +278,7 @@ __global__ __launch_bounds__(kSumThreads) void sum_runs_kernel(SumArgs a)
             double *to = a.part + (size_t)b * 2u * a.D + c;
 #pragma unroll
             for (int j = 0; j < 4; ++j) to[j] = acc[j];
-            if (unit == 0) atomicOr(&s_all, through ? kPartHead | kPartThrough : kPartHead);
+            if (mine == 0) atomicOr(&s_all, through ? kPartHead | kPartThrough : kPartHead);
         }
         if (state & kPartTail) {
             double acc[4];
@@ -251,73 +289,103 @@ __global__ __launch_bounds__(kSumThreads) void sum_runs_kernel(SumArgs a)
                 double *to = a.part + ((size_t)b * 2u + 1u) * a.D + c;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) to[j] = acc[j];
-                if (unit == 0) {
+                if (mine == 0) {
                     atomicOr(&s_all, (uint32_t)kPartTail);
                     s_dest = row;
+                    s_key_of_tail = s_key[tail_at + 1];
                 }
             } else {
                 write_sum(a, row, c, acc);
             }
         }
     }
+    if (a.blocks == 1) return;
     __syncthreads();
     if (tid == 0) {
         a.state[b] = s_all;
-        if (s_all & kPartTail) a.dest[b] = s_dest;
+        if (s_all & kPartTail) {
+            const uint64_t far = ((uint64_t)b + kLongJoin) * a.per;
+            const uint32_t kind = far < valid && a.sk[far] == s_key_of_tail ? 1u : 0u;
+            a.join[(size_t)kind * a.blocks + atomicAdd(&a.ctl->joins[kind], 1u)] = uint2{b, s_dest};
+        }
     }
 }
 
-// The runs that began in one workgroup of sum_runs_kernel and ended in a later one.
-__global__ __launch_bounds__(kSumThreads) void join_runs_kernel(SumArgs a)
+// one behind the last workgroup that has a part of the run that begins in b
+__device__ __forceinline__ uint32_t run_end(const SumArgs &a, uint32_t b)
 {
-    __shared__ double s_part[kSumThreads][4];
-    const uint32_t b = blockIdx.x, tid = threadIdx.x, lane = lane_id();
-    if (!(a.state[b] & kPartTail)) return;
-    uint32_t end = b + 1u;                               // one behind the last workgroup that has a part of the run
+    uint32_t end = b + 1u;
     for (;;) {
-        const bool through = end + lane < a.blocks && (a.state[end + lane] & kPartThrough);
-        const unsigned long long ends = ~__ballot(through);
-        if (ends) {
-            end += (uint32_t)__builtin_ctzll(ends) + 1u;
-            break;
-        }
+        const uint32_t at = end + lane_id();
+        const unsigned long long ends = ~__ballot(at < a.blocks && (a.state[at] & kPartThrough));
+        if (ends) return min(end + (uint32_t)__builtin_ctzll(ends) + 1u, a.blocks);
         end += kWave;
     }
-    end = min(end, a.blocks);
-    const uint32_t team = a.d4.div(tid), unit = tid - team * a.d4.d, c = unit * 4u;
-    const uint32_t parts = end - (b + 1u), each = (parts + a.teams - 1) / a.teams;
-    double acc[4] = {0, 0, 0, 0};
-    if (team < a.teams) {
-        const uint32_t lo = min(b + 1u + team * each, end), hi = min(lo + each, end);
-#pragma unroll 4
-        for (uint32_t t = lo; t < hi; ++t) {
-            const double2 *p = (const double2 *)(a.part + (size_t)t * 2u * a.D + c);
-            const double2 x = p[0], y = p[1];
-            acc[0] += x.x;
-            acc[1] += x.y;
-            acc[2] += y.x;
-            acc[3] += y.y;
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s_part[tid][j] = acc[j];
-    }
-    __syncthreads();
-    if (team != 0) return;
-    const double2 *p = (const double2 *)(a.part + ((size_t)b * 2u + 1u) * a.D + c);
-    const double2 x = p[0], y = p[1];
-    acc[0] = x.x;
-    acc[1] = x.y;
-    acc[2] = y.x;
-    acc[3] = y.y;
-    for (uint32_t t = 0; t < a.teams; ++t)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] += s_part[t * a.d4.d + unit][j];
-    write_sum(a, a.dest[b], c, acc);
 }
 
-__global__ __launch_bounds__(kSumThreads) void clear_rows_kernel(const TokenControl *ctl, f32x4 *to, uint64_t n)
+__device__ __forceinline__ void add_part(const SumArgs &a, uint32_t b, uint32_t which, uint32_t c, double (&acc)[4])
 {
-    if (ctl && ctl->bad) return;
+    const double2 *p = (const double2 *)(a.part + ((size_t)b * 2u + which) * a.D + c);
+    const double2 x = p[0], y = p[1];
+    acc[0] += x.x;
+    acc[1] += x.y;
+    acc[2] += y.x;
+    acc[3] += y.y;
+}
+
+// The runs that began in one workgroup of sum_runs_kernel and ended in a later one.  Short ones: a team each, part after part.
+// Long ones, by the last `wide` workgroups: a job is a run and 64 columns, whose parts are added up by as many lanes side by side
+// as there are, each a range of them in order.
+__global__ __launch_bounds__(kSumThreads) void join_runs_kernel(SumArgs a, uint32_t wide)
+{
+    __shared__ double s_part[kSumThreads][4];
+    const uint32_t tid = threadIdx.x, narrow = gridDim.x - wide;
+    if (blockIdx.x < narrow) {
+        const uint32_t team = a.units.div(tid), c = (tid - team * a.units.d) * 4u, cnt = a.ctl->joins[0];
+        if (team >= a.teams) return;
+        for (uint32_t i = blockIdx.x * a.teams + team; i < cnt; i += narrow * a.teams) {
+            const uint2 what = a.join[i];
+            double acc[4] = {0, 0, 0, 0};
+            add_part(a, what.x, 1u, c, acc);
+            for (uint32_t b = what.x + 1u; b < a.blocks; ++b) {
+                const bool on = (a.state[b] & kPartThrough) != 0;
+                add_part(a, b, 0u, c, acc);
+                if (!on) break;
+            }
+            write_sum(a, what.y, c, acc);
+        }
+        return;
+    }
+    const uint32_t units = min(a.quads, kJoinUnits), groups = (a.quads + units - 1) / units, slices = kSumThreads / units;
+    const uint32_t slice = tid / units, jobs = a.ctl->joins[1] * groups;
+    for (uint32_t job = blockIdx.x - narrow; job < jobs; job += wide) {
+        const uint2 what = a.join[(size_t)a.blocks + job / groups];
+        const uint32_t unit = job % groups * units + tid % units, c = unit * 4u;
+        const uint32_t begin = what.x + 1u, parts = run_end(a, what.x) - begin, each = (parts + slices - 1) / slices;
+        const bool live = slice < slices && unit < a.quads;
+        double acc[4] = {0, 0, 0, 0};
+        if (live) {
+            const uint32_t lo = min(slice * each, parts), hi = min(lo + each, parts);
+#pragma unroll 4
+            for (uint32_t t = lo; t < hi; ++t) add_part(a, begin + t, 0u, c, acc);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s_part[tid][j] = acc[j];
+        }
+        __syncthreads();
+        if (live && slice == 0) {
+            double all[4] = {0, 0, 0, 0};
+            add_part(a, what.x, 1u, c, all);
+            for (uint32_t t = 0; t < slices && t * each < parts; ++t)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) all[j] += s_part[t * units + tid][j];
+            write_sum(a, what.y, c, all);
+        }
+        __syncthreads();
+    }
+}
+
+__global__ __launch_bounds__(kSumThreads) void clear_rows_kernel(f32x4 *to, uint64_t n)
+{
     for (uint64_t i = (uint64_t)blockIdx.x * kSumThreads + threadIdx.x; i < n; i += (uint64_t)gridDim.x * kSumThreads)
         to[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 }
@@ -328,13 +396,17 @@ __global__ void no_rows_kernel(uint64_t *count)
 }
 
 // ---- host side -------------------------------------------------------------------------------------------------------------
-struct SumPlan { uint32_t teams, chunk, per, blocks; };
+struct SumPlan { uint32_t units, teams, chunk, per, blocks, slices; };
 static SumPlan sum_plan(uint32_t n, uint32_t D)
 {
     SumPlan p;
-    p.teams = (uint32_t)kSumThreads / (D / 4u);
-    const uint32_t most = kSumMost / p.teams < kChunkMax ? kSumMost / p.teams : kChunkMax;
-    p.chunk = (uint32_t)(((uint64_t)n + (uint64_t)p.teams * kSumBlocks - 1) / ((uint64_t)p.teams * kSumBlocks));
+    const uint32_t quads = D / 4u;
+    p.units = n <= kOneBlock && quads > kOneUnits ? kOneUnits : quads;
+    p.slices = (quads + p.units - 1) / p.units;
+    p.teams = (uint32_t)kSumThreads / p.units;
+    const uint32_t room = kSumMost / p.teams, most = n <= kOneBlock || room < kChunkMax ? room : kChunkMax;
+    const uint64_t wanted = n <= kOneBlock ? p.teams : (uint64_t)p.teams * kSumBlocks;
+    p.chunk = (uint32_t)((n + wanted - 1) / wanted);
     if (p.chunk < kChunkMin) p.chunk = kChunkMin;
     if (p.chunk > most) p.chunk = most;
     p.per = p.teams * p.chunk;
@@ -342,18 +414,18 @@ static SumPlan sum_plan(uint32_t n, uint32_t D)
     return p;
 }
 
-EmbedGradLayout embed_grad_layout(size_t off, uint32_t max_batch, uint32_t D)
+EmbedGradLayout embed_grad_layout(size_t off, uint32_t max_batch, uint32_t D, int key_bits)
 {
-    // the most workgroups that any batch of up to max_batch tokens takes
-    const SumPlan p = sum_plan(max_batch, D);
-    const uint64_t least = ((uint64_t)max_batch + (uint64_t)p.teams * kChunkMin - 1) / ((uint64_t)p.teams * kChunkMin);
-    const uint32_t blocks = p.blocks > kSumBlocks ? p.blocks : (uint32_t)(least < kSumBlocks ? least : kSumBlocks);
     EmbedGradLayout l;
+    l.sort = token_sort_layout(off, max_batch, key_bits);
+    off = l.sort.end;
+    // the most workgroups that any batch of up to max_batch tokens takes: more than kSumBlocks have as many positions as one can
+    const SumPlan p = sum_plan(max_batch, D);
+    const uint32_t blocks = max_batch <= kOneBlock ? 1u : p.blocks > kSumBlocks ? p.blocks : kSumBlocks;
     auto take = [&](size_t bytes) { const size_t o = off; off = (off + bytes + 255) / 256 * 256; return o; };
-    l.off_ctl = take(sizeof(TokenControl));
     l.off_first = take((size_t)blocks * 4);
     l.off_state = take((size_t)blocks * 4);
-    l.off_dest = take((size_t)blocks * 4);
+    l.off_join = take((size_t)blocks * 2 * sizeof(uint2));
     l.off_part = take((size_t)blocks * 2 * D * sizeof(double));
     l.end = off;
     return l;
@@ -364,40 +436,40 @@ void launch_embed_grad(const Scratch &s, const EmbedGradLayout &l, const Geometr
                        uint64_t *out_keys, float *out, uint64_t *count, bool accumulate, int cus, hipStream_t st)
 {
     const bool dense = !out_keys;
-    const dim3 clear_grid((uint32_t)cus * 8u), threads(kSumThreads);
-    const uint64_t quads = (uint64_t)g.rows * (g.D / 4u);
+    const dim3 threads(kSumThreads);
+    ClearJob clear{nullptr, 0};
+    if (dense && !accumulate) clear = ClearJob{out, (uint64_t)g.rows * (g.D / 4u)};
     if (n == 0) {
         if (!dense) hipLaunchKernelGGL(no_rows_kernel, dim3(1), dim3(64), 0, st, count);
-        else if (!accumulate)
-            hipLaunchKernelGGL(clear_rows_kernel, clear_grid, threads, 0, st, (const TokenControl *)nullptr, (f32x4 *)out, quads);
+        if (clear.to) hipLaunchKernelGGL(clear_rows_kernel, dim3((uint32_t)cus * 8u), threads, 0, st, (f32x4 *)clear.to, clear.sixteens);
         return;
     }
     char *base = (char *)s.hdr;
+    const TokenSort sorted = launch_token_sort(s, l.sort, keys, n, padding, g.rows, key_bits, clear, cus, st);
     SumArgs a{};
     const SumPlan p = sum_plan(n, g.D);
-    a.n = n; a.rows = g.rows; a.D = g.D; a.d4 = make_divider(g.D / 4u);
+    a.sk = sorted.sk; a.si = sorted.si; a.ctl = sorted.ctl;
+    a.n = n; a.D = g.D; a.quads = g.D / 4u; a.units = make_divider(p.units);
     a.teams = p.teams; a.chunk = p.chunk; a.per = p.per; a.blocks = p.blocks;
     a.d = d; a.stride = stride; a.scale = (double)scale; a.accumulate = accumulate ? 1u : 0u;
-    a.ctl = (TokenControl *)(base + l.off_ctl);
     a.first = (uint32_t *)(base + l.off_first);
     a.state = (uint32_t *)(base + l.off_state);
-    a.dest = (uint32_t *)(base + l.off_dest);
+    a.join = (uint2 *)(base + l.off_join);
     a.part = (double *)(base + l.off_part);
     a.out_keys = out_keys; a.out = out; a.count = count;
-    hipLaunchKernelGGL(token_begin_kernel, dim3(1), dim3(64), 0, st, a.ctl);
-    hipLaunchKernelGGL(token_keys_kernel, dim3((n + kTokenTile - 1) / kTokenTile), dim3(kTokenThreads), 0, st, keys, n, padding,
-                       g.rows, s.keys[1], s.vals[1], s.hdr, a.ctl);
-    if (dense && !accumulate) hipLaunchKernelGGL(clear_rows_kernel, clear_grid, threads, 0, st, a.ctl, (f32x4 *)out, quads);
-    uint32_t *sk, *si;
-    launch_sort_pairs(s, g, n, key_bits, &sk, &si, st);
-    a.sk = sk; a.si = si;
-    hipLaunchKernelGGL(count_heads_kernel, dim3(a.blocks), threads, 0, st, a);
-    hipLaunchKernelGGL(scan_heads_kernel, dim3(1), threads, 0, st, a);
+    a.counting = a.blocks == 1 ? kAllHere : n <= kRankMost ? kCountKeys : a.blocks <= kScanBlocks ? kAddCounts : kScanned;
+    if (!dense && (a.counting == kAddCounts || a.counting == kScanned)) {
+        hipLaunchKernelGGL(count_heads_kernel, dim3(a.blocks), threads, 0, st, a);
+        if (a.counting == kScanned) hipLaunchKernelGGL(scan_heads_kernel, dim3(1), dim3(1024), 0, st, a);
+    }
     with_type(type, [&](auto t) {
-        if (dense) hipLaunchKernelGGL((sum_runs_kernel<decltype(t), true>), dim3(a.blocks), threads, 0, st, a);
-        else hipLaunchKernelGGL((sum_runs_kernel<decltype(t), false>), dim3(a.blocks), threads, 0, st, a);
+        if (dense) hipLaunchKernelGGL((sum_runs_kernel<decltype(t), true>), dim3(a.blocks, p.slices), threads, 0, st, a);
+        else hipLaunchKernelGGL((sum_runs_kernel<decltype(t), false>), dim3(a.blocks, p.slices), threads, 0, st, a);
     });
-    hipLaunchKernelGGL(join_runs_kernel, dim3(a.blocks), threads, 0, st, a);
+    if (a.blocks > 1) {
+        const uint32_t narrow = (a.blocks + a.teams - 1) / a.teams, most = (uint32_t)cus * 8u, wide = (uint32_t)cus;
+        hipLaunchKernelGGL(join_runs_kernel, dim3((narrow < most ? narrow : most) + wide), threads, 0, st, a, wide);
+    }
 }
 
 }  // namespace ecrm

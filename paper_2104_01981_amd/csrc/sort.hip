@@ -85,23 +85,6 @@ __global__ void clear_buffer_kernel(Header *h)
     }
 }
 
-// Tile a block works on.  Workgroups go to the 8 XCDs (each with its own L2) round-robin by block id;
-// with this map every XCD gets a contiguous range of tiles, so the short runs that neighbouring
-// tiles write next to each other in a digit's output range meet in one L2 instead of in memory.
-#ifndef ECRM_XCD_TILES
-#define ECRM_XCD_TILES 1
-#endif
-__device__ __forceinline__ uint32_t tile_of_block(uint32_t b, uint32_t nblocks)
-{
-#if ECRM_XCD_TILES
-    constexpr uint32_t X = 8;
-    const uint32_t q = nblocks / X, r = nblocks % X, xcd = b % X, i = b / X;
-    return xcd < r ? xcd * (q + 1u) + i : r * (q + 1u) + (xcd - r) * q + i;
-#else
-    return b;
-#endif
-}
-
 // Sort key of one caller key in the first pass, the same in the histogram and in the scatter:
 // out-of-range keys keep their low bits (the batch is rejected anyway), held-back items get `rows`.
 __device__ __forceinline__ uint32_t first_pass_key(uint64_t k64, uint32_t rows, const Divider &dk, const Divider &dS,
@@ -398,28 +381,6 @@ void launch_sort(const Scratch &s, const Geometry &g, const RecoveryView &rv, co
         else
             launch_sort_pass<kSortIpt>(s, g, rv, p == 0, kin, vin, s.keys[out], s.vals[out], n, n_dev, shift, bits, count,
                                        bs, packed, st);
-        cur = out;
-        shift += bits;
-    }
-    *sorted_keys = s.keys[cur];
-    *sorted_vals = s.vals[cur];
-}
-
-// Pairs (row id, index) that lie in the second pair of buffers.
-void launch_sort_pairs(const Scratch &s, const Geometry &g, uint32_t n, int key_bits, uint32_t **sorted_keys, uint32_t **sorted_vals,
-                       hipStream_t st)
-{
-    const RecoveryView none{};
-    const int passes = sort_passes(key_bits);
-    int shift = 0, cur = 1;
-    for (int p = 0; p < passes; ++p) {
-        const int bits = digit_bits(key_bits - shift, passes - p), out = cur ^ 1;
-        if (n <= kSmallSortBatch)
-            launch_sort_pass<kSmallSortIpt>(s, g, none, false, s.keys[cur], s.vals[cur], s.keys[out], s.vals[out], n, nullptr, shift, bits,
-                                            0u, 0u, 0u, st);
-        else
-            launch_sort_pass<kSortIpt>(s, g, none, false, s.keys[cur], s.vals[cur], s.keys[out], s.vals[out], n, nullptr, shift, bits,
-                                       0u, 0u, 0u, st);
         cur = out;
         shift += bits;
     }

@@ -1,0 +1,492 @@
+// Groups a batch's tokens for the gradient of the lookup: (row, index) pairs in ascending order of the row, and of the index for
+// one row.  Padding tokens are left out, a token that is no row marks the batch.
+//
+// Up to kRankMost tokens: one launch.  A token's place is the number of tokens before it in the order, and each wave counts
+// that for eight tokens over all keys in LDS -- n^2 comparisons, which the device does at 10^13 a second.
+// More: a radix sort of digits of up to 11 bits, two launches to a digit: counts of each tile, then a stable scatter that ranks
+// a tile's items with wave ballots and writes them in runs.  Every workgroup of the scatter adds up the counts of the tiles before
+// its own by itself; of more than kDirectTiles tiles they are first added up in groups, by a launch in between.
+#include "ecrm_internal.h"
+
+namespace ecrm {
+
+constexpr int kRankThreads = 256;
+constexpr uint32_t kRankItems = 8;                       // tokens of a wave
+constexpr int kTokenThreads = 512;
+constexpr int kTokenWaves = kTokenThreads / kWave;
+constexpr int kTokenBits = 11;                           // of a digit, at most
+constexpr uint32_t kDirectTiles = 128;
+constexpr uint32_t kBadTile = 0x80000000u;
+
+struct TokenPass {
+    const uint64_t *keys64;                              // first digit: the caller's
+    const uint32_t *keys, *vals;                         // others
+    uint32_t *keys_out, *vals_out;
+    uint32_t n;
+    uint64_t padding;
+    uint32_t rows;
+    int shift, bits;
+    uint32_t tiles, group, groups;                       // group: tiles of one
+    uint16_t *table;                                     // [tiles][bins]; grouped: of 32 bits
+    uint32_t *sums;                                      // [groups][bins]
+    uint32_t *flags;                                     // [tiles] padding tokens, kBadTile
+    TokenControl *ctl;
+    Header *hdr;
+    ClearJob clear;                                      // by the workgroups behind the tiles'
+};
+
+// a share of the clearing for each of `blocks` workgroups
+__device__ __forceinline__ void clear_share(const ClearJob &c, uint32_t block, uint32_t blocks, uint32_t threads)
+{
+    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+    u4 *to = (u4 *)c.to;
+    for (uint64_t i = (uint64_t)block * threads + threadIdx.x; i < c.sixteens; i += (uint64_t)blocks * threads)
+        to[i] = u4{0u, 0u, 0u, 0u};
+}
+
+__device__ __forceinline__ bool is_padding(uint64_t key, uint64_t padding) { return key == padding && key != ECRM_NO_PADDING; }
+
+__global__ __launch_bounds__(kRankThreads) void token_rank_kernel(TokenPass a)
+{
+    __shared__ __align__(16) uint32_t s_key[kRankMost];
+    __shared__ uint32_t s_pads, s_bad;
+    if (blockIdx.x >= a.tiles) {
+        clear_share(a.clear, blockIdx.x - a.tiles, gridDim.x - a.tiles, kRankThreads);
+        return;
+    }
+    const uint32_t tid = threadIdx.x, lane = lane_id(), wave = tid / kWave, n = a.n;
+    if (tid == 0) s_pads = s_bad = 0;
+    __syncthreads();
+    const uint32_t room = (n + 255u) / 256u * 256u;      // what a wave looks at a time
+    uint32_t pads = 0;
+    bool bad = false;
+#pragma unroll 4
+    for (uint32_t i = tid; i < room; i += kRankThreads) {
+        const uint64_t key = i < n ? a.keys64[i] : 0ull;
+        const bool pad = i < n && is_padding(key, a.padding);
+        bad |= i < n && !pad && key >= (uint64_t)a.rows;
+        pads += pad ? 1u : 0u;
+        s_key[i] = i < n && !pad ? (uint32_t)key : kNoKey;
+    }
+    if (blockIdx.x == 0) {
+        if (pads) atomicAdd(&s_pads, pads);
+        if (bad) s_bad = 1;
+    }
+    __syncthreads();
+    if (blockIdx.x == 0 && tid == 0) {
+        a.ctl->bad = s_bad;
+        a.ctl->valid = n - s_pads;
+        a.ctl->joins[0] = a.ctl->joins[1] = 0;
+        if (s_bad) atomicOr(&a.hdr->err_sticky, 1u);
+    }
+    const uint32_t i0 = (blockIdx.x * (kRankThreads / kWave) + wave) * kRankItems;
+    if (i0 >= n) return;
+    uint32_t key[kRankItems], less[kRankItems];
+#pragma unroll
+    for (uint32_t q = 0; q < kRankItems; ++q) {
+        key[q] = s_key[i0 + q];                          // i0 + q < room
+        less[q] = 0;
+    }
+    // below: every token; of equal ones those before it.  The eight themselves are looked at last.
+    for (uint32_t j = lane * 4u; j < room; j += 4u * kWave) {
+        const uint4 k = *(const uint4 *)(s_key + j);
+        const bool own = j / kRankItems == i0 / kRankItems;
+        const uint32_t one = j < i0 ? 1u : 0u;
+#pragma unroll
+        for (uint32_t q = 0; q < kRankItems; ++q) {
+            const uint32_t below = own ? 0u : key[q] + one;
+            less[q] += (k.x < below ? 1u : 0u) + (k.y < below ? 1u : 0u) + (k.z < below ? 1u : 0u) + (k.w < below ? 1u : 0u);
+        }
+    }
+    // eight sums over the wave: halves are exchanged, so that lane l ends up with that of token bits(l)
+#pragma unroll
+    for (uint32_t h = kRankItems / 2u, by = 1; h; h /= 2u, by *= 2u) {
+        const bool upper = (lane & by) != 0;
+#pragma unroll
+        for (uint32_t q = 0; q < h; ++q) {
+            const uint32_t keep = upper ? less[q + h] : less[q], give = upper ? less[q] : less[q + h];
+            less[q] = keep + (uint32_t)__shfl_xor((int)give, (int)by, kWave);
+        }
+    }
+#pragma unroll
+    for (int by = kRankItems; by < kWave; by *= 2) less[0] += (uint32_t)__shfl_xor((int)less[0], by, kWave);
+    if (lane >= kRankItems) return;
+    const uint32_t mine = ((lane & 1u) << 2) | (lane & 2u) | (lane >> 2), i = i0 + mine, x = s_key[i];
+    uint32_t at = less[0];
+#pragma unroll
+    for (uint32_t q = 0; q < kRankItems; ++q) {
+        const uint32_t k = s_key[i0 + q];
+        at += k < x || (k == x && q < mine) ? 1u : 0u;
+    }
+    if (i < n && !is_padding(a.keys64[i], a.padding)) {
+        a.keys_out[at] = x;
+        a.vals_out[at] = i;
+    }
+}
+
+// The sort key of item i, false where there is none.
+template <bool FIRST>
+__device__ __forceinline__ bool token_at(const TokenPass &a, uint32_t i, uint32_t n, uint32_t &key, bool &pad, bool &bad)
+{
+    pad = bad = false;
+    if (i >= n) return false;
+    if (!FIRST) {
+        key = a.keys[i];
+        return true;
+    }
+    const uint64_t k = a.keys64[i];
+    pad = is_padding(k, a.padding);
+    bad = !pad && k >= (uint64_t)a.rows;                 // keeps its low bits: the batch is rejected anyway
+    key = (uint32_t)k;
+    return !pad;
+}
+
+template <bool FIRST, int IPT, bool GROUPED>
+__global__ __launch_bounds__(kTokenThreads) void token_hist_kernel(TokenPass a)
+{
+    __shared__ uint32_t s_hist[1 << kTokenBits];
+    __shared__ uint32_t s_pads, s_bad;
+    if (blockIdx.x >= a.tiles) {
+        clear_share(a.clear, blockIdx.x - a.tiles, gridDim.x - a.tiles, kTokenThreads);
+        return;
+    }
+    const uint32_t tid = threadIdx.x, bins = 1u << a.bits, n = FIRST ? a.n : a.ctl->valid;
+    for (uint32_t i = tid; i < bins; i += kTokenThreads) s_hist[i] = 0;
+    if (FIRST && tid == 0) s_pads = s_bad = 0;
+    __syncthreads();
+    const uint32_t tile = tile_of_block(blockIdx.x, a.tiles), tile0 = tile * (uint32_t)(kTokenThreads * IPT);
+    uint32_t pads = 0;
+    bool any_bad = false;
+#pragma unroll
+    for (int r = 0; r < IPT; ++r) {
+        uint32_t key = 0;
+        bool pad, bad;
+        if (token_at<FIRST>(a, tile0 + r * kTokenThreads + tid, n, key, pad, bad)) atomicAdd(&s_hist[(key >> a.shift) & (bins - 1u)], 1u);
+        pads += pad ? 1u : 0u;
+        any_bad |= bad;
+    }
+    if (FIRST) {
+        if (pads) atomicAdd(&s_pads, pads);
+        if (any_bad) s_bad = 1;
+    }
+    __syncthreads();
+    for (uint32_t i = tid; i < bins; i += kTokenThreads) {
+        if (GROUPED) ((uint32_t *)a.table)[(size_t)tile * bins + i] = s_hist[i];
+        else a.table[(size_t)tile * bins + i] = (uint16_t)s_hist[i];
+    }
+    if (FIRST && tid == 0) {
+        a.flags[tile] = s_pads | (s_bad ? kBadTile : 0u);
+        if (s_bad) atomicOr(&a.hdr->err_sticky, 1u);
+        if (tile == 0) a.ctl->joins[0] = a.ctl->joins[1] = 0;
+    }
+}
+
+// Of a group of tiles and a digit value: exclusive sums over the group's tiles in place, and their total.
+__global__ __launch_bounds__(256) void token_groups_kernel(TokenPass a)
+{
+    const uint32_t bins = 1u << a.bits, bin = blockIdx.y * 256u + threadIdx.x, g = blockIdx.x;
+    if (bin >= bins) return;
+    uint32_t *at = (uint32_t *)a.table + (size_t)g * a.group * bins + bin;
+    const uint32_t cnt = min(a.group, a.tiles - g * a.group);
+    uint32_t sum = 0;
+    constexpr uint32_t U = 16;
+    for (uint32_t t0 = 0; t0 < cnt; t0 += U) {
+        uint32_t c[U];
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) c[u] = t0 + u < cnt ? at[(size_t)(t0 + u) * bins] : 0u;
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+            if (t0 + u < cnt) at[(size_t)(t0 + u) * bins] = sum;
+            sum += c[u];
+        }
+    }
+    a.sums[(size_t)g * bins + bin] = sum;
+}
+
+// exclusive sum of v over the workgroup
+__device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t *s_wave)
+{
+    const uint32_t lane = lane_id(), wave = threadIdx.x / kWave;
+    uint32_t incl = v;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        const uint32_t t = (uint32_t)__shfl_up((int)incl, d, kWave);
+        if (lane >= (uint32_t)d) incl += t;
+    }
+    if (lane == kWave - 1) s_wave[wave] = incl;
+    __syncthreads();
+    uint32_t before = incl - v;
+#pragma unroll
+    for (uint32_t w = 0; w < (uint32_t)kTokenWaves; ++w) before += w < wave ? s_wave[w] : 0u;
+    __syncthreads();
+    return before;
+}
+
+// LDS of a scatter
+static size_t scatter_lds(int bits, int ipt)
+{
+    const size_t bins = (size_t)1 << bits, tile = (size_t)kTokenThreads * ipt;
+    return tile * 8 + bins * 8 + kTokenWaves * bins * 2;
+}
+
+// PER: digit values of a thread
+template <bool FIRST, int IPT, int PER, bool GROUPED>
+__global__ __launch_bounds__(kTokenThreads) void token_scatter_kernel(TokenPass a)
+{
+    constexpr uint32_t kTile = kTokenThreads * IPT;
+    extern __shared__ __align__(16) uint32_t lds[];
+    __shared__ uint32_t s_wave[kTokenWaves];
+    const uint32_t tid = threadIdx.x, wave = tid / kWave, lane = lane_id();
+    const uint32_t bins = 1u << a.bits;
+    uint32_t *s_keys = lds, *s_vals = lds + kTile, *s_start = lds + 2 * kTile, *s_base = s_start + bins;
+    uint16_t *s_cnt = (uint16_t *)(s_base + bins);       // [waves][bins] counts, then offsets, of a wave
+    if (blockIdx.x >= a.tiles) {
+        clear_share(a.clear, blockIdx.x - a.tiles, gridDim.x - a.tiles, kTokenThreads);
+        return;
+    }
+    const uint32_t n = FIRST ? a.n : a.ctl->valid;
+    const uint32_t tile = tile_of_block(blockIdx.x, a.tiles), tile0 = tile * kTile;
+    if (FIRST && blockIdx.x == 0) {                      // what the first counting has found
+        uint32_t pads = 0, bad = 0;
+        for (uint32_t t = tid; t < a.tiles; t += kTokenThreads) {
+            pads += a.flags[t] & ~kBadTile;
+            bad |= a.flags[t] & kBadTile;
+        }
+        const uint32_t before = sum_before(pads, s_wave);
+        if (tid == kTokenThreads - 1) a.ctl->valid = a.n - (before + pads);
+        const uint32_t bads = sum_before(bad ? 1u : 0u, s_wave) + (bad ? 1u : 0u);
+        if (tid == kTokenThreads - 1) a.ctl->bad = bads ? 1u : 0u;
+    }
+    if (tile0 >= n) return;
+
+    uint32_t key[IPT], val[IPT], rank[IPT];
+    bool there[IPT];
+#pragma unroll
+    for (int r = 0; r < IPT; ++r) {
+        const uint32_t i = tile0 + wave * (kWave * IPT) + r * kWave + lane;
+        bool pad, bad;
+        key[r] = 0;
+        there[r] = token_at<FIRST>(a, i, n, key[r], pad, bad);
+        val[r] = FIRST ? i : there[r] ? a.vals[i] : 0u;
+    }
+    // the thread's digit values: items of them in the tiles before, and in all
+    const uint32_t bin = tid * PER;
+    uint32_t before[PER] = {}, all[PER] = {};
+    if (bin < bins) {
+        if (GROUPED) {
+            constexpr uint32_t U = 32 / PER;
+            typedef uint32_t Counts __attribute__((ext_vector_type(PER)));
+            const uint32_t g = tile / a.group;
+            const Counts here = *(const Counts *)((const uint32_t *)a.table + (size_t)tile * bins + bin);
+            for (uint32_t t0 = 0; t0 < a.groups; t0 += U) {
+                Counts c[U];
+#pragma unroll
+                for (uint32_t u = 0; u < U; ++u) c[u] = *(const Counts *)(a.sums + (size_t)min(t0 + u, a.groups - 1u) * bins + bin);
+#pragma unroll
+                for (uint32_t u = 0; u < U; ++u)
+#pragma unroll
+                    for (int q = 0; q < PER; ++q) {
+                        all[q] += t0 + u < a.groups ? c[u][q] : 0u;
+                        before[q] += t0 + u < g ? c[u][q] : 0u;
+                    }
+            }
+#pragma unroll
+            for (int q = 0; q < PER; ++q) before[q] += here[q];
+        } else {
+            constexpr uint32_t U = 64 / PER;
+            typedef uint16_t Counts __attribute__((ext_vector_type(PER)));
+            for (uint32_t t0 = 0; t0 < a.tiles; t0 += U) {
+                Counts c[U];
+#pragma unroll
+                for (uint32_t u = 0; u < U; ++u) c[u] = *(const Counts *)(a.table + (size_t)min(t0 + u, a.tiles - 1u) * bins + bin);
+#pragma unroll
+                for (uint32_t u = 0; u < U; ++u)
+#pragma unroll
+                    for (int q = 0; q < PER; ++q) {
+                        all[q] += t0 + u < a.tiles ? (uint32_t)c[u][q] : 0u;
+                        before[q] += t0 + u < tile ? (uint32_t)c[u][q] : 0u;
+                    }
+            }
+        }
+    }
+    for (uint32_t i = tid; i < kTokenWaves * bins / 2u; i += kTokenThreads) ((uint32_t *)s_cnt)[i] = 0;
+    __syncthreads();
+
+    // rank inside the wave, whose items are ordered (r, lane): equal digits are matched with ballots
+    uint16_t *cnt = s_cnt + wave * bins;
+#pragma unroll
+    for (int r = 0; r < IPT; ++r) {
+        const uint32_t digit = (key[r] >> a.shift) & (bins - 1u);
+        unsigned long long peers = __ballot(there[r]);
+        for (int b = 0; b < a.bits; ++b) {
+            const bool bit = (digit >> b) & 1u;
+            const unsigned long long bal = __ballot(bit);
+            peers &= bit ? bal : ~bal;
+        }
+        const uint32_t below = (uint32_t)__popcll(peers & ((1ull << lane) - 1ull));
+        const uint32_t old = cnt[digit];
+        __builtin_amdgcn_wave_barrier();
+        if (there[r] && below == 0) cnt[digit] = (uint16_t)(old + (uint32_t)__popcll(peers));
+        __builtin_amdgcn_wave_barrier();
+        rank[r] = old + below;
+    }
+    __syncthreads();
+
+    uint32_t total[PER] = {}, mine = 0, in_all = 0;
+    if (bin < bins) {
+#pragma unroll
+        for (int q = 0; q < PER; ++q) {
+            uint32_t t[kTokenWaves];
+#pragma unroll
+            for (int w = 0; w < kTokenWaves; ++w) t[w] = s_cnt[w * bins + bin + q];
+#pragma unroll
+            for (int w = 0; w < kTokenWaves; ++w) {
+                s_cnt[w * bins + bin + q] = (uint16_t)total[q];
+                total[q] += t[w];
+            }
+            mine += total[q];
+            in_all += all[q];
+        }
+    }
+    uint32_t start = sum_before(mine, s_wave), global = sum_before(in_all, s_wave);
+    if (bin < bins) {
+#pragma unroll
+        for (int q = 0; q < PER; ++q) {
+            s_start[bin + q] = start;
+            s_base[bin + q] = global + before[q] - start;
+            start += total[q];
+            global += all[q];
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < IPT; ++r) {
+        if (!there[r]) continue;
+        const uint32_t digit = (key[r] >> a.shift) & (bins - 1u), at = s_start[digit] + cnt[digit] + rank[r];
+        s_keys[at] = key[r];
+        s_vals[at] = val[r];
+    }
+    // items of the tile
+    if (tid == kTokenThreads - 1) s_wave[0] = start;
+    __syncthreads();
+    const uint32_t items = s_wave[0];
+    for (uint32_t i = tid; i < items; i += kTokenThreads) {
+        const uint32_t k = s_keys[i], to = s_base[(k >> a.shift) & (bins - 1u)] + i;
+        a.keys_out[to] = k;
+        a.vals_out[to] = s_vals[i];
+    }
+}
+
+// ---- host side -------------------------------------------------------------------------------------------------------------
+// Items of a thread: few for small batches, so that they spread over the compute units.
+static int items_of(uint32_t n) { return n <= 64u * 1024u ? 2 : n <= kDirectTiles * 2048u ? 4 : 8; }
+// Digits: wide ones for few launches; in large batches at most 9 bits, so that what a tile writes of one digit value is some
+// tens of bytes on end.
+static int token_passes(int key_bits, int ipt)
+{
+    const int most = ipt == 8 ? 9 : kTokenBits;
+    return (key_bits + most - 1) / most;
+}
+static uint32_t group_of(uint32_t tiles)                 // tiles of a group: as many groups, about
+{
+    uint32_t g = 8;
+    while ((uint64_t)g * g < tiles) ++g;
+    return g;
+}
+static uint32_t tiles_of(uint32_t n, int ipt) { return (uint32_t)(((uint64_t)n + kTokenThreads * ipt - 1) / (kTokenThreads * ipt)); }
+
+TokenSortLayout token_sort_layout(size_t off, uint32_t max_batch, int key_bits)
+{
+    TokenSortLayout l;
+    auto take = [&](size_t bytes) { const size_t o = off; off = (off + bytes + 255) / 256 * 256; return o; };
+    size_t tiles = 0, table = 0, sums = 0;
+    const uint32_t ends[3] = {64u * 1024u, kDirectTiles * 2048u, 0xFFFFFFFFu};
+    for (int c = 0; c < 3 && max_batch > kRankMost; ++c) {       // the largest batch of each number of items to a thread
+        const uint32_t n = max_batch < ends[c] ? max_batch : ends[c];
+        const int ipt = items_of(n), passes = token_passes(key_bits, ipt);
+        const size_t bins = (size_t)1 << ((key_bits + passes - 1) / passes);
+        const size_t t = tiles_of(n, ipt), g = group_of((uint32_t)t);
+        if (t > tiles) tiles = t;
+        if (t * bins * (ipt == 8 ? 4 : 2) > table) table = t * bins * (ipt == 8 ? 4 : 2);
+        if (ipt == 8 && (t + g - 1) / g * bins > sums) sums = (t + g - 1) / g * bins;
+    }
+    l.off_ctl = take(sizeof(TokenControl));
+    l.off_flags = take(tiles * 4);
+    l.off_table = take(table);
+    l.off_groups = take(sums * 4);
+    l.end = off;
+    return l;
+}
+
+template <bool FIRST, int IPT>
+static void launch_scatter(const TokenPass &a, uint32_t clears, hipStream_t st)
+{
+    constexpr bool grouped = IPT == 8;
+    const dim3 grid(a.tiles + clears), block(kTokenThreads);
+    const size_t lds = scatter_lds(a.bits, IPT);
+    if (a.bits <= 9) hipLaunchKernelGGL((token_scatter_kernel<FIRST, IPT, 1, grouped>), grid, block, lds, st, a);
+    else if (a.bits == 10) hipLaunchKernelGGL((token_scatter_kernel<FIRST, IPT, 2, grouped>), grid, block, lds, st, a);
+    else hipLaunchKernelGGL((token_scatter_kernel<FIRST, IPT, 4, grouped>), grid, block, lds, st, a);
+}
+
+template <int IPT>
+static void launch_token_pass(const TokenPass &a, bool first, uint32_t clears, hipStream_t st)
+{
+    constexpr bool grouped = IPT == 8;
+    const dim3 hist(a.tiles), block(kTokenThreads);
+    if (first) hipLaunchKernelGGL((token_hist_kernel<true, IPT, grouped>), hist, block, 0, st, a);
+    else hipLaunchKernelGGL((token_hist_kernel<false, IPT, grouped>), hist, block, 0, st, a);
+    if (grouped) hipLaunchKernelGGL(token_groups_kernel, dim3(a.groups, ((1u << a.bits) + 255u) / 256u), dim3(256), 0, st, a);
+    if (first) launch_scatter<true, IPT>(a, clears, st);
+    else launch_scatter<false, IPT>(a, clears, st);
+}
+
+TokenSort launch_token_sort(const Scratch &s, const TokenSortLayout &l, const uint64_t *keys, uint32_t n, uint64_t padding, uint32_t rows,
+                            int key_bits, ClearJob clear, int cus, hipStream_t st)
+{
+    char *base = (char *)s.hdr;
+    TokenPass a{};
+    a.keys64 = keys; a.n = n; a.padding = padding; a.rows = rows; a.hdr = s.hdr;
+    a.ctl = (TokenControl *)(base + l.off_ctl);
+    a.flags = (uint32_t *)(base + l.off_flags);
+    a.table = (uint16_t *)(base + l.off_table);
+    a.sums = (uint32_t *)(base + l.off_groups);
+    TokenSort r;
+    r.ctl = a.ctl;
+    const uint32_t clears = clear.to ? (uint32_t)cus * 4u : 0u;
+    if (n <= kRankMost) {
+        const uint32_t each = kRankItems * (kRankThreads / kWave);
+        a.tiles = (n + each - 1) / each;
+        a.keys_out = s.keys[0]; a.vals_out = s.vals[0];
+        a.clear = clear;
+        hipLaunchKernelGGL(token_rank_kernel, dim3(a.tiles + clears), dim3(kRankThreads), 0, st, a);
+        r.sk = s.keys[0];
+        r.si = s.vals[0];
+        return r;
+    }
+    const int ipt = items_of(n), passes = token_passes(key_bits, ipt);
+    a.tiles = tiles_of(n, ipt);
+    a.group = group_of(a.tiles);
+    a.groups = (a.tiles + a.group - 1) / a.group;
+    // the clearing, a part beside each digit's scatter
+    const uint64_t part = (clear.sixteens + passes - 1) / passes;
+    int shift = 0;
+    for (int p = 0; p < passes; ++p) {
+        const int out = p & 1;
+        a.shift = shift;
+        a.bits = (key_bits - shift + passes - p - 1) / (passes - p);
+        a.keys = s.keys[out ^ 1]; a.vals = s.vals[out ^ 1];
+        a.keys_out = s.keys[out]; a.vals_out = s.vals[out];
+        a.clear.to = clear.to ? (char *)clear.to + p * part * 16 : nullptr;
+        a.clear.sixteens = (uint64_t)p * part >= clear.sixteens ? 0 : clear.sixteens - p * part < part ? clear.sixteens - p * part : part;
+        if (ipt == 2) launch_token_pass<2>(a, p == 0, clears, st);
+        else if (ipt == 4) launch_token_pass<4>(a, p == 0, clears, st);
+        else launch_token_pass<8>(a, p == 0, clears, st);
+        shift += a.bits;
+        r.sk = s.keys[out];
+        r.si = s.vals[out];
+    }
+    return r;
+}
+
+}  // namespace ecrm
