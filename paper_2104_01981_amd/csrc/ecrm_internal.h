@@ -289,7 +289,7 @@ struct TokenControl {
     uint32_t bad;                  // the batch has a key out of range: nothing of it counts
     uint32_t valid;                // tokens that are rows; they are what the sort leaves
     uint32_t distinct;             // distinct rows among them, where one kernel counts them for all
-    uint32_t joins[2];             // runs that go over several workgroups, and over many
+    uint32_t joins;                // runs that go over many workgroups
 };
 // Grouping of a batch's tokens (token_sort.hip): its arrays in the scratch buffer, from byte `off` on, and what a call makes of them.
 struct TokenSortLayout { size_t off_ctl, off_flags, off_table, off_groups, end; };
@@ -306,7 +306,7 @@ constexpr uint32_t kRankMost = 8192;   // tokens of a batch that is sorted in on
 // The arrays of a gradient call.
 struct EmbedGradLayout {
     TokenSortLayout sort;
-    size_t off_first, off_state, off_join, off_part, end;
+    size_t off_first, off_group, off_state, off_dest, off_join, off_part, end;
 };
 EmbedGradLayout embed_grad_layout(size_t off, uint32_t max_batch, uint32_t D, int key_bits);
 // out_keys null: the dense form
@@ -350,6 +350,8 @@ __device__ __forceinline__ uint32_t tile_of_block(uint32_t b, uint32_t nblocks)
     return b;
 #endif
 }
+
+__device__ __forceinline__ bool is_padding(uint64_t key, uint64_t padding) { return key == padding && key != ECRM_NO_PADDING; }
 
 // What workgroups of one launch leave each other is written and read by relaxed atomics of device scope: they pass by the
 // caches that the XCDs do not share.  published() waits until a wave's are done, so that a flag or a count written next is

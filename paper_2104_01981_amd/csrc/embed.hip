@@ -73,7 +73,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(EmbedArgs a)
     const uint32_t cnt = (uint32_t)(a.n - first < a.per ? a.n - first : a.per);
     const bool in = lane < cnt;
     const uint64_t key = in ? a.keys[first + lane] : 0ull;
-    const bool pad = in && key == a.padding && key != ECRM_NO_PADDING, bad = in && !pad && key >= (uint64_t)a.geo.rows;
+    const bool pad = in && is_padding(key, a.padding), bad = in && !pad && key >= (uint64_t)a.geo.rows;
     if (bad) atomicOr(&a.hdr->err_sticky, 1u);
     const uint32_t x = pad ? kNoKey : (uint32_t)key;
     bool lost = false;

@@ -11,20 +11,29 @@ namespace ecrm {
 
 constexpr int kSumThreads = 256;
 constexpr uint32_t kSumMost = 2048;       // sorted positions of a workgroup, at most
-constexpr uint32_t kOneBlock = 2048;      // batches of so many tokens are cut by columns, not by positions: nothing is left to join
-constexpr uint32_t kOneUnits = 4;         // of four columns, of a workgroup there
+constexpr uint32_t kSortHere = 256;       // batches of so many tokens are sorted by every workgroup for itself
+constexpr uint32_t kOneBlock = 1536;      // batches of so many tokens are cut by columns, not by positions: nothing is left to join
+constexpr uint32_t kOneUnits = 2;         // of four columns, of a workgroup there
 constexpr uint32_t kSumBlocks = 2048;     // workgroups, unless that would be more positions to one than there is room for
-constexpr uint32_t kScanBlocks = 4096;    // from more on their counts are added up by a launch of its own
+constexpr uint32_t kCountThreads = 1024;
+constexpr uint32_t kCountGroup = 8;       // workgroups whose distinct rows are counted together
+constexpr uint32_t kScanGroups = 512;     // from more on these counts are added up by a launch of its own
 constexpr uint32_t kChunkMin = 4, kChunkMax = 128;
+constexpr uint64_t kStreamBytes = 100ull << 20;
 constexpr uint32_t kJoinUnits = 16;       // of four columns, of a job
 constexpr uint32_t kLongJoin = 16;        // workgroups from which on a run is a long one
 
-// What a workgroup has of a run that goes on before it (and maybe behind it) and of one that begins in it and goes on behind it.
-enum { kPartHead = 1, kPartThrough = 2, kPartTail = 4 };
+// What a workgroup has of a run that goes on before it (and maybe behind it) and of one that begins in it and goes on behind it
+// (by more than kLongJoin workgroups).
+enum { kPartHead = 1, kPartThrough = 2, kPartTail = 4, kPartLong = 8 };
 // Where the number of distinct rows before a workgroup's positions comes from.
 enum { kCountKeys = 0, kAddCounts = 1, kScanned = 2, kAllHere = 3 };
 
 struct SumArgs {
+    const uint64_t *keys;            // up to kSortHere tokens: the caller's
+    uint64_t padding;
+    uint32_t rows;
+    Header *hdr;
     const uint32_t *sk, *si;         // sorted: row, index of the gradient
     uint32_t n, D;
     uint32_t quads;                  // D / 4
@@ -37,47 +46,73 @@ struct SumArgs {
     double scale;
     uint32_t accumulate;             // dense: add to what is there
     TokenControl *ctl;
-    uint32_t *first;                 // [blocks] distinct rows that begin in the workgroup's positions; scanned: before them
+    uint32_t groups;                 // of kCountGroup workgroups
+    uint32_t *first;                 // [blocks] distinct rows that begin in the group's positions before the workgroup's
+    uint32_t *group;                 // [groups] distinct rows that begin in it; scanned: before it
     uint32_t *state;                 // [blocks] kPart*
-    uint2 *join;                     // [2][blocks] workgroups with a kPartTail and the rows of the output that it belongs to, in any
-                                     // order: of runs over up to kLongJoin workgroups, and of longer ones
+    uint32_t *dest;                  // [blocks] row of the output that a kPartTail belongs to
+    uint32_t *join;                  // [blocks] workgroups with a kPartLong, in any order
     double *part;                    // [blocks][2][D]: head, tail
     uint64_t *out_keys;              // rows form
     float *out;
     uint64_t *count;
 };
 
-// sum of v over the workgroup, to all
-__device__ __forceinline__ uint32_t block_total(uint32_t v, uint32_t *s_wave)
+// sums of v and w over the workgroup, to all
+__device__ __forceinline__ uint32_t block_totals(uint32_t v, uint32_t w, uint2 *s_wave, uint32_t &of_w)
 {
 #pragma unroll
-    for (int by = 1; by < kWave; by <<= 1) v += (uint32_t)__shfl_xor((int)v, by, kWave);
-    if (lane_id() == 0) s_wave[threadIdx.x / kWave] = v;
+    for (int by = 1; by < kWave; by <<= 1) {
+        v += (uint32_t)__shfl_xor((int)v, by, kWave);
+        w += (uint32_t)__shfl_xor((int)w, by, kWave);
+    }
+    if (lane_id() == 0) s_wave[threadIdx.x / kWave] = uint2{v, w};
     __syncthreads();
-    v = 0;
+    v = of_w = 0;
 #pragma unroll
-    for (int w = 0; w < kSumThreads / kWave; ++w) v += s_wave[w];
-    __syncthreads();
+    for (int i = 0; i < kSumThreads / kWave; ++i) {
+        v += s_wave[i].x;
+        of_w += s_wave[i].y;
+    }
     return v;
 }
 
-__global__ __launch_bounds__(kSumThreads) void count_heads_kernel(SumArgs a)
+__global__ __launch_bounds__(kCountThreads) void count_heads_kernel(SumArgs a)
 {
-    __shared__ uint32_t s_wave[kSumThreads / kWave];
-    const uint32_t valid = a.ctl->valid, pos0 = blockIdx.x * a.per, end = min(pos0 + a.per, valid);
-    uint32_t heads = 0;
-    for (uint32_t p = pos0 + threadIdx.x; p < end; p += kSumThreads) heads += p == 0 || a.sk[p - 1] != a.sk[p] ? 1u : 0u;
-    heads = block_total(heads, s_wave);
-    if (threadIdx.x == 0) a.first[blockIdx.x] = heads;
+    __shared__ uint32_t s_heads[kCountGroup];
+    const uint32_t tid = threadIdx.x;
+    if (tid < kCountGroup) s_heads[tid] = 0;
+    __syncthreads();
+    const uint64_t pos0 = (uint64_t)blockIdx.x * kCountGroup * a.per;
+    const uint32_t cnt = (uint32_t)min((uint64_t)kCountGroup * a.per, a.n - pos0), valid = a.ctl->valid;
+    for (uint32_t i0 = 0; i0 < cnt; i0 += kCountThreads) {
+        const uint32_t i = i0 + tid, p = min((uint32_t)pos0 + i, a.n - 1u), key = a.sk[p], last = a.sk[p ? p - 1u : 0u];
+        const bool head = i < cnt && p < valid && (p == 0 || key != last);
+        // a wave's at once where they are one workgroup's
+        const uint32_t w0 = (i - lane_id()) / a.per;
+        if ((i - lane_id() + kWave - 1u) / a.per == w0) {
+            const unsigned long long m = __ballot(head);
+            if (lane_id() == 0 && m) atomicAdd(&s_heads[w0], (uint32_t)__popcll(m));
+        } else if (head) {
+            atomicAdd(&s_heads[i / a.per], 1u);
+        }
+    }
+    __syncthreads();
+    if (tid >= kCountGroup) return;
+    uint32_t before = 0;
+    for (uint32_t j = 0; j < tid; ++j) before += s_heads[j];
+    const uint32_t b = blockIdx.x * kCountGroup + tid;
+    if (b < a.blocks) a.first[b] = before;
+    if (tid == kCountGroup - 1) a.group[blockIdx.x] = before + s_heads[tid];
 }
 
-// exclusive sums of the workgroups' counts in place; their total is the number of distinct rows
+// exclusive sums of the groups' counts in place; their total is the number of distinct rows
 __global__ __launch_bounds__(1024) void scan_heads_kernel(SumArgs a)
 {
     __shared__ uint32_t s_wave[16];
     uint32_t carry = 0;
-    for (uint32_t b0 = 0; b0 < a.blocks; b0 += 1024u) {
-        const uint32_t i = b0 + threadIdx.x, v = i < a.blocks ? a.first[i] : 0u;
+    for (uint32_t b0 = 0; b0 < a.groups; b0 += 1024u) {
+        const uint32_t i = b0 + threadIdx.x, v = i < a.groups ? a.group[i] : 0u;
         uint32_t incl = v;
 #pragma unroll
         for (int d = 1; d < kWave; d <<= 1) {
@@ -91,33 +126,36 @@ __global__ __launch_bounds__(1024) void scan_heads_kernel(SumArgs a)
             if (w < threadIdx.x / kWave) before += s_wave[w];
             carry += s_wave[w];
         }
-        if (i < a.blocks) a.first[i] = before + incl - v;
+        if (i < a.groups) a.group[i] = before + incl - v;
         __syncthreads();
     }
     if (threadIdx.x == 0) a.ctl->distinct = carry;
 }
 
 // The distinct rows before sorted position pos0, and (valid, not SCANNED) in all.
-__device__ __forceinline__ uint32_t distinct_before(const SumArgs &a, uint32_t pos0, uint32_t valid, uint32_t *s_wave, uint32_t &distinct)
+__device__ __forceinline__ uint32_t distinct_before(const SumArgs &a, uint32_t pos0, uint32_t valid, uint2 *s_wave, uint32_t &distinct)
 {
     if (a.counting == kScanned) {
         distinct = a.ctl->distinct;
-        return a.first[blockIdx.x];
+        return a.group[blockIdx.x / kCountGroup] + a.first[blockIdx.x];
     }
     const uint32_t tid = threadIdx.x;
     uint32_t before = 0, all = 0;
     if (a.counting == kAddCounts) {
-#pragma unroll 4
-        for (uint32_t b = tid; b < a.blocks; b += kSumThreads) {
-            const uint32_t c = a.first[b];
-            all += c;
-            before += b < blockIdx.x ? c : 0u;
+        const uint32_t own = blockIdx.x / kCountGroup;
+        const uint32_t here = a.first[blockIdx.x];
+#pragma unroll
+        for (uint32_t j = 0; j < kScanGroups / kSumThreads; ++j) {
+            const uint32_t g = j * kSumThreads + tid, c = a.group[min(g, a.groups - 1u)];
+            all += g < a.groups ? c : 0u;
+            before += g < own ? c : 0u;
         }
+        if (tid == 0) before += here;
     } else {
 #pragma unroll 2
         for (uint32_t p = tid * 4u; p < valid; p += 4u * kSumThreads) {
             const uint4 k = *(const uint4 *)(a.sk + p);        // room for a multiple of four
-            const uint32_t last = p ? a.sk[p - 1u] : kNoKey;
+            const uint32_t left = a.sk[p ? p - 1u : 0u], last = p ? left : kNoKey;
             const uint32_t h[4] = {k.x != last ? 1u : 0u, k.y != k.x ? 1u : 0u, k.z != k.y ? 1u : 0u, k.w != k.z ? 1u : 0u};
 #pragma unroll
             for (uint32_t q = 0; q < 4u; ++q) {
@@ -126,10 +164,10 @@ __device__ __forceinline__ uint32_t distinct_before(const SumArgs &a, uint32_t p
             }
         }
     }
-    distinct = block_total(all, s_wave);
-    return block_total(before, s_wave);
+    return block_totals(before, all, s_wave, distinct);
 }
 
+template <bool STREAM>
 __device__ __forceinline__ void write_sum(const SumArgs &a, uint32_t row, uint32_t c, const double (&v)[4])
 {
     f32x4 *to = (f32x4 *)(a.out + (size_t)row * a.D + c);
@@ -143,32 +181,92 @@ __device__ __forceinline__ void write_sum(const SumArgs &a, uint32_t row, uint32
         s[2] += (double)old.z;
         s[3] += (double)old.w;
     }
-    *to = f32x4{(float)s[0], (float)s[1], (float)s[2], (float)s[3]};
+    const f32x4 sum = {(float)s[0], (float)s[1], (float)s[2], (float)s[3]};
+    if (STREAM) __builtin_nontemporal_store(sum, to);
+    else *to = sum;
 }
 
-template <typename T, bool DENSE>
+// Sorts the batch's tokens, one to a thread, into s_key (position i's at i + 1) and s_idx: how many are rows; none if one is bad.
+__device__ __forceinline__ uint32_t sort_here(const SumArgs &a, uint32_t *s_raw, uint32_t *s_key, uint32_t *s_idx, uint2 *s_wave)
+{
+    const uint32_t tid = threadIdx.x, n = a.n;
+    const uint64_t word = a.keys[min(tid, n - 1u)];
+    const bool in = tid < n, pad = in && is_padding(word, a.padding), bad = in && !pad && word >= (uint64_t)a.rows;
+    const uint32_t key = in && !pad ? (uint32_t)word : kNoKey;
+    s_raw[tid] = key;
+    uint32_t bads;
+    const uint32_t pads = block_totals(pad ? 1u : 0u, bad ? 1u : 0u, s_wave, bads);      // a barrier
+    const uint32_t valid = bads ? 0u : n - pads, wave0 = tid / kWave * kWave, end = (n + 3u) / 4u * 4u;
+    if (bads && tid == 0 && blockIdx.y == 0) atomicOr(&a.hdr->err_sticky, 1u);
+    uint32_t at = 0;                                     // tokens before: of equal ones those of smaller index
+#pragma unroll 8
+    for (uint32_t j = 0; j < wave0; j += 4u) {
+        const uint4 k = *(const uint4 *)(s_raw + j);
+        at += (k.x <= key ? 1u : 0u) + (k.y <= key ? 1u : 0u) + (k.z <= key ? 1u : 0u) + (k.w <= key ? 1u : 0u);
+    }
+#pragma unroll 4
+    for (uint32_t j = wave0; j < min(wave0 + kWave, end); j += 4u) {
+        const uint4 k = *(const uint4 *)(s_raw + j);
+        at += (k.x < key || (k.x == key && j < tid) ? 1u : 0u) + (k.y < key || (k.y == key && j + 1u < tid) ? 1u : 0u) +
+              (k.z < key || (k.z == key && j + 2u < tid) ? 1u : 0u) + (k.w < key || (k.w == key && j + 3u < tid) ? 1u : 0u);
+    }
+#pragma unroll 8
+    for (uint32_t j = wave0 + kWave; j < end; j += 4u) {
+        const uint4 k = *(const uint4 *)(s_raw + j);
+        at += (k.x < key ? 1u : 0u) + (k.y < key ? 1u : 0u) + (k.z < key ? 1u : 0u) + (k.w < key ? 1u : 0u);
+    }
+    if (in && !pad && !bads) {
+        s_key[at + 1u] = key;
+        s_idx[at] = tid;
+    }
+    if (tid == 0) s_key[0] = s_key[valid + 1u] = kNoKey;
+    return valid;
+}
+
+// STREAM: more goes through than the memory-side cache holds.  HERE: up to kSortHere tokens, sorted here.
+template <typename T, bool DENSE, bool STREAM, bool HERE>
 __global__ __launch_bounds__(kSumThreads) void sum_runs_kernel(SumArgs a)
 {
     typedef typename Quad<T>::type Four;
-    constexpr uint32_t U = 4;                            // rows in flight
-    __shared__ uint32_t s_key[kSumMost + 2];             // position i's at i + 1
-    __shared__ uint32_t s_idx[kSumMost];
-    __shared__ unsigned long long s_head[kSumMost / kWave];
-    __shared__ uint32_t s_rank[kSumMost / kWave];        // of the heads before it
-    __shared__ uint32_t s_state[kSumThreads], s_all, s_dest, s_key_of_tail, s_wave[kSumThreads / kWave];
+    constexpr uint32_t U = STREAM ? 8 : 4;               // rows in flight
+    extern __shared__ uint32_t lds[];
+    uint32_t *s_key = lds, *s_idx = lds + a.per + 2u;    // position i's key at i + 1
+    __shared__ unsigned long long s_head[DENSE ? 1 : kSumMost / kWave];
+    __shared__ uint32_t s_rank[DENSE ? 1 : kSumMost / kWave];          // of the heads before it
+    __shared__ uint32_t s_state[kSumThreads], s_all, s_dest, s_key_of_tail, s_all_heads;
+    __shared__ uint2 s_wave[kSumThreads / kWave];
+    __shared__ unsigned long long s_through[kSumThreads / kWave];
     __shared__ double s_part[2][kSumThreads][4];
     const uint32_t tid = threadIdx.x, b = blockIdx.x;
     const uint32_t pos0 = b * a.per, room = min(a.per, a.n - pos0);
     const bool lists = !DENSE && blockIdx.y == 0;        // the keys are written once, not for every slice of columns
-    for (uint32_t i = tid; i < room + 2u; i += kSumThreads) {          // behind `valid` the buffers hold anything
-        s_key[i] = pos0 + i >= 1u && pos0 + i - 1u < a.n ? a.sk[pos0 + i - 1u] : kNoKey;
-        if (i < room) s_idx[i] = a.si[pos0 + i];
-    }
+    uint32_t valid;
     s_state[tid] = 0;
     if (tid == 0) s_all = 0;
-    const uint32_t valid = a.ctl->bad ? 0u : a.ctl->valid, cnt = pos0 < valid ? min(room, valid - pos0) : 0u;
+    if (HERE) {
+        __shared__ __align__(16) uint32_t s_raw[HERE ? kSortHere : 1];
+        valid = sort_here(a, s_raw, s_key, s_idx, s_wave);
+    } else {
+        for (uint32_t i0 = 0; i0 < room + 2u; i0 += 4u * kSumThreads) {    // behind `valid` the buffers hold anything
+            uint32_t key[4], idx[4];
+#pragma unroll
+            for (uint32_t q = 0; q < 4u; ++q) {
+                const uint32_t i = i0 + q * kSumThreads + tid;
+                key[q] = a.sk[min(max(pos0 + i, 1u) - 1u, a.n - 1u)];
+                idx[q] = a.si[min(pos0 + i, a.n - 1u)];
+            }
+#pragma unroll
+            for (uint32_t q = 0; q < 4u; ++q) {
+                const uint32_t i = i0 + q * kSumThreads + tid;
+                if (i < room + 2u) s_key[i] = pos0 + i >= 1u && pos0 + i - 1u < a.n ? key[q] : kNoKey;
+                if (i < room) s_idx[i] = idx[q];
+            }
+        }
+        valid = a.ctl->bad ? 0u : a.ctl->valid;
+    }
+    const uint32_t cnt = pos0 < valid ? min(room, valid - pos0) : 0u;
     __syncthreads();
-    if (cnt < room || pos0 + room == valid) {
+    if (!HERE && (cnt < room || pos0 + room == valid)) {
         if (tid == 0) s_key[cnt + 1u] = kNoKey;
         __syncthreads();
     }
@@ -181,7 +279,10 @@ __global__ __launch_bounds__(kSumThreads) void sum_runs_kernel(SumArgs a)
     Four v[U];
     auto load = [&](uint32_t i0) {
 #pragma unroll
-        for (uint32_t q = 0; q < U; ++q) v[q] = *(const Four *)(d + (size_t)s_idx[min(i0 + q, hi - 1u)] * a.stride);
+        for (uint32_t q = 0; q < U; ++q) {
+            const Four *row = (const Four *)(d + (size_t)s_idx[min(i0 + q, hi - 1u)] * a.stride);
+            v[q] = STREAM ? __builtin_nontemporal_load(row) : *row;
+        }
     };
     if (live && lo < hi) load(lo);
     if (!DENSE) {
@@ -202,10 +303,10 @@ __global__ __launch_bounds__(kSumThreads) void sum_runs_kernel(SumArgs a)
                 if (tid >= (uint32_t)by) incl += t;
             }
             if (tid < words) s_rank[tid] = first + incl - heads;
-            if (tid == kWave / 2 - 1) s_wave[0] = incl;
+            if (tid == kWave / 2 - 1) s_all_heads = incl;
         }
         __syncthreads();
-        if (a.counting == kAllHere) distinct = s_wave[0];
+        if (a.counting == kAllHere) distinct = s_all_heads;
         if (valid == 0) distinct = 0;
         if (lists) {
             if (b == 0 && tid == 0) *a.count = distinct;
@@ -245,7 +346,7 @@ __global__ __launch_bounds__(kSumThreads) void sum_runs_kernel(SumArgs a)
                     state = kPartHead;
                     before = false;
                 } else {
-                    write_sum(a, DENSE ? s_key[i + 1] : rank(i), c, acc);
+                    write_sum<STREAM>(a, DENSE ? s_key[i + 1] : rank(i), c, acc);
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) acc[j] = 0;
@@ -260,32 +361,45 @@ __global__ __launch_bounds__(kSumThreads) void sum_runs_kernel(SumArgs a)
         if (mine == 0) s_state[team] = state;
     }
     __syncthreads();
+    const unsigned long long through = __ballot((s_state[tid] & kPartThrough) != 0);       // of teams; there are no more than threads
+    if (lane_id() == 0) s_through[tid / kWave] = through;
+    __syncthreads();
     if (live) {
         const uint32_t state = s_state[team];
-        auto join = [&](uint32_t t, double (&acc)[4], bool through) {       // the run goes on behind team t
-            while (through && ++t < a.teams) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[j] += s_part[0][t * a.units.d + mine][j];
-                through = (s_state[t] & kPartThrough) != 0;
+        // adds the parts behind team t's of a run that goes on there: does it go on behind the workgroup, too?
+        auto join = [&](uint32_t t, double (&acc)[4]) {
+            uint32_t end = a.teams;                      // the first behind t that the run does not go on behind
+            for (uint32_t w = (t + 1u) / kWave; w < (uint32_t)(kSumThreads / kWave); ++w) {
+                unsigned long long ends = ~s_through[w];
+                if (w == (t + 1u) / kWave) ends &= ~0ull << ((t + 1u) % kWave);
+                if (ends) {
+                    end = min(end, w * kWave + (uint32_t)__builtin_ctzll(ends));
+                    break;
+                }
             }
-            return through;
+            const uint32_t last = min(end + 1u, a.teams);
+#pragma unroll 4
+            for (uint32_t p = t + 1u; p < last; ++p)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[j] += s_part[0][p * a.units.d + mine][j];
+            return end == a.teams;
         };
         if (team == 0 && (state & kPartHead)) {
             double acc[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) acc[j] = s_part[0][tid][j];
-            const bool through = join(0, acc, (state & kPartThrough) != 0);
+            const bool on = (state & kPartThrough) && join(0, acc);
             double *to = a.part + (size_t)b * 2u * a.D + c;
 #pragma unroll
             for (int j = 0; j < 4; ++j) to[j] = acc[j];
-            if (mine == 0) atomicOr(&s_all, through ? kPartHead | kPartThrough : kPartHead);
+            if (mine == 0) atomicOr(&s_all, on ? kPartHead | kPartThrough : kPartHead);
         }
         if (state & kPartTail) {
             double acc[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) acc[j] = s_part[1][tid][j];
             const uint32_t row = DENSE ? s_key[tail_at + 1] : rank(tail_at);
-            if (join(team, acc, true)) {
+            if (join(team, acc)) {
                 double *to = a.part + ((size_t)b * 2u + 1u) * a.D + c;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) to[j] = acc[j];
@@ -295,19 +409,23 @@ __global__ __launch_bounds__(kSumThreads) void sum_runs_kernel(SumArgs a)
                     s_key_of_tail = s_key[tail_at + 1];
                 }
             } else {
-                write_sum(a, row, c, acc);
+                write_sum<STREAM>(a, row, c, acc);
             }
         }
     }
     if (a.blocks == 1) return;
     __syncthreads();
     if (tid == 0) {
-        a.state[b] = s_all;
-        if (s_all & kPartTail) {
+        uint32_t state = s_all;
+        if (state & kPartTail) {
+            a.dest[b] = s_dest;
             const uint64_t far = ((uint64_t)b + kLongJoin) * a.per;
-            const uint32_t kind = far < valid && a.sk[far] == s_key_of_tail ? 1u : 0u;
-            a.join[(size_t)kind * a.blocks + atomicAdd(&a.ctl->joins[kind], 1u)] = uint2{b, s_dest};
+            if (far < valid && a.sk[far] == s_key_of_tail) {
+                state |= kPartLong;
+                a.join[atomicAdd(&a.ctl->joins, 1u)] = b;
+            }
         }
+        a.state[b] = state;
     }
 }
 
@@ -341,27 +459,29 @@ __global__ __launch_bounds__(kSumThreads) void join_runs_kernel(SumArgs a, uint3
     __shared__ double s_part[kSumThreads][4];
     const uint32_t tid = threadIdx.x, narrow = gridDim.x - wide;
     if (blockIdx.x < narrow) {
-        const uint32_t team = a.units.div(tid), c = (tid - team * a.units.d) * 4u, cnt = a.ctl->joins[0];
+        const uint32_t team = a.units.div(tid), c = (tid - team * a.units.d) * 4u;
         if (team >= a.teams) return;
-        for (uint32_t i = blockIdx.x * a.teams + team; i < cnt; i += narrow * a.teams) {
-            const uint2 what = a.join[i];
+        for (uint32_t first = blockIdx.x * a.teams + team; first < a.blocks; first += narrow * a.teams) {
+            if ((a.state[first] & (kPartTail | kPartLong)) != kPartTail) continue;
+            const uint32_t to = a.dest[first];
             double acc[4] = {0, 0, 0, 0};
-            add_part(a, what.x, 1u, c, acc);
-            for (uint32_t b = what.x + 1u; b < a.blocks; ++b) {
-                const bool on = (a.state[b] & kPartThrough) != 0;
-                add_part(a, b, 0u, c, acc);
-                if (!on) break;
-            }
-            write_sum(a, what.y, c, acc);
+            add_part(a, first, 1u, c, acc);
+            uint32_t on = 0;                             // the workgroups behind: does the run go on behind them, too?
+#pragma unroll
+            for (uint32_t j = 0; j < kLongJoin; ++j) on |= (a.state[min(first + 1u + j, a.blocks - 1u)] & kPartThrough ? 1u : 0u) << j;
+            const uint32_t parts = (uint32_t)__builtin_ctz(~on) + 1u;
+#pragma unroll 4
+            for (uint32_t j = 0; j < parts; ++j) add_part(a, first + 1u + j, 0u, c, acc);
+            write_sum<false>(a, to, c, acc);
         }
         return;
     }
     const uint32_t units = min(a.quads, kJoinUnits), groups = (a.quads + units - 1) / units, slices = kSumThreads / units;
-    const uint32_t slice = tid / units, jobs = a.ctl->joins[1] * groups;
+    const uint32_t slice = tid / units, jobs = a.ctl->joins * groups;
     for (uint32_t job = blockIdx.x - narrow; job < jobs; job += wide) {
-        const uint2 what = a.join[(size_t)a.blocks + job / groups];
+        const uint32_t first = a.join[job / groups];
         const uint32_t unit = job % groups * units + tid % units, c = unit * 4u;
-        const uint32_t begin = what.x + 1u, parts = run_end(a, what.x) - begin, each = (parts + slices - 1) / slices;
+        const uint32_t begin = first + 1u, parts = run_end(a, first) - begin, each = (parts + slices - 1) / slices;
         const bool live = slice < slices && unit < a.quads;
         double acc[4] = {0, 0, 0, 0};
         if (live) {
@@ -374,11 +494,11 @@ __global__ __launch_bounds__(kSumThreads) void join_runs_kernel(SumArgs a, uint3
         __syncthreads();
         if (live && slice == 0) {
             double all[4] = {0, 0, 0, 0};
-            add_part(a, what.x, 1u, c, all);
+            add_part(a, first, 1u, c, all);
             for (uint32_t t = 0; t < slices && t * each < parts; ++t)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) all[j] += s_part[t * units + tid][j];
-            write_sum(a, what.y, c, all);
+            write_sum<false>(a, a.dest[first], c, all);
         }
         __syncthreads();
     }
@@ -424,11 +544,22 @@ EmbedGradLayout embed_grad_layout(size_t off, uint32_t max_batch, uint32_t D, in
     const uint32_t blocks = max_batch <= kOneBlock ? 1u : p.blocks > kSumBlocks ? p.blocks : kSumBlocks;
     auto take = [&](size_t bytes) { const size_t o = off; off = (off + bytes + 255) / 256 * 256; return o; };
     l.off_first = take((size_t)blocks * 4);
+    l.off_group = take(((size_t)blocks / kCountGroup + 1) * 4);
     l.off_state = take((size_t)blocks * 4);
-    l.off_join = take((size_t)blocks * 2 * sizeof(uint2));
+    l.off_dest = take((size_t)blocks * 4);
+    l.off_join = take((size_t)blocks * 4);
     l.off_part = take((size_t)blocks * 2 * D * sizeof(double));
     l.end = off;
     return l;
+}
+
+template <typename T, bool DENSE>
+static void launch_sum(const SumArgs &a, dim3 grid, size_t lds, bool stream, hipStream_t st)
+{
+    const dim3 threads(kSumThreads);
+    if (a.keys) hipLaunchKernelGGL((sum_runs_kernel<T, DENSE, false, true>), grid, threads, lds, st, a);
+    else if (stream) hipLaunchKernelGGL((sum_runs_kernel<T, DENSE, true, false>), grid, threads, lds, st, a);
+    else hipLaunchKernelGGL((sum_runs_kernel<T, DENSE, false, false>), grid, threads, lds, st, a);
 }
 
 void launch_embed_grad(const Scratch &s, const EmbedGradLayout &l, const Geometry &g, int key_bits, const uint64_t *keys,
@@ -445,26 +576,35 @@ void launch_embed_grad(const Scratch &s, const EmbedGradLayout &l, const Geometr
         return;
     }
     char *base = (char *)s.hdr;
-    const TokenSort sorted = launch_token_sort(s, l.sort, keys, n, padding, g.rows, key_bits, clear, cus, st);
     SumArgs a{};
+    if (n <= kSortHere && !clear.to) {
+        a.keys = keys; a.padding = padding; a.rows = g.rows; a.hdr = s.hdr;
+    } else {
+        const TokenSort sorted = launch_token_sort(s, l.sort, keys, n, padding, g.rows, key_bits, clear, cus, st);
+        a.sk = sorted.sk; a.si = sorted.si; a.ctl = sorted.ctl;
+    }
     const SumPlan p = sum_plan(n, g.D);
-    a.sk = sorted.sk; a.si = sorted.si; a.ctl = sorted.ctl;
     a.n = n; a.D = g.D; a.quads = g.D / 4u; a.units = make_divider(p.units);
     a.teams = p.teams; a.chunk = p.chunk; a.per = p.per; a.blocks = p.blocks;
     a.d = d; a.stride = stride; a.scale = (double)scale; a.accumulate = accumulate ? 1u : 0u;
     a.first = (uint32_t *)(base + l.off_first);
+    a.group = (uint32_t *)(base + l.off_group);
+    a.groups = (a.blocks + kCountGroup - 1) / kCountGroup;
     a.state = (uint32_t *)(base + l.off_state);
-    a.join = (uint2 *)(base + l.off_join);
+    a.dest = (uint32_t *)(base + l.off_dest);
+    a.join = (uint32_t *)(base + l.off_join);
     a.part = (double *)(base + l.off_part);
     a.out_keys = out_keys; a.out = out; a.count = count;
-    a.counting = a.blocks == 1 ? kAllHere : n <= kRankMost ? kCountKeys : a.blocks <= kScanBlocks ? kAddCounts : kScanned;
+    a.counting = a.blocks == 1 ? kAllHere : n <= kRankMost ? kCountKeys : a.groups <= kScanGroups ? kAddCounts : kScanned;
     if (!dense && (a.counting == kAddCounts || a.counting == kScanned)) {
-        hipLaunchKernelGGL(count_heads_kernel, dim3(a.blocks), threads, 0, st, a);
+        hipLaunchKernelGGL(count_heads_kernel, dim3(a.groups), dim3(kCountThreads), 0, st, a);
         if (a.counting == kScanned) hipLaunchKernelGGL(scan_heads_kernel, dim3(1), dim3(1024), 0, st, a);
     }
+    const size_t lds = ((size_t)a.per * 2 + 2) * 4;
+    const uint64_t moved = (uint64_t)n * g.D * type_bytes(type) + (dense ? (uint64_t)g.rows : n) * g.D * 4u;
     with_type(type, [&](auto t) {
-        if (dense) hipLaunchKernelGGL((sum_runs_kernel<decltype(t), true>), dim3(a.blocks, p.slices), threads, 0, st, a);
-        else hipLaunchKernelGGL((sum_runs_kernel<decltype(t), false>), dim3(a.blocks, p.slices), threads, 0, st, a);
+        if (dense) launch_sum<decltype(t), true>(a, dim3(a.blocks, p.slices), lds, moved > kStreamBytes, st);
+        else launch_sum<decltype(t), false>(a, dim3(a.blocks, p.slices), lds, moved > kStreamBytes, st);
     });
     if (a.blocks > 1) {
         const uint32_t narrow = (a.blocks + a.teams - 1) / a.teams, most = (uint32_t)cus * 8u, wide = (uint32_t)cus;

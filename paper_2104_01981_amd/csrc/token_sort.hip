@@ -16,6 +16,7 @@ constexpr int kTokenThreads = 512;
 constexpr int kTokenWaves = kTokenThreads / kWave;
 constexpr int kTokenBits = 11;                           // of a digit, at most
 constexpr uint32_t kDirectTiles = 128;
+constexpr uint32_t kLargeBatch = 2048u * 1024u;
 constexpr uint32_t kBadTile = 0x80000000u;
 
 struct TokenPass {
@@ -44,8 +45,6 @@ __device__ __forceinline__ void clear_share(const ClearJob &c, uint32_t block, u
         to[i] = u4{0u, 0u, 0u, 0u};
 }
 
-__device__ __forceinline__ bool is_padding(uint64_t key, uint64_t padding) { return key == padding && key != ECRM_NO_PADDING; }
-
 __global__ __launch_bounds__(kRankThreads) void token_rank_kernel(TokenPass a)
 {
     __shared__ __align__(16) uint32_t s_key[kRankMost];
@@ -62,7 +61,7 @@ __global__ __launch_bounds__(kRankThreads) void token_rank_kernel(TokenPass a)
     bool bad = false;
 #pragma unroll 4
     for (uint32_t i = tid; i < room; i += kRankThreads) {
-        const uint64_t key = i < n ? a.keys64[i] : 0ull;
+        const uint64_t key = a.keys64[min(i, n - 1u)];
         const bool pad = i < n && is_padding(key, a.padding);
         bad |= i < n && !pad && key >= (uint64_t)a.rows;
         pads += pad ? 1u : 0u;
@@ -76,7 +75,7 @@ __global__ __launch_bounds__(kRankThreads) void token_rank_kernel(TokenPass a)
     if (blockIdx.x == 0 && tid == 0) {
         a.ctl->bad = s_bad;
         a.ctl->valid = n - s_pads;
-        a.ctl->joins[0] = a.ctl->joins[1] = 0;
+        a.ctl->joins = 0;
         if (s_bad) atomicOr(&a.hdr->err_sticky, 1u);
     }
     const uint32_t i0 = (blockIdx.x * (kRankThreads / kWave) + wave) * kRankItems;
@@ -118,27 +117,27 @@ __global__ __launch_bounds__(kRankThreads) void token_rank_kernel(TokenPass a)
         const uint32_t k = s_key[i0 + q];
         at += k < x || (k == x && q < mine) ? 1u : 0u;
     }
-    if (i < n && !is_padding(a.keys64[i], a.padding)) {
+    if (i < n && x != kNoKey) {                          // no padding token
         a.keys_out[at] = x;
         a.vals_out[at] = i;
     }
 }
 
-// The sort key of item i, false where there is none.
+// Item i's word, or the last one's: loads without a branch, so that a thread's are in flight together.  Behind `valid` the
+// buffers of the later digits hold anything.
 template <bool FIRST>
-__device__ __forceinline__ bool token_at(const TokenPass &a, uint32_t i, uint32_t n, uint32_t &key, bool &pad, bool &bad)
+__device__ __forceinline__ uint64_t token_word(const TokenPass &a, uint32_t i)
 {
-    pad = bad = false;
-    if (i >= n) return false;
-    if (!FIRST) {
-        key = a.keys[i];
-        return true;
-    }
-    const uint64_t k = a.keys64[i];
-    pad = is_padding(k, a.padding);
-    bad = !pad && k >= (uint64_t)a.rows;                 // keeps its low bits: the batch is rejected anyway
-    key = (uint32_t)k;
-    return !pad;
+    const uint32_t at = min(i, a.n - 1u);
+    return FIRST ? a.keys64[at] : (uint64_t)a.keys[at];
+}
+// Is item i's word one to be sorted?  Its low 32 bits are its row; of a bad one too: the batch is rejected anyway.
+template <bool FIRST>
+__device__ __forceinline__ bool is_token(const TokenPass &a, uint32_t i, uint32_t n, uint64_t word, bool &pad, bool &bad)
+{
+    pad = FIRST && i < n && is_padding(word, a.padding);
+    bad = FIRST && i < n && !pad && word >= (uint64_t)a.rows;
+    return i < n && !pad;
 }
 
 template <bool FIRST, int IPT, bool GROUPED>
@@ -157,11 +156,14 @@ __global__ __launch_bounds__(kTokenThreads) void token_hist_kernel(TokenPass a)
     const uint32_t tile = tile_of_block(blockIdx.x, a.tiles), tile0 = tile * (uint32_t)(kTokenThreads * IPT);
     uint32_t pads = 0;
     bool any_bad = false;
+    uint64_t word[IPT];
+#pragma unroll
+    for (int r = 0; r < IPT; ++r) word[r] = token_word<FIRST>(a, tile0 + r * kTokenThreads + tid);
 #pragma unroll
     for (int r = 0; r < IPT; ++r) {
-        uint32_t key = 0;
         bool pad, bad;
-        if (token_at<FIRST>(a, tile0 + r * kTokenThreads + tid, n, key, pad, bad)) atomicAdd(&s_hist[(key >> a.shift) & (bins - 1u)], 1u);
+        if (is_token<FIRST>(a, tile0 + r * kTokenThreads + tid, n, word[r], pad, bad))
+            atomicAdd(&s_hist[((uint32_t)word[r] >> a.shift) & (bins - 1u)], 1u);
         pads += pad ? 1u : 0u;
         any_bad |= bad;
     }
@@ -177,7 +179,7 @@ __global__ __launch_bounds__(kTokenThreads) void token_hist_kernel(TokenPass a)
     if (FIRST && tid == 0) {
         a.flags[tile] = s_pads | (s_bad ? kBadTile : 0u);
         if (s_bad) atomicOr(&a.hdr->err_sticky, 1u);
-        if (tile == 0) a.ctl->joins[0] = a.ctl->joins[1] = 0;
+        if (tile == 0) a.ctl->joins = 0;
     }
 }
 
@@ -204,20 +206,21 @@ __global__ __launch_bounds__(256) void token_groups_kernel(TokenPass a)
 }
 
 // exclusive sum of v over the workgroup
-__device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t *s_wave)
+template <typename N>
+__device__ __forceinline__ N sum_before(N v, N *s_wave)
 {
     const uint32_t lane = lane_id(), wave = threadIdx.x / kWave;
-    uint32_t incl = v;
+    N incl = v;
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) {
-        const uint32_t t = (uint32_t)__shfl_up((int)incl, d, kWave);
+        const N t = __shfl_up(incl, d, kWave);
         if (lane >= (uint32_t)d) incl += t;
     }
     if (lane == kWave - 1) s_wave[wave] = incl;
     __syncthreads();
-    uint32_t before = incl - v;
+    N before = incl - v;
 #pragma unroll
-    for (uint32_t w = 0; w < (uint32_t)kTokenWaves; ++w) before += w < wave ? s_wave[w] : 0u;
+    for (uint32_t w = 0; w < (uint32_t)kTokenWaves; ++w) before += w < wave ? s_wave[w] : (N)0;
     __syncthreads();
     return before;
 }
@@ -235,7 +238,7 @@ __global__ __launch_bounds__(kTokenThreads) void token_scatter_kernel(TokenPass 
 {
     constexpr uint32_t kTile = kTokenThreads * IPT;
     extern __shared__ __align__(16) uint32_t lds[];
-    __shared__ uint32_t s_wave[kTokenWaves];
+    __shared__ unsigned long long s_wave[kTokenWaves];
     const uint32_t tid = threadIdx.x, wave = tid / kWave, lane = lane_id();
     const uint32_t bins = 1u << a.bits;
     uint32_t *s_keys = lds, *s_vals = lds + kTile, *s_start = lds + 2 * kTile, *s_base = s_start + bins;
@@ -252,23 +255,30 @@ __global__ __launch_bounds__(kTokenThreads) void token_scatter_kernel(TokenPass 
             pads += a.flags[t] & ~kBadTile;
             bad |= a.flags[t] & kBadTile;
         }
-        const uint32_t before = sum_before(pads, s_wave);
-        if (tid == kTokenThreads - 1) a.ctl->valid = a.n - (before + pads);
-        const uint32_t bads = sum_before(bad ? 1u : 0u, s_wave) + (bad ? 1u : 0u);
-        if (tid == kTokenThreads - 1) a.ctl->bad = bads ? 1u : 0u;
+        const unsigned long long own = (unsigned long long)(bad ? 1u : 0u) << 32 | pads, sums = sum_before(own, s_wave) + own;
+        if (tid == kTokenThreads - 1) {
+            a.ctl->valid = a.n - (uint32_t)sums;
+            a.ctl->bad = sums >> 32 ? 1u : 0u;
+        }
     }
-    if (tile0 >= n) return;
-
     uint32_t key[IPT], val[IPT], rank[IPT];
     bool there[IPT];
+    {
+        uint64_t word[IPT];
+        const uint32_t i0 = tile0 + wave * (kWave * IPT) + lane;
 #pragma unroll
-    for (int r = 0; r < IPT; ++r) {
-        const uint32_t i = tile0 + wave * (kWave * IPT) + r * kWave + lane;
-        bool pad, bad;
-        key[r] = 0;
-        there[r] = token_at<FIRST>(a, i, n, key[r], pad, bad);
-        val[r] = FIRST ? i : there[r] ? a.vals[i] : 0u;
+        for (int r = 0; r < IPT; ++r) {
+            word[r] = token_word<FIRST>(a, i0 + r * kWave);
+            val[r] = FIRST ? i0 + r * kWave : a.vals[min(i0 + r * kWave, a.n - 1u)];
+        }
+#pragma unroll
+        for (int r = 0; r < IPT; ++r) {
+            bool pad, bad;
+            there[r] = is_token<FIRST>(a, i0 + r * kWave, n, word[r], pad, bad);
+            key[r] = (uint32_t)word[r];
+        }
     }
+    if (tile0 >= n) return;
     // the thread's digit values: items of them in the tiles before, and in all
     const uint32_t bin = tid * PER;
     uint32_t before[PER] = {}, all[PER] = {};
@@ -348,7 +358,9 @@ __global__ __launch_bounds__(kTokenThreads) void token_scatter_kernel(TokenPass 
             in_all += all[q];
         }
     }
-    uint32_t start = sum_before(mine, s_wave), global = sum_before(in_all, s_wave);
+    // both sums at once
+    const unsigned long long sums = sum_before((unsigned long long)in_all << 32 | mine, s_wave);
+    uint32_t start = (uint32_t)sums, global = (uint32_t)(sums >> 32);
     if (bin < bins) {
 #pragma unroll
         for (int q = 0; q < PER; ++q) {
@@ -369,7 +381,7 @@ __global__ __launch_bounds__(kTokenThreads) void token_scatter_kernel(TokenPass 
     // items of the tile
     if (tid == kTokenThreads - 1) s_wave[0] = start;
     __syncthreads();
-    const uint32_t items = s_wave[0];
+    const uint32_t items = (uint32_t)s_wave[0];
     for (uint32_t i = tid; i < items; i += kTokenThreads) {
         const uint32_t k = s_keys[i], to = s_base[(k >> a.shift) & (bins - 1u)] + i;
         a.keys_out[to] = k;
@@ -379,13 +391,19 @@ __global__ __launch_bounds__(kTokenThreads) void token_scatter_kernel(TokenPass 
 
 // ---- host side -------------------------------------------------------------------------------------------------------------
 // Items of a thread: few for small batches, so that they spread over the compute units.
-static int items_of(uint32_t n) { return n <= 64u * 1024u ? 2 : n <= kDirectTiles * 2048u ? 4 : 8; }
+static int items_of(uint32_t n) { return n <= 64u * 1024u ? 2 : n <= kLargeBatch ? 4 : 8; }
+static bool is_grouped(uint32_t tiles) { return tiles > kDirectTiles; }
 // Digits: wide ones for few launches; in large batches at most 9 bits, so that what a tile writes of one digit value is some
 // tens of bytes on end.
-static int token_passes(int key_bits, int ipt)
+static int token_passes(int key_bits, bool grouped)
 {
-    const int most = ipt == 8 ? 9 : kTokenBits;
+    const int most = grouped ? 9 : kTokenBits;
     return (key_bits + most - 1) / most;
+}
+static int digit_of(int bits_left, int passes_left)      // spread evenly, wider ones first; eight values at least
+{
+    const int bits = (bits_left + passes_left - 1) / passes_left;
+    return bits < 3 ? 3 : bits;
 }
 static uint32_t group_of(uint32_t tiles)                 // tiles of a group: as many groups, about
 {
@@ -400,15 +418,15 @@ TokenSortLayout token_sort_layout(size_t off, uint32_t max_batch, int key_bits)
     TokenSortLayout l;
     auto take = [&](size_t bytes) { const size_t o = off; off = (off + bytes + 255) / 256 * 256; return o; };
     size_t tiles = 0, table = 0, sums = 0;
-    const uint32_t ends[3] = {64u * 1024u, kDirectTiles * 2048u, 0xFFFFFFFFu};
-    for (int c = 0; c < 3 && max_batch > kRankMost; ++c) {       // the largest batch of each number of items to a thread
+    const uint32_t ends[4] = {64u * 1024u, kDirectTiles * 4u * kTokenThreads, kLargeBatch, 0xFFFFFFFFu};
+    for (int c = 0; c < 4 && max_batch > kRankMost; ++c) {       // the largest batch of each kind
         const uint32_t n = max_batch < ends[c] ? max_batch : ends[c];
-        const int ipt = items_of(n), passes = token_passes(key_bits, ipt);
-        const size_t bins = (size_t)1 << ((key_bits + passes - 1) / passes);
-        const size_t t = tiles_of(n, ipt), g = group_of((uint32_t)t);
+        const size_t t = tiles_of(n, items_of(n)), g = group_of((uint32_t)t);
+        const bool grouped = is_grouped((uint32_t)t);
+        const size_t bins = (size_t)1 << digit_of(key_bits, token_passes(key_bits, grouped));
         if (t > tiles) tiles = t;
-        if (t * bins * (ipt == 8 ? 4 : 2) > table) table = t * bins * (ipt == 8 ? 4 : 2);
-        if (ipt == 8 && (t + g - 1) / g * bins > sums) sums = (t + g - 1) / g * bins;
+        if (t * bins * (grouped ? 4 : 2) > table) table = t * bins * (grouped ? 4 : 2);
+        if (grouped && (t + g - 1) / g * bins > sums) sums = (t + g - 1) / g * bins;
     }
     l.off_ctl = take(sizeof(TokenControl));
     l.off_flags = take(tiles * 4);
@@ -418,27 +436,26 @@ TokenSortLayout token_sort_layout(size_t off, uint32_t max_batch, int key_bits)
     return l;
 }
 
-template <bool FIRST, int IPT>
-static void launch_scatter(const TokenPass &a, uint32_t clears, hipStream_t st)
+template <bool FIRST, int IPT, bool GROUPED>
+static void launch_token_pass(const TokenPass &a, uint32_t clears, hipStream_t st)
 {
-    constexpr bool grouped = IPT == 8;
-    const dim3 grid(a.tiles + clears), block(kTokenThreads);
+    const dim3 hist(a.tiles), scatter(a.tiles + clears), block(kTokenThreads);
     const size_t lds = scatter_lds(a.bits, IPT);
-    if (a.bits <= 9) hipLaunchKernelGGL((token_scatter_kernel<FIRST, IPT, 1, grouped>), grid, block, lds, st, a);
-    else if (a.bits == 10) hipLaunchKernelGGL((token_scatter_kernel<FIRST, IPT, 2, grouped>), grid, block, lds, st, a);
-    else hipLaunchKernelGGL((token_scatter_kernel<FIRST, IPT, 4, grouped>), grid, block, lds, st, a);
+    hipLaunchKernelGGL((token_hist_kernel<FIRST, IPT, GROUPED>), hist, block, 0, st, a);
+    if (GROUPED) hipLaunchKernelGGL(token_groups_kernel, dim3(a.groups, ((1u << a.bits) + 255u) / 256u), dim3(256), 0, st, a);
+    if (a.bits <= 9) hipLaunchKernelGGL((token_scatter_kernel<FIRST, IPT, 1, GROUPED>), scatter, block, lds, st, a);
+    else if (GROUPED) return;                            // digits are narrower there
+    else if (a.bits == 10) hipLaunchKernelGGL((token_scatter_kernel<FIRST, IPT, GROUPED ? 1 : 2, GROUPED>), scatter, block, lds, st, a);
+    else hipLaunchKernelGGL((token_scatter_kernel<FIRST, IPT, GROUPED ? 1 : 4, GROUPED>), scatter, block, lds, st, a);
 }
 
-template <int IPT>
-static void launch_token_pass(const TokenPass &a, bool first, uint32_t clears, hipStream_t st)
+template <bool FIRST>
+static void launch_token_pass(const TokenPass &a, int ipt, uint32_t clears, hipStream_t st)
 {
-    constexpr bool grouped = IPT == 8;
-    const dim3 hist(a.tiles), block(kTokenThreads);
-    if (first) hipLaunchKernelGGL((token_hist_kernel<true, IPT, grouped>), hist, block, 0, st, a);
-    else hipLaunchKernelGGL((token_hist_kernel<false, IPT, grouped>), hist, block, 0, st, a);
-    if (grouped) hipLaunchKernelGGL(token_groups_kernel, dim3(a.groups, ((1u << a.bits) + 255u) / 256u), dim3(256), 0, st, a);
-    if (first) launch_scatter<true, IPT>(a, clears, st);
-    else launch_scatter<false, IPT>(a, clears, st);
+    if (ipt == 2) launch_token_pass<FIRST, 2, false>(a, clears, st);
+    else if (ipt == 8) launch_token_pass<FIRST, 8, true>(a, clears, st);
+    else if (is_grouped(a.tiles)) launch_token_pass<FIRST, 4, true>(a, clears, st);
+    else launch_token_pass<FIRST, 4, false>(a, clears, st);
 }
 
 TokenSort launch_token_sort(const Scratch &s, const TokenSortLayout &l, const uint64_t *keys, uint32_t n, uint64_t padding, uint32_t rows,
@@ -464,8 +481,9 @@ TokenSort launch_token_sort(const Scratch &s, const TokenSortLayout &l, const ui
         r.si = s.vals[0];
         return r;
     }
-    const int ipt = items_of(n), passes = token_passes(key_bits, ipt);
+    const int ipt = items_of(n);
     a.tiles = tiles_of(n, ipt);
+    const int passes = token_passes(key_bits, is_grouped(a.tiles));
     a.group = group_of(a.tiles);
     a.groups = (a.tiles + a.group - 1) / a.group;
     // the clearing, a part beside each digit's scatter
@@ -474,14 +492,13 @@ TokenSort launch_token_sort(const Scratch &s, const TokenSortLayout &l, const ui
     for (int p = 0; p < passes; ++p) {
         const int out = p & 1;
         a.shift = shift;
-        a.bits = (key_bits - shift + passes - p - 1) / (passes - p);
+        a.bits = digit_of(key_bits - shift, passes - p);
         a.keys = s.keys[out ^ 1]; a.vals = s.vals[out ^ 1];
         a.keys_out = s.keys[out]; a.vals_out = s.vals[out];
         a.clear.to = clear.to ? (char *)clear.to + p * part * 16 : nullptr;
         a.clear.sixteens = (uint64_t)p * part >= clear.sixteens ? 0 : clear.sixteens - p * part < part ? clear.sixteens - p * part : part;
-        if (ipt == 2) launch_token_pass<2>(a, p == 0, clears, st);
-        else if (ipt == 4) launch_token_pass<4>(a, p == 0, clears, st);
-        else launch_token_pass<8>(a, p == 0, clears, st);
+        if (p == 0) launch_token_pass<true>(a, ipt, clears, st);
+        else launch_token_pass<false>(a, ipt, clears, st);
         shift += a.bits;
         r.sk = s.keys[out];
         r.si = s.vals[out];

@@ -175,7 +175,7 @@ def test_lookup_leaves_rows_of_bad_tokens_and_says_so():
 
 
 # ---- gradient --------------------------------------------------------------------------------------------------------------
-SIZES = [1, 2, 3, 5, 31, 64, 257, 1023, 1024, 1025, 4097, 8192, 8193]
+SIZES = [1, 2, 3, 5, 31, 64, 100, 255, 256, 257, 1023, 1024, 1025, 4097, 8192, 8193]
 
 
 @pytest.mark.parametrize("D", [4, 12, 36, 128, 252, 512, 1020, 1024])
