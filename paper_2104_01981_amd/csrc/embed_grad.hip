@@ -14,11 +14,11 @@ constexpr uint32_t kSumMost = 2048;       // sorted positions of a workgroup, at
 constexpr uint32_t kSortHere = 256;       // batches of so many tokens are sorted by every workgroup for itself
 constexpr uint32_t kOneBlock = 1536;      // batches of so many tokens are cut by columns, not by positions: nothing is left to join
 constexpr uint32_t kOneUnits = 2;         // of four columns, of a workgroup there
-constexpr uint32_t kSumBlocks = 2048;     // workgroups, unless that would be more positions to one than there is room for
+constexpr uint32_t kSumBlocks = 1024;     // workgroups, unless that would be more positions to one than there is room for
 constexpr uint32_t kCountThreads = 1024;
 constexpr uint32_t kCountGroup = 8;       // workgroups whose distinct rows are counted together
 constexpr uint32_t kScanGroups = 512;     // from more on these counts are added up by a launch of its own
-constexpr uint32_t kChunkMin = 4, kChunkMax = 128;
+constexpr uint32_t kChunkMin = 4;
 constexpr uint64_t kStreamBytes = 100ull << 20;
 constexpr uint32_t kJoinUnits = 16;       // of four columns, of a job
 constexpr uint32_t kLongJoin = 16;        // workgroups from which on a run is a long one
@@ -228,7 +228,7 @@ template <typename T, bool DENSE, bool STREAM, bool HERE>
 __global__ __launch_bounds__(kSumThreads) void sum_runs_kernel(SumArgs a)
 {
     typedef typename Quad<T>::type Four;
-    constexpr uint32_t U = STREAM ? 8 : 4;               // rows in flight
+        constexpr uint32_t U = STREAM ? 8 : 4;               // rows in flight
     extern __shared__ uint32_t lds[];
     uint32_t *s_key = lds, *s_idx = lds + a.per + 2u;    // position i's key at i + 1
     __shared__ unsigned long long s_head[DENSE ? 1 : kSumMost / kWave];
@@ -524,7 +524,8 @@ static SumPlan sum_plan(uint32_t n, uint32_t D)
     p.units = n <= kOneBlock && quads > kOneUnits ? kOneUnits : quads;
     p.slices = (quads + p.units - 1) / p.units;
     p.teams = (uint32_t)kSumThreads / p.units;
-    const uint32_t room = kSumMost / p.teams, most = n <= kOneBlock || room < kChunkMax ? room : kChunkMax;
+    const uint32_t room = kSumMost / p.teams, chunk_max = D <= 256 ? 32u : D <= 512 ? 64u : 128u;
+    const uint32_t most = n <= kOneBlock || room < chunk_max ? room : chunk_max;
     const uint64_t wanted = n <= kOneBlock ? p.teams : (uint64_t)p.teams * kSumBlocks;
     p.chunk = (uint32_t)((n + wanted - 1) / wanted);
     if (p.chunk < kChunkMin) p.chunk = kChunkMin;
