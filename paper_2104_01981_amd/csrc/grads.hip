@@ -94,30 +94,29 @@ __device__ __forceinline__ uint32_t counted_end(const GradTable &g, const GradCh
     return end <= (int64_t)c.from ? c.from : end < (int64_t)c.to ? (uint32_t)end : c.to;
 }
 
-template <typename T>
-struct Sixteen {                          // 16 bytes of elements
-    static constexpr uint32_t N = 16 / sizeof(T);
+template <typename T, uint32_t N>
+struct Several {
     typedef T type __attribute__((ext_vector_type(N)));
 };
 
 // elements [v, v + N) of a chunk, zeros where they are not the tensor's
-template <typename T>
-__device__ __forceinline__ typename Sixteen<T>::type some_of(const T *p, uint32_t v, uint32_t from, uint32_t to)
+template <typename T, uint32_t N>
+__device__ __forceinline__ typename Several<T, N>::type some_of(const T *p, uint32_t v, uint32_t from, uint32_t to)
 {
-    typename Sixteen<T>::type r;
+    typename Several<T, N>::type r;
 #pragma unroll
-    for (uint32_t j = 0; j < Sixteen<T>::N; ++j) r[j] = v + j >= from && v + j < to ? p[v + j] : (T)0.0f;
+    for (uint32_t j = 0; j < N; ++j) r[j] = v + j >= from && v + j < to ? p[v + j] : (T)0.0f;
     return r;
 }
 
 // A lane's elements of a chunk, N at a time: f(first of them, the N).  A chunk that is the tensor's as a whole -- most are --
 // is loaded without a branch, all of it in flight.
 // STREAM: it is not read again soon.
-template <typename T, bool STREAM, typename F>
+template <typename T, uint32_t N, bool STREAM, typename F>
 __device__ __forceinline__ void over_chunk(const void *base, uint32_t from, uint32_t to, F f)
 {
-    typedef typename Sixteen<T>::type Vec;
-    constexpr uint32_t N = Sixteen<T>::N, U = kGradBytes / 16 / kGradThreads;
+    typedef typename Several<T, N>::type Vec;
+    constexpr uint32_t U = kGradBytes / (N * sizeof(T)) / kGradThreads;
     const T *p = (const T *)base;
     if (from == 0 && to == U * N * kGradThreads) {
         Vec x[U];
@@ -133,17 +132,18 @@ __device__ __forceinline__ void over_chunk(const void *base, uint32_t from, uint
     for (uint32_t q = 0; q < U; ++q) {
         const uint32_t v = (q * kGradThreads + threadIdx.x) * N;
         if (v >= to) break;
-        f(v, v >= from && v + N <= to ? *(const Vec *)(p + v) : some_of<T>(p, v, from, to));
+        f(v, v >= from && v + N <= to ? *(const Vec *)(p + v) : some_of<T, N>(p, v, from, to));
     }
 }
 
 template <typename T, bool STREAM>
 __device__ __forceinline__ double square_chunk(const GradChunk &c, uint32_t to)
 {
+    constexpr uint32_t N = 16 / sizeof(T);
     double acc[2] = {0, 0};
-    over_chunk<T, STREAM>(c.base, c.from, to, [&](uint32_t, const typename Sixteen<T>::type &x) {
+    over_chunk<T, N, STREAM>(c.base, c.from, to, [&](uint32_t, const typename Several<T, N>::type &x) {
 #pragma unroll
-        for (uint32_t j = 0; j < Sixteen<T>::N; ++j) {
+        for (uint32_t j = 0; j < N; ++j) {
             const double g = (double)(float)x[j];
             acc[j & 1] = fma(g, g, acc[j & 1]);
         }
@@ -212,17 +212,13 @@ __global__ __launch_bounds__(kGradThreads) void norm_kernel(GradTable g, float *
 template <typename TO, bool STREAM, uint32_t N>
 __device__ __forceinline__ void store_some(TO *p, int64_t from, int64_t to, const float (&y)[N])
 {
-    constexpr uint32_t M = N * sizeof(TO) < 16 ? N : 16 / sizeof(TO);      // to a store
-    if (from <= 0 && to >= (int64_t)N && (uintptr_t)p % (M * sizeof(TO)) == 0) {
-        typedef TO Vec __attribute__((ext_vector_type(M)));
+    if (from <= 0 && to >= (int64_t)N && (uintptr_t)p % (N * sizeof(TO)) == 0) {
+        typedef typename Several<TO, N>::type Vec;
+        Vec r;
 #pragma unroll
-        for (uint32_t j0 = 0; j0 < N; j0 += M) {
-            Vec r;
-#pragma unroll
-            for (uint32_t j = 0; j < M; ++j) r[j] = (TO)y[j0 + j];
-            if (STREAM) __builtin_nontemporal_store(r, (Vec *)(p + j0));
-            else *(Vec *)(p + j0) = r;
-        }
+        for (uint32_t j = 0; j < N; ++j) r[j] = (TO)y[j];
+        if (STREAM) __builtin_nontemporal_store(r, (Vec *)p);
+        else *(Vec *)p = r;
         return;
     }
 #pragma unroll
@@ -233,9 +229,9 @@ __device__ __forceinline__ void store_some(TO *p, int64_t from, int64_t to, cons
 template <typename T, typename TO, bool STREAM>
 __device__ __forceinline__ void clip_chunk(const GradChunk &c, uint32_t to, void *out, double factor)
 {
-    constexpr uint32_t N = Sixteen<T>::N;
+    constexpr uint32_t N = 16 / (sizeof(T) > sizeof(TO) ? sizeof(T) : sizeof(TO));      // 16 bytes of the wider
     TO *o = (TO *)out + (int64_t)c.first;
-    over_chunk<T, STREAM>(c.base, c.from, to, [&](uint32_t v, const typename Sixteen<T>::type &x) {
+    over_chunk<T, N, STREAM>(c.base, c.from, to, [&](uint32_t v, const typename Several<T, N>::type &x) {
         float y[N];
         // the product in 64 bits, so that a 32-bit gradient is rounded once (a 16-bit one in 32 bits first)
 #pragma unroll

@@ -191,14 +191,15 @@ __global__ __launch_bounds__(256) void token_groups_kernel(TokenPass a)
     uint32_t *at = (uint32_t *)a.table + (size_t)g * a.group * bins + bin;
     const uint32_t cnt = min(a.group, a.tiles - g * a.group);
     uint32_t sum = 0;
-    constexpr uint32_t U = 16;
+    constexpr uint32_t U = 32;
     for (uint32_t t0 = 0; t0 < cnt; t0 += U) {
         uint32_t c[U];
 #pragma unroll
-        for (uint32_t u = 0; u < U; ++u) c[u] = t0 + u < cnt ? at[(size_t)(t0 + u) * bins] : 0u;
+        for (uint32_t u = 0; u < U; ++u) c[u] = at[(size_t)min(t0 + u, cnt - 1u) * bins];
 #pragma unroll
         for (uint32_t u = 0; u < U; ++u) {
-            if (t0 + u < cnt) at[(size_t)(t0 + u) * bins] = sum;
+            if (t0 + u >= cnt) continue;
+            at[(size_t)(t0 + u) * bins] = sum;
             sum += c[u];
         }
     }
@@ -328,10 +329,16 @@ __global__ __launch_bounds__(kTokenThreads) void token_scatter_kernel(TokenPass 
     for (int r = 0; r < IPT; ++r) {
         const uint32_t digit = (key[r] >> a.shift) & (bins - 1u);
         unsigned long long peers = __ballot(there[r]);
-        for (int b = 0; b < a.bits; ++b) {
+        auto match = [&](int b) {
             const bool bit = (digit >> b) & 1u;
             const unsigned long long bal = __ballot(bit);
             peers &= bit ? bal : ~bal;
+        };
+        if (PER == 1) {
+            for (int b = 0; b < a.bits; ++b) match(b);
+        } else {                                         // 10 bits, or 11
+#pragma unroll
+            for (int b = 0; b < (PER == 2 ? 10 : 11); ++b) match(b);
         }
         const uint32_t below = (uint32_t)__popcll(peers & ((1ull << lane) - 1ull));
         const uint32_t old = cnt[digit];
