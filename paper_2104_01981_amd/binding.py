@@ -141,7 +141,7 @@ def probe_row_traffic(table_a, table_b, table_rows, rows, write, sink, stream=No
 
 
 _NO_PADDING = 1 << 63
-_types = {}
+_types, _words = {}, set()
 
 
 def _type(t):
@@ -150,6 +150,14 @@ def _type(t):
         import torch
         _types.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
     return _types[t.dtype]
+
+
+def _is_words(t):
+    """Contiguous 64-bit integers in device memory?"""
+    if not _words:
+        import torch
+        _words.update({torch.int64, torch.uint64})
+    return t.is_cuda and t.dtype in _words and t.is_contiguous()
 
 
 def _key(padding):
@@ -178,7 +186,7 @@ class Grads:
             assert t.is_cuda and t.is_contiguous()
             to.data, to.elements, to.type = t.data_ptr(), t.numel(), _type(t)
             if rows is not None:
-                assert rows.is_cuda and rows.dtype in (torch.int64, torch.uint64) and rows.numel() == 1 and t.dim() == 2
+                assert _is_words(rows) and rows.numel() == 1 and t.dim() == 2
                 to.rows, to.row_elements = rows.data_ptr(), t.shape[1]
         rc = self._lib.ecrm_grads_create(table, C.c_uint32(len(items)), C.byref(self._grads))
         if rc != ECRM_OK:
@@ -202,17 +210,16 @@ class Grads:
 
     def norm(self, norm, stream=None, check=True):
         """norm: device tensor of one fp32 value."""
-        assert norm.is_cuda and norm.dtype.is_floating_point and norm.element_size() == 4 and norm.numel() == 1
-        rc = self._lib.ecrm_grads_norm(self._grads, _ptr(norm), _stream(stream))
+        assert norm.is_cuda and _type(norm) == 0 and norm.numel() == 1
+        rc = self._lib.ecrm_grads_norm(self._grads, norm.data_ptr(), _stream(stream))
         if check and rc != ECRM_OK:
             raise EcrmError(rc, "ecrm_grads_norm")
         return rc
 
     def clip(self, norm, max_norm, out=None, stream=None, check=True):
         """In place, or into the tensors of `out`, another list."""
-        assert norm.is_cuda and norm.dtype.is_floating_point and norm.element_size() == 4 and norm.numel() == 1
-        rc = self._lib.ecrm_grads_clip(self._grads, out._grads if out is not None else None, _ptr(norm), max_norm,
-                                       _stream(stream))
+        assert norm.is_cuda and _type(norm) == 0 and norm.numel() == 1
+        rc = self._lib.ecrm_grads_clip(self._grads, out._grads if out is not None else None, norm.data_ptr(), max_norm, _stream(stream))
         if check and rc != ECRM_OK:
             raise EcrmError(rc, "ecrm_grads_clip")
         return rc
@@ -365,7 +372,7 @@ class Ecrm:
     def embed(self, keys, out, scale=1.0, padding=None, lost_server=None, stream=None, check=True):
         """out: [n, D] of fp32, bf16 or fp16, rows at any multiple of 4 elements from each other."""
         n = keys.numel()
-        assert keys.is_cuda and keys.element_size() == 8 and keys.is_contiguous()
+        assert _is_words(keys)
         assert out.is_cuda and out.dim() == 2 and out.shape[0] == n and out.shape[1] == self.cfg.dim and (n == 0 or out.stride(1) == 1)
         rc = self._lib.ecrm_embed(self._ctx, keys.data_ptr(), n, _key(padding), scale,
                                   0xFFFFFFFF if lost_server is None else lost_server, out.data_ptr(), _type(out), _row(out),
@@ -376,7 +383,7 @@ class Ecrm:
 
     def _check_grad(self, keys, d_out):
         n = keys.numel()
-        assert keys.is_cuda and keys.element_size() == 8 and keys.is_contiguous()
+        assert _is_words(keys)
         assert d_out.is_cuda and d_out.dim() == 2 and d_out.shape[0] == n and d_out.shape[1] == self.cfg.dim
         assert n == 0 or d_out.stride(1) == 1
         return n
@@ -385,9 +392,9 @@ class Ecrm:
         """d_out: [n, D] of fp32, bf16 or fp16; out_keys [n] and out_grads [n, D] have room for as many distinct keys."""
         import torch
         n = self._check_grad(keys, d_out)
-        assert out_keys.is_cuda and out_keys.element_size() == 8 and out_keys.is_contiguous() and out_keys.numel() >= n
+        assert _is_words(out_keys) and out_keys.numel() >= n
         assert out_grads.is_cuda and out_grads.dtype == torch.float32 and out_grads.is_contiguous()
-        assert out_grads.numel() >= n * self.cfg.dim and count.element_size() == 8 and count.numel() == 1
+        assert out_grads.numel() >= n * self.cfg.dim and _is_words(count) and count.numel() == 1
         rc = self._lib.ecrm_embed_grad(self._ctx, keys.data_ptr(), d_out.data_ptr(), _type(d_out), _row(d_out), n, _key(padding),
                                        scale, out_keys.data_ptr(), out_grads.data_ptr(), count.data_ptr(), _stream(stream))
         if check and rc != ECRM_OK:

@@ -5,20 +5,33 @@
 // written at once, what a chunk has of runs that go on before or behind it is joined in LDS by the workgroup, and what a
 // workgroup has of runs that go on in its neighbours by a launch behind.  Sums are carried in 64 bits and rounded once, in
 // an order that follows from the sorted positions, n and D alone: no atomics, two runs give the same bits.
+//
+// What bounds it: in large batches memory -- 2^20 tokens of 128 floats, hardly any twice, 243 us, of which the sums 194: 980 MB
+// at 5 TB/s, what a copy reaches --, in small ones the trips to memory that follow from one another: a launch (up to kSortHere
+// tokens, 6.8 us for 64), two (up to kOneBlock, 11 us for 600), three (up to kRankMost), seven to twelve.  Of 2^16 tokens of text
+// with 256 floats in bf16, 43 us, the sums take 16, the sort 23 and the join 4.
 #include "types.h"
 
 namespace ecrm {
 
 constexpr int kSumThreads = 256;
 constexpr uint32_t kSumMost = 2048;       // sorted positions of a workgroup, at most
-constexpr uint32_t kSortHere = 256;       // batches of so many tokens are sorted by every workgroup for itself
-constexpr uint32_t kOneBlock = 1536;      // batches of so many tokens are cut by columns, not by positions: nothing is left to join
-constexpr uint32_t kOneUnits = 2;         // of four columns, of a workgroup there
-constexpr uint32_t kSumBlocks = 1024;     // workgroups, unless that would be more positions to one than there is room for
+// Batches of up to kSortHere tokens are sorted by every workgroup for itself (64 tokens: 6.8 us, with a launch for it 9.6; 256: 8.5
+// and 10).  Batches of up to kOneBlock tokens are cut by columns, not by positions: nothing is left to join (1024 tokens of text
+// 12.9 us, 14.8 with positions cut; 2048 18.1 and 16.0), kOneUnits times four columns to a workgroup (1, 2, 4: 600 tokens 11.1,
+// 11.3, 12.6, all one token 13.2, 13.1, 12.5; 1024 of 1024 floats 15.8, 14.0, 14.9).
+constexpr uint32_t kSortHere = 256, kOneBlock = 1536, kOneUnits = 2;
+// Workgroups, unless that would be more positions to one than there is room for.  2^16 tokens of 256 floats with 1024, 1536, 2048,
+// 4096: 44.3, 45.0, 46.7, 51.2 us (a run that goes over several costs a join); 2^20 of 128 floats 251, 253, 252, 243, so at most
+// chunk_max (below) positions to a team.
+constexpr uint32_t kSumBlocks = 1024;
+constexpr uint32_t kChunkMin = 4;         // positions of a team, which are on their way together
 constexpr uint32_t kCountThreads = 1024;
 constexpr uint32_t kCountGroup = 8;       // workgroups whose distinct rows are counted together
 constexpr uint32_t kScanGroups = 512;     // from more on these counts are added up by a launch of its own
-constexpr uint32_t kChunkMin = 4;
+// Where more than this goes in and out, rows are read and written past the caches, eight of a team in flight instead of four
+// (2^20 tokens of 128 floats 278 us, 289 as usual; 103 MiB, 40000 of 512 floats to a dense gradient, 49 and 54; 96 MiB, 2^16 of 256
+// floats, 51 and 48: there the rows are still in the memory-side cache from whoever wrote them).
 constexpr uint64_t kStreamBytes = 100ull << 20;
 constexpr uint32_t kJoinUnits = 16;       // of four columns, of a job
 constexpr uint32_t kLongJoin = 16;        // workgroups from which on a run is a long one
@@ -524,6 +537,7 @@ static SumPlan sum_plan(uint32_t n, uint32_t D)
     p.units = n <= kOneBlock && quads > kOneUnits ? kOneUnits : quads;
     p.slices = (quads + p.units - 1) / p.units;
     p.teams = (uint32_t)kSumThreads / p.units;
+    // what the parts of runs take in the scratch buffer grows with D * D / chunk_max: up to 32, 64, 128 bytes a token
     const uint32_t room = kSumMost / p.teams, chunk_max = D <= 256 ? 32u : D <= 512 ? 64u : 128u;
     const uint32_t most = n <= kOneBlock || room < chunk_max ? room : chunk_max;
     const uint64_t wanted = n <= kOneBlock ? p.teams : (uint64_t)p.teams * kSumBlocks;

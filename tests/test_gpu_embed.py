@@ -66,8 +66,12 @@ def reference(keys, d, scale, padding):
     real = (keys != padding).nonzero().flatten() if padding is not None else torch.arange(len(keys), device=DEV)
     names, where = torch.unique(keys[real], return_inverse=True)
     x = d[real].double()
-    sums = torch.zeros(len(names), d.shape[1], dtype=torch.float64, device=DEV).index_add_(0, where, x)
-    mags = torch.zeros_like(sums).index_add_(0, where, x.abs())
+    # of a few rows, several places each, so that not all of a token's terms meet in one
+    ways = max(1, min(64, (1 << 23) // max(1, len(names) * d.shape[1])))
+    where = where * ways + torch.arange(len(where), device=DEV) % ways
+    parts = torch.zeros(len(names) * ways, d.shape[1], dtype=torch.float64, device=DEV)
+    sums = parts.index_add(0, where, x).view(len(names), ways, -1).sum(1)
+    mags = parts.index_add(0, where, x.abs()).view(len(names), ways, -1).sum(1)
     return names, sums * scale, mags * abs(scale)
 
 
@@ -194,7 +198,7 @@ def test_gradient(D, kind):
                                         (1 << 22, 4, 300007, "text"), (1 << 12, 256, 100003, "one"), (4, 32, 50000, "uniform"),
                                         (1 << 16, 16, 600011, "runs"), (1 << 24, 8, 600011, "text"), (1 << 14, 1024, 20011, "text"), (1 << 11, 32, 65536, "text"), (1 << 12, 32, 65537, "uniform"),
                                         (1 << 20, 12, 262144, "runs"), (1 << 26, 4, 262145, "text"), ((1 << 22) + 4, 4, 2100003, "uniform"),
-                                        (1 << 9, 4, 5000011, "text")])
+                                        (1 << 9, 4, 5000011, "text"), (1 << 22, 8, 100003, "text"), ((1 << 22) - 4, 16, 262143, "uniform")])
 @pytest.mark.parametrize("t", [torch.float32, torch.bfloat16])
 def test_gradient_of_larger_batches(R, D, n, kind, t):
     tab = Table(R, D, max_batch=n)
@@ -314,6 +318,91 @@ def test_other_calls_in_between_keep_their_results():
         assert b.ctx.batch_stats() == stats
         for x, y in ((a.E, b.E), (a.A, b.A), (a.PE, b.PE), (a.PA, b.PA), (a.load, b.load)):
             assert torch.equal(x, y)
+
+
+class Large:
+    """A table of zeros, too large to be filled for a test."""
+
+    def __init__(self, R, D, max_batch):
+        self.R, self.D = R, D
+        self.E, A = torch.zeros(R, D, device=DEV), torch.empty(R, D, device=DEV)
+        P, load = torch.empty(2, R // 4, D, device=DEV), torch.zeros(2, 5, dtype=torch.int64, device=DEV)
+        self.ctx = Ecrm(R, D, max_batch=max_batch)
+        scratch = torch.empty(self.ctx.scratch_bytes(), dtype=torch.uint8, device=DEV)
+        self.ctx.bind(self.E, A, P[0], P[1], load[0], load[1], scratch)
+
+
+def test_rows_beyond_32_bit_offsets():
+    R, D, n = 1 << 28, 16, 5000                           # 2^32 floats to a table
+    tab = Large(R, D, n)
+    rng = np.random.default_rng(1)
+    rows = np.unique(np.concatenate([[0, 1, R - 1, R - 2, 1 << 27, (1 << 27) - 1], rng.integers(0, R, 500)]))
+    at = torch.from_numpy(rows).to(DEV)
+    tab.E[at] = torch.randn(len(rows), D, device=DEV)
+    keys = at[torch.from_numpy(rng.integers(0, len(rows), n)).to(DEV)]
+    out = torch.empty(n, D, device=DEV)
+    tab.ctx.embed(keys, out)
+    assert torch.equal(out, tab.E[keys])
+    d = gradients(n, D, torch.float32, 1)
+    names, sums, mags = check_grad(tab, keys, d)
+    tab.E.zero_()
+    tab.ctx.embed_grad_dense(keys, d, tab.E, accumulate=True)
+    close(tab.E[names], sums, mags, n)
+    assert int((tab.E[:, 0] != 0).sum()) <= len(names)
+    tab.ctx.embed_grad_dense(keys, d, tab.E)
+    close(tab.E[names], sums, mags, n)
+    assert tab.ctx.status() == 0
+
+
+def test_tokens_beyond_32_bit_offsets():
+    """Gradients of looked-up rows, and looked-up rows, that lie more than 2^32 bytes and 2^31 elements into their memory."""
+    R, D, n = 1 << 12, 1024, (1 << 21) + 77
+    tab = Large(R, D, n)
+    tab.E[:] = torch.randn(R, D, device=DEV)
+    keys = torch.full((n,), PAD, dtype=torch.int64, device=DEV)
+    keys[-500:] = torch.randint(0, R, (500,), device=DEV)
+    keys[:3] = 5
+    d = torch.empty(n, D, dtype=torch.bfloat16, device=DEV)
+    d[:3], d[-500:] = torch.randn(3, D, device=DEV), torch.randn(500, D, device=DEV)
+    ok, og = torch.empty(n, dtype=torch.int64, device=DEV), torch.empty(n, D, device=DEV)
+    count = torch.zeros(1, dtype=torch.int64, device=DEV)
+    tab.ctx.embed_grad(keys, d, ok, og, count, padding=PAD)
+    some = torch.cat([torch.arange(3, device=DEV), torch.arange(n - 500, n, device=DEV)])
+    names, sums, mags = reference(keys[some], d[some], 1.0, PAD)
+    u = int(count)
+    assert torch.equal(ok[:u], names) and bool((ok[u:] == -1).all())
+    close(og[:u], sums, mags, n)
+    d.fill_(7.0)
+    tab.ctx.embed(keys, d, padding=PAD)
+    assert torch.equal(d[-500:], tab.E[keys[-500:]].to(torch.bfloat16)) and not bool(d[1000:2000].any())
+    assert tab.ctx.status() == 0
+
+
+def test_during_a_recovery():
+    """Gradients between the calls of a recovery, whose updates wait in their buffer meanwhile: the tables end as without them; a
+    lookup sees what a degraded read sees."""
+    R, D, n, cap = 4 * 1000, 64, 3000, 4000
+    a, b = Table(R, D, max_batch=n + cap, seed=9), Table(R, D, max_batch=n + cap, seed=9)
+    for tab in (a, b):
+        bk, bg = torch.empty(2 * cap, dtype=torch.int64, device=DEV), torch.empty(2 * cap, D, device=DEV)
+        tab.ctx.fail_server(2)
+        tab.ctx.recovery_begin(2, 2, bk, bg, cap)
+        for step in range(2):
+            keys, g = tokens(R, n // 2, "uniform", step), gradients(n // 2, D, torch.float32, step).contiguous()
+            tab.ctx.recovery_lock()
+            tab.ctx.update(keys, g)
+            if tab is b:
+                waiting = b.ctx.recovery_state()
+                check_grad(b, tokens(R, 5000, "text", 7), gradients(5000, D, torch.bfloat16, 7))
+                read, out = torch.empty(n // 2, D, device=DEV), torch.empty(n // 2, D, device=DEV)
+                b.ctx.degraded_read(keys, 2, read)
+                b.ctx.embed(keys, out, lost_server=2)
+                assert torch.equal(read, out) and b.ctx.recovery_state() == waiting
+            tab.ctx.recovery_decode()
+            tab.ctx.recovery_unlock()
+        assert tab.ctx.status() == 0 and not tab.ctx.recovery_state()["active"]
+    for x, y in ((a.E, b.E), (a.A, b.A), (a.PE, b.PE), (a.PA, b.PA), (a.load, b.load)):
+        assert torch.equal(x, y)
 
 
 @pytest.mark.parametrize("n", [200, 40000])
