@@ -28,7 +28,7 @@ constexpr uint32_t kSumBlocks = 1024;
 constexpr uint32_t kChunkMin = 4;         // positions of a team, which are on their way together
 constexpr uint32_t kCountThreads = 1024;
 constexpr uint32_t kCountGroup = 8;       // workgroups whose distinct rows are counted together
-constexpr uint32_t kScanGroups = 512;     // from more on these counts are added up by a launch of its own
+constexpr uint32_t kScanGroups = 1024;    // from more on these counts are added up by a launch of its own
 // Where more than this goes in and out, rows are read and written past the caches, eight of a team in flight instead of four
 // (2^20 tokens of 128 floats 278 us, 289 as usual; 103 MiB, 40000 of 512 floats to a dense gradient, 49 and 54; 96 MiB, 2^16 of 256
 // floats, 51 and 48: there the rows are still in the memory-side cache from whoever wrote them).
