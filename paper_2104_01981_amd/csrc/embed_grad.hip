@@ -6,10 +6,10 @@
 // workgroup has of runs that go on in its neighbours by a launch behind.  Sums are carried in 64 bits and rounded once, in
 // an order that follows from the sorted positions, n and D alone: no atomics, two runs give the same bits.
 //
-// What bounds it: in large batches memory -- 2^20 tokens of 128 floats, hardly any twice, 243 us, of which the sums 194: 980 MB
-// at 5 TB/s, what a copy reaches --, in small ones the trips to memory that follow from one another: a launch (up to kSortHere
-// tokens, 6.8 us for 64), two (up to kOneBlock, 11 us for 600), three (up to kRankMost), seven to twelve.  Of 2^16 tokens of text
-// with 256 floats in bf16, 43 us, the sums take 16, the sort 23 and the join 4.
+// What bounds it: in large batches memory -- 2^20 tokens of 128 floats, hardly any twice, 239 us, of which the sums 181: 980 MB
+// at 5.4 TB/s, more than a copy reaches --, in small ones the trips to memory that follow from one another: a launch (up to
+// kSortHere tokens, 6.8 us for 64), two (up to kOneBlock, 11 us for 600), three to five (up to 2^16), nine to twelve.  Of 2^16
+// tokens of text with 256 floats in bf16, 42 us, the sums take 16, the sort 20 and the join 4.
 #include "types.h"
 
 namespace ecrm {
@@ -22,7 +22,7 @@ constexpr uint32_t kSumMost = 2048;       // sorted positions of a workgroup, at
 // 11.3, 12.6, all one token 13.2, 13.1, 12.5; 1024 of 1024 floats 15.8, 14.0, 14.9).
 constexpr uint32_t kSortHere = 256, kOneBlock = 1536, kOneUnits = 2;
 // Workgroups, unless that would be more positions to one than there is room for.  2^16 tokens of 256 floats with 1024, 1536, 2048,
-// 4096: 44.3, 45.0, 46.7, 51.2 us (a run that goes over several costs a join); 2^20 of 128 floats 251, 253, 252, 243, so at most
+// 4096 (with the radix sort): 44.3, 45.0, 46.7, 51.2 us (a run that goes over several costs a join); 2^20 of 128 floats 251, 253, 252, 243, so at most
 // chunk_max (below) positions to a team.
 constexpr uint32_t kSumBlocks = 1024;
 constexpr uint32_t kChunkMin = 4;         // positions of a team, which are on their way together

@@ -3,15 +3,17 @@
 //
 // Up to kRankMost tokens: one launch.  A token's place is the number of tokens before it in the order, and each wave counts
 // that for eight tokens over all keys in LDS -- n^2 comparisons, which the device does at 10^13 a second: 4.7 us for 600 tokens.
-// (A gradient of 8192 tokens takes 23.5 us so, 31.2 with the radix sort; 16384 44.2 and 33.0.)
+// (A gradient of 8192 tokens takes 23.2 us so, 24.3 with the next.)
+// Up to kMergeMost: two launches.  Tiles are sorted in LDS (7.4 us for 64 of them, three digits), then a token's place is what the
+// other tiles have below it, by binary search, all tiles going through the LDS of every workgroup (13 us: about 5 for the 700
+// steps of a token, 4 for the tiles' way to LDS).  A gradient of 12 000 tokens 25 us, of 2^16 with 256 floats 41.8; with the radix
+// sort 33 and 43.5.  (Tiles of 2048: 11 and 11 us instead of 7.4 and 13.)
 // More: a radix sort of digits of up to 11 bits, two launches to a digit: counts of each tile, then a stable scatter that ranks
 // a tile's items with wave ballots and writes them in runs.  Every workgroup of the scatter adds up the counts of the tiles before
-// its own by itself; of more than kDirectTiles tiles they are first added up in groups, by a launch in between.
-// What bounds it is latency.  Of the 8.5 us of a scatter of 2^16 items, 1024 digit values in 64 tiles, 2.1 go into the counts of the
-// other tiles (128 KB to every workgroup), 1 into the ranks, 1.4 into the sums over the workgroup, 0.3 into the writes; the rest is
-// the launch and the first trip to memory.  2^20 items of 22 bits: three digits of 4.9 (counts), 4.9 (groups), 11 us (scatter).
-// (The counts of 257 tiles without groups: a scatter of 21 us instead of 12; eight values and a few tiles to a thread, added up in
-// LDS: 11.9 instead of 9.2 of 2^16 items.)
+// its own by itself; of more than kDirectTiles tiles they are first added up in groups, by a launch in between.  What bounds it is
+// latency.  2^20 items of 22 bits: three digits of 4.9 (counts), 4.9 (groups), 11 us (scatter, of which 1 goes into the counts of the
+// other tiles, 1.5 into the ranks, 1 into the sums over the workgroup, 0.5 into the writes).
+// (The counts of 257 tiles without groups: a scatter of 21 us instead of 12.)
 #include "ecrm_internal.h"
 
 namespace ecrm {
@@ -23,6 +25,8 @@ constexpr int kTokenWaves = kTokenThreads / kWave;
 constexpr int kTokenBits = 11;                           // of a digit, at most
 constexpr uint32_t kDirectTiles = 128;
 constexpr uint32_t kLargeBatch = 2048u * 1024u;
+constexpr uint32_t kMergeTile = 1024, kMergeItems = 256, kMergeThreads = 1024;
+constexpr uint32_t kMergeMost = 64u * kMergeTile;        // tokens of a batch that is sorted in tiles, which are then merged
 constexpr uint32_t kBadTile = 0x80000000u;
 
 struct TokenPass {
@@ -49,6 +53,18 @@ __device__ __forceinline__ void clear_share(const ClearJob &c, uint32_t block, u
     u4 *to = (u4 *)c.to;
     for (uint64_t i = (uint64_t)block * threads + threadIdx.x; i < c.sixteens; i += (uint64_t)blocks * threads)
         to[i] = u4{0u, 0u, 0u, 0u};
+}
+
+// inclusive sum over the wave: within rows of 16 lanes, then over the rows
+__device__ __forceinline__ uint32_t wave_sums(uint32_t v)
+{
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, false);       // row_shr:1, 2, 4, 8
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xA, 0xF, false);       // row_bcast:15 to rows 1 and 3
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xC, 0xF, false);       // row_bcast:31 to rows 2 and 3
+    return v;
 }
 
 __global__ __launch_bounds__(kRankThreads) void token_rank_kernel(TokenPass a)
@@ -129,6 +145,161 @@ __global__ __launch_bounds__(kRankThreads) void token_rank_kernel(TokenPass a)
     }
 }
 
+// ---- tiles sorted, then merged -------------------------------------------------------------------------------------------------
+// Sorts a tile of kMergeTile tokens by `bits` bits, enough for rows and one value more: what is not a row comes last, as kNoKey.
+// Digits of up to 8 bits; a token's place is what the waves have of smaller digits, and the waves before of its own, and its rank
+// among the wave's.
+__global__ __launch_bounds__(kMergeTile) void token_tile_kernel(TokenPass a)
+{
+    constexpr uint32_t kWaves = kMergeTile / kWave, kBits = 8, kPer = (kWaves << kBits) / kMergeTile;
+    __shared__ uint32_t s_key[kMergeTile], s_val[kMergeTile], s_wave[kWaves], s_pads, s_bad;
+    __shared__ __align__(16) uint32_t s_cnt[kWaves << kBits];                      // [digit][wave]
+    if (blockIdx.x >= a.tiles) {
+        clear_share(a.clear, blockIdx.x - a.tiles, gridDim.x - a.tiles, kMergeTile);
+        return;
+    }
+    const uint32_t tid = threadIdx.x, wave = tid / kWave, lane = lane_id(), i = blockIdx.x * kMergeTile + tid;
+    const uint64_t word = a.keys64[min(i, a.n - 1u)];
+    const bool in = i < a.n, pad = in && is_padding(word, a.padding), bad = in && !pad && word >= (uint64_t)a.rows;
+    uint32_t key = in && !pad ? (uint32_t)word : a.rows, val = i;
+    if (tid == 0) s_pads = s_bad = 0;
+    const int passes = (a.bits + (int)kBits - 1) / (int)kBits;
+    int shift = 0;
+    for (int p = 0; p < passes; ++p) {
+        const int bits = (a.bits - shift + passes - p - 1) / (passes - p);
+        const uint32_t digit = (key >> shift) & ((1u << bits) - 1u), counters = kWaves << bits;
+        typedef uint32_t Counts __attribute__((ext_vector_type(kPer)));
+        Counts *mine = (Counts *)s_cnt + tid;            // kPer counters to a thread
+        const bool counting = tid * kPer < counters;
+        if (counting) *mine = (Counts)0u;
+        unsigned long long peers = ~0ull;                // of the wave's: those with the same digit
+        for (int b = 0; b < bits; ++b) {
+            const bool bit = (digit >> b) & 1u;
+            const unsigned long long bal = __ballot(bit);
+            peers &= bit ? bal : ~bal;
+        }
+        const uint32_t below = (uint32_t)__popcll(peers & ((1ull << lane) - 1ull));
+        __syncthreads();
+        if (below == 0) s_cnt[digit * kWaves + wave] = (uint32_t)__popcll(peers);
+        __syncthreads();
+        const Counts c = counting ? *mine : (Counts)0u;
+        uint32_t total = 0;
+#pragma unroll
+        for (uint32_t q = 0; q < kPer; ++q) total += c[q];
+        const uint32_t incl = wave_sums(total);
+        if (lane == kWave - 1) s_wave[wave] = incl;
+        __syncthreads();
+        uint32_t before = incl - total;
+#pragma unroll
+        for (uint32_t w = 0; w < kWaves; ++w) before += w < wave ? s_wave[w] : 0u;
+        Counts start;
+#pragma unroll
+        for (uint32_t q = 0; q < kPer; ++q) {
+            start[q] = before;
+            before += c[q];
+        }
+        if (counting) *mine = start;
+        __syncthreads();
+        const uint32_t at = s_cnt[digit * kWaves + wave] + below;
+        s_key[at] = key;
+        s_val[at] = val;
+        __syncthreads();
+        key = s_key[tid];
+        val = s_val[tid];
+        shift += bits;
+    }
+    if (in) {                                            // the places behind the batch's last token are the last ones here, too
+        a.keys_out[i] = key < a.rows ? key : kNoKey;
+        a.vals_out[i] = val;
+    }
+    const unsigned long long pads = __ballot(pad);
+    if (lane == 0 && pads) atomicAdd(&s_pads, (uint32_t)__popcll(pads));
+    if (bad) s_bad = 1;
+    __syncthreads();
+    if (tid == 0) {
+        a.flags[blockIdx.x] = s_pads | (s_bad ? kBadTile : 0u);
+        if (s_bad) atomicOr(&a.hdr->err_sticky, 1u);
+        if (blockIdx.x == 0) a.ctl->joins = 0;
+    }
+}
+
+// tokens of a sorted tile that are below `key`
+__device__ __forceinline__ uint32_t below_in_tile(const uint32_t *s_tile, uint32_t key)
+{
+    uint32_t at = 0;
+#pragma unroll
+    for (uint32_t step = kMergeTile / 2u; step; step /= 2u) at += s_tile[at + step - 1u] < key ? step : 0u;
+    return at + (s_tile[at] < key ? 1u : 0u);
+}
+
+// Places the tokens of sorted tiles: a workgroup kMergeItems of them, each by four lanes, which look its key up in a quarter of the
+// other tiles.  A token comes behind equal ones of earlier tiles and before those of later ones.
+__global__ __launch_bounds__(kMergeThreads) void token_merge_kernel(TokenPass a)
+{
+    constexpr uint32_t kRound = 16, kParts = kMergeThreads / kMergeItems, kEach = kRound / kParts;
+    constexpr uint32_t kQuads = kRound * kMergeTile / 4u / kMergeThreads;               // 16-byte loads of a thread in a round
+    __shared__ __align__(16) uint32_t s_key[kRound * kMergeTile];
+    __shared__ uint32_t s_sum[kParts][kMergeItems], s_pads, s_bad;
+    const uint32_t tid = threadIdx.x, n = a.n, blocks = (n + kMergeItems - 1) / kMergeItems;
+    if (blockIdx.x >= blocks) {
+        clear_share(a.clear, blockIdx.x - blocks, gridDim.x - blocks, kMergeThreads);
+        return;
+    }
+    const uint32_t item = tid % kMergeItems, part = tid / kMergeItems, i = blockIdx.x * kMergeItems + item, own = i / kMergeTile;
+    const uint32_t flag = a.flags[min(tid, a.tiles - 1u)];                         // no more tiles than threads
+    const uint32_t key = a.keys[min(i, n - 1u)], val = a.vals[min(i, n - 1u)];
+    uint4 next[kQuads];
+    auto load = [&](uint32_t u0) {
+#pragma unroll
+        for (uint32_t q = 0; q < kQuads; ++q) {
+            const uint32_t at = u0 * kMergeTile + (q * kMergeThreads + tid) * 4u;
+            next[q] = *(const uint4 *)(a.keys + min(at, (n - 1u) / 4u * 4u));      // room for a multiple of four
+            if (at >= n) next[q].x = kNoKey;
+            if (at + 1u >= n) next[q].y = kNoKey;
+            if (at + 2u >= n) next[q].z = kNoKey;
+            if (at + 3u >= n) next[q].w = kNoKey;
+        }
+    };
+    load(0);
+    if (tid == 0) s_pads = s_bad = 0;
+    __syncthreads();
+    if (tid < a.tiles) {
+        if (flag & ~kBadTile) atomicAdd(&s_pads, flag & ~kBadTile);
+        if (flag & kBadTile) s_bad = 1;
+    }
+    uint32_t before = 0;
+    for (uint32_t u0 = 0; u0 < a.tiles; u0 += kRound) {
+        if (u0) __syncthreads();                         // everybody is done with the round before
+#pragma unroll
+        for (uint32_t q = 0; q < kQuads; ++q) *(uint4 *)(s_key + (q * kMergeThreads + tid) * 4u) = next[q];
+        __syncthreads();
+        if (u0 + kRound < a.tiles) load(u0 + kRound);
+        uint32_t got[kEach];
+#pragma unroll
+        for (uint32_t q = 0; q < kEach; ++q) {
+            const uint32_t u = u0 + part * kEach + q;
+            got[q] = below_in_tile(s_key + (part * kEach + q) * kMergeTile, key + (u < own ? 1u : 0u));
+            if (u == own) got[q] = 0;
+        }
+#pragma unroll
+        for (uint32_t q = 0; q < kEach; ++q) before += got[q];
+    }
+    if (blockIdx.x == 0 && tid == 0) {
+        a.ctl->valid = n - s_pads;
+        a.ctl->bad = s_bad;
+    }
+    if (s_bad) return;                                   // such tiles are not sorted
+    s_sum[part][item] = before;
+    __syncthreads();
+    if (part || i >= n || key == kNoKey) return;
+    uint32_t at = i - own * kMergeTile;
+#pragma unroll
+    for (uint32_t p = 0; p < kParts; ++p) at += s_sum[p][item];
+    a.keys_out[at] = key;
+    a.vals_out[at] = val;
+}
+
+// ---- radix sort ------------------------------------------------------------------------------------------------------------------
 // Item i's word, or the last one's: loads without a branch, so that a thread's are in flight together.  Behind `valid` the
 // buffers of the later digits hold anything.
 template <bool FIRST>
@@ -403,9 +574,7 @@ __global__ __launch_bounds__(kTokenThreads) void token_scatter_kernel(TokenPass 
 }
 
 // ---- host side -------------------------------------------------------------------------------------------------------------
-// Items of a thread: few for small batches, so that they spread over the compute units (2^16 items with four: 50 us for 48; 2^20
-// with eight: 267 for 252).
-static int items_of(uint32_t n) { return n <= 64u * 1024u ? 2 : n <= kLargeBatch ? 4 : 8; }
+static int items_of(uint32_t n) { return n <= kLargeBatch ? 4 : 8; }     // of a thread (2^20 items with eight: 267 us for 252)
 static bool is_grouped(uint32_t tiles) { return tiles > kDirectTiles; }
 // Digits: wide ones for few launches; in large batches at most 9 bits, so that what a tile writes of one digit value is some
 // tens of bytes on end (2^20 items, two digits of 11 bits: scatters of 43 us instead of 12).
@@ -432,8 +601,9 @@ TokenSortLayout token_sort_layout(size_t off, uint32_t max_batch, int key_bits)
     TokenSortLayout l;
     auto take = [&](size_t bytes) { const size_t o = off; off = (off + bytes + 255) / 256 * 256; return o; };
     size_t tiles = 0, table = 0, sums = 0;
-    const uint32_t ends[4] = {64u * 1024u, kDirectTiles * 4u * kTokenThreads, kLargeBatch, 0xFFFFFFFFu};
-    for (int c = 0; c < 4 && max_batch > kRankMost; ++c) {       // the largest batch of each kind
+    const uint32_t ends[3] = {kDirectTiles * 4u * kTokenThreads, kLargeBatch, 0xFFFFFFFFu};
+    if (max_batch > kRankMost) tiles = kMergeMost / kMergeTile;
+    for (int c = 0; c < 3 && max_batch > kMergeMost; ++c) {      // the largest batch of each kind
         const uint32_t n = max_batch < ends[c] ? max_batch : ends[c];
         const size_t t = tiles_of(n, items_of(n)), g = group_of((uint32_t)t);
         const bool grouped = is_grouped((uint32_t)t);
@@ -466,8 +636,7 @@ static void launch_token_pass(const TokenPass &a, uint32_t clears, hipStream_t s
 template <bool FIRST>
 static void launch_token_pass(const TokenPass &a, int ipt, uint32_t clears, hipStream_t st)
 {
-    if (ipt == 2) launch_token_pass<FIRST, 2, false>(a, clears, st);
-    else if (ipt == 8) launch_token_pass<FIRST, 8, true>(a, clears, st);
+    if (ipt == 8) launch_token_pass<FIRST, 8, true>(a, clears, st);
     else if (is_grouped(a.tiles)) launch_token_pass<FIRST, 4, true>(a, clears, st);
     else launch_token_pass<FIRST, 4, false>(a, clears, st);
 }
@@ -491,6 +660,23 @@ TokenSort launch_token_sort(const Scratch &s, const TokenSortLayout &l, const ui
         a.keys_out = s.keys[0]; a.vals_out = s.vals[0];
         a.clear = clear;
         hipLaunchKernelGGL(token_rank_kernel, dim3(a.tiles + clears), dim3(kRankThreads), 0, st, a);
+        r.sk = s.keys[0];
+        r.si = s.vals[0];
+        return r;
+    }
+    if (n <= kMergeMost) {
+        const uint32_t blocks = (n + kMergeItems - 1) / kMergeItems;
+        const uint64_t half = clear.sixteens / 2u;       // of the clearing, beside either
+        a.tiles = (n + kMergeTile - 1) / kMergeTile;
+        a.bits = key_bits;
+        while (a.bits < 32 && (1ull << a.bits) <= rows) ++a.bits;
+        a.keys_out = s.keys[1]; a.vals_out = s.vals[1];
+        a.clear.to = clear.to; a.clear.sixteens = half;
+        hipLaunchKernelGGL(token_tile_kernel, dim3(a.tiles + clears), dim3(kMergeTile), 0, st, a);
+        a.keys = s.keys[1]; a.vals = s.vals[1];
+        a.keys_out = s.keys[0]; a.vals_out = s.vals[0];
+        a.clear.to = clear.to ? (char *)clear.to + half * 16 : nullptr; a.clear.sixteens = clear.sixteens - half;
+        hipLaunchKernelGGL(token_merge_kernel, dim3(blocks + clears), dim3(kMergeThreads), 0, st, a);
         r.sk = s.keys[0];
         r.si = s.vals[0];
         return r;

@@ -194,7 +194,7 @@ def test_gradient(D, kind):
     assert tab.ctx.status() == 0
 
 
-@pytest.mark.parametrize("R,D,n,kind", [(1 << 10, 128, 70001, "text"), (1 << 20, 128, 70001, "text"), (1 << 20, 64, 70001, "uniform"),
+@pytest.mark.parametrize("R,D,n,kind", [(1 << 10, 128, 70001, "text"), (1 << 20, 128, 65535, "text"), (1 << 17, 16, 40961, "runs"), (1 << 32 >> 6, 4, 30000, "text"), (1 << 20, 128, 70001, "text"), (1 << 20, 64, 70001, "uniform"),
                                         (1 << 22, 4, 300007, "text"), (1 << 12, 256, 100003, "one"), (4, 32, 50000, "uniform"),
                                         (1 << 16, 16, 600011, "runs"), (1 << 24, 8, 600011, "text"), (1 << 14, 1024, 20011, "text"), (1 << 11, 32, 65536, "text"), (1 << 12, 32, 65537, "uniform"),
                                         (1 << 20, 12, 262144, "runs"), (1 << 26, 4, 262145, "text"), ((1 << 22) + 4, 4, 2100003, "uniform"),
@@ -206,7 +206,7 @@ def test_gradient_of_larger_batches(R, D, n, kind, t):
     assert tab.ctx.status() == 0
 
 
-@pytest.mark.parametrize("n", [1, 100, 5000, 66000])
+@pytest.mark.parametrize("n", [1, 100, 1000, 5000, 20000, 66000])
 def test_gradient_of_padding_alone(n):
     tab = Table(1 << 10, 36, max_batch=n)
     keys = torch.full((n,), PAD, dtype=torch.int64, device=DEV)
@@ -219,7 +219,7 @@ def test_gradient_of_padding_alone(n):
     assert bool((dE == 0.0).all()) and tab.ctx.status() == 0
 
 
-@pytest.mark.parametrize("n", [40, 3000, 40000])
+@pytest.mark.parametrize("n", [40, 1000, 3000, 40000, 90000])
 def test_values_that_are_not_finite_stay_in_their_row(n):
     """... whether their run lies in one chunk or goes over many, and in padded places they do not count."""
     R, D = 1 << 10, 36
@@ -259,7 +259,7 @@ def test_dense_gradient(R, D, n, kind):
     assert torch.equal(dE[away], old[away]) and tab.ctx.status() == 0
 
 
-@pytest.mark.parametrize("n", [5, 3000, 70001])
+@pytest.mark.parametrize("n", [5, 700, 3000, 20000, 70001])
 @pytest.mark.parametrize("where", ["first", "last"])
 def test_a_bad_token_rejects_the_batch(n, where):
     R, D = 1 << 10, 36
@@ -405,7 +405,7 @@ def test_during_a_recovery():
         assert torch.equal(x, y)
 
 
-@pytest.mark.parametrize("n", [200, 40000])
+@pytest.mark.parametrize("n", [200, 1500, 5000, 40000, 100000])
 def test_in_a_graph(n):
     """Replays on new contents, with the program's own calls on the same context in between."""
     R, D = 1 << 12, 128
