@@ -25,6 +25,7 @@ constexpr uint32_t kSortHere = 256, kOneBlock = 1536, kOneUnits = 2;
 // 4096 (with the radix sort): 44.3, 45.0, 46.7, 51.2 us (a run that goes over several costs a join); 2^20 of 128 floats 251, 253, 252, 243, so at most
 // chunk_max (below) positions to a team.
 constexpr uint32_t kSumBlocks = 1024;
+constexpr uint32_t kPerMin = 8;           // positions of a workgroup, at least (4, 8, 16 of 1024 floats: 4096 tokens 24.7, 23.1, 24.8 us)
 constexpr uint32_t kChunkMin = 4;         // positions of a team, which are on their way together
 constexpr uint32_t kCountThreads = 1024;
 constexpr uint32_t kCountGroup = 8;       // workgroups whose distinct rows are counted together
@@ -236,12 +237,12 @@ __device__ __forceinline__ uint32_t sort_here(const SumArgs &a, uint32_t *s_raw,
     return valid;
 }
 
-// STREAM: more goes through than the memory-side cache holds.  HERE: up to kSortHere tokens, sorted here.
+// STREAM: rows are moved past the caches (kStreamBytes).  HERE: up to kSortHere tokens, sorted here.
 template <typename T, bool DENSE, bool STREAM, bool HERE>
 __global__ __launch_bounds__(kSumThreads) void sum_runs_kernel(SumArgs a)
 {
     typedef typename Quad<T>::type Four;
-        constexpr uint32_t U = STREAM ? 8 : 4;               // rows in flight
+    constexpr uint32_t U = STREAM ? 8 : 4;               // rows in flight
     extern __shared__ uint32_t lds[];
     uint32_t *s_key = lds, *s_idx = lds + a.per + 2u;    // position i's key at i + 1
     __shared__ unsigned long long s_head[DENSE ? 1 : kSumMost / kWave];
@@ -542,7 +543,8 @@ static SumPlan sum_plan(uint32_t n, uint32_t D)
     const uint32_t most = n <= kOneBlock || room < chunk_max ? room : chunk_max;
     const uint64_t wanted = n <= kOneBlock ? p.teams : (uint64_t)p.teams * kSumBlocks;
     p.chunk = (uint32_t)((n + wanted - 1) / wanted);
-    if (p.chunk < kChunkMin) p.chunk = kChunkMin;
+    const uint32_t chunk_min = p.teams * kChunkMin < kPerMin ? kPerMin / p.teams : kChunkMin;
+    if (p.chunk < chunk_min) p.chunk = chunk_min;
     if (p.chunk > most) p.chunk = most;
     p.per = p.teams * p.chunk;
     p.blocks = (n + p.per - 1) / p.per;
@@ -556,7 +558,9 @@ EmbedGradLayout embed_grad_layout(size_t off, uint32_t max_batch, uint32_t D, in
     off = l.sort.end;
     // the most workgroups that any batch of up to max_batch tokens takes: more than kSumBlocks have as many positions as one can
     const SumPlan p = sum_plan(max_batch, D);
-    const uint32_t blocks = max_batch <= kOneBlock ? 1u : p.blocks > kSumBlocks ? p.blocks : kSumBlocks;
+    const uint32_t per_min = p.teams * kChunkMin < kPerMin ? kPerMin : p.teams * kChunkMin;
+    const uint32_t least = (uint32_t)(((uint64_t)max_batch + per_min - 1) / per_min);
+    const uint32_t few = least < kSumBlocks ? least : kSumBlocks, blocks = max_batch <= kOneBlock ? 1u : p.blocks > few ? p.blocks : few;
     auto take = [&](size_t bytes) { const size_t o = off; off = (off + bytes + 255) / 256 * 256; return o; };
     l.off_first = take((size_t)blocks * 4);
     l.off_group = take(((size_t)blocks / kCountGroup + 1) * 4);

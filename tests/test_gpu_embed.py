@@ -31,9 +31,10 @@ class Table:
         self.PE, self.PA = torch.zeros(R // k, D, device=DEV), torch.zeros(R // k, D, device=DEV)
         self.load = torch.zeros(2, S, dtype=torch.int64, device=DEV)
         self.ctx = Ecrm(R, D, k, S, max_batch=max_batch)
-        self.scratch = torch.empty(self.ctx.scratch_bytes(), dtype=torch.uint8, device=DEV)
-        self.scratch.fill_(0xA5)                         # whatever lies in it
-        self.ctx.bind(self.E, self.A, self.PE, self.PA, self.load[0], self.load[1], self.scratch)
+        size = self.ctx.scratch_bytes()
+        self.scratch = torch.full((size + 4096,), 0xA5, dtype=torch.uint8, device=DEV)       # whatever lies in it
+        self.behind = self.scratch[size:]
+        self.ctx.bind(self.E, self.A, self.PE, self.PA, self.load[0], self.load[1], self.scratch[:size])
         self.ctx.encode()
 
 
@@ -204,6 +205,20 @@ def test_gradient_of_larger_batches(R, D, n, kind, t):
     tab = Table(R, D, max_batch=n)
     check_grad(tab, tokens(R, n, kind, n, padding=0.07), gradients(n, D, t, 5), scale=float(np.float32(D ** 0.5)))
     assert tab.ctx.status() == 0
+
+
+@pytest.mark.parametrize("D", [4, 128, 296, 1024])
+def test_scratch_of_exactly_the_batch(D):
+    """Contexts whose scratch buffer serves this batch and no larger one, at the sizes where the way changes."""
+    for n in (1, 256, 257, 1536, 1537, 8192, 8193, 65536, 65537, 262144, 262145):
+        if n * D > 1 << 26:
+            continue
+        for R in (1 << 11, (1 << 11) + 4, 1 << 21):
+            tab = Table(R, D if R < 1 << 20 or D <= 128 else 64, max_batch=n)
+            check_grad(tab, tokens(R, n, "text", n, padding=0.1), gradients(n, tab.D, torch.bfloat16, 1))
+            dE = torch.full((R, tab.D), 3.0, device=DEV)
+            tab.ctx.embed_grad_dense(tokens(R, n, "runs", n), gradients(n, tab.D, torch.float32, 2), dE)
+            assert bool((tab.behind == 0xA5).all()) and tab.ctx.status() == 0
 
 
 @pytest.mark.parametrize("n", [1, 100, 1000, 5000, 20000, 66000])
