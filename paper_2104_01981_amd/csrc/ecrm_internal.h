@@ -297,11 +297,18 @@ struct TokenSort {
     TokenControl *ctl;
     const uint32_t *sk, *si;       // [valid] rows in ascending order, and the indices of their tokens, ascending for a row
 };
-// Memory to be cleared beside the sort, which leaves most of the memory's rate unused; to null: none.
-struct ClearJob { void *to; uint64_t sixteens; };
+// What is done beside the sort, which leaves most of the memory's rate unused: 16-byte units first .. first + count - 1 of some memory
+// are cleared, or, of rows `stride` bytes apart, read, so that they are in the memory-side cache when the sums come to them.
+struct BesideJob {
+    void *to;                      // to be cleared, or null
+    const char *from;              // to be read, or null
+    uint64_t stride;
+    Divider row;                   // by the units of a row
+    uint64_t first, count;
+};
 TokenSortLayout token_sort_layout(size_t off, uint32_t max_batch, int key_bits);
 TokenSort launch_token_sort(const Scratch &s, const TokenSortLayout &l, const uint64_t *keys, uint32_t n, uint64_t padding, uint32_t rows,
-                            int key_bits, ClearJob clear, int cus, hipStream_t st);
+                            int key_bits, const BesideJob &beside, int cus, hipStream_t st);
 constexpr uint32_t kRankMost = 8192;   // tokens of a batch that is sorted in one launch
 // The arrays of a gradient call.
 struct EmbedGradLayout {

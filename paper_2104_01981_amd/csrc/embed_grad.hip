@@ -6,8 +6,8 @@
 // workgroup has of runs that go on in its neighbours by a launch behind.  Sums are carried in 64 bits and rounded once, in
 // an order that follows from the sorted positions, n and D alone: no atomics, two runs give the same bits.
 //
-// What bounds it: in large batches memory -- 2^20 tokens of 128 floats, hardly any twice, 239 us, of which the sums 181: 980 MB
-// at 5.4 TB/s, more than a copy reaches --, in small ones the trips to memory that follow from one another: a launch (up to
+// What bounds it: in large batches memory -- 2^20 tokens of 128 floats, hardly any twice, 228 us, of which the sums 170: 980 MB
+// at 5.8 TB/s, in part from the memory-side cache --, in small ones the trips to memory that follow from one another: a launch (up to
 // kSortHere tokens, 6.8 us for 64), two (up to kOneBlock, 11 us for 600), three to five (up to 2^16), nine to twelve.  Of 2^16
 // tokens of text with 256 floats in bf16, 42 us, the sums take 16, the sort 20 and the join 4.
 #include "types.h"
@@ -34,6 +34,10 @@ constexpr uint32_t kScanGroups = 1024;    // from more on these counts are added
 // (2^20 tokens of 128 floats 278 us, 289 as usual; 103 MiB, 40000 of 512 floats to a dense gradient, 49 and 54; 96 MiB, 2^16 of 256
 // floats, 51 and 48: there the rows are still in the memory-side cache from whoever wrote them).
 constexpr uint64_t kStreamBytes = 100ull << 20;
+// Of these rows a quarter, but no more than kNearBytes, is read into the memory-side cache beside the sort, the first ones: what was
+// written last is there anyway.  2^20 items of 128 floats 239 us without, 228 so; 65536 of 512 floats 77.6 and 73.0, with half of the
+// rows 71.8; 2^19 of text with 128 in bf16, where the sort has less to wait for, 99.7 and 100.9, with half of them 103.4.
+constexpr uint64_t kNearBytes = 114ull << 20;
 constexpr uint32_t kJoinUnits = 16;       // of four columns, of a job
 constexpr uint32_t kLongJoin = 16;        // workgroups from which on a run is a long one
 
@@ -587,19 +591,32 @@ void launch_embed_grad(const Scratch &s, const EmbedGradLayout &l, const Geometr
 {
     const bool dense = !out_keys;
     const dim3 threads(kSumThreads);
-    ClearJob clear{nullptr, 0};
-    if (dense && !accumulate) clear = ClearJob{out, (uint64_t)g.rows * (g.D / 4u)};
+    BesideJob beside{};
+    if (dense && !accumulate) {
+        beside.to = out;
+        beside.count = (uint64_t)g.rows * (g.D / 4u);
+    }
     if (n == 0) {
         if (!dense) hipLaunchKernelGGL(no_rows_kernel, dim3(1), dim3(64), 0, st, count);
-        if (clear.to) hipLaunchKernelGGL(clear_rows_kernel, dim3((uint32_t)cus * 8u), threads, 0, st, (f32x4 *)clear.to, clear.sixteens);
+        if (beside.to) hipLaunchKernelGGL(clear_rows_kernel, dim3((uint32_t)cus * 8u), threads, 0, st, (f32x4 *)beside.to, beside.count);
         return;
+    }
+    const uint32_t size = type_bytes(type);
+    const uint64_t moved = (uint64_t)n * g.D * size + (dense ? (uint64_t)g.rows : n) * g.D * 4u;
+    const bool stream = moved > kStreamBytes;
+    if (stream && !beside.to && n > kRankMost && g.D * size % 16u == 0 && stride * size % 16u == 0 && (uintptr_t)d % 16u == 0) {
+        const uint64_t units = (uint64_t)n * (g.D * size / 16u);
+        beside.from = (const char *)d;
+        beside.stride = stride * size;
+        beside.row = make_divider(g.D * size / 16u);
+        beside.count = units / 4u < kNearBytes / 16u ? units / 4u : kNearBytes / 16u;
     }
     char *base = (char *)s.hdr;
     SumArgs a{};
-    if (n <= kSortHere && !clear.to) {
+    if (n <= kSortHere && !beside.to) {
         a.keys = keys; a.padding = padding; a.rows = g.rows; a.hdr = s.hdr;
     } else {
-        const TokenSort sorted = launch_token_sort(s, l.sort, keys, n, padding, g.rows, key_bits, clear, cus, st);
+        const TokenSort sorted = launch_token_sort(s, l.sort, keys, n, padding, g.rows, key_bits, beside, cus, st);
         a.sk = sorted.sk; a.si = sorted.si; a.ctl = sorted.ctl;
     }
     const SumPlan p = sum_plan(n, g.D);
@@ -620,10 +637,9 @@ void launch_embed_grad(const Scratch &s, const EmbedGradLayout &l, const Geometr
         if (a.counting == kScanned) hipLaunchKernelGGL(scan_heads_kernel, dim3(1), dim3(1024), 0, st, a);
     }
     const size_t lds = ((size_t)a.per * 2 + 2) * 4;
-    const uint64_t moved = (uint64_t)n * g.D * type_bytes(type) + (dense ? (uint64_t)g.rows : n) * g.D * 4u;
     with_type(type, [&](auto t) {
-        if (dense) launch_sum<decltype(t), true>(a, dim3(a.blocks, p.slices), lds, moved > kStreamBytes, st);
-        else launch_sum<decltype(t), false>(a, dim3(a.blocks, p.slices), lds, moved > kStreamBytes, st);
+        if (dense) launch_sum<decltype(t), true>(a, dim3(a.blocks, p.slices), lds, stream, st);
+        else launch_sum<decltype(t), false>(a, dim3(a.blocks, p.slices), lds, stream, st);
     });
     if (a.blocks > 1) {
         const uint32_t narrow = (a.blocks + a.teams - 1) / a.teams, most = (uint32_t)cus * 8u, wide = (uint32_t)cus;

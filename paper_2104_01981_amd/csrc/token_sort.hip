@@ -43,16 +43,31 @@ struct TokenPass {
     uint32_t *flags;                                     // [tiles] padding tokens, kBadTile
     TokenControl *ctl;
     Header *hdr;
-    ClearJob clear;                                      // by the workgroups behind the tiles'
+    BesideJob beside;                                    // by the workgroups behind the tiles'
 };
 
-// a share of the clearing for each of `blocks` workgroups
-__device__ __forceinline__ void clear_share(const ClearJob &c, uint32_t block, uint32_t blocks, uint32_t threads)
+// a share of the job for each of `blocks` workgroups
+__device__ __forceinline__ void share_of(const BesideJob &job, uint32_t block, uint32_t blocks, uint32_t threads)
 {
     typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-    u4 *to = (u4 *)c.to;
-    for (uint64_t i = (uint64_t)block * threads + threadIdx.x; i < c.sixteens; i += (uint64_t)blocks * threads)
-        to[i] = u4{0u, 0u, 0u, 0u};
+    if (job.to) {
+        u4 *to = (u4 *)job.to + job.first;
+        for (uint64_t i = (uint64_t)block * threads + threadIdx.x; i < job.count; i += (uint64_t)blocks * threads)
+            to[i] = u4{0u, 0u, 0u, 0u};
+        return;
+    }
+    constexpr uint32_t U = 8;                            // loads in flight
+    const uint32_t lane = lane_id(), count = (uint32_t)job.count, waves = blocks * (threads / kWave);
+    for (uint32_t i0 = (block * (threads / kWave) + threadIdx.x / kWave) * (U * kWave); i0 < count; i0 += waves * (U * kWave)) {
+        u4 x[U];
+#pragma unroll
+        for (uint32_t q = 0; q < U; ++q) {
+            const uint32_t i = (uint32_t)job.first + min(i0 + q * kWave + lane, count - 1u), r = job.row.div(i);
+            x[q] = *(const u4 *)(job.from + r * job.stride + (size_t)(i - r * job.row.d) * 16u);
+        }
+#pragma unroll
+        for (uint32_t q = 0; q < U; ++q) asm volatile("" : : "v"(x[q]));        // to be in the cache is all
+    }
 }
 
 // inclusive sum over the wave: within rows of 16 lanes, then over the rows
@@ -72,7 +87,7 @@ __global__ __launch_bounds__(kRankThreads) void token_rank_kernel(TokenPass a)
     __shared__ __align__(16) uint32_t s_key[kRankMost];
     __shared__ uint32_t s_pads, s_bad;
     if (blockIdx.x >= a.tiles) {
-        clear_share(a.clear, blockIdx.x - a.tiles, gridDim.x - a.tiles, kRankThreads);
+        share_of(a.beside, blockIdx.x - a.tiles, gridDim.x - a.tiles, kRankThreads);
         return;
     }
     const uint32_t tid = threadIdx.x, lane = lane_id(), wave = tid / kWave, n = a.n;
@@ -155,7 +170,7 @@ __global__ __launch_bounds__(kMergeTile) void token_tile_kernel(TokenPass a)
     __shared__ uint32_t s_key[kMergeTile], s_val[kMergeTile], s_wave[kWaves], s_pads, s_bad;
     __shared__ __align__(16) uint32_t s_cnt[kWaves << kBits];                      // [digit][wave]
     if (blockIdx.x >= a.tiles) {
-        clear_share(a.clear, blockIdx.x - a.tiles, gridDim.x - a.tiles, kMergeTile);
+        share_of(a.beside, blockIdx.x - a.tiles, gridDim.x - a.tiles, kMergeTile);
         return;
     }
     const uint32_t tid = threadIdx.x, wave = tid / kWave, lane = lane_id(), i = blockIdx.x * kMergeTile + tid;
@@ -242,7 +257,7 @@ __global__ __launch_bounds__(kMergeThreads) void token_merge_kernel(TokenPass a)
     __shared__ uint32_t s_sum[kParts][kMergeItems], s_pads, s_bad;
     const uint32_t tid = threadIdx.x, n = a.n, blocks = (n + kMergeItems - 1) / kMergeItems;
     if (blockIdx.x >= blocks) {
-        clear_share(a.clear, blockIdx.x - blocks, gridDim.x - blocks, kMergeThreads);
+        share_of(a.beside, blockIdx.x - blocks, gridDim.x - blocks, kMergeThreads);
         return;
     }
     const uint32_t item = tid % kMergeItems, part = tid / kMergeItems, i = blockIdx.x * kMergeItems + item, own = i / kMergeTile;
@@ -322,10 +337,6 @@ __global__ __launch_bounds__(kTokenThreads) void token_hist_kernel(TokenPass a)
 {
     __shared__ uint32_t s_hist[1 << kTokenBits];
     __shared__ uint32_t s_pads, s_bad;
-    if (blockIdx.x >= a.tiles) {
-        clear_share(a.clear, blockIdx.x - a.tiles, gridDim.x - a.tiles, kTokenThreads);
-        return;
-    }
     const uint32_t tid = threadIdx.x, bins = 1u << a.bits, n = FIRST ? a.n : a.ctl->valid;
     for (uint32_t i = tid; i < bins; i += kTokenThreads) s_hist[i] = 0;
     if (FIRST && tid == 0) s_pads = s_bad = 0;
@@ -422,7 +433,7 @@ __global__ __launch_bounds__(kTokenThreads) void token_scatter_kernel(TokenPass 
     uint32_t *s_keys = lds, *s_vals = lds + kTile, *s_start = lds + 2 * kTile, *s_base = s_start + bins;
     uint16_t *s_cnt = (uint16_t *)(s_base + bins);       // [waves][bins] counts, then offsets, of a wave
     if (blockIdx.x >= a.tiles) {
-        clear_share(a.clear, blockIdx.x - a.tiles, gridDim.x - a.tiles, kTokenThreads);
+        share_of(a.beside, blockIdx.x - a.tiles, gridDim.x - a.tiles, kTokenThreads);
         return;
     }
     const uint32_t n = FIRST ? a.n : a.ctl->valid;
@@ -621,9 +632,9 @@ TokenSortLayout token_sort_layout(size_t off, uint32_t max_batch, int key_bits)
 }
 
 template <bool FIRST, int IPT, bool GROUPED>
-static void launch_token_pass(const TokenPass &a, uint32_t clears, hipStream_t st)
+static void launch_token_pass(const TokenPass &a, uint32_t helpers, hipStream_t st)
 {
-    const dim3 hist(a.tiles), scatter(a.tiles + clears), block(kTokenThreads);
+    const dim3 hist(a.tiles), scatter(a.tiles + helpers), block(kTokenThreads);
     const size_t lds = scatter_lds(a.bits, IPT);
     hipLaunchKernelGGL((token_hist_kernel<FIRST, IPT, GROUPED>), hist, block, 0, st, a);
     if (GROUPED) hipLaunchKernelGGL(token_groups_kernel, dim3(a.groups, ((1u << a.bits) + 255u) / 256u), dim3(256), 0, st, a);
@@ -634,15 +645,15 @@ static void launch_token_pass(const TokenPass &a, uint32_t clears, hipStream_t s
 }
 
 template <bool FIRST>
-static void launch_token_pass(const TokenPass &a, int ipt, uint32_t clears, hipStream_t st)
+static void launch_token_pass(const TokenPass &a, int ipt, uint32_t helpers, hipStream_t st)
 {
-    if (ipt == 8) launch_token_pass<FIRST, 8, true>(a, clears, st);
-    else if (is_grouped(a.tiles)) launch_token_pass<FIRST, 4, true>(a, clears, st);
-    else launch_token_pass<FIRST, 4, false>(a, clears, st);
+    if (ipt == 8) launch_token_pass<FIRST, 8, true>(a, helpers, st);
+    else if (is_grouped(a.tiles)) launch_token_pass<FIRST, 4, true>(a, helpers, st);
+    else launch_token_pass<FIRST, 4, false>(a, helpers, st);
 }
 
 TokenSort launch_token_sort(const Scratch &s, const TokenSortLayout &l, const uint64_t *keys, uint32_t n, uint64_t padding, uint32_t rows,
-                            int key_bits, ClearJob clear, int cus, hipStream_t st)
+                            int key_bits, const BesideJob &beside, int cus, hipStream_t st)
 {
     char *base = (char *)s.hdr;
     TokenPass a{};
@@ -651,32 +662,32 @@ TokenSort launch_token_sort(const Scratch &s, const TokenSortLayout &l, const ui
     a.flags = (uint32_t *)(base + l.off_flags);
     a.table = (uint16_t *)(base + l.off_table);
     a.sums = (uint32_t *)(base + l.off_groups);
+    a.beside = beside;
     TokenSort r;
     r.ctl = a.ctl;
-    const uint32_t clears = clear.to ? (uint32_t)cus * 4u : 0u;
+    const uint32_t helpers = beside.count ? (uint32_t)cus * 4u : 0u;
     if (n <= kRankMost) {
         const uint32_t each = kRankItems * (kRankThreads / kWave);
         a.tiles = (n + each - 1) / each;
         a.keys_out = s.keys[0]; a.vals_out = s.vals[0];
-        a.clear = clear;
-        hipLaunchKernelGGL(token_rank_kernel, dim3(a.tiles + clears), dim3(kRankThreads), 0, st, a);
+        hipLaunchKernelGGL(token_rank_kernel, dim3(a.tiles + helpers), dim3(kRankThreads), 0, st, a);
         r.sk = s.keys[0];
         r.si = s.vals[0];
         return r;
     }
     if (n <= kMergeMost) {
         const uint32_t blocks = (n + kMergeItems - 1) / kMergeItems;
-        const uint64_t half = clear.sixteens / 2u;       // of the clearing, beside either
         a.tiles = (n + kMergeTile - 1) / kMergeTile;
         a.bits = key_bits;
         while (a.bits < 32 && (1ull << a.bits) <= rows) ++a.bits;
         a.keys_out = s.keys[1]; a.vals_out = s.vals[1];
-        a.clear.to = clear.to; a.clear.sixteens = half;
-        hipLaunchKernelGGL(token_tile_kernel, dim3(a.tiles + clears), dim3(kMergeTile), 0, st, a);
+        a.beside.count = beside.count / 2u;              // half of the job beside either
+        hipLaunchKernelGGL(token_tile_kernel, dim3(a.tiles + helpers), dim3(kMergeTile), 0, st, a);
         a.keys = s.keys[1]; a.vals = s.vals[1];
         a.keys_out = s.keys[0]; a.vals_out = s.vals[0];
-        a.clear.to = clear.to ? (char *)clear.to + half * 16 : nullptr; a.clear.sixteens = clear.sixteens - half;
-        hipLaunchKernelGGL(token_merge_kernel, dim3(blocks + clears), dim3(kMergeThreads), 0, st, a);
+        a.beside.first = a.beside.count;
+        a.beside.count = beside.count - a.beside.first;
+        hipLaunchKernelGGL(token_merge_kernel, dim3(blocks + helpers), dim3(kMergeThreads), 0, st, a);
         r.sk = s.keys[0];
         r.si = s.vals[0];
         return r;
@@ -686,8 +697,6 @@ TokenSort launch_token_sort(const Scratch &s, const TokenSortLayout &l, const ui
     const int passes = token_passes(key_bits, is_grouped(a.tiles));
     a.group = group_of(a.tiles);
     a.groups = (a.tiles + a.group - 1) / a.group;
-    // the clearing, a part beside each digit's scatter
-    const uint64_t part = (clear.sixteens + passes - 1) / passes;
     int shift = 0;
     for (int p = 0; p < passes; ++p) {
         const int out = p & 1;
@@ -695,10 +704,10 @@ TokenSort launch_token_sort(const Scratch &s, const TokenSortLayout &l, const ui
         a.bits = digit_of(key_bits - shift, passes - p);
         a.keys = s.keys[out ^ 1]; a.vals = s.vals[out ^ 1];
         a.keys_out = s.keys[out]; a.vals_out = s.vals[out];
-        a.clear.to = clear.to ? (char *)clear.to + p * part * 16 : nullptr;
-        a.clear.sixteens = (uint64_t)p * part >= clear.sixteens ? 0 : clear.sixteens - p * part < part ? clear.sixteens - p * part : part;
-        if (p == 0) launch_token_pass<true>(a, ipt, clears, st);
-        else launch_token_pass<false>(a, ipt, clears, st);
+        a.beside.first = beside.count * p / passes;      // a part of the job beside each digit's scatter
+        a.beside.count = beside.count * (p + 1) / passes - a.beside.first;
+        if (p == 0) launch_token_pass<true>(a, ipt, helpers, st);
+        else launch_token_pass<false>(a, ipt, helpers, st);
         shift += a.bits;
         r.sk = s.keys[out];
         r.si = s.vals[out];

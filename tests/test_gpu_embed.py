@@ -207,6 +207,22 @@ def test_gradient_of_larger_batches(R, D, n, kind, t):
     assert tab.ctx.status() == 0
 
 
+@pytest.mark.parametrize("R,D,n,t,extra", [(1 << 14, 1024, 18001, torch.bfloat16, 8), (1 << 14, 1020, 18001, torch.float16, 0),
+                                           (1 << 12, 512, 27011, torch.float32, 4), (1 << 16, 256, 70001, torch.float16, 4),
+                                           (1 << 12, 36, 900001, torch.float32, 12), (1 << 18, 128, 300007, torch.bfloat16, 64)])
+def test_gradient_of_rows_past_the_caches(R, D, n, t, extra):
+    """Rows of more than 100 MiB together, some of which are read ahead: 16 bytes at a time where all of them are so aligned."""
+    tab = Table(R, D, max_batch=n)
+    keys, d = tokens(R, n, "text", n, padding=0.05), gradients(n, D, t, 7, extra=extra)
+    names, sums, mags = check_grad(tab, keys, d)
+    old = torch.randn(R, D, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV)
+    dE = old.clone()
+    tab.ctx.embed_grad_dense(keys, d, dE, padding=PAD, accumulate=True)
+    close(dE[names], sums + old[names].double(), mags + old[names].double().abs(), n)
+    away = torch.isin(torch.arange(R, device=DEV), names, invert=True)
+    assert torch.equal(dE[away], old[away]) and tab.ctx.status() == 0
+
+
 @pytest.mark.parametrize("D", [4, 128, 296, 1024])
 def test_scratch_of_exactly_the_batch(D):
     """Contexts whose scratch buffer serves this batch and no larger one, at the sizes where the way changes."""
