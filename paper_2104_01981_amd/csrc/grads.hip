@@ -1,9 +1,8 @@
 // The global norm of a list of gradients, and clipping: norm = sqrt(sum over all tensors and elements of g^2), and
 // g * min(1, max_norm / (norm + 1e-6)).
 //
-// The list becomes a table in device memory (ecrm_grads_bind): the tensors, and for each chunk of kGradBytes of one tensor's
-// memory which tensor's it is and where -- so that one launch goes over any number of tensors of any sizes, a workgroup a chunk at a
-// time.  What bounds both: memory, every element read once (and written once): the norm of 562 MB takes 89 us, 6.3 TB/s.
+// The list becomes a table in device memory (ecrm_grads_bind): the tensors, and for each chunk of one tensor's memory which
+// tensor's it is and where -- so that one launch goes over any number of tensors of any sizes, a workgroup a chunk at a time.  What bounds both: memory, every element read once (and written once): the norm of 562 MB takes 89 us, 6.3 TB/s.
 // Squares are summed in 64 bits: squares of 32-bit values neither overflow nor vanish there, and no order of the sum can be
 // seen in the 32 bits of the norm.
 #include <math.h>
@@ -17,12 +16,16 @@ using namespace ecrm;
 namespace ecrm {
 
 constexpr int kGradThreads = 256;
-constexpr uint32_t kGradBytes = 16384;    // of a chunk: four 16-byte loads of a lane (two: 96 us for the 95 below, eight: 169)
+// Of a chunk, in a list of up to kLongList: two 16-byte loads of a lane, in a longer one four.  4 KB, 8 KB, 16 KB: norm and clipping of 8 MB
+// into 17 MB 14.4, 13.8, 15.0 us, of 34 MB into as many 24.3, 24.2, 26.0; the norm of 34 MB 10.8, 10.6, 12.2, of 537 MB 91, 88, 87; norm and
+// clipping of 268 MB into as many 139, 142, 134.
+constexpr uint32_t kShortChunk = 8192, kLongChunk = 16384;
 // Of a list longer than the memory-side cache's 256 MiB what the norm reads last is what clipping, from the end on, finds there:
-// the last kNearChunks are read as usual, the others, and all that clipping moves in a list of more than kStreamChunks, past the
+// the last kNearChunks are read as usual, the others, and all that clipping moves in a list of more than kLongList, past the
 // caches.  2^28 elements, 562 MB: norm 95 us as usual, 87 all past the caches, 89 so; norm and clipping of 268 MB into as many: 164
 // as usual, 156 with loads past the caches, 135 with stores, 134 so (128 MiB near: 139).  A list of 8 MB into 17: 15.5 as usual, 16.3.
-constexpr uint32_t kNearChunks = (192u << 20) / kGradBytes, kStreamChunks = (128u << 20) / kGradBytes;
+constexpr uint64_t kLongList = 128ull << 20;
+constexpr uint32_t kNearChunks = (192u << 20) / kLongChunk;
 constexpr uint32_t kGradBlocks = 2048;    // workgroups of a launch, at most
 constexpr uint32_t kGradPart = 48;        // tensors that one launch writes into the table
 
@@ -35,7 +38,7 @@ struct GradTensor {
     uint32_t skew;                        // elements from the 16-byte boundary at or before data to data
 };
 struct GradPart { GradTensor t[kGradPart]; };
-// A chunk: kGradBytes of one tensor's memory from a 16-byte boundary on, of which the elements [from, to) are the tensor's.
+// A chunk: some bytes of one tensor's memory from a 16-byte boundary on, of which the elements [from, to) are the tensor's.
 struct GradChunk {
     const void *base;
     uint64_t first;                       // element of the tensor that base would be, from <= 0 where the tensor begins behind it
@@ -61,7 +64,7 @@ __global__ void write_table_kernel(GradPart p, uint32_t first, uint32_t cnt, Gra
 }
 
 __global__ __launch_bounds__(kGradThreads) void write_chunks_kernel(const GradTensor *tensors, uint32_t count, uint32_t chunks,
-                                                                    GradChunk *chunk)
+                                                                    uint32_t chunk_bytes, GradChunk *chunk)
 {
     const uint32_t i = blockIdx.x * kGradThreads + threadIdx.x;
     if (i >= chunks) return;
@@ -72,10 +75,10 @@ __global__ __launch_bounds__(kGradThreads) void write_chunks_kernel(const GradTe
         else hi = mid;
     }
     const GradTensor t = tensors[lo];
-    const uint32_t each = kGradBytes / type_bytes(t.type);
+    const uint32_t each = chunk_bytes / type_bytes(t.type);
     const uint64_t nth = i - t.first_chunk, end = t.elements + t.skew - nth * each;
     GradChunk c;
-    c.base = (const char *)t.data - (size_t)t.skew * type_bytes(t.type) + nth * kGradBytes;
+    c.base = (const char *)t.data - (size_t)t.skew * type_bytes(t.type) + nth * chunk_bytes;
     c.first = nth * each - t.skew;
     c.from = nth ? 0u : t.skew;
     c.to = (uint32_t)(end < each ? end : each);
@@ -112,11 +115,11 @@ __device__ __forceinline__ typename Several<T, N>::type some_of(const T *p, uint
 // A lane's elements of a chunk, N at a time: f(first of them, the N).  A chunk that is the tensor's as a whole -- most are --
 // is loaded without a branch, all of it in flight.
 // STREAM: it is not read again soon.
-template <typename T, uint32_t N, bool STREAM, typename F>
+template <typename T, uint32_t N, uint32_t BYTES, bool STREAM, typename F>
 __device__ __forceinline__ void over_chunk(const void *base, uint32_t from, uint32_t to, F f)
 {
     typedef typename Several<T, N>::type Vec;
-    constexpr uint32_t U = kGradBytes / (N * sizeof(T)) / kGradThreads;
+    constexpr uint32_t U = BYTES / (N * sizeof(T)) / kGradThreads;
     const T *p = (const T *)base;
     if (from == 0 && to == U * N * kGradThreads) {
         Vec x[U];
@@ -136,12 +139,12 @@ __device__ __forceinline__ void over_chunk(const void *base, uint32_t from, uint
     }
 }
 
-template <typename T, bool STREAM>
+template <typename T, uint32_t BYTES, bool STREAM>
 __device__ __forceinline__ double square_chunk(const GradChunk &c, uint32_t to)
 {
     constexpr uint32_t N = 16 / sizeof(T);
     double acc[2] = {0, 0};
-    over_chunk<T, N, STREAM>(c.base, c.from, to, [&](uint32_t, const typename Several<T, N>::type &x) {
+    over_chunk<T, N, BYTES, STREAM>(c.base, c.from, to, [&](uint32_t, const typename Several<T, N>::type &x) {
 #pragma unroll
         for (uint32_t j = 0; j < N; ++j) {
             const double g = (double)(float)x[j];
@@ -151,12 +154,12 @@ __device__ __forceinline__ double square_chunk(const GradChunk &c, uint32_t to)
     return acc[0] + acc[1];
 }
 
-template <bool STREAM>
+template <uint32_t BYTES, bool STREAM>
 __device__ __forceinline__ double squares(const GradChunk &c, uint32_t to, uint32_t type)
 {
-    if (type == ECRM_BF16) return square_chunk<__bf16, STREAM>(c, to);
-    if (type == ECRM_F16) return square_chunk<_Float16, STREAM>(c, to);
-    return square_chunk<float, STREAM>(c, to);
+    if (type == ECRM_BF16) return square_chunk<__bf16, BYTES, STREAM>(c, to);
+    if (type == ECRM_F16) return square_chunk<_Float16, BYTES, STREAM>(c, to);
+    return square_chunk<float, BYTES, STREAM>(c, to);
 }
 
 // sum over the workgroup, in an order that does not change, to thread 0
@@ -180,6 +183,8 @@ __device__ __forceinline__ bool arrive(uint32_t *counter, uint32_t members)
     return true;
 }
 
+// LONG: of a list of more than kLongList
+template <bool LONG>
 __global__ __launch_bounds__(kGradThreads) void norm_kernel(GradTable g, float *norm)
 {
     __shared__ double s_wave[kGradThreads / kWave];
@@ -190,7 +195,8 @@ __global__ __launch_bounds__(kGradThreads) void norm_kernel(GradTable g, float *
         const GradChunk c = next;
         next = g.chunk[min(i + gridDim.x, g.chunks - 1u)];
         const uint32_t to = counted_end(g, c), type = c.type & ~kCounted;
-        acc += i + kNearChunks < g.chunks ? squares<true>(c, to, type) : squares<false>(c, to, type);
+        if (!LONG) acc += squares<kShortChunk, false>(c, to, type);
+        else acc += i + kNearChunks < g.chunks ? squares<kLongChunk, true>(c, to, type) : squares<kLongChunk, false>(c, to, type);
     }
     const double sum = block_sum(acc, s_wave);
     // the last workgroup adds up what all have left, in the order of their numbers
@@ -226,30 +232,30 @@ __device__ __forceinline__ void store_some(TO *p, int64_t from, int64_t to, cons
         if ((int64_t)j >= from && (int64_t)j < to) p[j] = (TO)y[j];
 }
 
-template <typename T, typename TO, bool STREAM>
+template <typename T, typename TO, bool LONG>
 __device__ __forceinline__ void clip_chunk(const GradChunk &c, uint32_t to, void *out, double factor)
 {
     constexpr uint32_t N = 16 / (sizeof(T) > sizeof(TO) ? sizeof(T) : sizeof(TO));      // 16 bytes of the wider
     TO *o = (TO *)out + (int64_t)c.first;
-    over_chunk<T, N, STREAM>(c.base, c.from, to, [&](uint32_t v, const typename Several<T, N>::type &x) {
+    over_chunk<T, N, LONG ? kLongChunk : kShortChunk, LONG>(c.base, c.from, to, [&](uint32_t v, const typename Several<T, N>::type &x) {
         float y[N];
         // the product in 64 bits, so that a 32-bit gradient is rounded once (a 16-bit one in 32 bits first)
 #pragma unroll
         for (uint32_t j = 0; j < N; ++j) y[j] = (float)((double)(float)x[j] * factor);
-        store_some<TO, STREAM, N>(o + v, (int64_t)c.from - v, (int64_t)to - v, y);
+        store_some<TO, LONG, N>(o + v, (int64_t)c.from - v, (int64_t)to - v, y);
     });
 }
 
-template <typename T, bool STREAM>
+template <typename T, bool LONG>
 __device__ __forceinline__ void clip_to(const GradChunk &c, uint32_t to, void *out, uint32_t type, double factor)
 {
-    if (type == ECRM_BF16) clip_chunk<T, __bf16, STREAM>(c, to, out, factor);
-    else if (type == ECRM_F16) clip_chunk<T, _Float16, STREAM>(c, to, out, factor);
-    else clip_chunk<T, float, STREAM>(c, to, out, factor);
+    if (type == ECRM_BF16) clip_chunk<T, __bf16, LONG>(c, to, out, factor);
+    else if (type == ECRM_F16) clip_chunk<T, _Float16, LONG>(c, to, out, factor);
+    else clip_chunk<T, float, LONG>(c, to, out, factor);
 }
 
 // out: a table of as many tensors of as many elements; where it is the list's own, the call is in place
-template <bool STREAM>
+template <bool LONG>
 __global__ __launch_bounds__(kGradThreads) void clip_kernel(GradTable g, const GradTensor *out, const float *norm, double max_norm)
 {
     double factor = max_norm / ((double)*norm + 1e-6);
@@ -262,9 +268,9 @@ __global__ __launch_bounds__(kGradThreads) void clip_kernel(GradTable g, const G
         next = g.chunk[g.chunks - 1u - min(i + gridDim.x, g.chunks - 1u)];
         void *o = out[c.tensor].data;
         const uint32_t to = counted_end(g, c), type = c.type & ~kCounted, out_type = out[c.tensor].type;
-        if (type == ECRM_BF16) clip_to<__bf16, STREAM>(c, to, o, out_type, factor);
-        else if (type == ECRM_F16) clip_to<_Float16, STREAM>(c, to, o, out_type, factor);
-        else clip_to<float, STREAM>(c, to, o, out_type, factor);
+        if (type == ECRM_BF16) clip_to<__bf16, LONG>(c, to, o, out_type, factor);
+        else if (type == ECRM_F16) clip_to<_Float16, LONG>(c, to, o, out_type, factor);
+        else clip_to<float, LONG>(c, to, o, out_type, factor);
     }
 }
 
@@ -274,6 +280,7 @@ __global__ __launch_bounds__(kGradThreads) void clip_kernel(GradTable g, const G
 struct ecrm_grads {
     GradTensor *list;                     // [count], host memory
     uint32_t count, chunks;
+    bool is_long;
     size_t off_chunks, off_part, off_arrived, bytes;
     char *table;                          // bound device memory
 };
@@ -298,13 +305,14 @@ int ecrm_grads_create(const ecrm_tensor *tensors, uint32_t count, ecrm_grads **o
     if (!out || (count && !tensors)) return ECRM_EINVAL;
     *out = nullptr;
     if (count > (1u << 24)) return ECRM_EINVAL;
-    uint64_t chunks = 0;
+    uint64_t chunks = 0, bytes = 0;
     for (uint32_t i = 0; i < count; ++i) {
         const ecrm_tensor &t = tensors[i];
         if (t.type > ECRM_F16 || (t.elements && !t.data) || (uintptr_t)t.data % type_bytes(t.type)) return ECRM_EINVAL;
         if (t.elements > (1ull << 48)) return ECRM_EINVAL;
         if (t.rows && ((uintptr_t)t.rows % 8 || !t.row_elements || t.elements % t.row_elements)) return ECRM_EINVAL;
-        chunks += (t.elements + 8u) / (kGradBytes / type_bytes(t.type)) + 1u;
+        bytes += t.elements * type_bytes(t.type);
+        chunks += (t.elements + 8u) / (kShortChunk / type_bytes(t.type)) + 1u;
     }
     if (chunks > 0xFFFFFFFFull) return ECRM_EINVAL;
     ecrm_grads *g = new (std::nothrow) ecrm_grads;
@@ -317,6 +325,8 @@ int ecrm_grads_create(const ecrm_tensor *tensors, uint32_t count, ecrm_grads **o
     memset(g, 0, sizeof(*g));
     g->list = list;
     g->count = count;
+    g->is_long = bytes > kLongList;
+    const uint32_t chunk_bytes = g->is_long ? kLongChunk : kShortChunk;
     for (uint32_t i = 0; i < count; ++i) {
         const ecrm_tensor &t = tensors[i];
         GradTensor &to = list[i];
@@ -327,7 +337,7 @@ int ecrm_grads_create(const ecrm_tensor *tensors, uint32_t count, ecrm_grads **o
         to.type = t.type;
         to.first_chunk = g->chunks;
         to.skew = (uint32_t)((uintptr_t)t.data % 16 / type_bytes(t.type));
-        const uint32_t each = kGradBytes / type_bytes(t.type);
+        const uint32_t each = chunk_bytes / type_bytes(t.type);
         if (t.elements) g->chunks += (uint32_t)((t.elements + to.skew + each - 1) / each);
     }
     size_t off = 0;
@@ -368,7 +378,7 @@ int ecrm_grads_bind(ecrm_grads *g, void *table, size_t table_bytes, void *stream
     } while (first < g->count);
     if (g->chunks)
         hipLaunchKernelGGL(write_chunks_kernel, dim3((g->chunks + kGradThreads - 1) / kGradThreads), dim3(kGradThreads), 0, st,
-                           t.tensors, g->count, g->chunks, (GradChunk *)t.chunk);
+                           t.tensors, g->count, g->chunks, g->is_long ? kLongChunk : kShortChunk, (GradChunk *)t.chunk);
     return launched();
 }
 
@@ -378,7 +388,8 @@ int ecrm_grads_norm(ecrm_grads *g, float *norm, void *stream)
     if (!g->table) return ECRM_ENOTBOUND;
     if (!norm || (uintptr_t)norm % 4) return ECRM_EINVAL;
     const uint32_t blocks = g->chunks < kGradBlocks ? (g->chunks ? g->chunks : 1u) : kGradBlocks;
-    hipLaunchKernelGGL(norm_kernel, dim3(blocks), dim3(kGradThreads), 0, (hipStream_t)stream, table_of(g), norm);
+    hipLaunchKernelGGL((g->is_long ? norm_kernel<true> : norm_kernel<false>), dim3(blocks), dim3(kGradThreads), 0, (hipStream_t)stream,
+                       table_of(g), norm);
     return launched();
 }
 
@@ -394,8 +405,8 @@ int ecrm_grads_clip(ecrm_grads *g, const ecrm_grads *out, const float *norm, flo
     }
     if (!g->chunks) return ECRM_OK;
     const uint32_t blocks = g->chunks < kGradBlocks ? g->chunks : kGradBlocks;
-    hipLaunchKernelGGL((g->chunks > kStreamChunks ? clip_kernel<true> : clip_kernel<false>), dim3(blocks), dim3(kGradThreads), 0, (hipStream_t)stream, table_of(g),
-                       (const GradTensor *)(out ? out : g)->table, norm, (double)max_norm);
+    hipLaunchKernelGGL((g->is_long ? clip_kernel<true> : clip_kernel<false>), dim3(blocks), dim3(kGradThreads), 0, (hipStream_t)stream,
+                       table_of(g), (const GradTensor *)(out ? out : g)->table, norm, (double)max_norm);
     return launched();
 }
 

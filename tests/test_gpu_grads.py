@@ -85,6 +85,30 @@ def test_norm_and_clip(sizes, types, shift):
     assert all(not x.any() for x in src)
 
 
+@pytest.mark.parametrize("sizes,types", [([33554432], [F32]), ([33554433], [F32]), ([12000001, 4097, 9, 30000011, 0, 8193, 16385, 3], [F32, BF16]),
+                                         ([40000003, 24000005, 2, 16383], [F16, F32]), ([70000001, 1, 50000001], [BF16])])
+@pytest.mark.parametrize("shift", [(), (1, 3, 0, 2)])
+def test_long_lists(sizes, types, shift):
+    """Around 128 MiB, from which on chunks are larger, and beyond 192 MiB; with and without rows that the device counts."""
+    src = make(sizes, types, 3, shift=shift)
+    rows, count = torch.full((501, 36), float("nan"), device=DEV), torch.tensor([77], device=DEV)
+    rows[:77] = 1.5
+    norm = torch.zeros(1, device=DEV)
+    for counted in (False, True):
+        every = src + [rows[:77]] if counted else src
+        grads = Grads(src + [(rows, count)] if counted else src)
+        grads.norm(norm)
+        near(float(norm), norm_of(every))
+        out = make(sizes, [types[-1]], 1) + ([torch.full_like(rows, 5.0)] if counted else [])
+        grads.clip(norm, 0.25, out=Grads(out))
+        check_clipped([*out[:len(src)], out[-1][:77]] if counted else out, every, float(norm), 0.25)
+        assert not counted or bool((out[-1][77:] == 5.0).all())
+        del out
+    was = [x.clone() for x in src]
+    grads.clip(norm, 0.25)
+    check_clipped(src + [rows[:77]], was + [torch.full_like(rows[:77], 1.5)], float(norm), 0.25)
+
+
 def test_neighbours_are_left_alone():
     """Tensors inside one buffer with a value between each two of them."""
     buf = torch.full((40000,), 9.0, dtype=BF16, device=DEV)
