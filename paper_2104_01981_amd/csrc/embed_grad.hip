@@ -6,8 +6,8 @@
 // workgroup has of runs that go on in its neighbours by a launch behind.  Sums are carried in 64 bits and rounded once, in
 // an order that follows from the sorted positions, n and D alone: no atomics, two runs give the same bits.
 //
-// What bounds it: in large batches memory -- 2^20 tokens of 128 floats, hardly any twice, 228 us, of which the sums 170: 980 MB
-// at 5.8 TB/s, in part from the memory-side cache --, in small ones the trips to memory that follow from one another: a launch (up to
+// What bounds it: in large batches memory -- 2^20 tokens of 128 floats, hardly any twice, 228 us, of which the sums 164: 980 MB
+// at 6.0 TB/s, in part from the memory-side cache --, in small ones the trips to memory that follow from one another: a launch (up to
 // kSortHere tokens, 6.8 us for 64), two (up to kOneBlock, 11 us for 600), three to five (up to 2^16), nine to twelve.  Of 2^16
 // tokens of text with 256 floats in bf16, 42 us, the sums take 16, the sort 20 and the join 4.
 #include "types.h"
