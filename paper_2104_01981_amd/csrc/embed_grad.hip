@@ -36,7 +36,7 @@ constexpr uint32_t kScanGroups = 1024;    // from more on these counts are added
 constexpr uint64_t kStreamBytes = 100ull << 20;
 // Of these rows a quarter, but no more than kNearBytes, is read into the memory-side cache beside the sort, the first ones: what was
 // written last is there anyway.  2^20 items of 128 floats 239 us without, 228 so; 65536 of 512 floats 77.6 and 73.0, with half of the
-// rows 71.8; 2^19 of text with 128 in bf16, where the sort has less to wait for, 99.7 and 100.9, with half of them 103.4.
+// rows 71.8; 18001 of 1024 in bf16 45.6 and 44.9; 2^19 of text with 128 in bf16 99.7 and 100.9, with half of them 103.4.
 constexpr uint64_t kNearBytes = 114ull << 20;
 constexpr uint32_t kJoinUnits = 16;       // of four columns, of a job
 constexpr uint32_t kLongJoin = 16;        // workgroups from which on a run is a long one
