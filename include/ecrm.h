@@ -98,7 +98,10 @@ size_t ecrm_scratch_bytes(const ecrm_ctx *ctx);
  * ecrm_scratch_bytes() long; its contents are private to the library while bound.  The load
  * counters are accumulated into, never cleared.  Returns EINVAL for a NULL / misaligned table,
  * ESCRATCH for the scratch buffer, ESTATE while a recovery is in progress (the updates waiting in its
- * buffer would be lost), EHIP if the device cannot be queried.  Call it outside a stream capture. */
+ * buffer would be lost), EHIP if the device cannot be queried.  Call it outside a stream capture.
+ * The first call after it that enqueues anything -- ecrm_encode, where the parities are not there already -- also clears the
+ * status and the counts in scratch, on its stream: order every call on another stream behind it, and make it outside a
+ * stream capture, or each replay clears them again. */
 int ecrm_bind(ecrm_ctx *ctx, float *E, float *A, float *PE, float *PA,
               uint64_t *load_data, uint64_t *load_parity, void *scratch, size_t scratch_bytes);
 
@@ -246,7 +249,8 @@ int ecrm_recovery_read(ecrm_ctx *ctx, const uint64_t *keys, uint64_t n, float *o
  * 8 bytes, memory the device can write.  padding: any value, a row of the table or not (-1, -100); ECRM_NO_PADDING (2^63):
  * there is none.  scale has to be finite.  The
  * gradient calls use the scratch buffer (call them on the update stream; n <= max_batch, else EBATCH) but no table, and leave
- * what ecrm_batch_stats reports; the lookup uses none.  All only enqueue. */
+ * what ecrm_batch_stats reports; the lookup uses of it the sticky status alone, so that it may run on any stream behind the
+ * first call after ecrm_bind (see there).  All only enqueue. */
 enum { ECRM_F32 = 0, ECRM_BF16 = 1, ECRM_F16 = 2 };
 #define ECRM_NO_KEY 0xFFFFFFFFFFFFFFFFull
 #define ECRM_NO_PADDING 0x8000000000000000ull

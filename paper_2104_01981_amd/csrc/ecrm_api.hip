@@ -315,6 +315,7 @@ int ecrm_encode(ecrm_ctx *c, void *stream)
     if (!c) return ECRM_EINVAL;
     if (!c->bound) return ECRM_ENOTBOUND;
     if (c->rv.active) return ECRM_ESTATE;      // rows of the lost server are not there to be summed
+    init_if_needed(c, (hipStream_t)stream);    // so that no read on another stream, or in a graph, is the one that clears the header
     launch_encode(c->geo, c->t.E, c->t.A, c->t.PE, c->t.PA, c->grid_blocks, (hipStream_t)stream);
     return check_launch();
 }

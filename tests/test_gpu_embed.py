@@ -518,3 +518,44 @@ def test_refusals():
     assert int(count) == 0 and bool((dE == 1).all())
     tab.ctx.embed_grad_dense(none, d[:0, :D], dE)
     assert bool((dE == 0).all()) and tab.ctx.status() == 0
+
+
+def fresh(R=1 << 10, D=36, n=64):
+    """A context that has been bound and encoded, whose next call is its first one; the scratch buffer held anything."""
+    tab = Table(R, D, max_batch=n)
+    bad = torch.full((n,), R, dtype=torch.int64, device=DEV)
+    torch.cuda.synchronize()
+    return tab, bad, torch.zeros(n, D, device=DEV)
+
+
+def test_a_first_lookup_on_another_stream_clears_nothing():
+    """The lookup is held up on its stream until an update behind it on the main one has found a bad key."""
+    tab, bad, grads = fresh()
+    keys, out = tokens(tab.R, 64, "uniform", 1), torch.empty(64, tab.D, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+        tab.ctx.embed(keys, out)
+    tab.ctx.update(bad, grads)
+    torch.cuda.current_stream().synchronize()
+    side.synchronize()
+    assert tab.ctx.status() == ECRM_EKEYRANGE and tab.ctx.batch_stats()["rejected"] == 1
+    assert torch.equal(out, tab.E[keys])
+
+
+def test_a_first_lookup_in_a_graph_clears_nothing_when_it_is_replayed():
+    tab, bad, grads = fresh()
+    keys, out = tokens(tab.R, 64, "uniform", 1), torch.empty(64, tab.D, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        tab.ctx.embed(keys, out)
+    tab.ctx.update(bad, grads)
+    for _ in range(3):
+        out.fill_(5.0)
+        graph.replay()
+        assert tab.ctx.status() == ECRM_EKEYRANGE and tab.ctx.batch_stats()["rejected"] == 1
+        assert torch.equal(out, tab.E[keys])
+    tab.ctx.clear_status()
+    graph.replay()
+    assert tab.ctx.status() == 0
