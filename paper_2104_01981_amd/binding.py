@@ -219,7 +219,10 @@ class Grads:
     def clip(self, norm, max_norm, out=None, stream=None, check=True):
         """In place, or into the tensors of `out`, another list."""
         assert norm.is_cuda and _type(norm) == 0 and norm.numel() == 1
-        rc = self._lib.ecrm_grads_clip(self._grads, out._grads if out is not None else None, norm.data_ptr(), max_norm, _stream(stream))
+        if out is not None and not out._grads:           # destroyed: NULL would be "in place"
+            rc = ECRM_EINVAL
+        else:
+            rc = self._lib.ecrm_grads_clip(self._grads, out._grads if out is not None else None, norm.data_ptr(), max_norm, _stream(stream))
         if check and rc != ECRM_OK:
             raise EcrmError(rc, "ecrm_grads_clip")
         return rc

@@ -221,3 +221,20 @@ def test_refusals():
         Grads([torch.ones(10, dtype=torch.float64, device=DEV)])
     torch.cuda.synchronize()
     assert bool((x == 1).all())
+
+
+def test_a_destroyed_list_is_refused():
+    """... and is not taken for "in place"."""
+    x, y, norm = torch.ones(100, device=DEV), torch.zeros(100, device=DEV), torch.full((1,), 10.0, device=DEV)
+    grads, out = Grads([x]), Grads([y])
+    out.destroy()
+    with pytest.raises(EcrmError) as e:
+        grads.clip(norm, 1.0, out=out)
+    assert e.value.code == ECRM_EINVAL and grads.clip(norm, 1.0, out=out, check=False) == ECRM_EINVAL
+    grads.destroy()
+    for call in (lambda: grads.norm(norm), lambda: grads.clip(norm, 1.0)):
+        with pytest.raises(EcrmError) as e:
+            call()
+        assert e.value.code == ECRM_EINVAL
+    torch.cuda.synchronize()
+    assert bool((x == 1).all()) and not y.any() and float(norm) == 10.0
