@@ -131,6 +131,14 @@ def _stream(stream):
     return _raw_stream()
 
 
+def _stream_object(stream):
+    """The torch stream of a call: the one given, which may be any object with an address, or the current one."""
+    import torch
+    if stream is None:
+        return torch.cuda.current_stream()
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream)
+
+
 def probe_row_traffic(table_a, table_b, table_rows, rows, write, sink, stream=None):
     """ecrm_probe_row_traffic (measurement aid): rows of 128 floats at rows[i], alternately from the two tables."""
     rc = load_library().ecrm_probe_row_traffic(_ptr(table_a), _ptr(table_b), C.c_uint64(table_rows), _ptr(rows),
@@ -173,7 +181,8 @@ def _row(t):
 class Grads:
     """A list of gradient tensors: their global norm, and clipping (ecrm_grads_<name>).  An item is a contiguous tensor, or a
     pair (rows of a gradient [n, D], device tensor with the number of rows that count).  The tensors are kept alive, and
-    have to stay where they are; make a new list when they move."""
+    have to stay where they are; make a new list when they move.  The list is written on `stream`: order its use on other streams
+    behind that.  It may be dropped while calls are still to run, on whatever streams; a graph that uses it needs it kept."""
 
     def __init__(self, tensors, stream=None):
         import torch
@@ -192,10 +201,24 @@ class Grads:
         if rc != ECRM_OK:
             raise EcrmError(rc, "ecrm_grads_create")
         size = self._lib.ecrm_grads_bytes(self._grads)
-        self._keep = (items, torch.empty(size, dtype=torch.uint8, device=items[0][0].device))
-        rc = self._lib.ecrm_grads_bind(self._grads, _ptr(self._keep[1]), C.c_size_t(size), _stream(stream))
+        with torch.cuda.stream(_stream_object(stream)):  # memory that stream has done with
+            self._keep = (items, torch.empty(size, dtype=torch.uint8, device=items[0][0].device))
+        self._streams = set()
+        rc = self._lib.ecrm_grads_bind(self._grads, _ptr(self._keep[1]), C.c_size_t(size), self._on(stream))
         if rc != ECRM_OK:
             raise EcrmError(rc, "ecrm_grads_bind")
+
+    def _on(self, stream):
+        """Address of a call's stream.  The allocator learns that the list's memory is used there: who drops the list may hold
+        nothing else of it, and the memory has to wait for what that stream has still to run."""
+        address = _stream(stream)
+        if address not in self._streams:
+            self._streams.add(address)
+            use = _stream_object(stream)
+            items, table = self._keep
+            for t in [table] + [t for item in items for t in item if t is not None]:
+                t.record_stream(use)
+        return address
 
     def destroy(self):
         if self._grads:
@@ -211,7 +234,7 @@ class Grads:
     def norm(self, norm, stream=None, check=True):
         """norm: device tensor of one fp32 value."""
         assert norm.is_cuda and _type(norm) == 0 and norm.numel() == 1
-        rc = self._lib.ecrm_grads_norm(self._grads, norm.data_ptr(), _stream(stream))
+        rc = self._lib.ecrm_grads_norm(self._grads, norm.data_ptr(), self._on(stream))
         if check and rc != ECRM_OK:
             raise EcrmError(rc, "ecrm_grads_norm")
         return rc
@@ -222,7 +245,9 @@ class Grads:
         if out is not None and not out._grads:           # destroyed: NULL would be "in place"
             rc = ECRM_EINVAL
         else:
-            rc = self._lib.ecrm_grads_clip(self._grads, out._grads if out is not None else None, norm.data_ptr(), max_norm, _stream(stream))
+            if out is not None:
+                out._on(stream)
+            rc = self._lib.ecrm_grads_clip(self._grads, out._grads if out is not None else None, norm.data_ptr(), max_norm, self._on(stream))
         if check and rc != ECRM_OK:
             raise EcrmError(rc, "ecrm_grads_clip")
         return rc

@@ -238,3 +238,57 @@ def test_a_destroyed_list_is_refused():
         assert e.value.code == ECRM_EINVAL
     torch.cuda.synchronize()
     assert bool((x == 1).all()) and not y.any() and float(norm) == 10.0
+
+
+def test_lists_that_are_dropped_before_a_stream_has_used_them():
+    """Their memory is nobody else's until then: the lists' own and their tensors'."""
+    sizes = [5000, 70001, 3]
+    src = make(sizes, [BF16], 1)
+    want = norm_of(src)
+    norm, kept = torch.zeros(1, device=DEV), make(sizes, [F32], 1)
+    side = torch.cuda.Stream()
+    grads, out = Grads(src), Grads(kept)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)
+    grads.norm(norm, stream=side)
+    with torch.cuda.stream(side):          # named, or the current one
+        grads.clip(norm, 0.5, out=out)
+    was = [x.clone() for x in src]
+    used = {t.data_ptr(): t.numel() * t.element_size() for g in (grads, out) for t in (g._keep[1],)}
+    used.update({t.data_ptr(): t.numel() * t.element_size() for t in src})
+    del grads, out, src
+    again = [torch.empty(n, dtype=torch.uint8, device=DEV) for n in used.values() for _ in range(3)]
+    assert not side.query()                # still held up
+    assert not {t.data_ptr() for t in again} & set(used)
+    side.synchronize()
+    near(float(norm), want)
+    check_clipped(kept, was, float(norm), 0.5)
+
+
+def test_a_list_that_is_written_on_another_stream():
+    """Its table is memory of that stream."""
+    x, norm = torch.full((70001,), 2.0, device=DEV), torch.zeros(1, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    size = Grads([x])._keep[1].numel()
+    held = torch.empty(size, dtype=torch.uint8, device=DEV)
+    free = held.data_ptr()
+    torch.cuda._sleep(200_000_000)
+    held.zero_()                           # still to come on the main stream
+    del held
+    grads = Grads([x], stream=side)
+    assert grads._keep[1].data_ptr() != free
+    grads.norm(norm, stream=side)
+    side.synchronize()
+    near(float(norm), norm_of([x]))
+
+    class Address:                         # a stream of another library
+        cuda_stream = side.cuda_stream
+
+    norm.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    other = Grads([x], stream=Address)
+    other.norm(norm, stream=Address)
+    side.synchronize()
+    near(float(norm), norm_of([x]))
