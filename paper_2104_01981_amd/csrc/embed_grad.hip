@@ -613,7 +613,9 @@ void launch_embed_grad(const Scratch &s, const EmbedGradLayout &l, const Geometr
     }
     char *base = (char *)s.hdr;
     SumArgs a{};
-    if (n <= kSortHere && !beside.to) {
+    // every workgroup of the sums reads the tokens where it sorts them itself: not where the first one writes the distinct keys
+    const bool in_place = out_keys && out_keys < keys + n && keys < out_keys + n;
+    if (n <= kSortHere && !beside.to && !in_place) {
         a.keys = keys; a.padding = padding; a.rows = g.rows; a.hdr = s.hdr;
     } else {
         const TokenSort sorted = launch_token_sort(s, l.sort, keys, n, padding, g.rows, key_bits, beside, cus, st);

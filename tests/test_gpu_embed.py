@@ -559,3 +559,21 @@ def test_a_first_lookup_in_a_graph_clears_nothing_when_it_is_replayed():
     tab.ctx.clear_status()
     graph.replay()
     assert tab.ctx.status() == 0
+
+
+@pytest.mark.parametrize("D", [8, 36, 128])
+def test_distinct_keys_in_the_tokens_place(D):
+    """... or over a part of them: the tokens have been read by then, in batches of every size."""
+    tab = Table(1 << 11, D, max_batch=70001)
+    for n in (1, 2, 64, 200, 256, 257, 2000, 9000, 70001):
+        keys, d = tokens(tab.R, n, "text", n, padding=0.1), gradients(n, D, torch.bfloat16, 1)
+        names, grads = run_grad(tab, keys, d)
+        for shift in (0, 1):
+            words = torch.full((n + 1,), 77, dtype=torch.int64, device=DEV)
+            words[:n] = keys
+            og, count = torch.full((n, D), 77.0, device=DEV), torch.zeros(1, dtype=torch.int64, device=DEV)
+            tab.ctx.embed_grad(words[:n], d, words[shift:shift + n], og, count, padding=PAD)
+            u = int(count)
+            assert torch.equal(words[shift:shift + u], names) and bool((words[shift + u:shift + n] == -1).all())
+            assert torch.equal(og[:u], grads) and bool((og[u:] == 77.0).all())
+    assert tab.ctx.status() == 0
