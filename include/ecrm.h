@@ -245,7 +245,8 @@ int ecrm_recovery_read(ecrm_ctx *ctx, const uint64_t *keys, uint64_t n, float *o
  *                       accumulate = 1 the sums are added to dE (one rounding) and other rows are left alone.  A rejected batch
  *                       has no tokens: dE becomes zero, or is left alone.
  *
- * out_keys may be keys (or overlap them).
+ * out overlaps no token and no row that is looked up.  out_keys may be keys (or overlap them); otherwise out_keys, out_grads,
+ * count and dE overlap neither each other nor keys nor rows of d_out.  What of this the pointers show is refused with EINVAL.
  * d_out and out: device memory aligned to four elements, stride >= D and a multiple of 4; out_grads and dE: 16 bytes; count:
  * 8 bytes, memory the device can write.  padding: any value, a row of the table or not (-1, -100); ECRM_NO_PADDING (2^63):
  * there is none.  scale has to be finite.  The

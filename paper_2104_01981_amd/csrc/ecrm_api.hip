@@ -672,6 +672,19 @@ static bool rows_ok(const ecrm_ctx *c, const void *p, uint32_t type, uint64_t st
     return type <= ECRM_F16 && stride >= c->cfg.dim && stride % 4 == 0 && aligned(p, 4 * type_bytes(type));
 }
 
+// Have the n rows and the bytes at p no byte in common?  p may lie between the rows.
+static bool rows_apart(const void *rows, uint64_t n, uint64_t row_bytes, uint64_t stride_bytes, const void *p, uint64_t bytes)
+{
+    const uintptr_t r = (uintptr_t)rows, lo = (uintptr_t)p;
+    if (!n || !bytes || lo + bytes <= r) return true;
+    const uint64_t i = lo < r + row_bytes ? 0 : (lo - r - row_bytes) / stride_bytes + 1;        // the first row that ends behind p
+    return i >= n || r + i * stride_bytes >= lo + bytes;
+}
+static bool apart(const void *a, uint64_t a_bytes, const void *b, uint64_t b_bytes)
+{
+    return rows_apart(a, a_bytes != 0, a_bytes, a_bytes, b, b_bytes);
+}
+
 int ecrm_embed(ecrm_ctx *c, const uint64_t *keys, uint64_t n, uint64_t padding, float scale, uint32_t lost_server, void *out,
                uint32_t type, uint64_t stride, void *stream)
 {
@@ -681,6 +694,7 @@ int ecrm_embed(ecrm_ctx *c, const uint64_t *keys, uint64_t n, uint64_t padding, 
     if (!isfinite(scale)) return ECRM_EINVAL;
     if (n == 0) return ECRM_OK;
     if (!aligned(keys, 8) || !rows_ok(c, out, type, stride)) return ECRM_EINVAL;
+    if (!rows_apart(out, n, c->cfg.dim * type_bytes(type), stride * type_bytes(type), keys, n * 8)) return ECRM_EINVAL;
     init_if_needed(c, (hipStream_t)stream);
     launch_embed(c->s, c->geo, c->t.E, c->t.PE, keys, n, padding, scale, lost_server, out, type, stride, c->cus, (hipStream_t)stream);
     return check_launch();
@@ -693,6 +707,14 @@ static int run_embed_grad(ecrm_ctx *c, const uint64_t *keys, const void *d, uint
     if (n > c->lay.max_batch) return ECRM_EBATCH;
     if (!isfinite(scale)) return ECRM_EINVAL;
     if (n && (!aligned(keys, 8) || !rows_ok(c, d, type, stride))) return ECRM_EINVAL;
+    // What is written overlaps nothing that is read, but for the distinct keys: they may take the tokens' place (launch_embed_grad).
+    const uint64_t D = c->cfg.dim, row = D * type_bytes(type), step = stride * type_bytes(type);
+    const uint64_t out_bytes = (out_keys ? n : c->cfg.rows) * D * 4;
+    if (n && (!apart(keys, n * 8, out, out_bytes) || !rows_apart(d, n, row, step, out, out_bytes))) return ECRM_EINVAL;
+    if (n && out_keys &&
+        (!rows_apart(d, n, row, step, out_keys, n * 8) || !apart(out, out_bytes, out_keys, n * 8) || !apart(keys, n * 8, count, 8) ||
+         !rows_apart(d, n, row, step, count, 8) || !apart(out, out_bytes, count, 8) || !apart(out_keys, n * 8, count, 8)))
+        return ECRM_EINVAL;
     init_if_needed(c, (hipStream_t)stream);
     launch_embed_grad(c->s, c->elay, c->geo, c->key_bits, keys, d, type, stride, (uint32_t)n, padding, scale, out_keys, out, count,
                       accumulate, c->cus, (hipStream_t)stream);

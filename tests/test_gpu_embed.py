@@ -577,3 +577,41 @@ def test_distinct_keys_in_the_tokens_place(D):
             assert torch.equal(words[shift:shift + u], names) and bool((words[shift + u:shift + n] == -1).all())
             assert torch.equal(og[:u], grads) and bool((og[u:] == 77.0).all())
     assert tab.ctx.status() == 0
+
+
+def test_overlaps_are_refused():
+    D, n = 36, 100
+    tab = Table(1 << 10, D, max_batch=n)
+    bytes_ = torch.zeros(1 << 20, dtype=torch.uint8, device=DEV)
+
+    def at(byte, shape, dtype):
+        size = int(np.prod(shape)) * torch.empty(0, dtype=dtype).element_size()
+        return bytes_[byte:byte + size].view(dtype).view(shape)
+
+    row = 4 * D
+    keys, wide = at(0, (n,), torch.int64), at(1024, (n, 4 * D), torch.float32)
+    d, behind = wide[:, D:2 * D], 1024 + n * 4 * row
+    ok, og, count = at(behind, (n,), torch.int64), at(behind + 1024, (n, D), torch.float32), at(behind + 1024 + n * row, (1,), torch.int64)
+    tab.ctx.embed_grad(keys, d, ok, og, count)           # one behind the other
+    assert int(count) == 1 and tab.ctx.status() == 0
+    bytes_.zero_()
+    word = lambda byte: at(byte, (1,), torch.int64)  # noqa: E731
+    words, rows = (lambda byte: at(byte, (n,), torch.int64)), (lambda byte: at(byte, (n, D), torch.float32))
+    last = 1024 + (n - 1) * 4 * row + 2 * row            # behind the last row of d
+    bad = [(ok, rows(n * 8 - 16), count), (ok, rows(1024), count), (ok, rows(1024 + row - 16), count), (ok, rows(last - 16), count),
+           (words(1024 + row), og, count), (words(last - 8), og, count), (words(behind + 1024 - 792), og, count), (words(behind + 1024 + n * row - 8), og, count),
+           (ok, og, word(0)), (ok, og, word(n * 8 - 8)), (ok, og, word(1024 + row)), (ok, og, word(last - 8)), (ok, og, word(behind)),
+           (ok, og, word(behind + 1024 + 8))]
+    for a, b, c in bad:
+        assert tab.ctx.embed_grad(keys, d, a, b, c, check=False) == ECRM_EINVAL
+    assert tab.ctx.embed_grad(keys, d, ok, og, word(last)) == 0 and tab.ctx.embed_grad(keys, d, ok, og, word(n * 8)) == 0
+    assert tab.ctx.embed_grad(keys, d, ok, og, word(1024 + 3 * 4 * row + 2 * row)) == 0       # between two rows of d
+    bytes_.zero_()
+    for byte in (0, n * 8 - 8):
+        assert tab.ctx.embed(at(byte, (n,), torch.int64), at(0 if byte else 512, (n, D), torch.float32), check=False) == ECRM_EINVAL
+    dE = at(1 << 18, (1 << 10, D), torch.float32)
+    for accumulate in (False, True):
+        assert tab.ctx.embed_grad_dense(at(1 << 18, (n,), torch.int64), d, dE, accumulate=accumulate, check=False) == ECRM_EINVAL
+        assert tab.ctx.embed_grad_dense(keys, dE[:n], dE, accumulate=accumulate, check=False) == ECRM_EINVAL
+        assert tab.ctx.embed_grad_dense(keys, d, dE, accumulate=accumulate) == 0
+    assert tab.ctx.status() == 0 and not bytes_.any()
