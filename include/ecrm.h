@@ -70,7 +70,8 @@ typedef struct {
                            with A holding v                                                       */
     float lr;           /* learning rate, used as its exact fp32 value                           */
     float eps;          /* Adagrad epsilon (under the square root), >= 0                         */
-    uint64_t max_batch; /* largest n ever passed to ecrm_update, 1 .. 2^31 (sizes the scratch)   */
+    uint64_t max_batch; /* largest n ever passed to ecrm_update or a gradient call (ecrm_embed_grad,
+                           ecrm_embed_grad_dense), 1 .. 2^31 (sizes the scratch)                 */
     float momentum;     /* ECRM_OPT_MOMENTUM only: coefficient in [0, 1)                          */
     uint32_t combine;   /* 0: several updates to one entry inside a call are applied one after the
                            other in arrival order (asynchronous training, Sec. 2.1).
@@ -89,13 +90,15 @@ int ecrm_create(const ecrm_config *cfg, ecrm_ctx **out);
 void ecrm_destroy(ecrm_ctx *ctx);
 
 /* Sizes in bytes: one data table (R*D*4), one parity table (R/k*D*4; the memory overhead of the
- * code is therefore (k+1)/k, Sec. 2.4 / 3.1), and the scratch buffer ecrm_bind needs. */
+ * code is therefore (k+1)/k, Sec. 2.4 / 3.1), and the scratch buffer for ecrm_bind: for all calls, or for
+ * all but ecrm_embed_grad and ecrm_embed_grad_dense, which at a large dim need more. */
 size_t ecrm_data_bytes(const ecrm_ctx *ctx);
 size_t ecrm_parity_bytes(const ecrm_ctx *ctx);
 size_t ecrm_scratch_bytes(const ecrm_ctx *ctx);
+size_t ecrm_update_scratch_bytes(const ecrm_ctx *ctx);
 
 /* Attaches caller-owned device buffers.  scratch must be 256-byte aligned and at least
- * ecrm_scratch_bytes() long; its contents are private to the library while bound.  The load
+ * ecrm_update_scratch_bytes() long; its contents are private to the library while bound.  The load
  * counters are accumulated into, never cleared.  Returns EINVAL for a NULL / misaligned table,
  * ESCRATCH for the scratch buffer, ESTATE while a recovery is in progress (the updates waiting in its
  * buffer would be lost), EHIP if the device cannot be queried.  Call it outside a stream capture.
@@ -250,7 +253,8 @@ int ecrm_recovery_read(ecrm_ctx *ctx, const uint64_t *keys, uint64_t n, float *o
  * d_out and out: device memory aligned to four elements, stride >= D and a multiple of 4; out_grads and dE: 16 bytes; count:
  * 8 bytes, memory the device can write.  padding: any value, a row of the table or not (-1, -100); ECRM_NO_PADDING (2^63):
  * there is none.  scale has to be finite.  The
- * gradient calls use the scratch buffer (call them on the update stream; n <= max_batch, else EBATCH) but no table, and leave
+ * gradient calls use the scratch buffer (call them on the update stream; n <= max_batch, else EBATCH; bound with less than
+ * ecrm_scratch_bytes they give ESCRATCH) but no table, and leave
  * what ecrm_batch_stats reports; the lookup uses of it the sticky status alone, so that it may run on any stream behind the
  * first call after ecrm_bind (see there).  All only enqueue. */
 enum { ECRM_F32 = 0, ECRM_BF16 = 1, ECRM_F16 = 2 };

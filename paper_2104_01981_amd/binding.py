@@ -17,7 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.environ.get("ECRM_LIBRARY") or os.path.join(_HERE, "libecrm.so")
 _lib = None
 
-SYMBOLS = ["ecrm_create", "ecrm_destroy", "ecrm_data_bytes", "ecrm_parity_bytes", "ecrm_scratch_bytes",
+SYMBOLS = ["ecrm_create", "ecrm_destroy", "ecrm_data_bytes", "ecrm_parity_bytes", "ecrm_scratch_bytes", "ecrm_update_scratch_bytes",
            "ecrm_bind", "ecrm_encode", "ecrm_route", "ecrm_update", "ecrm_update_static", "ecrm_status", "ecrm_clear_status",
            "ecrm_tune", "ecrm_probe_row_traffic", "ecrm_profile", "ecrm_profile_read", "ecrm_batch_stats", "ecrm_host_placement", "ecrm_strerror",
            "ecrm_fail_server", "ecrm_recover_server", "ecrm_degraded_read",
@@ -59,7 +59,7 @@ def load_library():
         lib.ecrm_create.argtypes = [C.POINTER(EcrmConfig), C.POINTER(C.c_void_p)]
         lib.ecrm_destroy.argtypes = [vp]
         lib.ecrm_destroy.restype = None
-        for name in ("ecrm_data_bytes", "ecrm_parity_bytes", "ecrm_scratch_bytes"):
+        for name in ("ecrm_data_bytes", "ecrm_parity_bytes", "ecrm_scratch_bytes", "ecrm_update_scratch_bytes"):
             getattr(lib, name).argtypes = [vp]
             getattr(lib, name).restype = C.c_size_t
         lib.ecrm_bind.argtypes = [vp, f32p, f32p, f32p, f32p, u64p, u64p, vp, C.c_size_t]
@@ -285,6 +285,10 @@ class Ecrm:
 
     def scratch_bytes(self):
         return self._lib.ecrm_scratch_bytes(self._ctx)
+
+    def update_scratch_bytes(self):
+        """What is enough for a context whose gradient calls (embed_grad, embed_grad_dense) are not used."""
+        return self._lib.ecrm_update_scratch_bytes(self._ctx)
 
     def bind_raw(self, E, A, PE, PA, load_data, load_parity, scratch, scratch_bytes):
         """ecrm_bind with raw integer addresses (for error-path tests)."""

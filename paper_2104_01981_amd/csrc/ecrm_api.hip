@@ -35,6 +35,7 @@ struct ecrm_ctx {
     bool has_partial2;
     // bound state
     bool bound, need_init;
+    bool grad_room;           // the scratch buffer has room for the gradient calls, too
     Tables t;
     Scratch s;
     bool have_device;         // cus, grid sizes known (ecrm_bind, or the first ecrm_update_static)
@@ -240,7 +241,6 @@ int ecrm_create(const ecrm_config *cfg, ecrm_ctx **out)
     c->lay = make_layout((uint32_t)cfg->max_batch, cfg->dim, cfg->k, cfg->servers, c->has_partial2);
     c->slay = make_layout(ECRM_STATIC_MAX_BATCH, cfg->dim, cfg->k, cfg->servers, c->has_partial2);
     c->elay = embed_grad_layout(c->lay.off_hist, (uint32_t)cfg->max_batch, cfg->dim, c->key_bits);
-    if (c->elay.end > c->lay.bytes) c->lay.bytes = c->elay.end;
     *out = c;
     return ECRM_OK;
 }
@@ -256,7 +256,8 @@ void ecrm_destroy(ecrm_ctx *c)
 
 size_t ecrm_data_bytes(const ecrm_ctx *c) { return c ? (size_t)c->cfg.rows * c->cfg.dim * 4 : 0; }
 size_t ecrm_parity_bytes(const ecrm_ctx *c) { return c ? (size_t)(c->cfg.rows / c->cfg.k) * c->cfg.dim * 4 : 0; }
-size_t ecrm_scratch_bytes(const ecrm_ctx *c) { return c ? c->lay.bytes : 0; }
+size_t ecrm_scratch_bytes(const ecrm_ctx *c) { return !c ? 0 : c->elay.end > c->lay.bytes ? c->elay.end : c->lay.bytes; }
+size_t ecrm_update_scratch_bytes(const ecrm_ctx *c) { return c ? c->lay.bytes : 0; }
 
 static bool aligned(const void *p, size_t a) { return p && ((uintptr_t)p % a) == 0; }
 
@@ -292,6 +293,7 @@ int ecrm_bind(ecrm_ctx *c, float *E, float *A, float *PE, float *PA, uint64_t *l
     c->t.E = E; c->t.A = A; c->t.PE = PE; c->t.PA = PA;
     c->t.load_data = (unsigned long long *)load_data;
     c->t.load_parity = (unsigned long long *)load_parity;
+    c->grad_room = scratch_bytes >= c->elay.end;
     c->bound = true;
     c->need_init = true;      // the first enqueue clears the header on its stream
     return ECRM_OK;
@@ -704,6 +706,7 @@ static int run_embed_grad(ecrm_ctx *c, const uint64_t *keys, const void *d, uint
                           uint64_t padding, float scale, uint64_t *out_keys, float *out, uint64_t *count, bool accumulate,
                           void *stream)
 {
+    if (!c->grad_room) return ECRM_ESCRATCH;
     if (n > c->lay.max_batch) return ECRM_EBATCH;
     if (!isfinite(scale)) return ECRM_EINVAL;
     if (n && (!aligned(keys, 8) || !rows_ok(c, d, type, stride))) return ECRM_EINVAL;

@@ -60,3 +60,18 @@ def test_gradient_lists_on_the_host(lib):
     assert lib.ecrm_grads_norm(None, 4096, None) == binding.ECRM_EINVAL
     assert lib.ecrm_grads_clip(None, None, 4096, 1.0, None) == binding.ECRM_EINVAL
     assert lib.ecrm_grads_bind(None, 4096, 0, None) == binding.ECRM_EINVAL
+
+
+@pytest.mark.parametrize("dim,max_batch,updates,more", [(1024, 8192, 984064, True), (512, 8192, 876032, True), (256, 65536, 2916608, True),
+                                                        (128, 100, 12032, False), (4, 1, 7168, False), (1024, 1 << 20, 114678784, True),
+                                                        (128, 1 << 24, 531264512, False)])
+def test_scratch_without_room_for_gradients(lib, dim, max_batch, updates, more):
+    """Callers without gradient calls need what they needed before there were any; some geometries need no more with them."""
+    cfg = binding.EcrmConfig(rows=1 << 22, dim=dim, k=4, servers=5, optimizer=0, lr=0.01, eps=1e-8, max_batch=max_batch)
+    ctx = C.c_void_p(0)
+    assert lib.ecrm_create(C.byref(cfg), C.byref(ctx)) == 0
+    assert lib.ecrm_update_scratch_bytes(ctx) == updates
+    every = lib.ecrm_scratch_bytes(ctx)
+    assert every > updates if more else every == updates
+    lib.ecrm_destroy(ctx)
+    assert lib.ecrm_update_scratch_bytes(None) == 0 and lib.ecrm_scratch_bytes(None) == 0

@@ -10,7 +10,7 @@ import torch
 
 import oracle
 import synth_inputs as si
-from paper_2104_01981_amd import ECRM_EBATCH, ECRM_EINVAL, ECRM_EKEYRANGE, Ecrm, EcrmError
+from paper_2104_01981_amd import ECRM_EBATCH, ECRM_EINVAL, ECRM_EKEYRANGE, ECRM_ESCRATCH, Ecrm, EcrmError
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -615,3 +615,35 @@ def test_overlaps_are_refused():
         assert tab.ctx.embed_grad_dense(keys, dE[:n], dE, accumulate=accumulate, check=False) == ECRM_EINVAL
         assert tab.ctx.embed_grad_dense(keys, d, dE, accumulate=accumulate) == 0
     assert tab.ctx.status() == 0 and not bytes_.any()
+
+
+def test_a_context_without_room_for_gradients():
+    """... updates and looks up in the smaller scratch buffer as any other, and refuses the gradient calls."""
+    R, D, n = 4 * 500, 1024, 3000
+    a, b = Table(R, D, max_batch=n, seed=9), Table(R, D, max_batch=n, seed=9)
+    size = b.ctx.update_scratch_bytes()
+    assert size < b.ctx.scratch_bytes()
+    args = (b.E, b.A, b.PE, b.PA, b.load[0], b.load[1])
+    with pytest.raises(EcrmError) as e:
+        b.ctx.bind(*args, b.scratch[:size - 1])
+    assert e.value.code == ECRM_ESCRATCH
+    b.scratch.fill_(0xA5)
+    b.ctx.bind(*args, b.scratch[:size])
+    keys, g = tokens(R, n, "text", 1), gradients(n, D, torch.float32, 2).contiguous()
+    ok, og, count = torch.full((n,), 7, dtype=torch.int64, device=DEV), torch.full((n, D), 7.0, device=DEV), torch.full((1,), 7, dtype=torch.int64, device=DEV)
+    dE = torch.full((R, D), 7.0, device=DEV)
+    for m in (n, 1):
+        for tab in (a, b):
+            tab.ctx.update(keys[:m], g[:m])
+        assert b.ctx.embed_grad(keys[:m], g[:m], ok, og, count, check=False) == ECRM_ESCRATCH
+        assert b.ctx.embed_grad_dense(keys[:m], g[:m], dE, check=False) == ECRM_ESCRATCH
+    for x in (ok, og, count, dE):
+        assert bool((x == 7).all())
+    for x, y in ((a.E, b.E), (a.A, b.A), (a.PE, b.PE), (a.PA, b.PA), (a.load, b.load)):
+        assert torch.equal(x, y)
+    out = torch.empty(n, D, device=DEV)
+    b.ctx.embed(keys, out)
+    assert torch.equal(out, b.E[keys]) and a.ctx.status() == b.ctx.status() == 0
+    assert bool((b.scratch[size:] == 0xA5).all())
+    b.ctx.bind(*args, b.scratch[:b.ctx.scratch_bytes()])
+    check_grad(b, keys, g)
