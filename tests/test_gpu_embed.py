@@ -647,3 +647,73 @@ def test_a_context_without_room_for_gradients():
     assert bool((b.scratch[size:] == 0xA5).all())
     b.ctx.bind(*args, b.scratch[:b.ctx.scratch_bytes()])
     check_grad(b, keys, g)
+
+
+@pytest.mark.parametrize("R,D,n,kind", [(1 << 20, 128, (1 << 21) + (1 << 18), "uniform"), (1 << 18, 128, (1 << 21) + 100003, "text"),
+                                        (1 << 20, 256, 2100003, "uniform")])
+def test_counts_that_are_added_up_by_a_launch(R, D, n, kind):
+    """More than 1024 (2048) groups of workgroups, with rows that begin in all of them."""
+    tab = Table(R, D, max_batch=n)
+    check_grad(tab, tokens(R, n, kind, n, padding=0.03), gradients(n, D, torch.bfloat16, 5))
+    assert tab.ctx.status() == 0
+
+
+@pytest.mark.parametrize("n", [300007, 2100003])
+def test_large_batches_of_padding_and_of_bad_tokens(n):
+    """The radix sort whose counts are added up in groups, with four items to a thread and with eight."""
+    R, D = 1 << 12, 12
+    tab = Table(R, D, max_batch=n)
+    keys, d = tokens(R, n, "text", n, padding=0.1), gradients(n, D, torch.float32, 2)
+    pads, nans = torch.full((n,), PAD, dtype=torch.int64, device=DEV), torch.full((n, D), float("nan"), device=DEV)
+    names, grads = run_grad(tab, pads, nans)
+    assert len(names) == 0 and tab.ctx.status() == 0
+    for accumulate in (True, False):
+        dE = torch.full((R, D), 3.0, device=DEV)
+        tab.ctx.embed_grad_dense(pads, nans, dE, padding=PAD, accumulate=accumulate)
+        assert bool((dE == (3.0 if accumulate else 0.0)).all())
+    for where, what in ((0, R), (n // 2, 1 << 40), (n - 1, -1)):
+        bad = keys.clone()
+        bad[where] = what
+        names, grads = run_grad(tab, bad, d)
+        assert len(names) == 0 and tab.ctx.status() == ECRM_EKEYRANGE
+        for accumulate in (False, True):
+            dE = torch.full((R, D), 3.0, device=DEV)
+            tab.ctx.embed_grad_dense(bad, d, dE, padding=PAD, accumulate=accumulate)
+            assert bool((dE == (3.0 if accumulate else 0.0)).all())
+        tab.ctx.clear_status()
+        pads[where] = keys[where] = 5                     # one token alone
+        names, grads = run_grad(tab, pads, d)
+        assert names.tolist() == [5] and torch.equal(grads[0], d[(pads == 5)].double().sum(0).float()) and tab.ctx.status() == 0
+        pads[where] = PAD
+        check_grad(tab, keys, d)
+
+
+@pytest.mark.parametrize("n", [300007, 2100003])
+def test_large_batches_in_a_graph(n):
+    R, D = 1 << 18, 8
+    tab = Table(R, D, max_batch=n)
+    keys, d = tokens(R, n, "text", 1, padding=0.1), gradients(n, D, torch.bfloat16, 1)
+    ok, og = torch.empty(n, dtype=torch.int64, device=DEV), torch.empty(n, D, device=DEV)
+    count, dE = torch.empty(1, dtype=torch.int64, device=DEV), torch.empty(R, D, device=DEV)
+
+    def step():
+        tab.ctx.embed_grad(keys, d, ok, og, count, padding=PAD)
+        tab.ctx.embed_grad_dense(keys, d, dE, padding=PAD)
+
+    step()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step()
+    for rep in range(4):
+        keys.copy_(tokens(R, n, ("uniform", "one", "text", "runs")[rep], rep, padding=0.1))
+        d.copy_(gradients(n, D, torch.bfloat16, 20 + rep))
+        ok.fill_(5), og.fill_(5.0), dE.fill_(5.0)
+        graph.replay()
+        got = [x.clone() for x in (ok, og, count, dE)]
+        ok.fill_(5), og.fill_(5.0), dE.fill_(5.0)
+        step()
+        for x, y in zip(got, (ok, og, count, dE)):
+            assert torch.equal(x, y), rep
+        torch.cuda.synchronize()
+    assert tab.ctx.status() == 0
