@@ -279,13 +279,13 @@ int ecrm_embed_grad_dense(ecrm_ctx *ctx, const uint64_t *keys, const void *d_out
  *                    private to the library while bound, and used by every call on the handle: calls that overlap in time race;
  *                    order them, and the streams they are on, as for a context.
  * ecrm_grads_norm    *norm (device) = square root of the sum of the squares of all elements, summed in fp64 in an order that
- *                    follows from the list alone, rounded once.  Not finite if an element is not, or the norm is beyond fp32.
+ *                    follows from the list and its addresses' 16-byte alignment, rounded once.  Not finite if an element is not, or the norm is beyond fp32.
  * ecrm_grads_clip    out[t][e] = list[t][e] * min(1, max_norm / (*norm + 1e-6)), rounded to the type of out[t]; out = NULL:
  *                    in place, where nothing is written when the factor is 1.  *norm is read on the device: what
  *                    ecrm_grads_norm left, or what a job of several devices made of theirs.  An infinite norm gives the factor 0,
  *                    one that is not a number a factor that is none.  out: a bound list of as many tensors with as many elements
  *                    each (its rows are not looked at); a tensor of out is the list's own memory, of the same type, or overlaps
- *                    none of it.  max_norm has to be finite and not negative. */
+ *                    none of it.  Tensors that are written overlap none of each other.  max_norm has to be finite and not negative. */
 typedef struct {
     void *data;
     uint64_t elements;

@@ -6,10 +6,12 @@
 // workgroup has of runs that go on in its neighbours by a launch behind.  Sums are carried in 64 bits and rounded once, in
 // an order that follows from the sorted positions, n and D alone: no atomics, two runs give the same bits.
 //
-// What bounds it: in large batches memory -- 2^20 tokens of 128 floats, hardly any twice, 228 us, of which the sums 164: 980 MB
-// at 6.0 TB/s, in part from the memory-side cache --, in small ones the trips to memory that follow from one another: a launch (up to
-// kSortHere tokens, 6.8 us for 64), two (up to kOneBlock, 11 us for 600), three to five (up to 2^16), nine to twelve.  Of 2^16
-// tokens of text with 256 floats in bf16, 42 us, the sums take 16, the sort 20 and the join 4.
+// What bounds it: in large batches memory -- 2^20 tokens of 128 floats, hardly any twice, 228 us, of which the sums 164: 933 MB
+// at 5.7 TB/s, in part from the memory-side cache --, in small ones the trips to memory that follow from one another: a launch (up to
+// kSortHere tokens, 6.8 us for 64), two (up to kOneBlock, 11 us for 600), three (up to kRankMost), five (up to 2^16; four for the dense
+// form, which counts no rows), then two for each digit of the sort, or three, and three or four behind it: five to nine up to 2^18
+// tokens, six to sixteen beyond (twelve for rows of 19 to 27 bits).  Of 2^16 tokens of text with 256 floats in bf16, 42 us, the sums
+// take 16, the sort 20 and the join 4.
 #include "types.h"
 
 namespace ecrm {
@@ -30,12 +32,15 @@ constexpr uint32_t kChunkMin = 4;         // positions of a team, which are on t
 constexpr uint32_t kCountThreads = 1024;
 constexpr uint32_t kCountGroup = 8;       // workgroups whose distinct rows are counted together
 constexpr uint32_t kScanGroups = 1024;    // from more on these counts are added up by a launch of its own
-// Where more than this goes in and out, rows are read and written past the caches, eight of a team in flight instead of four
-// (2^20 tokens of 128 floats 278 us, 289 as usual; 103 MiB, 40000 of 512 floats to a dense gradient, 49 and 54; 96 MiB, 2^16 of 256
-// floats, 51 and 48: there the rows are still in the memory-side cache from whoever wrote them).
+// Where more than this goes in and out -- the rows, and the output as if no token came twice --, rows are read and written past the
+// caches, eight of a team in flight instead of four.  Whether that pays depends on where the rows are, which nobody here knows.  Time
+// so / as usual, widths 64 to 1024, 16 and 32 bits (rows; dense; added to what is there), in batches by turns, 600 MiB of them:
+// up to 60 MiB 0.98; 1.03; 1.04, 60 to 100 1.05; 0.98; 0.96, 100 to 200 of text 0.98; 0.98; 0.96, of unlike tokens 1.03; 1.02; 0.98,
+// 200 to 300 of text 0.96; 0.94; 0.91, of unlike tokens 1.07; 1.02; 0.97, beyond 400 0.94 for rows, beyond 300 0.90 to 0.99 for the others.
+// With one batch again and again, which the memory-side cache holds as a whole, it loses 3 to 14 % up to 300 MiB and gains as much beyond 400.
 constexpr uint64_t kStreamBytes = 100ull << 20;
 // Of these rows a quarter, but no more than kNearBytes, is read into the memory-side cache beside the sort, the first ones: what was
-// written last is there anyway.  2^20 items of 128 floats 239 us without, 228 so; 65536 of 512 floats 77.6 and 73.0, with half of the
+// written last is there anyway.  120 MB: of 2^20 items 160 MB took 231 us, 240 MB 235.  2^20 items of 128 floats 239 us without, 228 so; 65536 of 512 floats 77.6 and 73.0, with half of the
 // rows 71.8; 18001 of 1024 in bf16 45.6 and 44.9; 2^19 of text with 128 in bf16 99.7 and 100.9, with half of them 103.4.
 constexpr uint64_t kNearBytes = 114ull << 20;
 constexpr uint32_t kJoinUnits = 16;       // of four columns, of a job
@@ -542,7 +547,8 @@ static SumPlan sum_plan(uint32_t n, uint32_t D)
     p.units = n <= kOneBlock && quads > kOneUnits ? kOneUnits : quads;
     p.slices = (quads + p.units - 1) / p.units;
     p.teams = (uint32_t)kSumThreads / p.units;
-    // what the parts of runs take in the scratch buffer grows with D * D / chunk_max: up to 32, 64, 128 bytes a token
+    // What the parts of runs take in the scratch buffer grows with D * D / chunk_max: of large batches 32, 64, 128 bytes a token.  The
+    // up to kSumBlocks workgroups of smaller ones have 16 * D each, however few their tokens: 2 KB a token of 8192 with 1024 floats.
     const uint32_t room = kSumMost / p.teams, chunk_max = D <= 256 ? 32u : D <= 512 ? 64u : 128u;
     const uint32_t most = n <= kOneBlock || room < chunk_max ? room : chunk_max;
     const uint64_t wanted = n <= kOneBlock ? p.teams : (uint64_t)p.teams * kSumBlocks;

@@ -3,8 +3,8 @@
 //
 // The list becomes a table in device memory (ecrm_grads_bind): the tensors, and for each chunk of one tensor's memory which
 // tensor's it is and where -- so that one launch goes over any number of tensors of any sizes, a workgroup a chunk at a time.  What bounds both: memory, every element read once (and written once): the norm of 562 MB takes 89 us, 6.3 TB/s.
-// Squares are summed in 64 bits: squares of 32-bit values neither overflow nor vanish there, and no order of the sum can be
-// seen in the 32 bits of the norm.
+// Squares are summed in 64 bits: squares of 32-bit values neither overflow nor vanish there.  The order of the sum follows from the
+// list, the 16-byte alignment of its addresses included, so that two runs give the same bits.
 #include <math.h>
 #include <new>
 #include <string.h>
