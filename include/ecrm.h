@@ -250,7 +250,7 @@ int ecrm_recovery_read(ecrm_ctx *ctx, const uint64_t *keys, uint64_t n, float *o
  *
  * out overlaps no token and no row that is looked up.  out_keys may be keys (or overlap them); otherwise out_keys, out_grads,
  * count and dE overlap neither each other nor keys nor rows of d_out.  What of this the pointers show is refused with EINVAL.
- * d_out and out: device memory aligned to four elements, stride >= D and a multiple of 4; out_grads and dE: 16 bytes; count:
+ * d_out and out: device memory aligned to four elements, stride >= D and a multiple of 4, for several rows at most 2^48; out_grads and dE: 16 bytes; count:
  * 8 bytes, memory the device can write.  padding: any value, a row of the table or not (-1, -100); ECRM_NO_PADDING (2^63):
  * there is none.  scale has to be finite.  The
  * gradient calls use the scratch buffer (call them on the update stream; n <= max_batch, else EBATCH; bound with less than

@@ -668,10 +668,10 @@ int ecrm_degraded_read(ecrm_ctx *c, const uint64_t *keys, uint64_t n, uint32_t l
     return check_launch();
 }
 
-// rows of `type` elements: four of them are loaded at once
-static bool rows_ok(const ecrm_ctx *c, const void *p, uint32_t type, uint64_t stride)
+// n rows of `type` elements: four of them are loaded at once.  No two rows are farther apart than any memory reaches.
+static bool rows_ok(const ecrm_ctx *c, const void *p, uint32_t type, uint64_t n, uint64_t stride)
 {
-    return type <= ECRM_F16 && stride >= c->cfg.dim && stride % 4 == 0 && aligned(p, 4 * type_bytes(type));
+    return type <= ECRM_F16 && stride >= c->cfg.dim && stride % 4 == 0 && (n == 1 || stride <= 1ull << 48) && aligned(p, 4 * type_bytes(type));
 }
 
 // Have the n rows and the bytes at p no byte in common?  p may lie between the rows.
@@ -679,6 +679,7 @@ static bool rows_apart(const void *rows, uint64_t n, uint64_t row_bytes, uint64_
 {
     const uintptr_t r = (uintptr_t)rows, lo = (uintptr_t)p;
     if (!n || !bytes || lo + bytes <= r) return true;
+    if (n == 1) return r + row_bytes <= lo;              // whatever the stride
     const uint64_t i = lo < r + row_bytes ? 0 : (lo - r - row_bytes) / stride_bytes + 1;        // the first row that ends behind p
     return i >= n || r + i * stride_bytes >= lo + bytes;
 }
@@ -695,7 +696,7 @@ int ecrm_embed(ecrm_ctx *c, const uint64_t *keys, uint64_t n, uint64_t padding, 
     if (lost_server != ECRM_NO_SERVER && lost_server >= c->geo.S) return ECRM_EINVAL;
     if (!isfinite(scale)) return ECRM_EINVAL;
     if (n == 0) return ECRM_OK;
-    if (!aligned(keys, 8) || !rows_ok(c, out, type, stride)) return ECRM_EINVAL;
+    if (!aligned(keys, 8) || !rows_ok(c, out, type, n, stride)) return ECRM_EINVAL;
     if (!rows_apart(out, n, c->cfg.dim * type_bytes(type), stride * type_bytes(type), keys, n * 8)) return ECRM_EINVAL;
     init_if_needed(c, (hipStream_t)stream);
     launch_embed(c->s, c->geo, c->t.E, c->t.PE, keys, n, padding, scale, lost_server, out, type, stride, c->cus, (hipStream_t)stream);
@@ -709,7 +710,7 @@ static int run_embed_grad(ecrm_ctx *c, const uint64_t *keys, const void *d, uint
     if (!c->grad_room) return ECRM_ESCRATCH;
     if (n > c->lay.max_batch) return ECRM_EBATCH;
     if (!isfinite(scale)) return ECRM_EINVAL;
-    if (n && (!aligned(keys, 8) || !rows_ok(c, d, type, stride))) return ECRM_EINVAL;
+    if (n && (!aligned(keys, 8) || !rows_ok(c, d, type, n, stride))) return ECRM_EINVAL;
     // What is written overlaps nothing that is read, but for the distinct keys: they may take the tokens' place (launch_embed_grad).
     const uint64_t D = c->cfg.dim, row = D * type_bytes(type), step = stride * type_bytes(type);
     const uint64_t out_bytes = (out_keys ? n : c->cfg.rows) * D * 4;

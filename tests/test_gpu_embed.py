@@ -717,3 +717,21 @@ def test_large_batches_in_a_graph(n):
             assert torch.equal(x, y), rep
         torch.cuda.synchronize()
     assert tab.ctx.status() == 0
+
+
+def test_strides_beyond_any_memory():
+    """... do not matter to a single row, and are refused for more."""
+    D = 36
+    tab = Table(1 << 10, D, max_batch=4)
+    keys, d = torch.tensor([7, 9], device=DEV), torch.ones(2, D, device=DEV)
+    out, ok, og, count = torch.zeros(2, D, device=DEV), torch.zeros(2, dtype=torch.int64, device=DEV), torch.zeros(2, D, device=DEV), torch.zeros(1, dtype=torch.int64, device=DEV)
+    dE, lib, raw = torch.zeros(1 << 10, D, device=DEV), tab.ctx._lib, tab.ctx._ctx
+    k, none = keys.data_ptr(), 1 << 63
+    for n, code in ((2, ECRM_EINVAL), (1, 0)):
+        for stride in ((1 << 62), (1 << 64) - 4, (1 << 48) + 4):
+            assert lib.ecrm_embed(raw, k, n, none, 1.0, 0xFFFFFFFF, out.data_ptr(), 0, stride, None) == code
+            assert lib.ecrm_embed_grad(raw, k, d.data_ptr(), 0, stride, n, none, 1.0, ok.data_ptr(), og.data_ptr(), count.data_ptr(), None) == code
+            assert lib.ecrm_embed_grad_dense(raw, k, d.data_ptr(), 0, stride, n, none, 1.0, dE.data_ptr(), 0, None) == code
+        assert code == 0 or not (out.any() or og.any() or dE.any())
+    assert torch.equal(out[0], tab.E[7]) and int(count) == 1 and int(ok[0]) == 7 and bool((og[0] == 1).all()) and float(dE.sum()) == D
+    assert tab.ctx.status() == 0
