@@ -301,6 +301,82 @@ int ecrm_grads_bind(ecrm_grads *grads, void *table, size_t table_bytes, void *hi
 int ecrm_grads_norm(ecrm_grads *grads, float *norm, void *hip_stream);
 int ecrm_grads_clip(ecrm_grads *grads, const ecrm_grads *out, const float *norm, float max_norm, void *hip_stream);
 
+/* Dropout whose masks are drawn where they are needed and never stored.  A mask is fixed by state (device memory, 8-byte aligned):
+ * state[0] a seed, state[1] + offset (modulo 2^64) the mask's number.  A program keeps one state, gives every place of its model
+ * an offset of its own and adds the number of places to state[1] once a step; in a captured graph, too, where each replay then draws
+ * other masks.  The gradient of a place is the same mask's.
+ *   Row i, column j:  w = Philox4x32-10(counter (j / 8, i, number, number >> 32), key (seed, seed >> 32)), four words;
+ *   b = the 16 bits of w[(j % 8) / 2], the lower ones for even j;  the element is dropped if b < t = 2^16 p, rounded to nearest even,
+ *   and multiplied by c = 2^16 / (2^16 - t) otherwise.  With t = 2^16 all are dropped.
+ * What is dropped is zero whatever it was, in gradients, too.  p: 0 .. 1.
+ *
+ * ecrm_dropout          out = residual + drop(x), formed in fp32, rounded once; residual = NULL: out = drop(x), and, of the gradient of
+ *                       that, the gradient of x.  rows x cols elements of `type`; cols a multiple of 4, up to 2^24; up to 2^32
+ *                       rows, as far from each other as ecrm_embed allows.  out is x or residual (of the same stride), or overlaps neither, nor state.
+ * ecrm_embed_dropout    ecrm_embed with out = drop(scale * entry), row i of the mask for out[i]; n <= 2^32.
+ * ecrm_embed_grad_dropout, ecrm_embed_grad_dense_dropout
+ *                       the gradients of that: what was dropped of a row of d_out counts for nothing, and sums are multiplied by c, too,
+ *                       before the one rounding. */
+typedef struct {
+    const uint64_t *state;
+    uint64_t offset;
+    double p;
+} ecrm_mask;
+int ecrm_dropout(const ecrm_mask *mask, const void *x, uint64_t x_stride, const void *residual, uint64_t residual_stride, void *out,
+                 uint64_t out_stride, uint32_t type, uint64_t rows, uint32_t cols, void *hip_stream);
+int ecrm_embed_dropout(ecrm_ctx *ctx, const uint64_t *keys, uint64_t n, uint64_t padding, float scale, uint32_t lost_server,
+                       const ecrm_mask *mask, void *out, uint32_t type, uint64_t stride, void *hip_stream);
+int ecrm_embed_grad_dropout(ecrm_ctx *ctx, const uint64_t *keys, const void *d_out, uint32_t type, uint64_t stride, uint64_t n,
+                            uint64_t padding, float scale, const ecrm_mask *mask, uint64_t *out_keys, float *out_grads,
+                            uint64_t *count, void *hip_stream);
+int ecrm_embed_grad_dense_dropout(ecrm_ctx *ctx, const uint64_t *keys, const void *d_out, uint32_t type, uint64_t stride, uint64_t n,
+                                  uint64_t padding, float scale, const ecrm_mask *mask, float *dE, int accumulate, void *hip_stream);
+
+/* A gated feed-forward block between the lookup and its gradient.  With weights Wg, Wu [F][D] and Wd [D][F], for each row x of n:
+ *     g = x Wg^T,  u = x Wu^T,  h = act(g) * u,  out = residual + drop(h Wd^T)
+ * and, from the gradient d of out,
+ *     e = drop(d),  b = e Wd,  dg = b * u * act'(g),  du = b * act(g),
+ *     d_x = add + dg Wg + du Wu,  d_gate = dg^T x,  d_up = du^T x,  d_down = e^T h.
+ * act: ECRM_SILU g / (1 + e^-g), ECRM_GELU g (1 + erf(g / sqrt 2)) / 2, ECRM_RELU max(g, 0) with the derivative 0 at 0.
+ * Sums are formed in fp32, in an order that follows from the sizes alone; in 16-bit types h, dg, du and e are rounded to the type
+ * between the products, and so are the saved g and u.  Needs no ecrm_ctx.
+ *
+ * ecrm_ffn_create    checks the configuration and makes a host-side handle (destroy it with ecrm_ffn_destroy; NULL is allowed).
+ * ecrm_ffn_bytes     size of the workspace that ecrm_ffn_bind needs.
+ * ecrm_ffn_bind      hands over weights and workspace (256-byte aligned, else ESCRATCH) and learns the device: call it outside a
+ *                    stream capture.  The workspace holds nothing from one call for the next: handles may share one.  Calls that use one
+ *                    and overlap in time race; order them, and the streams they are on, as for a context.
+ * ecrm_ffn_forward   residual = NULL: none.  mask = NULL: no dropout.  saved (room for [n][2 F], contiguous): receives g and u, a
+ *                    row's F of g first, for the backward pass; NULL: not wanted.
+ * ecrm_ffn_backward  only with config.training.  saved, x, mask: the forward call's.  add (NULL: nothing): what d_x is added to --
+ *                    d_out where residual was x.  d_x = NULL: not wanted.  d_gate, d_up [F][D] and d_down [D][F], contiguous: all
+ *                    three or none (NULL).  Their type is the block's or ECRM_F32; with accumulate = 1 they are added to.
+ *                    n = 0 leaves weight gradients of zero (accumulate: as they are).
+ *
+ * Rows: device memory aligned to four elements, strides multiples of 4, at least D (F for Wd), at most 2^20.  n <= max_rows, else
+ * EBATCH.  out is x or residual (of the same stride) or overlaps neither; d_x is add or d_out (of the same stride) or overlaps no input;
+ * what is written overlaps no other input, no weight, no workspace, no state and nothing else that is written.  What of this the pointers show is
+ * refused with EINVAL.  Calls only enqueue. */
+enum { ECRM_SILU = 0, ECRM_GELU = 1, ECRM_RELU = 2 };
+typedef struct {
+    uint32_t dim, hidden; /* D, F: multiples of 4, 4 .. 65536 */
+    uint32_t type;        /* of all that is read and written: ECRM_F32, ECRM_BF16, ECRM_F16 */
+    uint32_t activation;
+    uint64_t max_rows;    /* largest n, 1 .. 2^26 */
+    uint32_t training;    /* 1: the workspace has room for ecrm_ffn_backward */
+} ecrm_ffn_config;
+typedef struct ecrm_ffn ecrm_ffn;
+int ecrm_ffn_create(const ecrm_ffn_config *config, ecrm_ffn **out);
+void ecrm_ffn_destroy(ecrm_ffn *ffn);
+size_t ecrm_ffn_bytes(const ecrm_ffn *ffn);
+int ecrm_ffn_bind(ecrm_ffn *ffn, const void *gate, uint64_t gate_stride, const void *up, uint64_t up_stride, const void *down,
+                  uint64_t down_stride, void *workspace, size_t workspace_bytes);
+int ecrm_ffn_forward(ecrm_ffn *ffn, const void *x, uint64_t x_stride, uint64_t n, const void *residual, uint64_t residual_stride,
+                     const ecrm_mask *mask, void *out, uint64_t out_stride, void *saved, void *hip_stream);
+int ecrm_ffn_backward(ecrm_ffn *ffn, const void *x, uint64_t x_stride, const void *saved, const void *d_out, uint64_t d_out_stride,
+                      uint64_t n, const ecrm_mask *mask, const void *add, uint64_t add_stride, void *d_x, uint64_t d_x_stride,
+                      void *d_gate, void *d_up, void *d_down, uint32_t weight_type, int accumulate, void *hip_stream);
+
 /* Waits for the stream, then returns ECRM_OK, or EKEYRANGE if any batch since the last
  * ecrm_clear_status (or bind) carried a bad key, EBUFFER if one overflowed the recovery buffer, or
  * EHIP if the runtime reports an error. */

@@ -24,6 +24,8 @@ SYMBOLS = ["ecrm_create", "ecrm_destroy", "ecrm_data_bytes", "ecrm_parity_bytes"
            "ecrm_recovery_begin", "ecrm_recovery_lock", "ecrm_recovery_decode", "ecrm_recovery_unlock",
            "ecrm_recovery_state", "ecrm_recovery_read",
            "ecrm_embed", "ecrm_embed_grad", "ecrm_embed_grad_dense",
+           "ecrm_dropout", "ecrm_embed_dropout", "ecrm_embed_grad_dropout", "ecrm_embed_grad_dense_dropout",
+           "ecrm_ffn_create", "ecrm_ffn_destroy", "ecrm_ffn_bytes", "ecrm_ffn_bind", "ecrm_ffn_forward", "ecrm_ffn_backward",
            "ecrm_grads_create", "ecrm_grads_destroy", "ecrm_grads_bytes", "ecrm_grads_bind", "ecrm_grads_norm", "ecrm_grads_clip"]
 
 
@@ -36,6 +38,15 @@ class EcrmConfig(C.Structure):
 class EcrmTensor(C.Structure):
     _fields_ = [("data", C.c_void_p), ("elements", C.c_uint64), ("rows", C.c_void_p), ("row_elements", C.c_uint32),
                 ("type", C.c_uint32)]
+
+
+class EcrmMask(C.Structure):
+    _fields_ = [("state", C.c_void_p), ("offset", C.c_uint64), ("p", C.c_double)]
+
+
+class EcrmFfnConfig(C.Structure):
+    _fields_ = [("dim", C.c_uint32), ("hidden", C.c_uint32), ("type", C.c_uint32), ("activation", C.c_uint32),
+                ("max_rows", C.c_uint64), ("training", C.c_uint32)]
 
 
 class EcrmError(RuntimeError):
@@ -98,6 +109,19 @@ def load_library():
         lib.ecrm_grads_bind.argtypes = [vp, vp, C.c_size_t, vp]
         lib.ecrm_grads_norm.argtypes = [vp, f32p, vp]
         lib.ecrm_grads_clip.argtypes = [vp, vp, f32p, f32, vp]
+        mask = C.POINTER(EcrmMask)
+        lib.ecrm_dropout.argtypes = [mask, vp, u64, vp, u64, vp, u64, u32, u64, u32, vp]
+        lib.ecrm_embed_dropout.argtypes = [vp, u64p, u64, u64, f32, u32, mask, vp, u32, u64, vp]
+        lib.ecrm_embed_grad_dropout.argtypes = [vp, u64p, vp, u32, u64, u64, u64, f32, mask, u64p, f32p, u64p, vp]
+        lib.ecrm_embed_grad_dense_dropout.argtypes = [vp, u64p, vp, u32, u64, u64, u64, f32, mask, f32p, C.c_int, vp]
+        lib.ecrm_ffn_create.argtypes = [C.POINTER(EcrmFfnConfig), C.POINTER(C.c_void_p)]
+        lib.ecrm_ffn_destroy.argtypes = [vp]
+        lib.ecrm_ffn_destroy.restype = None
+        lib.ecrm_ffn_bytes.argtypes = [vp]
+        lib.ecrm_ffn_bytes.restype = C.c_size_t
+        lib.ecrm_ffn_bind.argtypes = [vp, vp, u64, vp, u64, vp, u64, vp, C.c_size_t]
+        lib.ecrm_ffn_forward.argtypes = [vp, vp, u64, u64, vp, u64, mask, vp, u64, vp, vp]
+        lib.ecrm_ffn_backward.argtypes = [vp, vp, u64, vp, vp, u64, u64, mask, vp, u64, vp, u64, vp, vp, vp, u32, C.c_int, vp]
         lib.ecrm_strerror.argtypes = [C.c_int]
         lib.ecrm_strerror.restype = C.c_char_p
         _lib = lib
@@ -253,6 +277,131 @@ class Grads:
         return rc
 
 
+class Dropout:
+    """The masks of one place of a model (ecrm_mask): probability, device tensor of two 64-bit integers -- a seed and the number of masks
+    drawn before, which the program adds to, once a step -- and the place's offset among those of a step.  The state is kept alive."""
+
+    def __init__(self, p, state, offset=0):
+        assert _is_words(state) and state.numel() == 2
+        self._lib = load_library()
+        self.state = state
+        self.mask = EcrmMask(state.data_ptr(), offset & 0xFFFFFFFFFFFFFFFF, p)
+
+    def apply(self, x, out, residual=None, stream=None, check=True):
+        """out = residual + dropout(x); the gradient of x is apply(gradient of out).  x, out, residual: [rows, cols] of fp32, bf16 or
+        fp16, rows at any multiple of 4 elements from each other; out may be x or residual."""
+        assert _is_rows(x, x.shape[0], x.shape[-1], x.dtype) and _is_rows(out, x.shape[0], x.shape[1], x.dtype)
+        assert residual is None or _is_rows(residual, x.shape[0], x.shape[1], x.dtype)
+        rc = self._lib.ecrm_dropout(self.mask, x.data_ptr(), _row(x), *_optional(residual), out.data_ptr(), _row(out), _type(x),
+                                    x.shape[0], x.shape[1], _stream(stream))
+        if check and rc != ECRM_OK:
+            raise EcrmError(rc, "ecrm_dropout")
+        return rc
+
+
+def _is_rows(t, rows, cols, dtype):
+    """A matrix in device memory whose rows have their elements side by side?"""
+    return (t.is_cuda and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols and t.dtype == dtype
+            and (rows == 0 or cols < 2 or t.stride(1) == 1))
+
+
+def _optional(t):
+    """Address and distance of the rows of a matrix that need not be there."""
+    return (None, 0) if t is None else (t.data_ptr(), _row(t))
+
+
+class FeedForward:
+    """A gated feed-forward block (ecrm_ffn_<name>) with the weights gate, up [hidden, dim] and down [dim, hidden], which are kept alive
+    and have to stay where they are.  activation: "silu", "gelu" or "relu".  Its workspace, for calls of up to max_rows rows and, with
+    training, the backward pass, may be another block's (workspace=other.workspace) if no two calls on them overlap in time.  The
+    block may be dropped while calls are still to run, on whatever streams; a graph that uses it needs it kept."""
+
+    ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
+
+    def __init__(self, gate, up, down, max_rows, activation="silu", training=False, workspace=None, stream=None):
+        import torch
+        self._lib = load_library()
+        self._ffn = C.c_void_p(0)
+        self.hidden, self.dim = gate.shape
+        self.dtype, self.max_rows = gate.dtype, max_rows
+        assert _is_rows(gate, self.hidden, self.dim, self.dtype) and _is_rows(up, self.hidden, self.dim, self.dtype)
+        assert _is_rows(down, self.dim, self.hidden, self.dtype)
+        assert gate.device == up.device == down.device and gate.device.index == torch.cuda.current_device()
+        cfg = EcrmFfnConfig(self.dim, self.hidden, _type(gate), self.ACTIVATIONS[activation], max_rows, 1 if training else 0)
+        rc = self._lib.ecrm_ffn_create(C.byref(cfg), C.byref(self._ffn))
+        if rc != ECRM_OK:
+            raise EcrmError(rc, "ecrm_ffn_create")
+        if workspace is None:
+            with torch.cuda.stream(_stream_object(stream)):  # memory that stream has done with
+                workspace = torch.empty(self.workspace_bytes(), dtype=torch.uint8, device=gate.device)
+        assert workspace.is_cuda and workspace.is_contiguous() and workspace.device == gate.device
+        self.workspace = workspace
+        self._keep, self._streams = (gate, up, down, workspace), set()
+        rc = self._lib.ecrm_ffn_bind(self._ffn, gate.data_ptr(), _row(gate), up.data_ptr(), _row(up), down.data_ptr(), _row(down),
+                                     workspace.data_ptr(), workspace.numel() * workspace.element_size())
+        if rc != ECRM_OK:
+            raise EcrmError(rc, "ecrm_ffn_bind")
+
+    def workspace_bytes(self):
+        return self._lib.ecrm_ffn_bytes(self._ffn)
+
+    def _on(self, stream):
+        """Address of a call's stream; the allocator learns that weights and workspace are used there."""
+        address = _stream(stream)
+        if address not in self._streams:
+            self._streams.add(address)
+            use = _stream_object(stream)
+            for t in self._keep:
+                t.record_stream(use)
+        return address
+
+    def destroy(self):
+        if self._ffn:
+            self._lib.ecrm_ffn_destroy(self._ffn)
+            self._ffn = C.c_void_p(0)
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+    def forward(self, x, out, residual=None, dropout=None, saved=None, stream=None, check=True):
+        """out = residual + dropout(block(x)); x, out, residual: [n, dim], rows at any multiple of 4 elements from each other; out may be
+        x or residual.  saved [n, 2 * hidden]: what the backward pass needs."""
+        n, t = x.shape[0], self.dtype
+        assert _is_rows(x, n, self.dim, t) and _is_rows(out, n, self.dim, t)
+        assert residual is None or _is_rows(residual, n, self.dim, t)
+        assert saved is None or (_is_rows(saved, n, 2 * self.hidden, t) and saved.is_contiguous())
+        rc = self._lib.ecrm_ffn_forward(self._ffn, x.data_ptr(), _row(x), n, *_optional(residual), dropout.mask if dropout else None,
+                                        out.data_ptr(), _row(out), saved.data_ptr() if saved is not None else None, self._on(stream))
+        if check and rc != ECRM_OK:
+            raise EcrmError(rc, "ecrm_ffn_forward")
+        return rc
+
+    def backward(self, x, saved, d_out, d_x=None, d_gate=None, d_up=None, d_down=None, add=None, dropout=None, accumulate=False,
+                 stream=None, check=True):
+        """x, saved, dropout: the forward call's.  d_x = add + gradient of x (add: d_out where the residual was x); d_x may be add or d_out.
+        d_gate, d_up, d_down: contiguous, of the block's type or fp32, all or none; accumulate: added to."""
+        n, t = x.shape[0], self.dtype
+        assert _is_rows(x, n, self.dim, t) and _is_rows(d_out, n, self.dim, t)
+        assert _is_rows(saved, n, 2 * self.hidden, t) and saved.is_contiguous()
+        assert d_x is None or _is_rows(d_x, n, self.dim, t)
+        assert add is None or _is_rows(add, n, self.dim, t)
+        weights = [w for w in (d_gate, d_up, d_down) if w is not None]
+        assert all(w.is_cuda and w.is_contiguous() and w.dtype == weights[0].dtype for w in weights)
+        assert d_gate is None or tuple(d_gate.shape) == (self.hidden, self.dim)
+        assert d_up is None or tuple(d_up.shape) == (self.hidden, self.dim)
+        assert d_down is None or tuple(d_down.shape) == (self.dim, self.hidden)
+        rc = self._lib.ecrm_ffn_backward(self._ffn, x.data_ptr(), _row(x), saved.data_ptr(), d_out.data_ptr(), _row(d_out), n,
+                                         dropout.mask if dropout else None, *_optional(add), *_optional(d_x),
+                                         *[w.data_ptr() if w is not None else None for w in (d_gate, d_up, d_down)],
+                                         _type(weights[0]) if weights else 0, 1 if accumulate else 0, self._on(stream))
+        if check and rc != ECRM_OK:
+            raise EcrmError(rc, "ecrm_ffn_backward")
+        return rc
+
+
 class Ecrm:
     """One context of the library.  Method names mirror the C entry points (ecrm_<name>)."""
 
@@ -401,16 +550,20 @@ class Ecrm:
             raise EcrmError(rc, "ecrm_recovery_state")
         return dict(active=bool(a.value), next_chunk=int(nx.value), chunks=int(ch.value), buffered=int(bf.value))
 
-    def embed(self, keys, out, scale=1.0, padding=None, lost_server=None, stream=None, check=True):
+    def embed(self, keys, out, scale=1.0, padding=None, lost_server=None, stream=None, check=True, dropout=None):
         """out: [n, D] of fp32, bf16 or fp16, rows at any multiple of 4 elements from each other."""
         n = keys.numel()
         assert _is_words(keys)
         assert out.is_cuda and out.dim() == 2 and out.shape[0] == n and out.shape[1] == self.cfg.dim and (n == 0 or out.stride(1) == 1)
-        rc = self._lib.ecrm_embed(self._ctx, keys.data_ptr(), n, _key(padding), scale,
-                                  0xFFFFFFFF if lost_server is None else lost_server, out.data_ptr(), _type(out), _row(out),
-                                  _stream(stream))
+        lost = 0xFFFFFFFF if lost_server is None else lost_server
+        if dropout is None:
+            rc = self._lib.ecrm_embed(self._ctx, keys.data_ptr(), n, _key(padding), scale, lost, out.data_ptr(), _type(out), _row(out),
+                                      _stream(stream))
+        else:
+            rc = self._lib.ecrm_embed_dropout(self._ctx, keys.data_ptr(), n, _key(padding), scale, lost, dropout.mask, out.data_ptr(),
+                                              _type(out), _row(out), _stream(stream))
         if check and rc != ECRM_OK:
-            raise EcrmError(rc, "ecrm_embed")
+            raise EcrmError(rc, "ecrm_embed" if dropout is None else "ecrm_embed_dropout")
         return rc
 
     def _check_grad(self, keys, d_out):
@@ -420,28 +573,37 @@ class Ecrm:
         assert n == 0 or d_out.stride(1) == 1
         return n
 
-    def embed_grad(self, keys, d_out, out_keys, out_grads, count, scale=1.0, padding=None, stream=None, check=True):
-        """d_out: [n, D] of fp32, bf16 or fp16; out_keys [n] and out_grads [n, D] have room for as many distinct keys."""
+    def embed_grad(self, keys, d_out, out_keys, out_grads, count, scale=1.0, padding=None, stream=None, check=True, dropout=None):
+        """d_out: [n, D] of fp32, bf16 or fp16; out_keys [n] and out_grads [n, D] have room for as many distinct keys.  dropout: the
+        lookup's."""
         import torch
         n = self._check_grad(keys, d_out)
         assert _is_words(out_keys) and out_keys.numel() >= n
         assert out_grads.is_cuda and out_grads.dtype == torch.float32 and out_grads.is_contiguous()
         assert out_grads.numel() >= n * self.cfg.dim and _is_words(count) and count.numel() == 1
-        rc = self._lib.ecrm_embed_grad(self._ctx, keys.data_ptr(), d_out.data_ptr(), _type(d_out), _row(d_out), n, _key(padding),
-                                       scale, out_keys.data_ptr(), out_grads.data_ptr(), count.data_ptr(), _stream(stream))
+        batch = (self._ctx, keys.data_ptr(), d_out.data_ptr(), _type(d_out), _row(d_out), n, _key(padding), scale)
+        out = (out_keys.data_ptr(), out_grads.data_ptr(), count.data_ptr(), _stream(stream))
+        if dropout is None:
+            rc = self._lib.ecrm_embed_grad(*batch, *out)
+        else:
+            rc = self._lib.ecrm_embed_grad_dropout(*batch, dropout.mask, *out)
         if check and rc != ECRM_OK:
-            raise EcrmError(rc, "ecrm_embed_grad")
+            raise EcrmError(rc, "ecrm_embed_grad" if dropout is None else "ecrm_embed_grad_dropout")
         return rc
 
-    def embed_grad_dense(self, keys, d_out, out, scale=1.0, padding=None, accumulate=False, stream=None, check=True):
-        """out: [R, D] fp32."""
+    def embed_grad_dense(self, keys, d_out, out, scale=1.0, padding=None, accumulate=False, stream=None, check=True, dropout=None):
+        """out: [R, D] fp32.  dropout: the lookup's."""
         import torch
         n = self._check_grad(keys, d_out)
         assert out.is_cuda and out.dtype == torch.float32 and out.is_contiguous() and tuple(out.shape) == (self.cfg.rows, self.cfg.dim)
-        rc = self._lib.ecrm_embed_grad_dense(self._ctx, keys.data_ptr(), d_out.data_ptr(), _type(d_out), _row(d_out), n,
-                                             _key(padding), scale, out.data_ptr(), 1 if accumulate else 0, _stream(stream))
+        batch = (self._ctx, keys.data_ptr(), d_out.data_ptr(), _type(d_out), _row(d_out), n, _key(padding), scale)
+        to = (out.data_ptr(), 1 if accumulate else 0, _stream(stream))
+        if dropout is None:
+            rc = self._lib.ecrm_embed_grad_dense(*batch, *to)
+        else:
+            rc = self._lib.ecrm_embed_grad_dense_dropout(*batch, dropout.mask, *to)
         if check and rc != ECRM_OK:
-            raise EcrmError(rc, "ecrm_embed_grad_dense")
+            raise EcrmError(rc, "ecrm_embed_grad_dense" if dropout is None else "ecrm_embed_grad_dense_dropout")
         return rc
 
     def status(self, stream=None):

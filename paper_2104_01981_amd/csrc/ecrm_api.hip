@@ -5,7 +5,7 @@
 #include <new>
 #include <string.h>
 
-#include "types.h"
+#include "mask.h"
 
 using namespace ecrm;
 
@@ -688,28 +688,52 @@ static bool apart(const void *a, uint64_t a_bytes, const void *b, uint64_t b_byt
     return rows_apart(a, a_bytes != 0, a_bytes, a_bytes, b, b_bytes);
 }
 
+static int run_embed(ecrm_ctx *c, const uint64_t *keys, uint64_t n, uint64_t padding, float scale, uint32_t lost_server,
+                     const ecrm_mask *mask, void *out, uint32_t type, uint64_t stride, void *stream)
+{
+    MaskArgs m;
+    double factor;
+    if (lost_server != ECRM_NO_SERVER && lost_server >= c->geo.S) return ECRM_EINVAL;
+    if (!isfinite(scale)) return ECRM_EINVAL;
+    if (mask && (!make_mask(mask, m, factor) || n > 1ull << 32)) return ECRM_EINVAL;
+    if (n == 0) return ECRM_OK;
+    if (!aligned(keys, 8) || !rows_ok(c, out, type, n, stride)) return ECRM_EINVAL;
+    const uint64_t row = c->cfg.dim * type_bytes(type), step = stride * type_bytes(type);
+    if (!rows_apart(out, n, row, step, keys, n * 8)) return ECRM_EINVAL;
+    if (mask && !rows_apart(out, n, row, step, mask->state, 16)) return ECRM_EINVAL;
+    init_if_needed(c, (hipStream_t)stream);
+    launch_embed(c->s, c->geo, c->t.E, c->t.PE, keys, n, padding, scale, lost_server, mask ? &m : nullptr, out, type, stride, c->cus,
+                 (hipStream_t)stream);
+    return check_launch();
+}
+
 int ecrm_embed(ecrm_ctx *c, const uint64_t *keys, uint64_t n, uint64_t padding, float scale, uint32_t lost_server, void *out,
                uint32_t type, uint64_t stride, void *stream)
 {
     if (!c) return ECRM_EINVAL;
     if (!c->bound) return ECRM_ENOTBOUND;
-    if (lost_server != ECRM_NO_SERVER && lost_server >= c->geo.S) return ECRM_EINVAL;
-    if (!isfinite(scale)) return ECRM_EINVAL;
-    if (n == 0) return ECRM_OK;
-    if (!aligned(keys, 8) || !rows_ok(c, out, type, n, stride)) return ECRM_EINVAL;
-    if (!rows_apart(out, n, c->cfg.dim * type_bytes(type), stride * type_bytes(type), keys, n * 8)) return ECRM_EINVAL;
-    init_if_needed(c, (hipStream_t)stream);
-    launch_embed(c->s, c->geo, c->t.E, c->t.PE, keys, n, padding, scale, lost_server, out, type, stride, c->cus, (hipStream_t)stream);
-    return check_launch();
+    return run_embed(c, keys, n, padding, scale, lost_server, nullptr, out, type, stride, stream);
+}
+
+int ecrm_embed_dropout(ecrm_ctx *c, const uint64_t *keys, uint64_t n, uint64_t padding, float scale, uint32_t lost_server,
+                       const ecrm_mask *mask, void *out, uint32_t type, uint64_t stride, void *stream)
+{
+    if (!c) return ECRM_EINVAL;
+    if (!c->bound) return ECRM_ENOTBOUND;
+    if (!mask) return ECRM_EINVAL;
+    return run_embed(c, keys, n, padding, scale, lost_server, mask, out, type, stride, stream);
 }
 
 static int run_embed_grad(ecrm_ctx *c, const uint64_t *keys, const void *d, uint32_t type, uint64_t stride, uint64_t n,
-                          uint64_t padding, float scale, uint64_t *out_keys, float *out, uint64_t *count, bool accumulate,
-                          void *stream)
+                          uint64_t padding, float scale, const ecrm_mask *mask, uint64_t *out_keys, float *out, uint64_t *count,
+                          bool accumulate, void *stream)
 {
+    MaskArgs m;
+    double factor = 1.0;
     if (!c->grad_room) return ECRM_ESCRATCH;
     if (n > c->lay.max_batch) return ECRM_EBATCH;
     if (!isfinite(scale)) return ECRM_EINVAL;
+    if (mask && !make_mask(mask, m, factor)) return ECRM_EINVAL;
     if (n && (!aligned(keys, 8) || !rows_ok(c, d, type, n, stride))) return ECRM_EINVAL;
     // What is written overlaps nothing that is read, but for the distinct keys: they may take the tokens' place (launch_embed_grad).
     const uint64_t D = c->cfg.dim, row = D * type_bytes(type), step = stride * type_bytes(type);
@@ -719,28 +743,63 @@ static int run_embed_grad(ecrm_ctx *c, const uint64_t *keys, const void *d, uint
         (!rows_apart(d, n, row, step, out_keys, n * 8) || !apart(out, out_bytes, out_keys, n * 8) || !apart(keys, n * 8, count, 8) ||
          !rows_apart(d, n, row, step, count, 8) || !apart(out, out_bytes, count, 8) || !apart(out_keys, n * 8, count, 8)))
         return ECRM_EINVAL;
+    if (n && mask && (!apart(mask->state, 16, out, out_bytes) || (out_keys && (!apart(mask->state, 16, out_keys, n * 8) ||
+                                                                                !apart(mask->state, 16, count, 8)))))
+        return ECRM_EINVAL;
     init_if_needed(c, (hipStream_t)stream);
-    launch_embed_grad(c->s, c->elay, c->geo, c->key_bits, keys, d, type, stride, (uint32_t)n, padding, scale, out_keys, out, count,
-                      accumulate, c->cus, (hipStream_t)stream);
+    launch_embed_grad(c->s, c->elay, c->geo, c->key_bits, keys, d, type, stride, (uint32_t)n, padding, (double)scale * factor,
+                      mask ? &m : nullptr, out_keys, out, count, accumulate, c->cus, (hipStream_t)stream);
     return check_launch();
+}
+
+static int run_embed_grad_rows(ecrm_ctx *c, const uint64_t *keys, const void *d_out, uint32_t type, uint64_t stride, uint64_t n,
+                               uint64_t padding, float scale, const ecrm_mask *mask, uint64_t *out_keys, float *out_grads, uint64_t *count,
+                               void *stream)
+{
+    if (!c->bound) return ECRM_ENOTBOUND;
+    if (!aligned(count, 8) || (n && (!aligned(out_keys, 8) || !aligned(out_grads, 16)))) return ECRM_EINVAL;
+    return run_embed_grad(c, keys, d_out, type, stride, n, padding, scale, mask, out_keys, out_grads, count, false, stream);
 }
 
 int ecrm_embed_grad(ecrm_ctx *c, const uint64_t *keys, const void *d_out, uint32_t type, uint64_t stride, uint64_t n,
                     uint64_t padding, float scale, uint64_t *out_keys, float *out_grads, uint64_t *count, void *stream)
 {
     if (!c) return ECRM_EINVAL;
+    return run_embed_grad_rows(c, keys, d_out, type, stride, n, padding, scale, nullptr, out_keys, out_grads, count, stream);
+}
+
+int ecrm_embed_grad_dropout(ecrm_ctx *c, const uint64_t *keys, const void *d_out, uint32_t type, uint64_t stride, uint64_t n,
+                            uint64_t padding, float scale, const ecrm_mask *mask, uint64_t *out_keys, float *out_grads, uint64_t *count,
+                            void *stream)
+{
+    if (!c) return ECRM_EINVAL;
     if (!c->bound) return ECRM_ENOTBOUND;
-    if (!aligned(count, 8) || (n && (!aligned(out_keys, 8) || !aligned(out_grads, 16)))) return ECRM_EINVAL;
-    return run_embed_grad(c, keys, d_out, type, stride, n, padding, scale, out_keys, out_grads, count, false, stream);
+    if (!mask) return ECRM_EINVAL;
+    return run_embed_grad_rows(c, keys, d_out, type, stride, n, padding, scale, mask, out_keys, out_grads, count, stream);
+}
+
+static int run_embed_grad_dense(ecrm_ctx *c, const uint64_t *keys, const void *d_out, uint32_t type, uint64_t stride, uint64_t n,
+                                uint64_t padding, float scale, const ecrm_mask *mask, float *dE, int accumulate, void *stream)
+{
+    if (!c->bound) return ECRM_ENOTBOUND;
+    if (!aligned(dE, 16)) return ECRM_EINVAL;
+    return run_embed_grad(c, keys, d_out, type, stride, n, padding, scale, mask, nullptr, dE, nullptr, accumulate != 0, stream);
 }
 
 int ecrm_embed_grad_dense(ecrm_ctx *c, const uint64_t *keys, const void *d_out, uint32_t type, uint64_t stride, uint64_t n,
                           uint64_t padding, float scale, float *dE, int accumulate, void *stream)
 {
     if (!c) return ECRM_EINVAL;
+    return run_embed_grad_dense(c, keys, d_out, type, stride, n, padding, scale, nullptr, dE, accumulate, stream);
+}
+
+int ecrm_embed_grad_dense_dropout(ecrm_ctx *c, const uint64_t *keys, const void *d_out, uint32_t type, uint64_t stride, uint64_t n,
+                                  uint64_t padding, float scale, const ecrm_mask *mask, float *dE, int accumulate, void *stream)
+{
+    if (!c) return ECRM_EINVAL;
     if (!c->bound) return ECRM_ENOTBOUND;
-    if (!aligned(dE, 16)) return ECRM_EINVAL;
-    return run_embed_grad(c, keys, d_out, type, stride, n, padding, scale, nullptr, dE, nullptr, accumulate != 0, stream);
+    if (!mask) return ECRM_EINVAL;
+    return run_embed_grad_dense(c, keys, d_out, type, stride, n, padding, scale, mask, dE, accumulate, stream);
 }
 
 int ecrm_status(ecrm_ctx *c, void *stream)

@@ -281,9 +281,10 @@ void launch_degraded_read(const Scratch &s, const Geometry &g, const float *E, c
                           const float *PA, const uint64_t *keys, uint64_t n, uint32_t lost, float *out_E,
                           float *out_A, int cus, hipStream_t st);
 
+struct MaskArgs;                   // mask.h; null: no dropout
 void launch_embed(const Scratch &s, const Geometry &g, const float *E, const float *PE, const uint64_t *keys, uint64_t n,
-                  uint64_t padding, float scale, uint32_t lost, void *out, uint32_t type, uint64_t stride, int cus,
-                  hipStream_t st);
+                  uint64_t padding, float scale, uint32_t lost, const MaskArgs *mask, void *out, uint32_t type, uint64_t stride,
+                  int cus, hipStream_t st);
 // What the kernels of a gradient call tell each other.
 struct TokenControl {
     uint32_t bad;                  // the batch has a key out of range: nothing of it counts
@@ -318,8 +319,9 @@ struct EmbedGradLayout {
 EmbedGradLayout embed_grad_layout(size_t off, uint32_t max_batch, uint32_t D, int key_bits);
 // out_keys null: the dense form
 void launch_embed_grad(const Scratch &s, const EmbedGradLayout &l, const Geometry &g, int key_bits, const uint64_t *keys,
-                       const void *d, uint32_t type, uint64_t stride, uint32_t n, uint64_t padding, float scale,
-                       uint64_t *out_keys, float *out, uint64_t *count, bool accumulate, int cus, hipStream_t st);
+                       const void *d, uint32_t type, uint64_t stride, uint32_t n, uint64_t padding, double scale,
+                       const MaskArgs *mask, uint64_t *out_keys, float *out, uint64_t *count, bool accumulate, int cus,
+                       hipStream_t st);
 
 // What a batch that was held back in part, or a replay, leaves of the recovery buffer (one thread, after everything of the
 // batch has been appended or released).

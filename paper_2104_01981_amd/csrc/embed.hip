@@ -5,7 +5,7 @@
 // belong to, so that rows of any width use all lanes, and keeps several of them in flight; what is written is read by somebody
 // else later.  2^20 tokens of 128 floats to bf16, out of 2^22 rows: 157 us, 4.8 TB/s, what a copy reaches (163 with the stores
 // kept in the caches; 162 with loads past them, too); 2^16 to fp32 while a server is down 16 us.
-#include "types.h"
+#include "mask.h"
 
 namespace ecrm {
 
@@ -25,6 +25,8 @@ struct EmbedArgs {
     Header *hdr;
     Geometry geo;
     Divider d4;              // by D / 4
+    MaskArgs mask;           // with dropout
+    uint32_t first;          // row of the first token in the mask
 };
 
 // The tokens of a wave that are handled alike, row and place in the wave's range: how many there are.
@@ -63,7 +65,7 @@ __device__ __forceinline__ f32x4 decode4(const EmbedArgs &a, uint32_t x, uint32_
     return f32x4{(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
 }
 
-template <typename T>
+template <typename T, bool DROP>
 __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(EmbedArgs a)
 {
     typedef typename Quad<T>::type Four;
@@ -84,6 +86,9 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(EmbedArgs a)
         lost = a.geo.dS.mod(g + 1u + j) == a.lost;
     }
     T *out = (T *)a.out + first * a.stride;
+    MaskKey mask{};
+    if (DROP) mask = mask_key(a.mask);
+    const uint32_t row0 = a.first + (uint32_t)first;     // with dropout there are at most 2^32
 
     // the product is formed in 32 bits, then rounded to the type: half a step of the type and 2^-24 in all
     const uint32_t plain = gather_tokens(in && !bad && !lost, x, list), total = plain * a.d4.d;
@@ -91,13 +96,22 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(EmbedArgs a)
     for (uint32_t u0 = 0; u0 < total; u0 += U * kWave) {
         f32x4 e[U];
         size_t to[U];
+        uint32_t row[U], col[U];
+        uint2 bits[U];
 #pragma unroll
         for (uint32_t q = 0; q < U; ++q) {
             const uint32_t u = min(u0 + q * kWave + lane, total - 1u), r = a.d4.div(u), c = (u - r * a.d4.d) * 4u;
             const uint2 what = list[r];
             to[q] = what.y * a.stride + c;
+            row[q] = row0 + what.y;
+            col[q] = c;
             e[q] = f32x4{0.f, 0.f, 0.f, 0.f};
             if (what.x != kNoKey) e[q] = *(const f32x4 *)(a.E + (size_t)what.x * D + c) * a.scale;
+        }
+        if (DROP) {                                      // lanes 2i and 2i + 1 have quads 2j and 2j + 1 if a row has an even number
+            mask_quads<U>(mask, row, col, a.d4.d % 2u == 0, bits);
+#pragma unroll
+            for (uint32_t q = 0; q < U; ++q) e[q] = drop4(e[q], bits[q], mask);
         }
 #pragma unroll
         for (uint32_t q = 0; q < U; ++q)
@@ -109,20 +123,24 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(EmbedArgs a)
     for (uint32_t u = lane; u < decoded; u += kWave) {
         const uint32_t r = a.d4.div(u), c = (u - r * a.d4.d) * 4u;
         const uint2 what = list[r];
-        __builtin_nontemporal_store(round4<T>(decode4(a, what.x, c) * a.scale), (Four *)(out + what.y * a.stride + c));
+        f32x4 e = decode4(a, what.x, c) * a.scale;
+        if (DROP) e = drop4(e, mask_quad(mask, row0 + what.y, c), mask);
+        __builtin_nontemporal_store(round4<T>(e), (Four *)(out + what.y * a.stride + c));
     }
 }
 
 void launch_embed(const Scratch &s, const Geometry &g, const float *E, const float *PE, const uint64_t *keys, uint64_t n,
-                  uint64_t padding, float scale, uint32_t lost, void *out, uint32_t type, uint64_t stride, int cus,
-                  hipStream_t st)
+                  uint64_t padding, float scale, uint32_t lost, const MaskArgs *mask, void *out, uint32_t type, uint64_t stride,
+                  int cus, hipStream_t st)
 {
     EmbedArgs a{};
     a.E = E; a.PE = PE; a.hdr = s.hdr; a.geo = g; a.lost = lost; a.scale = scale; a.padding = padding; a.stride = stride;
     a.d4 = make_divider(g.D / 4u);
+    if (mask) a.mask = *mask;
     for (uint64_t at = 0; at < n; at += kEmbedSlice) {
         a.n = n - at < kEmbedSlice ? n - at : kEmbedSlice;
         a.keys = keys + at;
+        a.first = (uint32_t)at;
         a.out = (char *)out + at * stride * type_bytes(type);
         const uint64_t waves = (uint64_t)cus * 32u;              // as many as are resident
         a.per = (uint32_t)((a.n + waves - 1) / waves);
@@ -130,7 +148,8 @@ void launch_embed(const Scratch &s, const Geometry &g, const float *E, const flo
         const uint64_t per_block = (uint64_t)a.per * kEmbedWaves;
         const dim3 grid((uint32_t)((a.n + per_block - 1) / per_block)), block(kEmbedThreads);
         with_type(type, [&](auto t) {
-            hipLaunchKernelGGL((embed_kernel<decltype(t)>), grid, block, 0, st, a);
+            if (mask) hipLaunchKernelGGL((embed_kernel<decltype(t), true>), grid, block, 0, st, a);
+            else hipLaunchKernelGGL((embed_kernel<decltype(t), false>), grid, block, 0, st, a);
         });
     }
 }

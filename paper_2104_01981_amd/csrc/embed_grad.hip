@@ -12,7 +12,7 @@
 // form, which counts no rows), then two for each digit of the sort, or three, and three or four behind it: five to nine up to 2^18
 // tokens, six to sixteen beyond (twelve for rows of 19 to 27 bits).  Of 2^16 tokens of text with 256 floats in bf16, 42 us, the sums
 // take 16, the sort 20 and the join 4.
-#include "types.h"
+#include "mask.h"
 
 namespace ecrm {
 
@@ -66,6 +66,7 @@ struct SumArgs {
     uint32_t counting;
     const void *d;                   // [n][stride] gradients of the looked-up rows
     uint64_t stride;
+    MaskArgs mask;                   // with dropout: which elements of d count; its factor is in the scale
     double scale;
     uint32_t accumulate;             // dense: add to what is there
     TokenControl *ctl;
@@ -246,8 +247,8 @@ __device__ __forceinline__ uint32_t sort_here(const SumArgs &a, uint32_t *s_raw,
     return valid;
 }
 
-// STREAM: rows are moved past the caches (kStreamBytes).  HERE: up to kSortHere tokens, sorted here.
-template <typename T, bool DENSE, bool STREAM, bool HERE>
+// STREAM: rows are moved past the caches (kStreamBytes).  HERE: up to kSortHere tokens, sorted here.  DROP: the lookup had dropout.
+template <typename T, bool DENSE, bool STREAM, bool HERE, bool DROP>
 __global__ __launch_bounds__(kSumThreads) void sum_runs_kernel(SumArgs a)
 {
     typedef typename Quad<T>::type Four;
@@ -349,14 +350,27 @@ __global__ __launch_bounds__(kSumThreads) void sum_runs_kernel(SumArgs a)
     if (live) {
         uint32_t state = 0;
         double acc[4] = {0, 0, 0, 0};
+        MaskKey mask{};
+        if (DROP) mask = mask_key(a.mask);
         bool before = lo < hi && s_key[lo] == s_key[lo + 1], open = false;     // the run begins before the chunk; is not at its end
         for (uint32_t i0 = lo; i0 < hi; i0 += U) {
             if (i0 != lo) load(i0);
+            uint2 bits[U];
+            if (DROP) {                                  // lanes 2i and 2i + 1 have columns 8j and 8j + 4 if teams begin at even ones
+                uint32_t row[U], col[U];
+#pragma unroll
+                for (uint32_t q = 0; q < U; ++q) {
+                    row[q] = s_idx[min(i0 + q, hi - 1u)];
+                    col[q] = c;
+                }
+                mask_quads<U>(mask, row, col, a.units.d % 2u == 0 && a.quads % 2u == 0, bits);
+            }
 #pragma unroll
             for (uint32_t q = 0; q < U; ++q) {
                 const uint32_t i = i0 + q;
                 if (i >= hi) break;
-                const f32x4 g = widen4<T>(v[q]);
+                f32x4 g = widen4<T>(v[q]);
+                if (DROP) g = keep4(g, bits[q], mask.border);
                 acc[0] += (double)g.x;
                 acc[1] += (double)g.y;
                 acc[2] += (double)g.z;
@@ -582,18 +596,19 @@ EmbedGradLayout embed_grad_layout(size_t off, uint32_t max_batch, uint32_t D, in
     return l;
 }
 
-template <typename T, bool DENSE>
+template <typename T, bool DENSE, bool DROP>
 static void launch_sum(const SumArgs &a, dim3 grid, size_t lds, bool stream, hipStream_t st)
 {
     const dim3 threads(kSumThreads);
-    if (a.keys) hipLaunchKernelGGL((sum_runs_kernel<T, DENSE, false, true>), grid, threads, lds, st, a);
-    else if (stream) hipLaunchKernelGGL((sum_runs_kernel<T, DENSE, true, false>), grid, threads, lds, st, a);
-    else hipLaunchKernelGGL((sum_runs_kernel<T, DENSE, false, false>), grid, threads, lds, st, a);
+    if (a.keys) hipLaunchKernelGGL((sum_runs_kernel<T, DENSE, false, true, DROP>), grid, threads, lds, st, a);
+    else if (stream) hipLaunchKernelGGL((sum_runs_kernel<T, DENSE, true, false, DROP>), grid, threads, lds, st, a);
+    else hipLaunchKernelGGL((sum_runs_kernel<T, DENSE, false, false, DROP>), grid, threads, lds, st, a);
 }
 
 void launch_embed_grad(const Scratch &s, const EmbedGradLayout &l, const Geometry &g, int key_bits, const uint64_t *keys,
-                       const void *d, uint32_t type, uint64_t stride, uint32_t n, uint64_t padding, float scale,
-                       uint64_t *out_keys, float *out, uint64_t *count, bool accumulate, int cus, hipStream_t st)
+                       const void *d, uint32_t type, uint64_t stride, uint32_t n, uint64_t padding, double scale,
+                       const MaskArgs *mask, uint64_t *out_keys, float *out, uint64_t *count, bool accumulate, int cus,
+                       hipStream_t st)
 {
     const bool dense = !out_keys;
     const dim3 threads(kSumThreads);
@@ -630,7 +645,7 @@ void launch_embed_grad(const Scratch &s, const EmbedGradLayout &l, const Geometr
     const SumPlan p = sum_plan(n, g.D);
     a.n = n; a.D = g.D; a.quads = g.D / 4u; a.units = make_divider(p.units);
     a.teams = p.teams; a.chunk = p.chunk; a.per = p.per; a.blocks = p.blocks;
-    a.d = d; a.stride = stride; a.scale = (double)scale; a.accumulate = accumulate ? 1u : 0u;
+    a.d = d; a.stride = stride; a.scale = scale; a.accumulate = accumulate ? 1u : 0u;
     a.first = (uint32_t *)(base + l.off_first);
     a.group = (uint32_t *)(base + l.off_group);
     a.groups = (a.blocks + kCountGroup - 1) / kCountGroup;
@@ -639,6 +654,7 @@ void launch_embed_grad(const Scratch &s, const EmbedGradLayout &l, const Geometr
     a.join = (uint32_t *)(base + l.off_join);
     a.part = (double *)(base + l.off_part);
     a.out_keys = out_keys; a.out = out; a.count = count;
+    if (mask) a.mask = *mask;
     a.counting = a.blocks == 1 ? kAllHere : n <= kRankMost ? kCountKeys : a.groups <= kScanGroups ? kAddCounts : kScanned;
     if (!dense && (a.counting == kAddCounts || a.counting == kScanned)) {
         hipLaunchKernelGGL(count_heads_kernel, dim3(a.groups), dim3(kCountThreads), 0, st, a);
@@ -646,8 +662,12 @@ void launch_embed_grad(const Scratch &s, const EmbedGradLayout &l, const Geometr
     }
     const size_t lds = ((size_t)a.per * 2 + 2) * 4;
     with_type(type, [&](auto t) {
-        if (dense) launch_sum<decltype(t), true>(a, dim3(a.blocks, p.slices), lds, stream, st);
-        else launch_sum<decltype(t), false>(a, dim3(a.blocks, p.slices), lds, stream, st);
+        typedef decltype(t) T;
+        const dim3 grid(a.blocks, p.slices);
+        if (mask && dense) launch_sum<T, true, true>(a, grid, lds, stream, st);
+        else if (mask) launch_sum<T, false, true>(a, grid, lds, stream, st);
+        else if (dense) launch_sum<T, true, false>(a, grid, lds, stream, st);
+        else launch_sum<T, false, false>(a, grid, lds, stream, st);
     });
     if (a.blocks > 1) {
         const uint32_t narrow = (a.blocks + a.teams - 1) / a.teams, most = (uint32_t)cus * 8u, wide = (uint32_t)cus;

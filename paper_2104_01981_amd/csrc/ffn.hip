@@ -1,0 +1,347 @@
+// The gated feed-forward block and its gradients: h = act(x Wg^T) * (x Wu^T) in one launch, out = residual + drop(h Wd^T) in a second;
+// backward, from the gradient of out: that of h together with dg, du and h (one launch), the three weights' (one), x's (one).
+#include "products.h"
+
+#include <new>
+#include <string.h>
+
+namespace ecrm {
+
+// ---- which tiles -----------------------------------------------------------------------------------------------------------------
+enum { kTile256 = 0, kTile128 = 1, kTile64 = 2, kTilings = 3 };
+struct TilingSize { uint32_t side, waves, resident; };
+constexpr TilingSize kSizes[kTilings] = {{256, 8, 1}, {128, 4, 2}, {64, 4, 4}};
+constexpr size_t kPartMost = 32u << 20;          // bytes of the parts of split products, at most
+
+struct Plan { uint32_t tiling, splits, each; };
+
+static uint32_t tiles_of(const ProductArgs &a, int kind, uint32_t side)
+{
+    uint64_t tiles = 0;
+    for (uint32_t i = 0; i < a.products; ++i) {
+        const uint32_t columns = kind == kGate ? side / 2u : side;
+        tiles += (uint64_t)((a.p[i].M + side - 1) / side) * ((a.p[i].N + columns - 1) / columns);
+    }
+    return (uint32_t)tiles;
+}
+
+static Plan plan_product(const ProductArgs &a, int kind, uint32_t type, int cus, size_t room)
+{
+    const uint32_t elements = kRowBytes / type_bytes(type), half = (a.p[0].K + elements - 1) / elements, k_tiles = kind == kInput ? 2 * half : half;
+    Plan best{};
+    double least = 0;
+    for (uint32_t t = 0; t < kTilings; ++t) {
+        const TilingSize &z = kSizes[t];
+        const uint32_t tiles = tiles_of(a, kind, z.side), slots = (uint32_t)cus * z.resident;
+        for (uint32_t splits = 1; splits <= k_tiles && splits <= 64u; splits *= 2) {
+            const uint32_t each = (k_tiles + splits - 1) / splits, parts = (k_tiles + each - 1) / each;
+            if (parts > 1 && (uint64_t)tiles * parts * z.side * z.side * 4u > room) break;
+            const double rounds = (double)((tiles * (uint64_t)parts + slots - 1) / slots);
+            const double rate = t == kTile256 ? 1.0 : t == kTile128 ? 0.8 : 0.5;
+            const double work = (double)z.side * z.side / 65536.0 * z.resident / rate;
+            double cost = rounds * (work * each + 2.0);
+            if (parts > 1) cost += 6.0 + (double)tiles * parts * z.side * z.side / 65536.0 / cus;
+            if (!best.splits || cost < least) {
+                best = Plan{t, parts, each};
+                least = cost;
+            }
+        }
+    }
+    return best;
+}
+
+template <typename T, int KIND, int BM, int BN, int WM, int WN>
+static void launch_tiling(const ProductArgs &a, hipStream_t st)
+{
+    typedef Tiling<T, KIND, BM, BN, WM, WN> L;
+    hipLaunchKernelGGL((product_kernel<T, KIND, BM, BN, WM, WN>), dim3(a.tiles * a.splits), dim3(L::kThreads), 0, st, a);
+    if (a.splits > 1)
+        hipLaunchKernelGGL((join_kernel<T, KIND, BM, BN, WM, WN>), dim3(a.tiles, L::MB * L::kNeed), dim3(L::kThreads), 0, st, a);
+}
+
+template <typename T, int KIND>
+static void launch_product(ProductArgs &a, uint32_t type, int cus, float *part, size_t room, hipStream_t st)
+{
+    const Plan plan = plan_product(a, KIND, type, cus, room);
+    const uint32_t side = kSizes[plan.tiling].side, columns = KIND == kGate ? side / 2u : side;
+    a.tiles = 0;
+    for (uint32_t i = 0; i < a.products; ++i) {
+        Product &p = a.p[i];
+        p.tiles_m = (p.M + side - 1) / side;
+        p.tiles_n = (p.N + columns - 1) / columns;
+        a.first[i] = a.tiles;
+        a.tiles += p.tiles_m * p.tiles_n;
+    }
+    a.splits = plan.splits;
+    a.each = plan.each;
+    a.part = part;
+    if (plan.tiling == kTile256) launch_tiling<T, KIND, 256, 256, 2, 4>(a, st);
+    else if (plan.tiling == kTile128) launch_tiling<T, KIND, 128, 128, 2, 2>(a, st);
+    else launch_tiling<T, KIND, 64, 64, 2, 2>(a, st);
+}
+
+__global__ __launch_bounds__(256) void clear_kernel(uint32_t *to, uint64_t words)
+{
+    for (uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x; i < words; i += (uint64_t)gridDim.x * 256u) to[i] = 0u;
+}
+
+}  // namespace ecrm
+
+using namespace ecrm;
+
+// ---- C ABI -----------------------------------------------------------------------------------------------------------------------
+struct ecrm_ffn {
+    ecrm_ffn_config cfg;
+    uint64_t pitch;                       // elements of a row of h, dg, du
+    uint64_t e_pitch;                     // of a row of e
+    size_t off_h, off_dg, off_du, off_e, off_part, part_bytes, bytes;
+    const void *gate, *up, *down;
+    uint64_t gate_stride, up_stride, down_stride;
+    char *work;
+    int cus;
+};
+
+namespace {
+
+constexpr uint64_t kStrideMost = 1u << 20;
+
+struct Rows { const void *p; uint64_t rows, cols, stride; };     // elements
+
+bool rows_fit(const ecrm_ffn *f, const Rows &r)
+{
+    const uint32_t size = type_bytes(f->cfg.type);
+    return r.p && (uintptr_t)r.p % (4 * size) == 0 && r.stride >= r.cols && r.stride % 4 == 0 && r.stride <= kStrideMost;
+}
+
+bool apart(uint32_t a_size, const Rows &a, uint32_t b_size, const Rows &b)
+{
+    return strided_apart(a.p, a.p ? a.rows : 0, a.cols * a_size, a.stride * a_size, b.p, b.p ? b.rows : 0, b.cols * b_size, b.stride * b_size);
+}
+
+// Is what is written clear of the weights, the workspace and the mask's state?
+bool clear_of_own(const ecrm_ffn *f, const ecrm_mask *mask, uint32_t size, const Rows &w)
+{
+    const uint32_t s = type_bytes(f->cfg.type);
+    const uint64_t D = f->cfg.dim, F = f->cfg.hidden;
+    return apart(size, w, s, Rows{f->gate, F, D, f->gate_stride}) && apart(size, w, s, Rows{f->up, F, D, f->up_stride}) &&
+           apart(size, w, s, Rows{f->down, D, F, f->down_stride}) && apart(size, w, 1, Rows{f->work, 1, f->bytes, f->bytes}) &&
+           (!mask || apart(size, w, 1, Rows{mask->state, 1, 16, 16}));
+}
+
+int launched() { return hipGetLastError() == hipSuccess ? ECRM_OK : ECRM_EHIP; }
+
+Product product(const void *a, uint64_t a_stride, const void *b, uint64_t b_stride, uint32_t M, uint32_t N, uint32_t K)
+{
+    Product p;
+    memset(&p, 0, sizeof(p));
+    p.a.p[0] = p.a.p[1] = a;
+    p.a.stride[0] = p.a.stride[1] = a_stride;
+    p.b.p[0] = p.b.p[1] = b;
+    p.b.stride[0] = p.b.stride[1] = b_stride;
+    p.M = M; p.N = N; p.K = K;
+    return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ecrm_ffn_create(const ecrm_ffn_config *cfg, ecrm_ffn **out)
+{
+    if (!out) return ECRM_EINVAL;
+    *out = nullptr;
+    if (!cfg || cfg->dim < 4 || cfg->dim % 4 || cfg->dim > 65536 || cfg->hidden < 4 || cfg->hidden % 4 || cfg->hidden > 65536) return ECRM_EINVAL;
+    if (cfg->type > ECRM_F16 || cfg->activation > ECRM_RELU || cfg->training > 1) return ECRM_EINVAL;
+    if (!cfg->max_rows || cfg->max_rows > (1ull << 26)) return ECRM_EINVAL;
+    ecrm_ffn *f = new (std::nothrow) ecrm_ffn;
+    if (!f) return ECRM_EINVAL;
+    memset(f, 0, sizeof(*f));
+    f->cfg = *cfg;
+    const uint64_t size = type_bytes(cfg->type), D = cfg->dim, F = cfg->hidden;
+    f->pitch = (F + 63) / 64 * 64;
+    f->e_pitch = (D + 63) / 64 * 64;
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t o = off; off = (off + bytes + 255) / 256 * 256; return o; };
+    f->off_h = take(cfg->max_rows * f->pitch * size);
+    if (cfg->training) {
+        f->off_dg = take(cfg->max_rows * f->pitch * size);
+        f->off_du = take(cfg->max_rows * f->pitch * size);
+        f->off_e = take(cfg->max_rows * f->e_pitch * size);
+    }
+    f->part_bytes = kPartMost;
+    f->off_part = take(f->part_bytes);
+    f->bytes = off;
+    *out = f;
+    return ECRM_OK;
+}
+
+void ecrm_ffn_destroy(ecrm_ffn *f) { delete f; }
+
+size_t ecrm_ffn_bytes(const ecrm_ffn *f) { return f ? f->bytes : 0; }
+
+int ecrm_ffn_bind(ecrm_ffn *f, const void *gate, uint64_t gate_stride, const void *up, uint64_t up_stride, const void *down,
+                  uint64_t down_stride, void *work, size_t work_bytes)
+{
+    if (!f) return ECRM_EINVAL;
+    const uint64_t D = f->cfg.dim, F = f->cfg.hidden;
+    const Rows g{gate, F, D, gate_stride}, u{up, F, D, up_stride}, d{down, D, F, down_stride};
+    if (!rows_fit(f, g) || !rows_fit(f, u) || !rows_fit(f, d)) return ECRM_EINVAL;
+    if (!work || (uintptr_t)work % 256 || work_bytes < f->bytes) return ECRM_ESCRATCH;
+    const Rows w{work, 1, f->bytes, f->bytes};
+    const uint32_t size = type_bytes(f->cfg.type);
+    if (!apart(1, w, size, g) || !apart(1, w, size, u) || !apart(1, w, size, d)) return ECRM_EINVAL;
+    int dev = 0, cus = 0;
+    if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus < 1)
+        return ECRM_EHIP;
+    f->gate = gate; f->up = up; f->down = down;
+    f->gate_stride = gate_stride; f->up_stride = up_stride; f->down_stride = down_stride;
+    f->work = (char *)work;
+    f->cus = cus;
+    return ECRM_OK;
+}
+
+int ecrm_ffn_forward(ecrm_ffn *f, const void *x, uint64_t x_stride, uint64_t n, const void *residual, uint64_t residual_stride,
+                     const ecrm_mask *mask, void *out, uint64_t out_stride, void *saved, void *stream)
+{
+    if (!f) return ECRM_EINVAL;
+    if (!f->work) return ECRM_ENOTBOUND;
+    if (n > f->cfg.max_rows) return ECRM_EBATCH;
+    ProductArgs a;
+    memset(&a, 0, sizeof(a));
+    double factor;
+    if (mask && !make_mask(mask, a.mask, factor)) return ECRM_EINVAL;
+    if (!n) return ECRM_OK;
+    const uint32_t D = f->cfg.dim, F = f->cfg.hidden, N = (uint32_t)n, type = f->cfg.type, size = type_bytes(type);
+    if (n == 1) x_stride = residual_stride = out_stride = D;             // of one row it says nothing
+    const Rows rx{x, n, D, x_stride}, rr{residual, n, D, residual_stride}, ro{out, n, D, out_stride}, rs{saved, n, 2ull * F, 2ull * F};
+    if (!rows_fit(f, rx) || !rows_fit(f, ro) || (residual && !rows_fit(f, rr))) return ECRM_EINVAL;
+    if (saved && (uintptr_t)saved % (4 * size)) return ECRM_EINVAL;
+    auto in_place = [&](const Rows &r) { return r.p == out && r.stride == out_stride; };
+    if ((!in_place(rx) && !apart(size, rx, size, ro)) || (residual && !in_place(rr) && !apart(size, rr, size, ro))) return ECRM_EINVAL;
+    if (!clear_of_own(f, mask, size, ro)) return ECRM_EINVAL;
+    if (saved && (!apart(size, rs, size, rx) || !apart(size, rs, size, rr) || !apart(size, rs, size, ro) || !clear_of_own(f, mask, size, rs)))
+        return ECRM_EINVAL;
+    hipStream_t st = (hipStream_t)stream;
+    void *h = f->work + f->off_h;
+    float *part = (float *)(f->work + f->off_part);
+    a.activation = f->cfg.activation;
+    a.products = 1;
+    with_type(type, [&](auto t) {
+        typedef decltype(t) T;
+        a.p[0] = product(x, x_stride, f->gate, f->gate_stride, N, F, D);
+        a.p[0].b.p[1] = f->up;
+        a.p[0].b.stride[1] = f->up_stride;
+        a.p[0].out = h;
+        a.p[0].out_stride = f->pitch;
+        a.p[0].out2 = saved;
+        launch_product<T, kGate>(a, type, f->cus, part, f->part_bytes, st);
+        a.p[0] = product(h, f->pitch, f->down, f->down_stride, N, D, F);
+        a.p[0].out = out;
+        a.p[0].out_stride = out_stride;
+        a.p[0].in = residual;
+        a.p[0].in_stride = residual_stride;
+        a.masked = mask ? 1u : 0u;
+        launch_product<T, kOut>(a, type, f->cus, part, f->part_bytes, st);
+    });
+    return launched();
+}
+
+int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void *saved, const void *d_out, uint64_t d_out_stride,
+                      uint64_t n, const ecrm_mask *mask, const void *add, uint64_t add_stride, void *d_x, uint64_t d_x_stride,
+                      void *d_gate, void *d_up, void *d_down, uint32_t weight_type, int accumulate, void *stream)
+{
+    if (!f) return ECRM_EINVAL;
+    if (!f->work) return ECRM_ENOTBOUND;
+    if (!f->cfg.training) return ECRM_ESCRATCH;
+    if (n > f->cfg.max_rows) return ECRM_EBATCH;
+    ProductArgs a;
+    memset(&a, 0, sizeof(a));
+    double factor;
+    if (mask && !make_mask(mask, a.mask, factor)) return ECRM_EINVAL;
+    const uint32_t D = f->cfg.dim, F = f->cfg.hidden, N = (uint32_t)n, type = f->cfg.type, size = type_bytes(type);
+    const bool weights = d_gate || d_up || d_down;
+    const uint32_t weight_size = type_bytes(weight_type);
+    const Rows rg{d_gate, F, D, D}, ru{d_up, F, D, D}, rd{d_down, D, F, F};
+    if (weights) {
+        if (!d_gate || !d_up || !d_down || (weight_type != type && weight_type != ECRM_F32)) return ECRM_EINVAL;
+        for (const Rows *r : {&rg, &ru, &rd})
+            if ((uintptr_t)r->p % (4 * weight_size) || !clear_of_own(f, mask, weight_size, *r)) return ECRM_EINVAL;
+        if (!apart(weight_size, rg, weight_size, ru) || !apart(weight_size, rg, weight_size, rd) || !apart(weight_size, ru, weight_size, rd)) return ECRM_EINVAL;
+    }
+    hipStream_t st = (hipStream_t)stream;
+    if (!n) {
+        if (weights && !accumulate)
+            for (void *p : {d_gate, d_up, d_down})
+                hipLaunchKernelGGL(clear_kernel, dim3((uint32_t)f->cus), dim3(256), 0, st, (uint32_t *)p, (uint64_t)D * F * weight_size / 4u);
+        return launched();
+    }
+    if (n == 1) x_stride = d_out_stride = add_stride = d_x_stride = D;   // of one row it says nothing
+    const Rows rx{x, n, D, x_stride}, rs{saved, n, 2ull * F, 2ull * F}, ro{d_out, n, D, d_out_stride}, ra{d_x ? add : nullptr, n, D, add_stride},
+        rdx{d_x, n, D, d_x_stride};
+    if (!rows_fit(f, rx) || !rows_fit(f, ro) || (d_x && !rows_fit(f, rdx)) || (ra.p && !rows_fit(f, ra))) return ECRM_EINVAL;
+    if (!saved || (uintptr_t)saved % (4 * size)) return ECRM_EINVAL;
+    if (weights)
+        for (const Rows *w : {&rg, &ru, &rd})
+            for (const Rows *r : {&rx, &rs, &ro, &ra, &rdx})
+                if (!apart(weight_size, *w, size, *r)) return ECRM_EINVAL;
+    if (d_x) {
+        auto in_place = [&](const Rows &r) { return r.p == d_x && r.stride == d_x_stride; };
+        if (!apart(size, rdx, size, rx) || !apart(size, rdx, size, rs) || (!in_place(ro) && !apart(size, rdx, size, ro)) ||
+            (!in_place(ra) && !apart(size, rdx, size, ra)) || !clear_of_own(f, mask, size, rdx))
+            return ECRM_EINVAL;
+    }
+    if (!weights && !d_x) return ECRM_OK;
+
+    void *h = f->work + f->off_h, *dg = f->work + f->off_dg, *du = f->work + f->off_du;
+    float *part = (float *)(f->work + f->off_part);
+    const void *e = d_out;
+    uint64_t e_stride = d_out_stride;
+    if (mask) {
+        e = f->work + f->off_e;
+        e_stride = f->e_pitch;
+        const int rc = ecrm_dropout(mask, d_out, d_out_stride, nullptr, 0, (void *)e, e_stride, type, n, D, stream);
+        if (rc != ECRM_OK) return rc;
+    }
+    a.activation = f->cfg.activation;
+    a.accumulate = accumulate ? 1u : 0u;
+    a.wide = weight_type == ECRM_F32 ? 1u : 0u;
+    with_type(type, [&](auto t) {
+        typedef decltype(t) T;
+        a.products = 1;
+        a.p[0] = product(e, e_stride, f->down, f->down_stride, N, F, D);
+        a.p[0].in = saved;
+        a.p[0].out = dg;
+        a.p[0].out2 = du;
+        a.p[0].out3 = h;
+        a.p[0].out_stride = f->pitch;
+        launch_product<T, kBack>(a, type, f->cus, part, f->part_bytes, st);
+        if (weights) {
+            a.products = 3;
+            a.p[0] = product(dg, f->pitch, x, x_stride, F, D, N);
+            a.p[0].out = d_gate;
+            a.p[0].out_stride = D;
+            a.p[1] = product(du, f->pitch, x, x_stride, F, D, N);
+            a.p[1].out = d_up;
+            a.p[1].out_stride = D;
+            a.p[2] = product(e, e_stride, h, f->pitch, D, F, N);
+            a.p[2].out = d_down;
+            a.p[2].out_stride = F;
+            launch_product<T, kWeights>(a, type, f->cus, part, f->part_bytes, st);
+        }
+        if (d_x) {                        // last: it may take the place of d_out
+            a.products = 1;
+            a.p[0] = product(dg, f->pitch, f->gate, f->gate_stride, N, D, F);
+            a.p[0].a.p[1] = du;
+            a.p[0].b.p[1] = f->up;
+            a.p[0].b.stride[1] = f->up_stride;
+            a.p[0].in = add;
+            a.p[0].in_stride = add_stride;
+            a.p[0].out = d_x;
+            a.p[0].out_stride = d_x_stride;
+            launch_product<T, kInput>(a, type, f->cus, part, f->part_bytes, st);
+        }
+    });
+    return launched();
+}
+
+}  // extern "C"
