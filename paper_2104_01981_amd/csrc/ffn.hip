@@ -8,43 +8,63 @@
 namespace ecrm {
 
 // ---- which tiles -----------------------------------------------------------------------------------------------------------------
+// What a product takes is estimated in us from what was measured (M, N of 1024 to 4096, all CUs in step): a tile's steps of 128 bytes of
+// K, alone on its CU and for each of several; the launch, a tile's begin and end.  16 bits: 64 x 64 0.50 and 0.17 a step, 128 x 128 0.65
+// and 0.47, 256 x 256 1.58; 32 bits: 0.62 and 0.46, 1.96 and 1.79 (256 x 256 is 7.2 and gains nothing).
 enum { kTile256 = 0, kTile128 = 1, kTile64 = 2, kTilings = 3 };
-struct TilingSize { uint32_t side, waves, resident; };
-constexpr TilingSize kSizes[kTilings] = {{256, 8, 1}, {128, 4, 2}, {64, 4, 4}};
+struct TilingCost { uint32_t side; double step[2], shared[2], launch, tile; };          // [0] 16 bits, [1] 32
+constexpr TilingCost kCosts[kTilings] = {{256, {1.58, 0}, {1.58, 0}, 3.0, 8.0}, {128, {0.65, 1.96}, {0.47, 1.79}, 5.0, 1.4},
+                                         {64, {0.50, 0.62}, {0.172, 0.46}, 2.5, 0.42}};
+constexpr uint32_t kSplitCounts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+constexpr double kJoinLaunch = 3.0, kJoinRate = 4.0e6;                                  // us; bytes a us
 constexpr size_t kPartMost = 32u << 20;          // bytes of the parts of split products, at most
 
-struct Plan { uint32_t tiling, splits, each; };
+// Rows up to `rows` of the results with one tiling, the others (if there are any) with another.
+struct Plan { uint32_t tiling, splits, each; double cost; };
+struct RowPlan { uint32_t rows; Plan main, rest; };
 
-static uint32_t tiles_of(const ProductArgs &a, int kind, uint32_t side)
+struct ProductSize { uint32_t M, N, K, halves, count; bool dual; };       // `count` of them
+
+static uint64_t tiles_of(const ProductSize &z, uint32_t M, uint32_t side)
 {
-    uint64_t tiles = 0;
-    for (uint32_t i = 0; i < a.products; ++i) {
-        const uint32_t columns = kind == kGate ? side / 2u : side;
-        tiles += (uint64_t)((a.p[i].M + side - 1) / side) * ((a.p[i].N + columns - 1) / columns);
-    }
-    return (uint32_t)tiles;
+    const uint32_t columns = z.dual ? side / 2u : side;
+    return (uint64_t)((M + side - 1) / side) * ((z.N + columns - 1) / columns) * z.count;
 }
 
-static Plan plan_product(const ProductArgs &a, int kind, uint32_t type, int cus, size_t room)
+static Plan plan_rows(const ProductSize &z, uint32_t M, uint32_t type, uint32_t cus, size_t room)
 {
-    const uint32_t elements = kRowBytes / type_bytes(type), half = (a.p[0].K + elements - 1) / elements, k_tiles = kind == kInput ? 2 * half : half;
+    const uint32_t wide = type == ECRM_F32 ? 1u : 0u, elements = kRowBytes / type_bytes(type);
+    const uint32_t k_tiles = (z.K + elements - 1) / elements * z.halves;
     Plan best{};
-    double least = 0;
-    for (uint32_t t = 0; t < kTilings; ++t) {
-        const TilingSize &z = kSizes[t];
-        const uint32_t tiles = tiles_of(a, kind, z.side), slots = (uint32_t)cus * z.resident;
-        for (uint32_t splits = 1; splits <= k_tiles && splits <= 64u; splits *= 2) {
+    for (uint32_t t = wide ? kTile128 : kTile256; t < kTilings; ++t) {
+        const TilingCost &c = kCosts[t];
+        const uint64_t tiles = tiles_of(z, M, c.side);
+        for (uint32_t splits : kSplitCounts) {
+            if (splits > k_tiles) break;
             const uint32_t each = (k_tiles + splits - 1) / splits, parts = (k_tiles + each - 1) / each;
-            if (parts > 1 && (uint64_t)tiles * parts * z.side * z.side * 4u > room) break;
-            const double rounds = (double)((tiles * (uint64_t)parts + slots - 1) / slots);
-            const double rate = t == kTile256 ? 1.0 : t == kTile128 ? 0.8 : 0.5;
-            const double work = (double)z.side * z.side / 65536.0 * z.resident / rate;
-            double cost = rounds * (work * each + 2.0);
-            if (parts > 1) cost += 6.0 + (double)tiles * parts * z.side * z.side / 65536.0 / cus;
-            if (!best.splits || cost < least) {
-                best = Plan{t, parts, each};
-                least = cost;
-            }
+            const double bytes = (double)tiles * parts * c.side * c.side * 4.0;
+            if (parts > 1 && bytes > (double)room) break;
+            const double there = (double)((tiles * parts + cus - 1) / cus), step = c.shared[wide] * there;
+            double cost = c.launch + c.tile * there + each * (step > c.step[wide] ? step : c.step[wide]);
+            if (parts > 1) cost += kJoinLaunch + 2.0 * bytes / kJoinRate;
+            if (!best.splits || cost < best.cost) best = Plan{t, parts, each, cost};
+        }
+    }
+    return best;
+}
+
+static RowPlan plan_product(const ProductSize &z, bool cut, uint32_t type, uint32_t cus, size_t room)
+{
+    RowPlan best{z.M, plan_rows(z, z.M, type, cus, room), Plan{}};
+    if (!cut) return best;
+    for (uint32_t side : {256u, 128u, 64u}) {
+        // as many rows of tiles as fill the CUs to the last, or as are whole
+        const uint64_t across = tiles_of(z, side, side), all = z.M / side, rounds = all * across / cus;
+        for (uint64_t down : {rounds * cus / across, all}) {
+            const uint32_t rows = (uint32_t)(down * side);
+            if (!rows || rows >= z.M) continue;
+            const Plan main = plan_rows(z, rows, type, cus, room), rest = plan_rows(z, z.M - rows, type, cus, room);
+            if (main.cost + rest.cost < best.main.cost + best.rest.cost) best = RowPlan{rows, main, rest};
         }
     }
     return best;
@@ -56,14 +76,13 @@ static void launch_tiling(const ProductArgs &a, hipStream_t st)
     typedef Tiling<T, KIND, BM, BN, WM, WN> L;
     hipLaunchKernelGGL((product_kernel<T, KIND, BM, BN, WM, WN>), dim3(a.tiles * a.splits), dim3(L::kThreads), 0, st, a);
     if (a.splits > 1)
-        hipLaunchKernelGGL((join_kernel<T, KIND, BM, BN, WM, WN>), dim3(a.tiles, L::MB * L::kNeed), dim3(L::kThreads), 0, st, a);
+        hipLaunchKernelGGL((join_kernel<T, KIND, BM, BN, WM, WN>), dim3(a.tiles, L::MB * L::kGroups), dim3(L::kThreads), 0, st, a);
 }
 
 template <typename T, int KIND>
-static void launch_product(ProductArgs &a, uint32_t type, int cus, float *part, size_t room, hipStream_t st)
+static void launch_planned(ProductArgs &a, const Plan &plan, hipStream_t st)
 {
-    const Plan plan = plan_product(a, KIND, type, cus, room);
-    const uint32_t side = kSizes[plan.tiling].side, columns = KIND == kGate ? side / 2u : side;
+    const uint32_t side = kCosts[plan.tiling].side, columns = KIND == kGate ? side / 2u : side;
     a.tiles = 0;
     for (uint32_t i = 0; i < a.products; ++i) {
         Product &p = a.p[i];
@@ -74,10 +93,58 @@ static void launch_product(ProductArgs &a, uint32_t type, int cus, float *part, 
     }
     a.splits = plan.splits;
     a.each = plan.each;
-    a.part = part;
-    if (plan.tiling == kTile256) launch_tiling<T, KIND, 256, 256, 2, 4>(a, st);
-    else if (plan.tiling == kTile128) launch_tiling<T, KIND, 128, 128, 2, 2>(a, st);
-    else launch_tiling<T, KIND, 64, 64, 2, 2>(a, st);
+    // both projections of kGate: 64 columns of each to a wave (32 of 64 x 64), whole lines of the results
+    if constexpr (sizeof(T) == 2) {
+        if (plan.tiling == kTile256) {
+            if constexpr (KIND == kGate) launch_tiling<T, KIND, 256, 256, 4, 2>(a, st);
+            else launch_tiling<T, KIND, 256, 256, 2, 4>(a, st);
+            return;
+        }
+    }
+    if (plan.tiling == kTile128) {
+        if constexpr (KIND == kGate) launch_tiling<T, KIND, 128, 128, 4, 1>(a, st);
+        else launch_tiling<T, KIND, 128, 128, 2, 2>(a, st);
+    } else {
+        if constexpr (KIND == kGate) launch_tiling<T, KIND, 64, 64, 4, 1>(a, st);
+        else launch_tiling<T, KIND, 64, 64, 2, 2>(a, st);
+    }
+}
+
+// The product's rows from `first` on.
+template <typename T, int KIND>
+static void skip_rows(ProductArgs &a, uint32_t first)
+{
+    Product &p = a.p[0];
+    auto on = [&](const void *q, uint64_t stride) { return q ? (void *)((T *)q + first * stride) : nullptr; };
+    for (int i = 0; i < 2; ++i) p.a.p[i] = on(p.a.p[i], p.a.stride[i]);
+    p.out = on(p.out, p.out_stride);
+    if (KIND == kGate) p.out2 = on(p.out2, 2ull * p.N);
+    if (KIND == kBack) {
+        p.in = on(p.in, 2ull * p.N);
+        p.out2 = on(p.out2, p.out_stride);
+        p.out3 = on(p.out3, p.out_stride);
+    } else {
+        p.in = on(p.in, p.in_stride);
+    }
+    a.first_row = first;
+    p.M -= first;
+}
+
+template <typename T, int KIND>
+static void launch_product(ProductArgs &a, const RowPlan &plan, hipStream_t st)
+{
+    if constexpr (KIND == kWeights) {
+        launch_planned<T, KIND>(a, plan.main, st);
+    } else {
+        const uint32_t M = a.p[0].M;
+        a.first_row = 0;
+        a.p[0].M = plan.rows;
+        launch_planned<T, KIND>(a, plan.main, st);
+        if (plan.rows == M) return;
+        a.p[0].M = M;
+        skip_rows<T, KIND>(a, plan.rows);
+        launch_planned<T, KIND>(a, plan.rest, st);
+    }
 }
 
 __global__ __launch_bounds__(256) void clear_kernel(uint32_t *to, uint64_t words)
@@ -99,6 +166,8 @@ struct ecrm_ffn {
     uint64_t gate_stride, up_stride, down_stride;
     char *work;
     int cus;
+    uint64_t planned[2];                  // rows that the plans are for: of the forward pass, of the backward pass
+    RowPlan plan[kKinds];
 };
 
 namespace {
@@ -106,6 +175,14 @@ namespace {
 constexpr uint64_t kStrideMost = 1u << 20;
 
 struct Rows { const void *p; uint64_t rows, cols, stride; };     // elements
+
+// Rows of the workspace: no power of two apart, or a tile's rows lie behind one another in the same channel of a cache (16384 x 4096 x
+// 4096 in bf16 with both operands' rows 8 KB apart 437-466 us, with 8.375 KB 416; 8.125 KB lies between).
+uint64_t pitch_of(uint64_t elements, uint64_t size)
+{
+    const uint64_t bytes = elements * size;
+    return ((bytes <= 384 ? 0 : (bytes - 384 + 511) / 512 * 512) + 384) / size;
+}
 
 bool rows_fit(const ecrm_ffn *f, const Rows &r)
 {
@@ -142,6 +219,23 @@ Product product(const void *a, uint64_t a_stride, const void *b, uint64_t b_stri
     return p;
 }
 
+// The plans of a pass over n rows: kept while n stays, since making them takes a few us.
+void make_plans(ecrm_ffn *f, bool backward, uint32_t n)
+{
+    if (f->planned[backward] == n) return;
+    const uint32_t D = f->cfg.dim, F = f->cfg.hidden, type = f->cfg.type, cus = (uint32_t)f->cus;
+    auto plan = [&](int kind, ProductSize z) { f->plan[kind] = plan_product(z, kind != kWeights, type, cus, f->part_bytes); };
+    if (!backward) {
+        plan(kGate, ProductSize{n, F, D, 1, 1, true});
+        plan(kOut, ProductSize{n, D, F, 1, 1, false});
+    } else {
+        plan(kBack, ProductSize{n, F, D, 1, 1, false});
+        plan(kInput, ProductSize{n, D, F, 2, 1, false});
+        plan(kWeights, ProductSize{F, D, n, 1, 3, false});
+    }
+    f->planned[backward] = n;
+}
+
 }  // namespace
 
 extern "C" {
@@ -158,8 +252,8 @@ int ecrm_ffn_create(const ecrm_ffn_config *cfg, ecrm_ffn **out)
     memset(f, 0, sizeof(*f));
     f->cfg = *cfg;
     const uint64_t size = type_bytes(cfg->type), D = cfg->dim, F = cfg->hidden;
-    f->pitch = (F + 63) / 64 * 64;
-    f->e_pitch = (D + 63) / 64 * 64;
+    f->pitch = pitch_of(F, size);
+    f->e_pitch = pitch_of(D, size);
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off = (off + bytes + 255) / 256 * 256; return o; };
     f->off_h = take(cfg->max_rows * f->pitch * size);
@@ -197,6 +291,7 @@ int ecrm_ffn_bind(ecrm_ffn *f, const void *gate, uint64_t gate_stride, const voi
     f->gate_stride = gate_stride; f->up_stride = up_stride; f->down_stride = down_stride;
     f->work = (char *)work;
     f->cus = cus;
+    f->planned[0] = f->planned[1] = 0;
     return ECRM_OK;
 }
 
@@ -223,7 +318,8 @@ int ecrm_ffn_forward(ecrm_ffn *f, const void *x, uint64_t x_stride, uint64_t n, 
         return ECRM_EINVAL;
     hipStream_t st = (hipStream_t)stream;
     void *h = f->work + f->off_h;
-    float *part = (float *)(f->work + f->off_part);
+    a.part = (float *)(f->work + f->off_part);
+    make_plans(f, false, N);
     a.activation = f->cfg.activation;
     a.products = 1;
     with_type(type, [&](auto t) {
@@ -234,14 +330,14 @@ int ecrm_ffn_forward(ecrm_ffn *f, const void *x, uint64_t x_stride, uint64_t n, 
         a.p[0].out = h;
         a.p[0].out_stride = f->pitch;
         a.p[0].out2 = saved;
-        launch_product<T, kGate>(a, type, f->cus, part, f->part_bytes, st);
+        launch_product<T, kGate>(a, f->plan[kGate], st);
         a.p[0] = product(h, f->pitch, f->down, f->down_stride, N, D, F);
         a.p[0].out = out;
         a.p[0].out_stride = out_stride;
         a.p[0].in = residual;
         a.p[0].in_stride = residual_stride;
         a.masked = mask ? 1u : 0u;
-        launch_product<T, kOut>(a, type, f->cus, part, f->part_bytes, st);
+        launch_product<T, kOut>(a, f->plan[kOut], st);
     });
     return launched();
 }
@@ -293,7 +389,7 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
     if (!weights && !d_x) return ECRM_OK;
 
     void *h = f->work + f->off_h, *dg = f->work + f->off_dg, *du = f->work + f->off_du;
-    float *part = (float *)(f->work + f->off_part);
+    a.part = (float *)(f->work + f->off_part);
     const void *e = d_out;
     uint64_t e_stride = d_out_stride;
     if (mask) {
@@ -302,6 +398,7 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
         const int rc = ecrm_dropout(mask, d_out, d_out_stride, nullptr, 0, (void *)e, e_stride, type, n, D, stream);
         if (rc != ECRM_OK) return rc;
     }
+    make_plans(f, true, N);
     a.activation = f->cfg.activation;
     a.accumulate = accumulate ? 1u : 0u;
     a.wide = weight_type == ECRM_F32 ? 1u : 0u;
@@ -314,7 +411,7 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
         a.p[0].out2 = du;
         a.p[0].out3 = h;
         a.p[0].out_stride = f->pitch;
-        launch_product<T, kBack>(a, type, f->cus, part, f->part_bytes, st);
+        launch_product<T, kBack>(a, f->plan[kBack], st);
         if (weights) {
             a.products = 3;
             a.p[0] = product(dg, f->pitch, x, x_stride, F, D, N);
@@ -326,7 +423,7 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
             a.p[2] = product(e, e_stride, h, f->pitch, D, F, N);
             a.p[2].out = d_down;
             a.p[2].out_stride = F;
-            launch_product<T, kWeights>(a, type, f->cus, part, f->part_bytes, st);
+            launch_product<T, kWeights>(a, f->plan[kWeights], st);
         }
         if (d_x) {                        // last: it may take the place of d_out
             a.products = 1;
@@ -338,7 +435,7 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
             a.p[0].in_stride = add_stride;
             a.p[0].out = d_x;
             a.p[0].out_stride = d_x_stride;
-            launch_product<T, kInput>(a, type, f->cus, part, f->part_bytes, st);
+            launch_product<T, kInput>(a, f->plan[kInput], st);
         }
     });
     return launched();

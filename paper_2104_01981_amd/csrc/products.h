@@ -14,8 +14,8 @@
 // upper half of a chunk that K ends in the middle of (K % 8 == 4, 16 bits) is cleared in LDS.  Both operands, since
 // zero times what is not finite is not zero.
 //
-// The results' 16 x 16 blocks are held transposed (weights are the first operand of the instruction): a lane has four consecutive
-// columns of a row.
+// The results' 16 x 16 blocks are held transposed (b is the first operand of the instruction): a lane has four consecutive columns of
+// a row.  Of 16-bit results two blocks make a pair, the columns dealt out to them by fours, so that a lane has eight: 16 bytes to an access.
 #pragma once
 
 #include "mask.h"
@@ -23,7 +23,6 @@
 namespace ecrm {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef __amdgpu_buffer_rsrc_t rsrc_t;
 typedef __attribute__((address_space(3))) char lds_t;
 
 // What becomes of a product.
@@ -59,7 +58,7 @@ struct ProductArgs {
     uint32_t splits, each;             // K tiles: cut into so many parts of at most so many
     float *part;                       // [tiles][splits][threads][..] where there are several
     uint32_t activation;
-    uint32_t masked;
+    uint32_t masked, first_row;        // row of the mask that row 0 of the results has
     MaskArgs mask;
     uint32_t accumulate, wide;         // kWeights: added to; in 32 bits whatever the type
 };
@@ -96,9 +95,35 @@ struct Fragment<float> {
 constexpr uint32_t kRowBytes = 128;              // of K, in a tile
 constexpr uint32_t kOutside = 0x7FFFFFFFu;       // an offset behind any operand's end
 
+// A value that is the same for the wave, in scalar registers: what a division gives lies in vector registers, and a load whose descriptor
+// or LDS address does would be made lane by lane.
+__device__ __forceinline__ uint32_t scalar(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+
+__device__ __forceinline__ const char *scalar(const char *p)
+{
+    return (const char *)((uint64_t)scalar((uint32_t)((uint64_t)p >> 32)) << 32 | scalar((uint32_t)(uint64_t)p));
+}
+
+// 64 lanes' 16 bytes each from a buffer (zeros behind its end) to the 1 KB of LDS at `to` + `behind`.  Written out because the compiler, which does not
+// tell the tiles' two halves apart where fragments are read transposed, waits for the load before the next such read (kInput with
+// K = 4096: 980 TFLOP/s that way, 1310 so).  Nothing but a wait for all loads and a barrier may come before the tile is read.
+__device__ __forceinline__ void load_to_lds(u32x4 buffer, uint32_t at, uint32_t from, uint32_t to, uint32_t behind)
+{
+    asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds"
+                 :: "s"(to), "i"(behind), "v"(at), "s"(buffer), "s"(from) : "memory", "scc");
+}
+__device__ __forceinline__ u32x4 buffer_of(const char *base, uint32_t bytes)
+{
+    return u32x4{(uint32_t)(uint64_t)base, (uint32_t)((uint64_t)base >> 32), bytes, 0x00020000u};
+}
+
 // ---- from memory to LDS ----------------------------------------------------------------------------------------------------------
+// Where two blocks of 16 columns lie in pairs, so that a lane's four results of either are eight consecutive ones: the column that row
+// r of the operand's tile is.
+__device__ __forceinline__ uint32_t column_of(uint32_t r) { return (r & ~31u) | (r >> 2 & 3u) << 3 | (r >> 4 & 1u) << 2 | (r & 3u); }
+
 // The part of a tile of ROWS rows (or columns) that a wave loads.
-template <typename T, bool COLUMNS, int ROWS, int WAVES>
+template <typename T, bool COLUMNS, int ROWS, int WAVES, bool PAIRS>
 struct Loader {
     static constexpr uint32_t kLoads = ROWS * kRowBytes / 1024 / WAVES, kElements = kRowBytes / sizeof(T);
     static_assert(kLoads >= 1 && ROWS * kRowBytes % (1024 * WAVES) == 0, "whole loads of a wave");
@@ -114,18 +139,19 @@ struct Loader {
         K = k;
         stride = (uint32_t)(elements * sizeof(T));
         if (!COLUMNS) {
-            base = (const char *)p + (uint64_t)first * stride;
+            base = scalar((const char *)p + (uint64_t)first * stride);
             const uint32_t rows = count > first ? min(count - first, (uint32_t)ROWS) : 0u;
-            end = rows ? (rows - 1u) * stride + K * (uint32_t)sizeof(T) : 0u;
+            end = scalar(rows ? (rows - 1u) * stride + K * (uint32_t)sizeof(T) : 0u);
 #pragma unroll
             for (uint32_t i = 0; i < kLoads; ++i) {
                 const uint32_t j = load + i, chunk = (lane % 8u) ^ ((lane / 16u) | (j & 1u) << 2);
-                at[i] = ((j - row0) * 8u + lane / 8u) * stride + chunk * 16u;
+                const uint32_t row = (j - row0) * 8u + lane / 8u;
+                at[i] = (PAIRS ? column_of(row) : row) * stride + chunk * 16u;
             }
         } else {
             constexpr uint32_t kBytes = ROWS * sizeof(T);
-            base = (const char *)p + (uint64_t)first * sizeof(T);
-            end = (count > first ? count - first : 0u) * (uint32_t)sizeof(T);
+            base = scalar((const char *)p + (uint64_t)first * sizeof(T));
+            end = scalar((count > first ? count - first : 0u) * (uint32_t)sizeof(T));
 #pragma unroll
             for (uint32_t i = 0; i < kLoads; ++i) {
                 const uint32_t byte = (load + i) * 1024u + lane * 16u, row = byte / kBytes, chunk = byte % kBytes / 16u;
@@ -135,29 +161,29 @@ struct Loader {
         }
     }
 
-    // K from k0 on, into the tile at `to`
-    __device__ __forceinline__ void issue(uint32_t k0, char *to, uint32_t load) const
+    // K from k0 on, into the tile at `tile`
+    __device__ __forceinline__ void issue(uint32_t k0, const char *tile, uint32_t load) const
     {
-        const uint32_t lane = lane_id();
-        const uint32_t left = K - k0;            // more than 0
+        const uint32_t lane = lane_id(), left = K - k0;  // more than 0
+        const uint32_t to = scalar((uint32_t)(uintptr_t)(lds_t *)tile + load * 1024u);
         if (!COLUMNS) {
-            const rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)end, 0x00020000);
+            const u32x4 buffer = buffer_of(base, end);
+            const uint32_t from = scalar(k0 * (uint32_t)sizeof(T));
+            if (left >= kElements) {
 #pragma unroll
-            for (uint32_t i = 0; i < kLoads; ++i) {
-                uint32_t from = at[i];
-                if (left < kElements) {
+                for (uint32_t i = 0; i < kLoads; ++i) load_to_lds(buffer, at[i], from, to, i * 1024u);
+            } else {
+#pragma unroll
+                for (uint32_t i = 0; i < kLoads; ++i) {
                     const uint32_t chunk = (lane % 8u) ^ ((lane / 16u) | ((load + i) & 1u) << 2);
-                    if (chunk * (16u / (uint32_t)sizeof(T)) >= left) from = kOutside;
+                    load_to_lds(buffer, chunk * (16u / (uint32_t)sizeof(T)) >= left ? kOutside : at[i], from, to, i * 1024u);
                 }
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_t *)(to + (load + i) * 1024u), 16, (int)from,
-                                                         (int)(k0 * (uint32_t)sizeof(T)), 0, 0);
             }
         } else {
-            const uint32_t rows = min(left, kElements), bytes = end ? (rows - 1u) * stride + end : 0u;
-            const rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)(base + (uint64_t)k0 * stride), 0, (int)bytes, 0x00020000);
+            const uint32_t rows = min(left, kElements);
+            const u32x4 buffer = buffer_of(scalar(base + (uint64_t)k0 * stride), scalar(end ? (rows - 1u) * stride + end : 0u));
 #pragma unroll
-            for (uint32_t i = 0; i < kLoads; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_t *)(to + (load + i) * 1024u), 16, (int)at[i], 0, 0, 0);
+            for (uint32_t i = 0; i < kLoads; ++i) load_to_lds(buffer, at[i], 0u, to, i * 1024u);
         }
     }
 };
@@ -172,7 +198,7 @@ __device__ __forceinline__ void clear_behind(char *tile, uint32_t left, uint32_t
 
 // ---- from LDS to registers -------------------------------------------------------------------------------------------------------
 // Fragments of the tile's 16-row blocks first .. first + N - 1, of half `s` of its K.
-template <typename T, bool COLUMNS, int ROWS, int N>
+template <typename T, bool COLUMNS, int ROWS, bool PAIRS, int N>
 __device__ __forceinline__ void read_fragments(const char *tile, uint32_t first, uint32_t s, u32x4 (&f)[N])
 {
     const uint32_t lane = lane_id(), i = lane % 16u, q = lane / 16u;
@@ -187,7 +213,9 @@ __device__ __forceinline__ void read_fragments(const char *tile, uint32_t first,
         const uint32_t row = s * 32u + q * 8u + i / 4u, by = ((i / 4u) | (q & 1u) << 2) & (kBytes / 32u - 1u);
 #pragma unroll
         for (int b = 0; b < N; ++b) {
-            const char *p = tile + row * kBytes + (((first + b) ^ by) * 32u) + (i % 4u) * 8u;
+            const uint32_t block = first + b;
+            const uint32_t chunk = PAIRS ? (block & ~1u) + i % 4u / 2u : block, in = PAIRS ? i % 2u * 16u + (block & 1u) * 8u : i % 4u * 8u;
+            const char *p = tile + row * kBytes + (chunk ^ by) * 32u + in;
             const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(p + 4u * kBytes));
             const uint2 x = __builtin_bit_cast(uint2, lo), y = __builtin_bit_cast(uint2, hi);
             f[b] = u32x4{x.x, x.y, y.x, y.y};
@@ -225,15 +253,15 @@ __device__ __forceinline__ float normal(float g, float &density)
     const float tail = 0.5f * poly * density;            // of the side g is on
     return g < 0.f ? tail : 1.0f - tail;
 }
-template <typename T>
-__device__ __forceinline__ float activation(uint32_t kind, float g, float &slope)
+template <typename T, uint32_t ACT>
+__device__ __forceinline__ float activation(float g, float &slope)
 {
-    if (kind == ECRM_SILU) {
+    if (ACT == ECRM_SILU) {
         const float q = logistic<T>(g);
         slope = q * (1.0f + g * (1.0f - q));
         return g * q;
     }
-    if (kind == ECRM_GELU) {
+    if (ACT == ECRM_GELU) {
         float density;
         const float q = normal<T>(g, density);
         slope = q + g * density * 0.39894228f;
@@ -243,59 +271,137 @@ __device__ __forceinline__ float activation(uint32_t kind, float g, float &slope
     return g > 0.f ? g : g != g ? g : 0.f;
 }
 
-// v: results (row, col .. col + 3); kGate: of the gate, w those of the up projection
-template <typename T, int KIND>
-__device__ __forceinline__ void finish(const ProductArgs &a, const Product &p, const MaskKey &mask, uint32_t row, uint32_t col, f32x4 v, f32x4 w)
+template <uint32_t V>
+struct Constant { static constexpr uint32_t value = V; };
+// f(Constant<activation>()): one branch for all that f does
+template <typename F>
+__device__ __forceinline__ void with_activation(uint32_t kind, F f)
 {
-    typedef typename Quad<T>::type Four;
-    if (row >= p.M || col >= p.N) return;
-    if (KIND == kGate) {
-        if (p.out2) {
-            T *s = (T *)p.out2 + (uint64_t)row * 2u * p.N + col;
-            *(Four *)s = round4<T>(v);
-            *(Four *)(s + p.N) = round4<T>(w);
-        }
-        f32x4 h;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float slope;
-            h[i] = activation<T>(a.activation, v[i], slope) * w[i];
-        }
-        *(Four *)((T *)p.out + (uint64_t)row * p.out_stride + col) = round4<T>(h);
-    } else if (KIND == kOut) {
-        if (a.masked) v = drop4(v, mask_quad(mask, row, col), mask);
-        if (p.in) v += widen4<T>(*(const Four *)((const T *)p.in + (uint64_t)row * p.in_stride + col));
-        *(Four *)((T *)p.out + (uint64_t)row * p.out_stride + col) = round4<T>(v);
-    } else if (KIND == kBack) {
-        const T *s = (const T *)p.in + (uint64_t)row * 2u * p.N + col;
-        const f32x4 g = widen4<T>(*(const Four *)s), u = widen4<T>(*(const Four *)(s + p.N));
-        f32x4 dg, du, h;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float slope;
-            const float x = activation<T>(a.activation, g[i], slope);
-            dg[i] = v[i] * u[i] * slope;
-            du[i] = v[i] * x;
-            h[i] = x * u[i];
-        }
-        const uint64_t to = (uint64_t)row * p.out_stride + col;
-        *(Four *)((T *)p.out + to) = round4<T>(dg);
-        *(Four *)((T *)p.out2 + to) = round4<T>(du);
-        *(Four *)((T *)p.out3 + to) = round4<T>(h);
-    } else if (KIND == kInput) {
-        if (p.in) v += widen4<T>(*(const Four *)((const T *)p.in + (uint64_t)row * p.in_stride + col));
-        *(Four *)((T *)p.out + (uint64_t)row * p.out_stride + col) = round4<T>(v);
-    } else {
-        const uint64_t at = (uint64_t)row * p.out_stride + col;
-        if (a.wide) {
-            f32x4 *to = (f32x4 *)((float *)p.out + at);
-            if (a.accumulate) v += *to;
-            *to = v;
+    if (kind == ECRM_SILU) f(Constant<ECRM_SILU>());
+    else if (kind == ECRM_GELU) f(Constant<ECRM_GELU>());
+    else f(Constant<ECRM_RELU>());
+}
+
+// 16 bytes of a row: eight consecutive elements of 16 bits, four of 32, in `quads` fours of which there are 1 or 2 (16 bits), or none.
+template <typename T>
+struct Piece {
+    static constexpr int kQuads = 16 / (4 * sizeof(T));
+    typedef u32x4 Loose __attribute__((aligned(8)));     // elements are aligned by fours
+    static __device__ __forceinline__ u32x4 read(const T *p, uint32_t quads)
+    {
+        if (quads >= (uint32_t)kQuads) return *(const Loose *)p;
+        const uint2 half = quads ? *(const uint2 *)p : uint2{0u, 0u};
+        return u32x4{half.x, half.y, 0u, 0u};
+    }
+    static __device__ __forceinline__ void write(T *p, uint32_t quads, u32x4 v)
+    {
+        if (quads >= (uint32_t)kQuads) *(Loose *)p = v;
+        else if (quads) *(uint2 *)p = uint2{v.x, v.y};
+    }
+    static __device__ __forceinline__ void widen(u32x4 v, f32x4 (&to)[kQuads])
+    {
+        if constexpr (sizeof(T) == 4) {
+            to[0] = __builtin_bit_cast(f32x4, v);
         } else {
-            Four *to = (Four *)((T *)p.out + at);
-            if (a.accumulate) v += widen4<T>(*to);
-            *to = round4<T>(v);
+            to[0] = widen4<T>(__builtin_bit_cast(typename Quad<T>::type, uint2{v.x, v.y}));
+            to[1] = widen4<T>(__builtin_bit_cast(typename Quad<T>::type, uint2{v.z, v.w}));
         }
+    }
+    static __device__ __forceinline__ u32x4 round(const f32x4 (&v)[kQuads])
+    {
+        if constexpr (sizeof(T) == 4) {
+            return __builtin_bit_cast(u32x4, v[0]);
+        } else {
+            const uint2 a = __builtin_bit_cast(uint2, round4<T>(v[0])), b = __builtin_bit_cast(uint2, round4<T>(v[1]));
+            return u32x4{a.x, a.y, b.x, b.y};
+        }
+    }
+};
+
+// Lanes l and l ^ 8 exchange: where a is a lane's 16 bytes of its row in one run of 64 bytes (of four lanes 16 apart), b those in the
+// next run, then afterwards a is of row l % 8, b of row l % 8 + 8, both in the first run for l % 16 < 8 and in the second for others: eight
+// rows of 128 bytes to an access instead of 16 of 64, whole lines.  And back.
+__device__ __forceinline__ void exchange(u32x4 &a, u32x4 &b)
+{
+    const bool upper = threadIdx.x & 8u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t give = upper ? a[i] : b[i];
+        const uint32_t got = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)give, 0x128, 0xF, 0xF, true);      // eight lanes on, of 16
+        a[i] = upper ? got : a[i];
+        b[i] = upper ? b[i] : got;
+    }
+}
+
+// What a lane reads for a piece of the results, and writes.
+enum { kReads = 2, kWrites = 3 };
+
+// A piece's results v (kGate: of the gate, w those of the up projection) with what was read, to what is written.
+template <typename T, int KIND>
+__device__ __forceinline__ void finish(const ProductArgs &a, const Product &p, const MaskKey &mask, uint32_t row, uint32_t col,
+                                       f32x4 (&v)[Piece<T>::kQuads], const f32x4 (&w)[Piece<T>::kQuads], const u32x4 (&in)[kReads],
+                                       u32x4 (&out)[kWrites])
+{
+    constexpr int W = Piece<T>::kQuads;
+    if (KIND == kGate) {
+        out[1] = Piece<T>::round(v);
+        out[2] = Piece<T>::round(w);
+        with_activation(a.activation, [&](auto act) {
+#pragma unroll
+            for (int q = 0; q < W; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float slope;
+                    v[q][i] = activation<T, decltype(act)::value>(v[q][i], slope) * w[q][i];
+                }
+        });
+        out[0] = Piece<T>::round(v);
+    } else if (KIND == kBack) {
+        f32x4 g[W], u[W], du[W];
+        Piece<T>::widen(in[0], g);
+        Piece<T>::widen(in[1], u);
+        with_activation(a.activation, [&](auto act) {
+#pragma unroll
+            for (int q = 0; q < W; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float slope;
+                    const float x = activation<T, decltype(act)::value>(g[q][i], slope);
+                    du[q][i] = v[q][i] * x;
+                    v[q][i] *= u[q][i] * slope;
+                    u[q][i] *= x;
+                }
+        });
+        out[0] = Piece<T>::round(v);
+        out[1] = Piece<T>::round(du);
+        out[2] = Piece<T>::round(u);
+    } else {
+        if (KIND == kOut && a.masked) {
+            const uint4 bits = mask_block(mask, a.first_row + row, col / 8u);
+            const bool upper = W == 1 && (col & 4u);
+            v[0] = drop4(v[0], upper ? uint2{bits.z, bits.w} : uint2{bits.x, bits.y}, mask);
+            if (W == 2) v[W - 1] = drop4(v[W - 1], uint2{bits.z, bits.w}, mask);
+        }
+        if (KIND == kWeights ? a.accumulate != 0u : p.in != nullptr) {
+            f32x4 more[W];
+            Piece<T>::widen(in[0], more);
+#pragma unroll
+            for (int q = 0; q < W; ++q) v[q] += more[q];
+        }
+        out[0] = Piece<T>::round(v);
+    }
+}
+
+// kWeights, results in 32 bits of operands in 16
+template <int W>
+__device__ __forceinline__ void write_wide(const ProductArgs &a, const Product &p, uint32_t row, uint32_t col, f32x4 (&v)[W])
+{
+    float *to = (float *)p.out + (uint64_t)row * p.out_stride + col;
+#pragma unroll
+    for (uint32_t q = 0; q < (uint32_t)W; ++q) {
+        if (row >= p.M || col + q * 4u >= p.N) break;
+        if (a.accumulate) v[q] += *(const f32x4 *)(to + q * 4u);
+        *(f32x4 *)(to + q * 4u) = v[q];
     }
 }
 
@@ -306,10 +412,10 @@ __device__ __forceinline__ uint32_t find_tile(const ProductArgs &a, uint32_t til
     if (a.products > 1 && tile >= a.first[1]) which = 1;
     if (a.products > 2 && tile >= a.first[2]) which = 2;
     const Product &p = a.p[which];
-    const uint32_t t = tile - a.first[which], group = 8u * p.tiles_n, g = t / group, in = t - g * group;
+    const uint32_t t = tile - a.first[which], group = 8u * p.tiles_n, g = scalar(t / group), in = t - g * group;
     const uint32_t rows = min(8u, p.tiles_m - g * 8u);
-    n = in / rows;
-    m = g * 8u + in - n * rows;
+    n = scalar(in / rows);
+    m = scalar(g * 8u + in - n * rows);
     return which;
 }
 
@@ -320,34 +426,113 @@ struct Tiling {
     static constexpr int kWaves = WM * WN, kThreads = kWaves * kWave;
     static constexpr int MB = BM / WM / 16, NB = BN / WN / 16, kNeed = kDual ? NB / 2 : NB;
     static constexpr uint32_t kColumns = kDual ? BN / 2 : BN, kElements = kRowBytes / sizeof(T);
-    static __device__ __forceinline__ void place(uint32_t m, uint32_t n, uint32_t tid, int mb, int nb, uint32_t &row, uint32_t &col)
+    // 16-bit results: two blocks of 16 columns in a pair, eight consecutive results to a lane.  A unit: the four lanes' 64 bytes of a row.
+    static constexpr int kPair = Piece<T>::kQuads, kUnits = kNeed / kPair, kTogether = kUnits % 2 ? 1 : 2, kGroups = kUnits / kTogether;
+    static_assert(kNeed % kPair == 0, "whole pairs");
+
+    // Of a lane: row and column of unit u of the wave's rows of blocks i.
+    static __device__ __forceinline__ void place(uint32_t m, uint32_t n, uint32_t i, uint32_t u, uint32_t &row, uint32_t &col)
     {
-        const uint32_t lane = tid % kWave, wave = tid / kWave, wm = wave / WN, wn = wave % WN;
-        row = m * BM + (wm * MB + mb) * 16u + lane % 16u;
-        col = n * kColumns + (wn * kNeed + nb) * 16u + lane / 16u * 4u;
+        const uint32_t lane = lane_id(), wave = scalar(threadIdx.x / kWave), wm = wave / WN, wn = wave % WN;
+        row = m * BM + (wm * MB + i) * 16u + lane % 16u;
+        col = n * kColumns + (wn * kNeed + u * kPair) * 16u + lane / 16u * 4u * kPair;
+    }
+    // Where the k-th of its pieces of group g lies in memory: as computed, or exchanged.
+    static __device__ __forceinline__ void place_line(uint32_t m, uint32_t n, uint32_t i, uint32_t g, uint32_t k, uint32_t &row, uint32_t &col)
+    {
+        const uint32_t lane = lane_id();
+        if (kTogether == 1) return place(m, n, i, g, row, col);
+        place(m, n, i, g * 2u + (lane >> 3 & 1u), row, col);
+        row = (row & ~15u) + (lane & 7u) + k * 8u;
+    }
+
+    struct In { u32x4 x[kTogether][kReads]; };
+    static __device__ __forceinline__ void fetch(const ProductArgs &a, const Product &p, uint32_t m, uint32_t n, uint32_t i, uint32_t g, In &in)
+    {
+        const bool any = KIND == kBack || ((KIND == kOut || KIND == kInput) && p.in) || (KIND == kWeights && a.accumulate && !a.wide);
+        if (!any) return;
+#pragma unroll
+        for (uint32_t k = 0; k < kTogether; ++k) {
+            uint32_t row, col;
+            place_line(m, n, i, g, k, row, col);
+            const uint32_t quads = row < p.M && col < p.N ? (p.N - col) / 4u : 0u;
+            if (KIND == kBack) {
+                const T *s = (const T *)p.in + (uint64_t)row * 2u * p.N + col;
+                in.x[k][0] = Piece<T>::read(s, quads);
+                in.x[k][1] = Piece<T>::read(s + p.N, quads);
+            } else if (KIND == kWeights) {
+                in.x[k][0] = Piece<T>::read((const T *)p.out + (uint64_t)row * p.out_stride + col, quads);
+            } else {
+                in.x[k][0] = Piece<T>::read((const T *)p.in + (uint64_t)row * p.in_stride + col, quads);
+            }
+        }
+    }
+    // The group's results: of(k, q) and of_up(k, q) are unit k's quad q.
+    template <typename F, typename G>
+    static __device__ __forceinline__ void finish_group(const ProductArgs &a, const Product &p, const MaskKey &mask, uint32_t m, uint32_t n, uint32_t i,
+                                                        uint32_t g, In &in, F of, G of_up)
+    {
+        constexpr int kIn = KIND == kBack ? 2 : KIND == kGate ? 0 : 1, kOuts = KIND == kBack || KIND == kGate ? 3 : 1;
+        u32x4 out[kTogether][kWrites];
+        if (kTogether == 2)
+#pragma unroll
+            for (int r = 0; r < kIn; ++r) exchange(in.x[0][r], in.x[kTogether - 1][r]);
+#pragma unroll
+        for (uint32_t k = 0; k < kTogether; ++k) {
+            uint32_t row, col;
+            place(m, n, i, g * kTogether + k, row, col);
+            f32x4 v[kPair], w[kPair];
+#pragma unroll
+            for (int q = 0; q < kPair; ++q) {
+                v[q] = of(k, q);
+                w[q] = of_up(k, q);
+            }
+            if (KIND == kWeights && a.wide) write_wide<kPair>(a, p, row, col, v);
+            else finish<T, KIND>(a, p, mask, row, col, v, w, in.x[k], out[k]);
+        }
+        if (KIND == kWeights && a.wide) return;
+        if (kTogether == 2)
+#pragma unroll
+            for (int r = 0; r < kOuts; ++r) exchange(out[0][r], out[kTogether - 1][r]);
+#pragma unroll
+        for (uint32_t k = 0; k < kTogether; ++k) {
+            uint32_t row, col;
+            place_line(m, n, i, g, k, row, col);
+            const uint32_t quads = row < p.M && col < p.N ? (p.N - col) / 4u : 0u;
+            const uint64_t at = (uint64_t)row * p.out_stride + col;
+            Piece<T>::write((T *)p.out + at, quads, out[k][0]);
+            if (KIND == kGate && p.out2) {
+                T *s = (T *)p.out2 + (uint64_t)row * 2u * p.N + col;
+                Piece<T>::write(s, quads, out[k][1]);
+                Piece<T>::write(s + p.N, quads, out[k][2]);
+            } else if (KIND == kBack) {
+                Piece<T>::write((T *)p.out2 + at, quads, out[k][1]);
+                Piece<T>::write((T *)p.out3 + at, quads, out[k][2]);
+            }
+        }
     }
 };
 
 template <typename T, int KIND, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM * WN * kWave) void product_kernel(ProductArgs a)
+__global__ __launch_bounds__(WM * WN * kWave, 2) void product_kernel(ProductArgs a)
 {
     typedef Tiling<T, KIND, BM, BN, WM, WN> L;
     constexpr int MB = L::MB, NB = L::NB, kWaves = L::kWaves;
     __shared__ __align__(1024) char s_a0[BM * kRowBytes], s_b0[BN * kRowBytes], s_a1[BM * kRowBytes], s_b1[BN * kRowBytes];
-    const uint32_t tid = threadIdx.x, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid / kWave)), wm = wave / WN, wn = wave % WN;
+    const uint32_t tid = threadIdx.x, wave = scalar(tid / kWave), wm = wave / WN, wn = wave % WN;
 
     // consecutive tiles on one XCD (workgroups go to the eight by turns), the parts of K one after the other
     const uint32_t all = a.tiles * a.splits, per = all / 8u, more = all % 8u, xcd = blockIdx.x % 8u;
     const uint32_t index = xcd * per + min(xcd, more) + blockIdx.x / 8u;
-    const uint32_t split = index / a.tiles, tile = index - split * a.tiles;
+    const uint32_t split = scalar(index / a.tiles), tile = index - split * a.tiles;
     uint32_t m, n;
     const Product &p = a.p[find_tile(a, tile, m, n)];
 
-    const uint32_t half_tiles = (p.K + L::kElements - 1u) / L::kElements, k_tiles = KIND == kInput ? 2u * half_tiles : half_tiles;
+    const uint32_t K = p.K, half_tiles = (K + L::kElements - 1u) / L::kElements, k_tiles = KIND == kInput ? 2u * half_tiles : half_tiles;
     const uint32_t begin = split * a.each, stop = min(begin + a.each, k_tiles);
 
-    typedef Loader<T, L::kColumnsA, BM, kWaves> LoadA;
-    typedef Loader<T, L::kColumnsB, BN, kWaves> LoadB;
+    typedef Loader<T, L::kColumnsA, BM, kWaves, false> LoadA;
+    typedef Loader<T, L::kColumnsB, BN, kWaves, L::kPair == 2> LoadB;
     LoadA la;
     LoadB lb;
     const uint32_t load_a = wave * LoadA::kLoads, load_b = wave * LoadB::kLoads;
@@ -387,8 +572,8 @@ __global__ __launch_bounds__(WM * WN * kWave) void product_kernel(ProductArgs a)
 #pragma unroll
         for (uint32_t s = 0; s < 2; ++s) {
             u32x4 fa[MB], fb[NB];
-            read_fragments<T, L::kColumnsA, BM, MB>(ta, wm * MB, s, fa);
-            read_fragments<T, L::kColumnsB, BN, NB>(tb, wn * NB, s, fb);
+            read_fragments<T, L::kColumnsA, BM, false, MB>(ta, wm * MB, s, fa);
+            read_fragments<T, L::kColumnsB, BN, L::kPair == 2, NB>(tb, wn * NB, s, fb);
 #pragma unroll
             for (int i = 0; i < MB; ++i)
 #pragma unroll
@@ -398,7 +583,7 @@ __global__ __launch_bounds__(WM * WN * kWave) void product_kernel(ProductArgs a)
     auto step = [&](uint32_t t, char *ta, char *tb, char *next_a, char *next_b) {
         __builtin_amdgcn_s_waitcnt(0);                   // this wave's part of the tile is there ...
         __syncthreads();                                 // ... and everybody's; nobody reads the other tile any more
-        const uint32_t left = p.K - (KIND == kInput && t >= half_tiles ? t - half_tiles : t) * L::kElements;
+        const uint32_t left = K - (KIND == kInput && t >= half_tiles ? t - half_tiles : t) * L::kElements;
         if (sizeof(T) == 2 && !(L::kColumnsA && L::kColumnsB) && left < L::kElements && left % 8u) {
             if (!L::kColumnsA) clear_behind<BM, L::kThreads>(ta, left, tid);
             if (!L::kColumnsB) clear_behind<BN, L::kThreads>(tb, left, tid);
@@ -423,36 +608,52 @@ __global__ __launch_bounds__(WM * WN * kWave) void product_kernel(ProductArgs a)
     }
     MaskKey mask{};
     if (KIND == kOut && a.masked) mask = mask_key(a.mask);
+    // What the next rows' results are finished with is on its way: a store could change it for all the compiler knows, which would wait
+    // for one block's after the other (kBack 16384 x 4096, K = 1024: 497 us; one row of blocks ahead 303).
+    constexpr uint32_t G = L::kGroups;
+    typename L::In in[2][G];
 #pragma unroll
-    for (int i = 0; i < MB; ++i)
+    for (uint32_t g = 0; g < G; ++g) L::fetch(a, p, m, n, 0u, g, in[0][g]);
 #pragma unroll
-        for (int j = 0; j < L::kNeed; ++j) {
-            uint32_t row, col;
-            L::place(m, n, tid, i, j, row, col);
-            finish<T, KIND>(a, p, mask, row, col, acc[i][j], acc[i][(j + L::kNeed) % NB]);
-        }
+    for (uint32_t i = 0; i < MB; ++i) {
+        if (i + 1u < MB)
+#pragma unroll
+            for (uint32_t g = 0; g < G; ++g) L::fetch(a, p, m, n, i + 1u, g, in[(i + 1u) % 2u][g]);
+#pragma unroll
+        for (uint32_t g = 0; g < G; ++g)
+            L::finish_group(a, p, mask, m, n, i, g, in[i % 2u][g],
+                            [&](uint32_t k, int q) { return acc[i][(g * L::kTogether + k) * L::kPair + q]; },
+                            [&](uint32_t k, int q) { return acc[i][((g * L::kTogether + k) * L::kPair + q + L::kNeed) % NB]; });
+    }
 }
 
-// Adds up what the parts of K gave, in order; a workgroup has one block of each of a tile's waves.
+// Adds up what the parts of K gave, in order; a workgroup has a group of each of a tile's waves.
 template <typename T, int KIND, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM * WN * kWave) void join_kernel(ProductArgs a)
 {
     typedef Tiling<T, KIND, BM, BN, WM, WN> L;
-    constexpr int NB = L::NB, MB = L::MB;
-    const uint32_t tile = blockIdx.x, tid = threadIdx.x, i = blockIdx.y / L::kNeed, j = blockIdx.y % L::kNeed;
-    uint32_t m, n, row, col;
+    constexpr uint32_t NB = L::NB, MB = L::MB, W = L::kPair, N = L::kTogether * W;
+    const uint32_t tile = blockIdx.x, i = blockIdx.y / L::kGroups, g = blockIdx.y % L::kGroups;
+    uint32_t m, n;
     const Product &p = a.p[find_tile(a, tile, m, n)];
-    const f32x4 *from = (const f32x4 *)a.part + (uint64_t)tile * a.splits * (MB * NB * L::kThreads) + (i * NB + j) * L::kThreads + tid;
-    f32x4 v = {0.f, 0.f, 0.f, 0.f}, w = v;
+    const f32x4 *from = (const f32x4 *)a.part + (uint64_t)tile * a.splits * (MB * NB * L::kThreads) + (i * NB + g * N) * L::kThreads + threadIdx.x;
+    typename L::In in;
+    L::fetch(a, p, m, n, i, g, in);
+    f32x4 v[N], w[N];
+#pragma unroll
+    for (uint32_t q = 0; q < N; ++q) v[q] = w[q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (uint32_t s = 0; s < a.splits; ++s) {
-        v += from[(uint64_t)s * (MB * NB * L::kThreads)];
-        if (L::kDual) w += from[(uint64_t)s * (MB * NB * L::kThreads) + L::kNeed * L::kThreads];
+        const f32x4 *part = from + (uint64_t)s * (MB * NB * L::kThreads);
+#pragma unroll
+        for (uint32_t q = 0; q < N; ++q) {
+            v[q] += part[q * L::kThreads];
+            if (L::kDual) w[q] += part[(q + L::kNeed) * L::kThreads];
+        }
     }
     MaskKey mask{};
     if (KIND == kOut && a.masked) mask = mask_key(a.mask);
-    L::place(m, n, tid, (int)i, (int)j, row, col);
-    finish<T, KIND>(a, p, mask, row, col, v, w);
+    L::finish_group(a, p, mask, m, n, i, g, in, [&](uint32_t k, int q) { return v[k * W + q]; }, [&](uint32_t k, int q) { return w[k * W + q]; });
 }
 
 }  // namespace ecrm
