@@ -12,11 +12,12 @@ namespace ecrm {
 // K, alone on its CU and for each of several; the launch, a tile's begin and end.  16 bits: 64 x 64 0.50 and 0.17 a step, 128 x 128 0.65
 // and 0.47, 256 x 256 1.58; 32 bits: 0.62 and 0.46, 1.96 and 1.79 (256 x 256 is 7.2 and gains nothing).
 enum { kTile256 = 0, kTile128 = 1, kTile64 = 2, kTilings = 3 };
-struct TilingCost { uint32_t side; double step[2], shared[2], launch, tile; };          // [0] 16 bits, [1] 32
-constexpr TilingCost kCosts[kTilings] = {{256, {1.58, 0}, {1.58, 0}, 3.0, 8.0}, {128, {0.65, 1.96}, {0.47, 1.79}, 5.0, 1.4},
-                                         {64, {0.50, 0.62}, {0.172, 0.46}, 2.5, 0.42}};
+struct TilingCost { uint32_t side, resident; double step[2], shared[2], launch, tile; };          // [0] 16 bits, [1] 32
+constexpr TilingCost kCosts[kTilings] = {{256, 1, {1.58, 0}, {1.58, 0}, 3.0, 8.0}, {128, 2, {0.65, 1.96}, {0.47, 1.79}, 5.0, 1.4},
+                                         {64, 5, {0.50, 0.62}, {0.172, 0.46}, 2.5, 0.42}};
 constexpr uint32_t kSplitCounts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
 constexpr double kJoinLaunch = 3.0, kJoinRate = 4.0e6;                                  // us; bytes a us
+constexpr uint32_t kSkinnyParts = 16;
 constexpr size_t kPartMost = 32u << 20;          // bytes of the parts of split products, at most
 
 // Rows up to `rows` of the results with one tiling, the others (if there are any) with another.
@@ -44,8 +45,9 @@ static Plan plan_rows(const ProductSize &z, uint32_t M, uint32_t type, uint32_t 
             const uint32_t each = (k_tiles + splits - 1) / splits, parts = (k_tiles + each - 1) / each;
             const double bytes = (double)tiles * parts * c.side * c.side * 4.0;
             if (parts > 1 && bytes > (double)room) break;
-            const double there = (double)((tiles * parts + cus - 1) / cus), step = c.shared[wide] * there;
-            double cost = c.launch + c.tile * there + each * (step > c.step[wide] ? step : c.step[wide]);
+            const uint64_t there = (tiles * parts + cus - 1) / cus;      // on a CU, as many at a time as are resident
+            auto step = [&](uint64_t n) { return n ? (c.shared[wide] * n > c.step[wide] ? c.shared[wide] * n : c.step[wide]) : 0.0; };
+            double cost = c.launch + c.tile * there + each * ((there / c.resident) * step(c.resident) + step(there % c.resident));
             if (parts > 1) cost += kJoinLaunch + 2.0 * bytes / kJoinRate;
             if (!best.splits || cost < best.cost) best = Plan{t, parts, each, cost};
         }
@@ -130,9 +132,32 @@ static void skip_rows(ProductArgs &a, uint32_t first)
     p.M -= first;
 }
 
-template <typename T, int KIND>
-static void launch_product(ProductArgs &a, const RowPlan &plan, hipStream_t st)
+// Up to 32 rows, of 32 bits up to 16, see skinny_kernel.  us forward so / by tiles, 16 and 32 rows: bf16 D = 128, F = 512 6.8 / 8.7, 8.2 /
+// 8.7; 1024, 1024 9.2 / 14.5, 11.5 / 14.6; 1024, 4096 15.1 / 19.8, 20.1 / 19.8.  fp32 8.0 / 12.6, 10.0 / 12.7; 15.2 / 21.4, 23.5 / 21.3;
+// 29.2 / 31.5, 44.3 / 31.4.
+template <typename T, int KIND, int XB>
+static void launch_skinny(ProductArgs &a, uint32_t cus, hipStream_t st)
 {
+    const Product &p = a.p[0];
+    const uint32_t blocks = (p.N + 15u) / 16u, steps = (p.K * (uint32_t)sizeof(T) + 63u) / 64u, wanted = (steps + kAtOnce - 1u) / kAtOnce;
+    uint32_t parts = 1;
+    if (KIND == kOut && blocks < cus) {                  // no more workgroups than CUs, eight waves at least to each
+        const uint32_t fit = cus / blocks, fill = wanted / 8u;
+        parts = fit < fill ? fit : fill;
+        parts = parts < 1u ? 1u : parts > kSkinnyParts ? kSkinnyParts : parts;
+    }
+    const uint32_t share = (wanted + parts - 1u) / parts, waves = share < Skinny<XB>::kWaves ? share : Skinny<XB>::kWaves;
+    hipLaunchKernelGGL((skinny_kernel<T, KIND, XB>), dim3(blocks, parts), dim3(waves * kWave), 0, st, a);
+}
+
+template <typename T, int KIND>
+static void launch_product(ProductArgs &a, const RowPlan &plan, int cus, hipStream_t st)
+{
+    if constexpr (KIND == kGate || KIND == kOut) {
+        if (a.p[0].M <= 16) return launch_skinny<T, KIND, 1>(a, (uint32_t)cus, st);
+        if constexpr (sizeof(T) == 2)
+            if (a.p[0].M <= 32) return launch_skinny<T, KIND, 2>(a, (uint32_t)cus, st);
+    }
     if constexpr (KIND == kWeights) {
         launch_planned<T, KIND>(a, plan.main, st);
     } else {
@@ -161,7 +186,8 @@ struct ecrm_ffn {
     ecrm_ffn_config cfg;
     uint64_t pitch;                       // elements of a row of h, dg, du
     uint64_t e_pitch;                     // of a row of e
-    size_t off_h, off_dg, off_du, off_e, off_part, part_bytes, bytes;
+    size_t off_h, off_dg, off_du, off_e, off_arrived, off_part, part_bytes, bytes;
+    uint32_t counters;
     const void *gate, *up, *down;
     uint64_t gate_stride, up_stride, down_stride;
     char *work;
@@ -262,6 +288,8 @@ int ecrm_ffn_create(const ecrm_ffn_config *cfg, ecrm_ffn **out)
         f->off_du = take(cfg->max_rows * f->pitch * size);
         f->off_e = take(cfg->max_rows * f->e_pitch * size);
     }
+    f->counters = (cfg->dim + 15u) / 16u * 2u;
+    f->off_arrived = take(f->counters * 4u);
     f->part_bytes = kPartMost;
     f->off_part = take(f->part_bytes);
     f->bytes = off;
@@ -320,6 +348,8 @@ int ecrm_ffn_forward(ecrm_ffn *f, const void *x, uint64_t x_stride, uint64_t n, 
     void *h = f->work + f->off_h;
     a.part = (float *)(f->work + f->off_part);
     make_plans(f, false, N);
+    a.arrived = (uint32_t *)(f->work + f->off_arrived);
+    a.clear = f->counters;
     a.activation = f->cfg.activation;
     a.products = 1;
     with_type(type, [&](auto t) {
@@ -330,14 +360,14 @@ int ecrm_ffn_forward(ecrm_ffn *f, const void *x, uint64_t x_stride, uint64_t n, 
         a.p[0].out = h;
         a.p[0].out_stride = f->pitch;
         a.p[0].out2 = saved;
-        launch_product<T, kGate>(a, f->plan[kGate], st);
+        launch_product<T, kGate>(a, f->plan[kGate], f->cus, st);
         a.p[0] = product(h, f->pitch, f->down, f->down_stride, N, D, F);
         a.p[0].out = out;
         a.p[0].out_stride = out_stride;
         a.p[0].in = residual;
         a.p[0].in_stride = residual_stride;
         a.masked = mask ? 1u : 0u;
-        launch_product<T, kOut>(a, f->plan[kOut], st);
+        launch_product<T, kOut>(a, f->plan[kOut], f->cus, st);
     });
     return launched();
 }
@@ -411,7 +441,7 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
         a.p[0].out2 = du;
         a.p[0].out3 = h;
         a.p[0].out_stride = f->pitch;
-        launch_product<T, kBack>(a, f->plan[kBack], st);
+        launch_product<T, kBack>(a, f->plan[kBack], f->cus, st);
         if (weights) {
             a.products = 3;
             a.p[0] = product(dg, f->pitch, x, x_stride, F, D, N);
@@ -423,7 +453,7 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
             a.p[2] = product(e, e_stride, h, f->pitch, D, F, N);
             a.p[2].out = d_down;
             a.p[2].out_stride = F;
-            launch_product<T, kWeights>(a, f->plan[kWeights], st);
+            launch_product<T, kWeights>(a, f->plan[kWeights], f->cus, st);
         }
         if (d_x) {                        // last: it may take the place of d_out
             a.products = 1;
@@ -435,7 +465,7 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
             a.p[0].in_stride = add_stride;
             a.p[0].out = d_x;
             a.p[0].out_stride = d_x_stride;
-            launch_product<T, kInput>(a, f->plan[kInput], st);
+            launch_product<T, kInput>(a, f->plan[kInput], f->cus, st);
         }
     });
     return launched();

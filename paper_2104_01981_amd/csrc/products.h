@@ -57,9 +57,11 @@ struct ProductArgs {
     uint32_t tiles;                    // in all
     uint32_t splits, each;             // K tiles: cut into so many parts of at most so many
     float *part;                       // [tiles][splits][threads][..] where there are several
+    uint32_t *arrived;                 // few rows: [column blocks][row blocks] parts that are there
     uint32_t activation;
     uint32_t masked, first_row;        // row of the mask that row 0 of the results has
     MaskArgs mask;
+    uint32_t clear;                    // few rows: of the counters
     uint32_t accumulate, wide;         // kWeights: added to; in 32 bits whatever the type
 };
 
@@ -293,6 +295,10 @@ struct Piece {
         const uint2 half = quads ? *(const uint2 *)p : uint2{0u, 0u};
         return u32x4{half.x, half.y, 0u, 0u};
     }
+    static __device__ __forceinline__ u32x4 read_or_zero(const T *p, uint32_t quads)
+    {
+        return quads ? read(p, quads) : u32x4{0u, 0u, 0u, 0u};
+    }
     static __device__ __forceinline__ void write(T *p, uint32_t quads, u32x4 v)
     {
         if (quads >= (uint32_t)kQuads) *(Loose *)p = v;
@@ -336,45 +342,38 @@ __device__ __forceinline__ void exchange(u32x4 &a, u32x4 &b)
 // What a lane reads for a piece of the results, and writes.
 enum { kReads = 2, kWrites = 3 };
 
-// A piece's results v (kGate: of the gate, w those of the up projection) with what was read, to what is written.
-template <typename T, int KIND>
-__device__ __forceinline__ void finish(const ProductArgs &a, const Product &p, const MaskKey &mask, uint32_t row, uint32_t col,
-                                       f32x4 (&v)[Piece<T>::kQuads], const f32x4 (&w)[Piece<T>::kQuads], const u32x4 (&in)[kReads],
-                                       u32x4 (&out)[kWrites])
+// W quads of results v (kGate: of the gate, w those of the up projection) with what was read, x and y, to what is written: v, and kGate
+// and kBack x and y.
+template <typename T, int KIND, int W>
+__device__ __forceinline__ void finish(const ProductArgs &a, const Product &p, const MaskKey &mask, uint32_t row, uint32_t col, f32x4 (&v)[W],
+                                       const f32x4 (&w)[W], f32x4 (&x)[W], f32x4 (&y)[W])
 {
-    constexpr int W = Piece<T>::kQuads;
     if (KIND == kGate) {
-        out[1] = Piece<T>::round(v);
-        out[2] = Piece<T>::round(w);
         with_activation(a.activation, [&](auto act) {
 #pragma unroll
-            for (int q = 0; q < W; ++q)
+            for (int q = 0; q < W; ++q) {
+                x[q] = v[q];
+                y[q] = w[q];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float slope;
                     v[q][i] = activation<T, decltype(act)::value>(v[q][i], slope) * w[q][i];
                 }
+            }
         });
-        out[0] = Piece<T>::round(v);
     } else if (KIND == kBack) {
-        f32x4 g[W], u[W], du[W];
-        Piece<T>::widen(in[0], g);
-        Piece<T>::widen(in[1], u);
         with_activation(a.activation, [&](auto act) {
 #pragma unroll
             for (int q = 0; q < W; ++q)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float slope;
-                    const float x = activation<T, decltype(act)::value>(g[q][i], slope);
-                    du[q][i] = v[q][i] * x;
-                    v[q][i] *= u[q][i] * slope;
-                    u[q][i] *= x;
+                    const float value = activation<T, decltype(act)::value>(x[q][i], slope);
+                    x[q][i] = v[q][i] * value;
+                    v[q][i] *= y[q][i] * slope;
+                    y[q][i] *= value;
                 }
         });
-        out[0] = Piece<T>::round(v);
-        out[1] = Piece<T>::round(du);
-        out[2] = Piece<T>::round(u);
     } else {
         if (KIND == kOut && a.masked) {
             const uint4 bits = mask_block(mask, a.first_row + row, col / 8u);
@@ -382,13 +381,9 @@ __device__ __forceinline__ void finish(const ProductArgs &a, const Product &p, c
             v[0] = drop4(v[0], upper ? uint2{bits.z, bits.w} : uint2{bits.x, bits.y}, mask);
             if (W == 2) v[W - 1] = drop4(v[W - 1], uint2{bits.z, bits.w}, mask);
         }
-        if (KIND == kWeights ? a.accumulate != 0u : p.in != nullptr) {
-            f32x4 more[W];
-            Piece<T>::widen(in[0], more);
+        if (KIND == kWeights ? a.accumulate != 0u : p.in != nullptr)
 #pragma unroll
-            for (int q = 0; q < W; ++q) v[q] += more[q];
-        }
-        out[0] = Piece<T>::round(v);
+            for (int q = 0; q < W; ++q) v[q] += x[q];
     }
 }
 
@@ -488,7 +483,16 @@ struct Tiling {
                 w[q] = of_up(k, q);
             }
             if (KIND == kWeights && a.wide) write_wide<kPair>(a, p, row, col, v);
-            else finish<T, KIND>(a, p, mask, row, col, v, w, in.x[k], out[k]);
+            if (KIND == kWeights && a.wide) continue;
+            f32x4 x[kPair], y[kPair];
+            if (kIn >= 1) Piece<T>::widen(in.x[k][0], x);
+            if (kIn >= 2) Piece<T>::widen(in.x[k][1], y);
+            finish<T, KIND, kPair>(a, p, mask, row, col, v, w, x, y);
+            out[k][0] = Piece<T>::round(v);
+            if (kOuts == 3) {
+                out[k][1] = Piece<T>::round(x);
+                out[k][2] = Piece<T>::round(y);
+            }
         }
         if (KIND == kWeights && a.wide) return;
         if (kTogether == 2)
@@ -654,6 +658,116 @@ __global__ __launch_bounds__(WM * WN * kWave) void join_kernel(ProductArgs a)
     MaskKey mask{};
     if (KIND == kOut && a.masked) mask = mask_key(a.mask);
     L::finish_group(a, p, mask, m, n, i, g, in, [&](uint32_t k, int q) { return v[k * W + q]; }, [&](uint32_t k, int q) { return w[k * W + q]; });
+}
+
+// ---- few rows --------------------------------------------------------------------------------------------------------------------
+// Up to 16 * XB rows: what counts is that all of the weights are on their way at once.  A workgroup has 16 columns of the results (of
+// both projections) and all of K or, where there are few columns and a long K, a part of it; its waves share that, every one with up to
+// kAtOnce steps of 64 bytes of 16 rows of weights in flight, straight into the registers of the matrix instructions, whose second operand
+// are the rows.  The waves' sums are added up in LDS, in order; those of several workgroups by the one that is there last, in order, too.
+constexpr uint32_t kAtOnce = 4;
+template <int XB>
+struct Skinny { static constexpr uint32_t kWaves = XB == 1 ? 16 : 8; };          // as the registers allow
+
+template <typename T, int KIND, int XB>
+__global__ __launch_bounds__(Skinny<XB>::kWaves * kWave) void skinny_kernel(ProductArgs a)
+{
+    constexpr int B = KIND == kGate ? 2 : 1;             // matrices of weights
+    constexpr uint32_t kChunk = 16 / sizeof(T), kStep = 4 * kChunk;
+    __shared__ f32x4 s_part[Skinny<XB>::kWaves][B * XB][kWave];
+    const Product &p = a.p[0];
+    const uint32_t lane = lane_id(), i = lane % 16u, q = lane / 16u, wave = scalar(threadIdx.x / kWave), waves = blockDim.x / kWave;
+    const uint32_t col0 = blockIdx.x * 16u, K = p.K, steps = (K + kStep - 1u) / kStep, sharing = waves * gridDim.y;
+    const uint32_t each = scalar((steps + sharing - 1u) / sharing), begin = (blockIdx.y * waves + wave) * each, stop = min(begin + each, steps);
+    if (KIND == kGate && blockIdx.x == 0 && blockIdx.y == 0)             // for the launch behind, kOut's
+        for (uint32_t c = threadIdx.x; c < a.clear; c += blockDim.x) a.arrived[c] = 0u;
+
+    const T *w[B], *x[XB];
+#pragma unroll
+    for (int b = 0; b < B; ++b) w[b] = (const T *)p.b.p[b] + (uint64_t)min(col0 + i, p.N - 1u) * p.b.stride[b] + q * kChunk;
+#pragma unroll
+    for (int r = 0; r < XB; ++r) x[r] = (const T *)p.a.p[0] + (uint64_t)min((uint32_t)r * 16u + i, p.M - 1u) * p.a.stride[0] + q * kChunk;
+
+    f32x4 acc[B][XB];
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+#pragma unroll
+        for (int r = 0; r < XB; ++r) acc[b][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (uint32_t s0 = begin; s0 < stop; s0 += kAtOnce) {
+        u32x4 fw[kAtOnce][B], fx[kAtOnce][XB];
+        if (s0 + kAtOnce <= stop && (s0 + kAtOnce) * kStep <= K) {
+#pragma unroll
+            for (uint32_t s = 0; s < kAtOnce; ++s) {
+#pragma unroll
+                for (int b = 0; b < B; ++b) fw[s][b] = Piece<T>::read(w[b] + (s0 + s) * kStep, 2u);
+#pragma unroll
+                for (int r = 0; r < XB; ++r) fx[s][r] = Piece<T>::read(x[r] + (s0 + s) * kStep, 2u);
+            }
+        } else {
+#pragma unroll
+            for (uint32_t s = 0; s < kAtOnce; ++s) {     // what is behind K, or the wave's part of it, is zero on both sides
+                const uint32_t k = (s0 + s) * kStep + q * kChunk, quads = s0 + s < stop && k < K ? (K - k) / 4u : 0u;
+#pragma unroll
+                for (int b = 0; b < B; ++b) fw[s][b] = Piece<T>::read_or_zero(w[b] + (s0 + s) * kStep, quads);
+#pragma unroll
+                for (int r = 0; r < XB; ++r) fx[s][r] = Piece<T>::read_or_zero(x[r] + (s0 + s) * kStep, quads);
+            }
+        }
+#pragma unroll
+        for (uint32_t s = 0; s < kAtOnce; ++s)
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+#pragma unroll
+                for (int r = 0; r < XB; ++r) acc[b][r] = Fragment<T>::multiply(fw[s][b], fx[s][r], acc[b][r]);
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+#pragma unroll
+        for (int r = 0; r < XB; ++r) s_part[wave][b * XB + r][lane] = acc[b][r];
+    __syncthreads();
+
+    // wave r finishes rows 16 r .. 16 r + 15 (where there are as few waves as rows of blocks, one may have several)
+    for (uint32_t r = wave; r < (uint32_t)XB; r += waves) {
+        const uint32_t row = r * 16u + i, col = col0 + q * 4u;
+        const bool there = row < p.M && col < p.N;
+        f32x4 v[1], up[1], in[1], y[1];
+        v[0] = up[0] = in[0] = y[0] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (KIND == kOut && p.in && there) in[0] = widen4<T>(*(const typename Quad<T>::type *)((const T *)p.in + (uint64_t)row * p.in_stride + col));
+        for (uint32_t s = 0; s < waves; ++s) {
+            v[0] += s_part[s][r][lane];
+            if (KIND == kGate) up[0] += s_part[s][(B - 1) * XB + r][lane];
+        }
+        if (KIND == kOut && gridDim.y > 1u) {
+            const uint32_t slot = blockIdx.x * XB + r;
+            double *parts = (double *)a.part + ((uint64_t)slot * gridDim.y * kWave + lane) * 2u;
+            const double2 mine = __builtin_bit_cast(double2, v[0]);
+            shared_store(parts + blockIdx.y * kWave * 2u, mine.x);
+            shared_store(parts + blockIdx.y * kWave * 2u + 1u, mine.y);
+            published();
+            uint32_t before = 0;
+            if (lane == 0) before = __hip_atomic_fetch_add(a.arrived + slot, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (scalar(before) + 1u < gridDim.y) continue;
+            v[0] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+            for (uint32_t s = 0; s < gridDim.y; ++s) {
+                double2 d;
+                d.x = shared_load(parts + s * kWave * 2u);
+                d.y = shared_load(parts + s * kWave * 2u + 1u);
+                v[0] += __builtin_bit_cast(f32x4, d);
+            }
+        }
+        MaskKey mask{};
+        if (KIND == kOut && a.masked) mask = mask_key(a.mask);
+        finish<T, KIND, 1>(a, p, mask, row, col, v, up, in, y);
+        if (!there) continue;
+        typedef typename Quad<T>::type Four;
+        *(Four *)((T *)p.out + (uint64_t)row * p.out_stride + col) = round4<T>(v[0]);
+        if (KIND == kGate && p.out2) {
+            T *s = (T *)p.out2 + (uint64_t)row * 2u * p.N + col;
+            *(Four *)s = round4<T>(in[0]);
+            *(Four *)(s + p.N) = round4<T>(y[0]);
+        }
+    }
 }
 
 }  // namespace ecrm
