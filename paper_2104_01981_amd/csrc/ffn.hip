@@ -16,15 +16,19 @@ struct TilingCost { uint32_t side, resident; double step[2], shared[2], launch, 
 constexpr TilingCost kCosts[kTilings] = {{256, 1, {1.58, 0}, {1.58, 0}, 3.0, 8.0}, {128, 2, {0.65, 1.96}, {0.47, 1.79}, 5.0, 1.4},
                                          {64, 5, {0.50, 0.62}, {0.172, 0.46}, 2.5, 0.42}};
 constexpr uint32_t kSplitCounts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
-constexpr double kJoinLaunch = 3.0, kJoinRate = 4.0e6;                                  // us; bytes a us
+constexpr double kJoinLaunch = 3.0, kJoinRate = 4.0e6;       // parts of the first product of a call, by a launch of their own: us; bytes a us
+constexpr double kJoinWait = 1.5, kJoinOne = 1.0e5;          // others by the workgroup that is there last
 constexpr uint32_t kSkinnyParts = 16;
 constexpr size_t kPartMost = 32u << 20;          // bytes of the parts of split products, at most
+constexpr uint32_t kCounters = kPartMost / (64u * 64u * 4u);
 
+struct Split { uint32_t splits, each; };
+// Products of one launch (the last of them with the splits of their own, where there are two sizes).
+struct Plan { uint32_t tiling; Split split[2]; double cost; };
 // Rows up to `rows` of the results with one tiling, the others (if there are any) with another.
-struct Plan { uint32_t tiling, splits, each; double cost; };
 struct RowPlan { uint32_t rows; Plan main, rest; };
 
-struct ProductSize { uint32_t M, N, K, halves, count; bool dual; };       // `count` of them
+struct ProductSize { uint32_t M, N, K, halves, count; bool dual, first; };       // `count` of them
 
 static uint64_t tiles_of(const ProductSize &z, uint32_t M, uint32_t side)
 {
@@ -32,69 +36,123 @@ static uint64_t tiles_of(const ProductSize &z, uint32_t M, uint32_t side)
     return (uint64_t)((M + side - 1) / side) * ((z.N + columns - 1) / columns) * z.count;
 }
 
-static Plan plan_rows(const ProductSize &z, uint32_t M, uint32_t type, uint32_t cus, size_t room)
+// What a launch of A tiles that take ta and B that take tb (ta >= tb), one after the other on so many at a time, takes.
+static double makespan(uint64_t A, double ta, uint64_t B, double tb, uint64_t slots)
+{
+    const uint64_t full = A / slots, busy = A % slots, idle = slots - busy;
+    double end = (double)(full + (busy ? 1 : 0)) * ta;
+    if (!B) return end;
+    const uint64_t beside = busy ? idle * (uint64_t)(ta / tb) : 0;       // done while the last of the others run
+    if (B > beside) end += (double)((B - beside + slots - 1) / slots) * tb;
+    return end;
+}
+
+// The sizes' products side by side (b.count = 0: a alone).
+static Plan plan_launch(const ProductSize &a, const ProductSize &b, uint32_t type, uint32_t cus, size_t room)
 {
     const uint32_t wide = type == ECRM_F32 ? 1u : 0u, elements = kRowBytes / type_bytes(type);
-    const uint32_t k_tiles = (z.K + elements - 1) / elements * z.halves;
+    const ProductSize *sizes[2] = {&a, &b};
     Plan best{};
     for (uint32_t t = wide ? kTile128 : kTile256; t < kTilings; ++t) {
         const TilingCost &c = kCosts[t];
-        const uint64_t tiles = tiles_of(z, M, c.side);
-        for (uint32_t splits : kSplitCounts) {
-            if (splits > k_tiles) break;
-            const uint32_t each = (k_tiles + splits - 1) / splits, parts = (k_tiles + each - 1) / each;
-            const double bytes = (double)tiles * parts * c.side * c.side * 4.0;
-            if (parts > 1 && bytes > (double)room) break;
-            const uint64_t there = (tiles * parts + cus - 1) / cus;      // on a CU, as many at a time as are resident
-            auto step = [&](uint64_t n) { return n ? (c.shared[wide] * n > c.step[wide] ? c.shared[wide] * n : c.step[wide]) : 0.0; };
-            double cost = c.launch + c.tile * there + each * ((there / c.resident) * step(c.resident) + step(there % c.resident));
-            if (parts > 1) cost += kJoinLaunch + 2.0 * bytes / kJoinRate;
-            if (!best.splits || cost < best.cost) best = Plan{t, parts, each, cost};
+        uint64_t tiles[2];
+        uint32_t k_tiles[2];
+        for (int i = 0; i < 2; ++i) {
+            tiles[i] = sizes[i]->count ? tiles_of(*sizes[i], sizes[i]->M, c.side) : 0;
+            k_tiles[i] = (sizes[i]->K + elements - 1) / elements * sizes[i]->halves;
+        }
+        auto split = [&](int i, uint32_t splits) {
+            const uint32_t each = (k_tiles[i] + splits - 1) / splits;
+            return Split{(k_tiles[i] + each - 1) / each, each};
+        };
+        const double part = (double)c.side * c.side * 4.0;
+        for (uint32_t sa : kSplitCounts) {
+            if (sa > k_tiles[0]) break;
+            const Split x = split(0, sa);
+            const double a_bytes = x.splits > 1 ? part * tiles[0] * x.splits : 0.0;
+            if (a_bytes > (double)room) break;
+            for (uint32_t sb : kSplitCounts) {
+                if (b.count ? sb > k_tiles[1] : sb > 1) break;
+                const Split y = b.count ? split(1, sb) : Split{1, 0};
+                const double bytes = a_bytes + (y.splits > 1 ? part * tiles[1] * y.splits : 0.0);
+                if (bytes > (double)room) break;
+                const uint64_t units = tiles[0] * x.splits + tiles[1] * y.splits, there = (units + cus - 1) / cus;
+                const double together = there < c.resident ? (double)there : (double)c.resident;
+                const double step = c.shared[wide] * together > c.step[wide] ? c.shared[wide] * together : c.step[wide];
+                auto unit = [&](int i, const Split &s) {
+                    return c.tile * together + s.each * step + (s.splits > 1 && !sizes[i]->first ? kJoinWait + s.splits * part / kJoinOne : 0.0);
+                };
+                const uint64_t slots = (uint64_t)(cus * together);
+                const double ua = unit(0, x), ub = b.count ? unit(1, y) : 1.0;
+                double cost = c.launch + (ua >= ub ? makespan(tiles[0] * x.splits, ua, tiles[1] * y.splits, ub, slots)
+                                                   : makespan(tiles[1] * y.splits, ub, tiles[0] * x.splits, ua, slots));
+                if (a.first && x.splits > 1) cost += kJoinLaunch + 2.0 * a_bytes / kJoinRate;
+                if (!best.split[0].splits || cost < best.cost) best = Plan{t, {x, y}, cost};
+            }
         }
     }
     return best;
 }
 
-static RowPlan plan_product(const ProductSize &z, bool cut, uint32_t type, uint32_t cus, size_t room)
+static RowPlan plan_rows(const ProductSize &z, uint32_t type, uint32_t cus, size_t room)
 {
-    RowPlan best{z.M, plan_rows(z, z.M, type, cus, room), Plan{}};
-    if (!cut) return best;
+    const ProductSize none{};
+    auto plan = [&](uint32_t rows) {
+        ProductSize part = z;
+        part.M = rows;
+        return plan_launch(part, none, type, cus, room);
+    };
+    RowPlan best{z.M, plan(z.M), Plan{}};
     for (uint32_t side : {256u, 128u, 64u}) {
         // as many rows of tiles as fill the CUs to the last, or as are whole
         const uint64_t across = tiles_of(z, side, side), all = z.M / side, rounds = all * across / cus;
         for (uint64_t down : {rounds * cus / across, all}) {
             const uint32_t rows = (uint32_t)(down * side);
             if (!rows || rows >= z.M) continue;
-            const Plan main = plan_rows(z, rows, type, cus, room), rest = plan_rows(z, z.M - rows, type, cus, room);
+            const Plan main = plan(rows), rest = plan(z.M - rows);
             if (main.cost + rest.cost < best.main.cost + best.rest.cost) best = RowPlan{rows, main, rest};
         }
     }
     return best;
 }
 
+// Gives the products of a launch their tiles, parts and workgroups, in order.
+static void lay_out(ProductArgs &a, uint32_t rows, uint32_t columns)
+{
+    a.workgroups = 0;
+    uint32_t part = 0, counter = 0;
+    for (uint32_t i = 0; i < a.products; ++i) {
+        Product &p = a.p[i];
+        p.tiles_m = (p.M + rows - 1) / rows;
+        p.tiles_n = (p.N + columns - 1) / columns;
+        const uint32_t tiles = p.tiles_m * p.tiles_n;
+        p.first = a.workgroups;
+        a.workgroups += tiles * p.splits;
+        if (p.splits == 1) continue;
+        p.part = part;
+        p.counter = counter;
+        part += tiles * p.splits;
+        counter += tiles;
+    }
+}
+
 template <typename T, int KIND, int BM, int BN, int WM, int WN>
-static void launch_tiling(const ProductArgs &a, hipStream_t st)
+static void launch_tiling(ProductArgs &a, hipStream_t st)
 {
     typedef Tiling<T, KIND, BM, BN, WM, WN> L;
-    hipLaunchKernelGGL((product_kernel<T, KIND, BM, BN, WM, WN>), dim3(a.tiles * a.splits), dim3(L::kThreads), 0, st, a);
-    if (a.splits > 1)
-        hipLaunchKernelGGL((join_kernel<T, KIND, BM, BN, WM, WN>), dim3(a.tiles, L::MB * L::kGroups), dim3(L::kThreads), 0, st, a);
+    lay_out(a, BM, L::kColumns);
+    hipLaunchKernelGGL((product_kernel<T, KIND, BM, BN, WM, WN>), dim3(a.workgroups), dim3(L::kThreads), 0, st, a);
+    if constexpr (L::kFirst)
+        if (a.p[0].splits > 1)
+            hipLaunchKernelGGL((join_kernel<T, KIND, BM, BN, WM, WN>), dim3(a.p[0].tiles_m * a.p[0].tiles_n, L::MB * L::kGroups), dim3(L::kThreads), 0, st, a);
 }
 
 template <typename T, int KIND>
 static void launch_planned(ProductArgs &a, const Plan &plan, hipStream_t st)
 {
-    const uint32_t side = kCosts[plan.tiling].side, columns = KIND == kGate ? side / 2u : side;
-    a.tiles = 0;
-    for (uint32_t i = 0; i < a.products; ++i) {
-        Product &p = a.p[i];
-        p.tiles_m = (p.M + side - 1) / side;
-        p.tiles_n = (p.N + columns - 1) / columns;
-        a.first[i] = a.tiles;
-        a.tiles += p.tiles_m * p.tiles_n;
-    }
-    a.splits = plan.splits;
-    a.each = plan.each;
+    a.products = 1;
+    a.p[0].splits = plan.split[0].splits;
+    a.p[0].each = plan.split[0].each;
     // both projections of kGate: 64 columns of each to a wave (32 of 64 x 64), whole lines of the results
     if constexpr (sizeof(T) == 2) {
         if (plan.tiling == kTile256) {
@@ -110,6 +168,40 @@ static void launch_planned(ProductArgs &a, const Plan &plan, hipStream_t st)
         if constexpr (KIND == kGate) launch_tiling<T, KIND, 64, 64, 4, 1>(a, st);
         else launch_tiling<T, KIND, 64, 64, 2, 2>(a, st);
     }
+}
+
+template <typename T, int BM, int BN, int WM, int WN>
+static void launch_gradients(ProductArgs &a, hipStream_t st)
+{
+    lay_out(a, BM, BN);
+    hipLaunchKernelGGL((gradients_kernel<T, BM, BN, WM, WN>), dim3(a.workgroups), dim3(WM * WN * kWave), 0, st, a);
+}
+
+// The weights' products, x's, or both.
+template <typename T>
+static void launch_gradients(ProductArgs &a, const Product *weights, const Product *input, const Plan &plan, hipStream_t st)
+{
+    a.products = 0;
+    auto take = [&](const Product *p, uint32_t count, const Split &s) {
+        for (uint32_t i = 0; i < count; ++i) {
+            Product &to = a.p[a.products++];
+            to = p[i];
+            to.splits = s.splits;
+            to.each = s.each;
+        }
+    };
+    // longest first
+    if (weights && input && plan.split[0].each < plan.split[1].each) {
+        take(input, 1, plan.split[1]);
+        take(weights, 3, plan.split[0]);
+    } else {
+        if (weights) take(weights, 3, plan.split[0]);
+        if (input) take(input, 1, plan.split[weights ? 1 : 0]);
+    }
+    if constexpr (sizeof(T) == 2)
+        if (plan.tiling == kTile256) return launch_gradients<T, 256, 256, 2, 4>(a, st);
+    if (plan.tiling == kTile128) launch_gradients<T, 128, 128, 2, 2>(a, st);
+    else launch_gradients<T, 64, 64, 2, 2>(a, st);
 }
 
 // The product's rows from `first` on.
@@ -158,18 +250,14 @@ static void launch_product(ProductArgs &a, const RowPlan &plan, int cus, hipStre
         if constexpr (sizeof(T) == 2)
             if (a.p[0].M <= 32) return launch_skinny<T, KIND, 2>(a, (uint32_t)cus, st);
     }
-    if constexpr (KIND == kWeights) {
-        launch_planned<T, KIND>(a, plan.main, st);
-    } else {
-        const uint32_t M = a.p[0].M;
-        a.first_row = 0;
-        a.p[0].M = plan.rows;
-        launch_planned<T, KIND>(a, plan.main, st);
-        if (plan.rows == M) return;
-        a.p[0].M = M;
-        skip_rows<T, KIND>(a, plan.rows);
-        launch_planned<T, KIND>(a, plan.rest, st);
-    }
+    const uint32_t M = a.p[0].M;
+    a.first_row = 0;
+    a.p[0].M = plan.rows;
+    launch_planned<T, KIND>(a, plan.main, st);
+    if (plan.rows == M) return;
+    a.p[0].M = M;
+    skip_rows<T, KIND>(a, plan.rows);
+    launch_planned<T, KIND>(a, plan.rest, st);
 }
 
 __global__ __launch_bounds__(256) void clear_kernel(uint32_t *to, uint64_t words)
@@ -181,6 +269,8 @@ __global__ __launch_bounds__(256) void clear_kernel(uint32_t *to, uint64_t words
 
 using namespace ecrm;
 
+enum { kPlanForward, kPlanBack, kPlanWeights, kPlanInput, kPlanBoth, kPlans };
+
 // ---- C ABI -----------------------------------------------------------------------------------------------------------------------
 struct ecrm_ffn {
     ecrm_ffn_config cfg;
@@ -188,12 +278,14 @@ struct ecrm_ffn {
     uint64_t e_pitch;                     // of a row of e
     size_t off_h, off_dg, off_du, off_e, off_arrived, off_part, part_bytes, bytes;
     uint32_t counters;
-    const void *gate, *up, *down;
+    const void *gate_weights, *up, *down;
     uint64_t gate_stride, up_stride, down_stride;
     char *work;
     int cus;
-    uint64_t planned[2];                  // rows that the plans are for: of the forward pass, of the backward pass
-    RowPlan plan[kKinds];
+    // plans, kept while the number of rows stays, since making them takes some us
+    uint64_t rows_of[kPlans];
+    RowPlan gate, out, back;
+    Plan gradients[3];
 };
 
 namespace {
@@ -226,7 +318,7 @@ bool clear_of_own(const ecrm_ffn *f, const ecrm_mask *mask, uint32_t size, const
 {
     const uint32_t s = type_bytes(f->cfg.type);
     const uint64_t D = f->cfg.dim, F = f->cfg.hidden;
-    return apart(size, w, s, Rows{f->gate, F, D, f->gate_stride}) && apart(size, w, s, Rows{f->up, F, D, f->up_stride}) &&
+    return apart(size, w, s, Rows{f->gate_weights, F, D, f->gate_stride}) && apart(size, w, s, Rows{f->up, F, D, f->up_stride}) &&
            apart(size, w, s, Rows{f->down, D, F, f->down_stride}) && apart(size, w, 1, Rows{f->work, 1, f->bytes, f->bytes}) &&
            (!mask || apart(size, w, 1, Rows{mask->state, 1, 16, 16}));
 }
@@ -245,21 +337,22 @@ Product product(const void *a, uint64_t a_stride, const void *b, uint64_t b_stri
     return p;
 }
 
-// The plans of a pass over n rows: kept while n stays, since making them takes a few us.
-void make_plans(ecrm_ffn *f, bool backward, uint32_t n)
+void make_plan(ecrm_ffn *f, int what, uint32_t n)
 {
-    if (f->planned[backward] == n) return;
+    if (f->rows_of[what] == n) return;
     const uint32_t D = f->cfg.dim, F = f->cfg.hidden, type = f->cfg.type, cus = (uint32_t)f->cus;
-    auto plan = [&](int kind, ProductSize z) { f->plan[kind] = plan_product(z, kind != kWeights, type, cus, f->part_bytes); };
-    if (!backward) {
-        plan(kGate, ProductSize{n, F, D, 1, 1, true});
-        plan(kOut, ProductSize{n, D, F, 1, 1, false});
+    const size_t room = f->part_bytes;
+    const ProductSize none{}, weights{F, D, n, 1, 3, false, false}, input{n, D, F, 2, 1, false, false};
+    if (what == kPlanForward) {
+        f->gate = plan_rows(ProductSize{n, F, D, 1, 1, true, true}, type, cus, room);
+        f->out = plan_rows(ProductSize{n, D, F, 1, 1, false, false}, type, cus, room);
+    } else if (what == kPlanBack) {
+        f->back = plan_rows(ProductSize{n, F, D, 1, 1, false, true}, type, cus, room);
     } else {
-        plan(kBack, ProductSize{n, F, D, 1, 1, false});
-        plan(kInput, ProductSize{n, D, F, 2, 1, false});
-        plan(kWeights, ProductSize{F, D, n, 1, 3, false});
+        f->gradients[what - kPlanWeights] = what == kPlanBoth ? plan_launch(weights, input, type, cus, room)
+                                                              : plan_launch(what == kPlanWeights ? weights : input, none, type, cus, room);
     }
-    f->planned[backward] = n;
+    f->rows_of[what] = n;
 }
 
 }  // namespace
@@ -288,7 +381,7 @@ int ecrm_ffn_create(const ecrm_ffn_config *cfg, ecrm_ffn **out)
         f->off_du = take(cfg->max_rows * f->pitch * size);
         f->off_e = take(cfg->max_rows * f->e_pitch * size);
     }
-    f->counters = (cfg->dim + 15u) / 16u * 2u;
+    f->counters = (cfg->dim + 15u) / 16u * 2u > kCounters ? (cfg->dim + 15u) / 16u * 2u : kCounters;
     f->off_arrived = take(f->counters * 4u);
     f->part_bytes = kPartMost;
     f->off_part = take(f->part_bytes);
@@ -315,11 +408,11 @@ int ecrm_ffn_bind(ecrm_ffn *f, const void *gate, uint64_t gate_stride, const voi
     int dev = 0, cus = 0;
     if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus < 1)
         return ECRM_EHIP;
-    f->gate = gate; f->up = up; f->down = down;
+    f->gate_weights = gate; f->up = up; f->down = down;
     f->gate_stride = gate_stride; f->up_stride = up_stride; f->down_stride = down_stride;
     f->work = (char *)work;
     f->cus = cus;
-    f->planned[0] = f->planned[1] = 0;
+    memset(f->rows_of, 0, sizeof(f->rows_of));
     return ECRM_OK;
 }
 
@@ -347,27 +440,26 @@ int ecrm_ffn_forward(ecrm_ffn *f, const void *x, uint64_t x_stride, uint64_t n, 
     hipStream_t st = (hipStream_t)stream;
     void *h = f->work + f->off_h;
     a.part = (float *)(f->work + f->off_part);
-    make_plans(f, false, N);
+    make_plan(f, kPlanForward, N);
     a.arrived = (uint32_t *)(f->work + f->off_arrived);
     a.clear = f->counters;
     a.activation = f->cfg.activation;
-    a.products = 1;
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
-        a.p[0] = product(x, x_stride, f->gate, f->gate_stride, N, F, D);
+        a.p[0] = product(x, x_stride, f->gate_weights, f->gate_stride, N, F, D);
         a.p[0].b.p[1] = f->up;
         a.p[0].b.stride[1] = f->up_stride;
         a.p[0].out = h;
         a.p[0].out_stride = f->pitch;
         a.p[0].out2 = saved;
-        launch_product<T, kGate>(a, f->plan[kGate], f->cus, st);
+        launch_product<T, kGate>(a, f->gate, f->cus, st);
         a.p[0] = product(h, f->pitch, f->down, f->down_stride, N, D, F);
         a.p[0].out = out;
         a.p[0].out_stride = out_stride;
         a.p[0].in = residual;
         a.p[0].in_stride = residual_stride;
         a.masked = mask ? 1u : 0u;
-        launch_product<T, kOut>(a, f->plan[kOut], f->cus, st);
+        launch_product<T, kOut>(a, f->out, f->cus, st);
     });
     return launched();
 }
@@ -428,44 +520,53 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
         const int rc = ecrm_dropout(mask, d_out, d_out_stride, nullptr, 0, (void *)e, e_stride, type, n, D, stream);
         if (rc != ECRM_OK) return rc;
     }
-    make_plans(f, true, N);
+    // where d_x takes the place of what the weights' products read, it comes behind them
+    const bool both = weights && d_x && !(e == d_out && d_x == d_out);
+    make_plan(f, kPlanBack, N);
+    if (both) {
+        make_plan(f, kPlanBoth, N);
+    } else {
+        if (weights) make_plan(f, kPlanWeights, N);
+        if (d_x) make_plan(f, kPlanInput, N);
+    }
     a.activation = f->cfg.activation;
     a.accumulate = accumulate ? 1u : 0u;
     a.wide = weight_type == ECRM_F32 ? 1u : 0u;
+    a.arrived = (uint32_t *)(f->work + f->off_arrived);
+    a.clear = f->counters;
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
-        a.products = 1;
         a.p[0] = product(e, e_stride, f->down, f->down_stride, N, F, D);
         a.p[0].in = saved;
         a.p[0].out = dg;
         a.p[0].out2 = du;
         a.p[0].out3 = h;
         a.p[0].out_stride = f->pitch;
-        launch_product<T, kBack>(a, f->plan[kBack], f->cus, st);
-        if (weights) {
-            a.products = 3;
-            a.p[0] = product(dg, f->pitch, x, x_stride, F, D, N);
-            a.p[0].out = d_gate;
-            a.p[0].out_stride = D;
-            a.p[1] = product(du, f->pitch, x, x_stride, F, D, N);
-            a.p[1].out = d_up;
-            a.p[1].out_stride = D;
-            a.p[2] = product(e, e_stride, h, f->pitch, D, F, N);
-            a.p[2].out = d_down;
-            a.p[2].out_stride = F;
-            launch_product<T, kWeights>(a, f->plan[kWeights], f->cus, st);
-        }
-        if (d_x) {                        // last: it may take the place of d_out
-            a.products = 1;
-            a.p[0] = product(dg, f->pitch, f->gate, f->gate_stride, N, D, F);
-            a.p[0].a.p[1] = du;
-            a.p[0].b.p[1] = f->up;
-            a.p[0].b.stride[1] = f->up_stride;
-            a.p[0].in = add;
-            a.p[0].in_stride = add_stride;
-            a.p[0].out = d_x;
-            a.p[0].out_stride = d_x_stride;
-            launch_product<T, kInput>(a, f->plan[kInput], f->cus, st);
+        launch_product<T, kBack>(a, f->back, f->cus, st);
+        Product w[3], in;
+        w[0] = product(dg, f->pitch, x, x_stride, F, D, N);
+        w[0].out = d_gate;
+        w[1] = product(du, f->pitch, x, x_stride, F, D, N);
+        w[1].out = d_up;
+        w[2] = product(e, e_stride, h, f->pitch, D, F, N);
+        w[2].out = d_down;
+        w[0].out_stride = w[1].out_stride = D;
+        w[2].out_stride = F;
+        for (Product &p : w) p.kind = kWeights;
+        in = product(dg, f->pitch, f->gate_weights, f->gate_stride, N, D, F);
+        in.a.p[1] = du;
+        in.b.p[1] = f->up;
+        in.b.stride[1] = f->up_stride;
+        in.in = add;
+        in.in_stride = add_stride;
+        in.out = d_x;
+        in.out_stride = d_x_stride;
+        in.kind = kInput;
+        if (both) {
+            launch_gradients<T>(a, w, &in, f->gradients[kPlanBoth - kPlanWeights], st);
+        } else {
+            if (weights) launch_gradients<T>(a, w, nullptr, f->gradients[0], st);
+            if (d_x) launch_gradients<T>(a, nullptr, &in, f->gradients[kPlanInput - kPlanWeights], st);
         }
     });
     return launched();

@@ -43,25 +43,28 @@ struct Operand {
 struct Product {
     Operand a, b;              // a: M rows of the result, b: N columns
     uint32_t M, N, K;          // kInput: K of each half;  kGate: N of each projection
-    uint32_t tiles_m, tiles_n;
     void *out;
     uint64_t out_stride;
     const void *in;            // kOut: residual;  kInput: what is added;  kBack: saved g and u
     uint64_t in_stride;
     void *out2, *out3;         // kGate: saved g and u (or null);  kBack: du, h
+    uint32_t kind;             // kInput or kWeights, where they are worked off side by side
+    uint32_t tiles_m, tiles_n;
+    uint32_t splits, each;     // K tiles: cut into so many parts of at most so many
+    uint32_t first;            // workgroup of its first tile's first part
+    uint32_t part;             // of several parts: its first tile's first one in ProductArgs::part, in tiles;
+    uint32_t counter;          // its first tile's in ProductArgs::arrived
 };
 
 struct ProductArgs {
-    Product p[3];
-    uint32_t products, first[3];       // tile of each product's first
-    uint32_t tiles;                    // in all
-    uint32_t splits, each;             // K tiles: cut into so many parts of at most so many
-    float *part;                       // [tiles][splits][threads][..] where there are several
-    uint32_t *arrived;                 // few rows: [column blocks][row blocks] parts that are there
+    Product p[4];
+    uint32_t products, workgroups;
+    float *part;
+    uint32_t *arrived;                 // parts of a tile that are there
+    uint32_t clear;                    // so many of them are cleared by the first launch of a call, for those behind it
     uint32_t activation;
     uint32_t masked, first_row;        // row of the mask that row 0 of the results has
     MaskArgs mask;
-    uint32_t clear;                    // few rows: of the counters
     uint32_t accumulate, wide;         // kWeights: added to; in 32 bits whatever the type
 };
 
@@ -400,23 +403,18 @@ __device__ __forceinline__ void write_wide(const ProductArgs &a, const Product &
     }
 }
 
-// Which product and tile: the tiles of eight rows of tiles go column by column, so that those that run at one time share operands.
-__device__ __forceinline__ uint32_t find_tile(const ProductArgs &a, uint32_t tile, uint32_t &m, uint32_t &n)
+// Where tile t of a product lies: the tiles of eight rows of tiles go column by column, so that those that run at one time share operands.
+__device__ __forceinline__ void find_tile(const Product &p, uint32_t t, uint32_t &m, uint32_t &n)
 {
-    uint32_t which = 0;
-    if (a.products > 1 && tile >= a.first[1]) which = 1;
-    if (a.products > 2 && tile >= a.first[2]) which = 2;
-    const Product &p = a.p[which];
-    const uint32_t t = tile - a.first[which], group = 8u * p.tiles_n, g = scalar(t / group), in = t - g * group;
-    const uint32_t rows = min(8u, p.tiles_m - g * 8u);
+    const uint32_t group = 8u * p.tiles_n, g = scalar(t / group), in = t - g * group, rows = min(8u, p.tiles_m - g * 8u);
     n = scalar(in / rows);
     m = scalar(g * 8u + in - n * rows);
-    return which;
 }
 
 template <typename T, int KIND, int BM, int BN, int WM, int WN>
 struct Tiling {
     static constexpr bool kColumnsA = KIND == kWeights, kColumnsB = KIND == kBack || KIND == kInput || KIND == kWeights;
+    static constexpr bool kFirst = KIND == kGate || KIND == kBack;       // of the launches of a call
     static constexpr bool kDual = KIND == kGate;         // half of the columns of a wave are the gate's, half the up projection's
     static constexpr int kWaves = WM * WN, kThreads = kWaves * kWave;
     static constexpr int MB = BM / WM / 16, NB = BN / WN / 16, kNeed = kDual ? NB / 2 : NB;
@@ -517,23 +515,37 @@ struct Tiling {
     }
 };
 
+__device__ __forceinline__ void store_part(f32x4 *p, f32x4 v)
+{
+    const double2 d = __builtin_bit_cast(double2, v);
+    shared_store((double *)p, d.x);
+    shared_store((double *)p + 1, d.y);
+}
+__device__ __forceinline__ f32x4 load_part(const f32x4 *p)
+{
+    double2 d;
+    d.x = shared_load((const double *)p);
+    d.y = shared_load((const double *)p + 1);
+    return __builtin_bit_cast(f32x4, d);
+}
+
+// One part of K of one tile of product p; `local`: the workgroup's place among those of the product.
 template <typename T, int KIND, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM * WN * kWave, 2) void product_kernel(ProductArgs a)
+__device__ __forceinline__ void run_tile(const ProductArgs &a, const Product &p, uint32_t local, char *s_a0, char *s_b0, char *s_a1, char *s_b1)
 {
     typedef Tiling<T, KIND, BM, BN, WM, WN> L;
     constexpr int MB = L::MB, NB = L::NB, kWaves = L::kWaves;
-    __shared__ __align__(1024) char s_a0[BM * kRowBytes], s_b0[BN * kRowBytes], s_a1[BM * kRowBytes], s_b1[BN * kRowBytes];
     const uint32_t tid = threadIdx.x, wave = scalar(tid / kWave), wm = wave / WN, wn = wave % WN;
 
     // consecutive tiles on one XCD (workgroups go to the eight by turns), the parts of K one after the other
-    const uint32_t all = a.tiles * a.splits, per = all / 8u, more = all % 8u, xcd = blockIdx.x % 8u;
-    const uint32_t index = xcd * per + min(xcd, more) + blockIdx.x / 8u;
-    const uint32_t split = scalar(index / a.tiles), tile = index - split * a.tiles;
+    const uint32_t tiles = p.tiles_m * p.tiles_n, all = tiles * p.splits, per = all / 8u, more = all % 8u, xcd = local % 8u;
+    const uint32_t index = xcd * per + min(xcd, more) + local / 8u;
+    const uint32_t split = scalar(index / tiles), tile = index - split * tiles;
     uint32_t m, n;
-    const Product &p = a.p[find_tile(a, tile, m, n)];
+    find_tile(p, tile, m, n);
 
     const uint32_t K = p.K, half_tiles = (K + L::kElements - 1u) / L::kElements, k_tiles = KIND == kInput ? 2u * half_tiles : half_tiles;
-    const uint32_t begin = split * a.each, stop = min(begin + a.each, k_tiles);
+    const uint32_t begin = split * p.each, stop = min(begin + p.each, k_tiles);
 
     typedef Loader<T, L::kColumnsA, BM, kWaves, false> LoadA;
     typedef Loader<T, L::kColumnsB, BN, kWaves, L::kPair == 2> LoadB;
@@ -602,13 +614,40 @@ __global__ __launch_bounds__(WM * WN * kWave, 2) void product_kernel(ProductArgs
         if (t + 1u < stop) step(t + 1u, s_a1, s_b1, s_a0, s_b0);
     }
 
-    if (a.splits > 1u) {
-        f32x4 *to = (f32x4 *)a.part + ((uint64_t)tile * a.splits + split) * (MB * NB * L::kThreads) + tid;
+    if (p.splits > 1u) {
+        const uint64_t size = MB * NB * L::kThreads;     // of a part, in f32x4
+        f32x4 *parts = (f32x4 *)a.part + (uint64_t)(p.part + tile * p.splits) * size + tid;
+        if (L::kFirst) {                                 // joined by a launch of its own
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) parts[split * size + (i * NB + j) * L::kThreads] = acc[i][j];
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < MB; ++i)
 #pragma unroll
-            for (int j = 0; j < NB; ++j) to[(i * NB + j) * L::kThreads] = acc[i][j];
-        return;
+            for (int j = 0; j < NB; ++j) store_part(parts + split * size + (i * NB + j) * L::kThreads, acc[i][j]);
+        // the one that is there last joins them, in order
+        published();
+        __syncthreads();
+        uint32_t *s_last = (uint32_t *)s_a0;
+        if (tid == 0) {
+            const uint32_t before = __hip_atomic_fetch_add(a.arrived + p.counter + tile, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            *s_last = before + 1u == p.splits;
+            if (before + 1u == p.splits) __hip_atomic_store(a.arrived + p.counter + tile, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (!scalar(*s_last)) return;
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (uint32_t s = 0; s < p.splits; ++s)
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) acc[i][j] += load_part(parts + s * size + (i * NB + j) * L::kThreads);
     }
     MaskKey mask{};
     if (KIND == kOut && a.masked) mask = mask_key(a.mask);
@@ -631,7 +670,29 @@ __global__ __launch_bounds__(WM * WN * kWave, 2) void product_kernel(ProductArgs
     }
 }
 
-// Adds up what the parts of K gave, in order; a workgroup has a group of each of a tile's waves.
+template <typename T, int KIND, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * kWave, 2) void product_kernel(ProductArgs a)
+{
+    __shared__ __align__(1024) char s_a0[BM * kRowBytes], s_b0[BN * kRowBytes], s_a1[BM * kRowBytes], s_b1[BN * kRowBytes];
+    if (Tiling<T, KIND, BM, BN, WM, WN>::kFirst && blockIdx.x == 0)
+        for (uint32_t c = threadIdx.x; c < a.clear; c += blockDim.x) a.arrived[c] = 0u;
+    run_tile<T, KIND, BM, BN, WM, WN>(a, a.p[0], blockIdx.x, s_a0, s_b0, s_a1, s_b1);
+}
+
+// The gradients of x and of the weights side by side: products that do not wait for each other, the tiles that take longest first.
+template <typename T, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * kWave, 2) void gradients_kernel(ProductArgs a)
+{
+    __shared__ __align__(1024) char s_a0[BM * kRowBytes], s_b0[BN * kRowBytes], s_a1[BM * kRowBytes], s_b1[BN * kRowBytes];
+    uint32_t which = 0;
+#pragma unroll
+    for (uint32_t i = 1; i < 4; ++i) which = i < a.products && blockIdx.x >= a.p[i].first ? i : which;
+    const Product &p = a.p[which];
+    if (p.kind == kInput) run_tile<T, kInput, BM, BN, WM, WN>(a, p, blockIdx.x - p.first, s_a0, s_b0, s_a1, s_b1);
+    else run_tile<T, kWeights, BM, BN, WM, WN>(a, p, blockIdx.x - p.first, s_a0, s_b0, s_a1, s_b1);
+}
+
+// Adds up what the parts of K of a call's first product gave, in order; a workgroup has a group of each of a tile's waves.
 template <typename T, int KIND, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM * WN * kWave) void join_kernel(ProductArgs a)
 {
@@ -639,15 +700,16 @@ __global__ __launch_bounds__(WM * WN * kWave) void join_kernel(ProductArgs a)
     constexpr uint32_t NB = L::NB, MB = L::MB, W = L::kPair, N = L::kTogether * W;
     const uint32_t tile = blockIdx.x, i = blockIdx.y / L::kGroups, g = blockIdx.y % L::kGroups;
     uint32_t m, n;
-    const Product &p = a.p[find_tile(a, tile, m, n)];
-    const f32x4 *from = (const f32x4 *)a.part + (uint64_t)tile * a.splits * (MB * NB * L::kThreads) + (i * NB + g * N) * L::kThreads + threadIdx.x;
+    const Product &p = a.p[0];
+    find_tile(p, tile, m, n);
+    const f32x4 *from = (const f32x4 *)a.part + (uint64_t)tile * p.splits * (MB * NB * L::kThreads) + (i * NB + g * N) * L::kThreads + threadIdx.x;
     typename L::In in;
     L::fetch(a, p, m, n, i, g, in);
     f32x4 v[N], w[N];
 #pragma unroll
     for (uint32_t q = 0; q < N; ++q) v[q] = w[q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (uint32_t s = 0; s < a.splits; ++s) {
+    for (uint32_t s = 0; s < p.splits; ++s) {
         const f32x4 *part = from + (uint64_t)s * (MB * NB * L::kThreads);
 #pragma unroll
         for (uint32_t q = 0; q < N; ++q) {
@@ -739,22 +801,15 @@ __global__ __launch_bounds__(Skinny<XB>::kWaves * kWave) void skinny_kernel(Prod
         }
         if (KIND == kOut && gridDim.y > 1u) {
             const uint32_t slot = blockIdx.x * XB + r;
-            double *parts = (double *)a.part + ((uint64_t)slot * gridDim.y * kWave + lane) * 2u;
-            const double2 mine = __builtin_bit_cast(double2, v[0]);
-            shared_store(parts + blockIdx.y * kWave * 2u, mine.x);
-            shared_store(parts + blockIdx.y * kWave * 2u + 1u, mine.y);
+            f32x4 *parts = (f32x4 *)a.part + (uint64_t)slot * gridDim.y * kWave + lane;
+            store_part(parts + blockIdx.y * kWave, v[0]);
             published();
             uint32_t before = 0;
             if (lane == 0) before = __hip_atomic_fetch_add(a.arrived + slot, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             if (scalar(before) + 1u < gridDim.y) continue;
             v[0] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-            for (uint32_t s = 0; s < gridDim.y; ++s) {
-                double2 d;
-                d.x = shared_load(parts + s * kWave * 2u);
-                d.y = shared_load(parts + s * kWave * 2u + 1u);
-                v[0] += __builtin_bit_cast(f32x4, d);
-            }
+            for (uint32_t s = 0; s < gridDim.y; ++s) v[0] += load_part(parts + s * kWave);
         }
         MaskKey mask{};
         if (KIND == kOut && a.masked) mask = mask_key(a.mask);
