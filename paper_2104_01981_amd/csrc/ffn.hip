@@ -17,10 +17,10 @@ constexpr TilingCost kCosts[kTilings] = {{256, 1, {1.58, 0}, {1.58, 0}, 3.0, 8.0
                                          {64, 5, {0.50, 0.62}, {0.172, 0.46}, 2.5, 0.42}};
 constexpr uint32_t kSplitCounts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
 constexpr double kJoinLaunch = 3.0, kJoinRate = 4.0e6;       // parts of the first product of a call, by a launch of their own: us; bytes a us
-constexpr double kJoinWait = 1.5, kJoinOne = 1.0e5;          // others by the workgroup that is there last
+constexpr double kJoinWait = 2.0, kJoinOne = 2.5e4;          // others by the workgroup that is there last
 constexpr uint32_t kSkinnyParts = 16;
 constexpr size_t kPartMost = 32u << 20;          // bytes of the parts of split products, at most
-constexpr uint32_t kCounters = kPartMost / (64u * 64u * 4u);
+constexpr uint32_t kCounters = kPartMost / (2u * 64u * 64u * 4u);       // tiles of two parts or more
 
 struct Split { uint32_t splits, each; };
 // Products of one launch (the last of them with the splits of their own, where there are two sizes).
@@ -36,14 +36,18 @@ static uint64_t tiles_of(const ProductSize &z, uint32_t M, uint32_t side)
     return (uint64_t)((M + side - 1) / side) * ((z.N + columns - 1) / columns) * z.count;
 }
 
-// What a launch of A tiles that take ta and B that take tb (ta >= tb), one after the other on so many at a time, takes.
+// What a launch of A tiles that take ta and then B that take tb, so many at a time, takes.
 static double makespan(uint64_t A, double ta, uint64_t B, double tb, uint64_t slots)
 {
-    const uint64_t full = A / slots, busy = A % slots, idle = slots - busy;
-    double end = (double)(full + (busy ? 1 : 0)) * ta;
-    if (!B) return end;
-    const uint64_t beside = busy ? idle * (uint64_t)(ta / tb) : 0;       // done while the last of the others run
-    if (B > beside) end += (double)((B - beside + slots - 1) / slots) * tb;
+    // the places that have one of the first kind more than the others, and those others
+    uint64_t n[2] = {A % slots, slots - A % slots};
+    double at[2] = {(double)(A / slots + 1) * ta, (double)(A / slots) * ta}, end = n[0] ? at[0] : at[1];
+    while (B) {
+        const int g = n[0] && at[0] <= at[1] ? 0 : 1;
+        at[g] += tb;
+        if (at[g] > end) end = at[g];
+        B -= B < n[g] ? B : n[g];
+    }
     return end;
 }
 
@@ -94,22 +98,23 @@ static Plan plan_launch(const ProductSize &a, const ProductSize &b, uint32_t typ
     return best;
 }
 
-static RowPlan plan_rows(const ProductSize &z, uint32_t type, uint32_t cus, size_t room)
+// z's products with its rows cut where that is faster, those up to the cut beside the other size's (other.count = 0: alone).
+static RowPlan plan_rows(const ProductSize &other, const ProductSize &z, uint32_t type, uint32_t cus, size_t room)
 {
     const ProductSize none{};
-    auto plan = [&](uint32_t rows) {
+    auto plan = [&](uint32_t rows, bool beside) {
         ProductSize part = z;
         part.M = rows;
-        return plan_launch(part, none, type, cus, room);
+        return beside && other.count ? plan_launch(other, part, type, cus, room) : plan_launch(part, none, type, cus, room);
     };
-    RowPlan best{z.M, plan(z.M), Plan{}};
+    RowPlan best{z.M, plan(z.M, true), Plan{}};
     for (uint32_t side : {256u, 128u, 64u}) {
         // as many rows of tiles as fill the CUs to the last, or as are whole
         const uint64_t across = tiles_of(z, side, side), all = z.M / side, rounds = all * across / cus;
         for (uint64_t down : {rounds * cus / across, all}) {
             const uint32_t rows = (uint32_t)(down * side);
             if (!rows || rows >= z.M) continue;
-            const Plan main = plan(rows), rest = plan(z.M - rows);
+            const Plan main = plan(rows, true), rest = plan(z.M - rows, false);
             if (main.cost + rest.cost < best.main.cost + best.rest.cost) best = RowPlan{rows, main, rest};
         }
     }
@@ -177,7 +182,7 @@ static void launch_gradients(ProductArgs &a, hipStream_t st)
     hipLaunchKernelGGL((gradients_kernel<T, BM, BN, WM, WN>), dim3(a.workgroups), dim3(WM * WN * kWave), 0, st, a);
 }
 
-// The weights' products, x's, or both.
+// The weights' products, those of x, or both.
 template <typename T>
 static void launch_gradients(ProductArgs &a, const Product *weights, const Product *input, const Plan &plan, hipStream_t st)
 {
@@ -284,8 +289,8 @@ struct ecrm_ffn {
     int cus;
     // plans, kept while the number of rows stays, since making them takes some us
     uint64_t rows_of[kPlans];
-    RowPlan gate, out, back;
-    Plan gradients[3];
+    RowPlan gate, out, back, input, both;
+    Plan weights;
 };
 
 namespace {
@@ -344,13 +349,14 @@ void make_plan(ecrm_ffn *f, int what, uint32_t n)
     const size_t room = f->part_bytes;
     const ProductSize none{}, weights{F, D, n, 1, 3, false, false}, input{n, D, F, 2, 1, false, false};
     if (what == kPlanForward) {
-        f->gate = plan_rows(ProductSize{n, F, D, 1, 1, true, true}, type, cus, room);
-        f->out = plan_rows(ProductSize{n, D, F, 1, 1, false, false}, type, cus, room);
+        f->gate = plan_rows(none, ProductSize{n, F, D, 1, 1, true, true}, type, cus, room);
+        f->out = plan_rows(none, ProductSize{n, D, F, 1, 1, false, false}, type, cus, room);
     } else if (what == kPlanBack) {
-        f->back = plan_rows(ProductSize{n, F, D, 1, 1, false, true}, type, cus, room);
+        f->back = plan_rows(none, ProductSize{n, F, D, 1, 1, false, true}, type, cus, room);
+    } else if (what == kPlanWeights) {
+        f->weights = plan_launch(weights, none, type, cus, room);
     } else {
-        f->gradients[what - kPlanWeights] = what == kPlanBoth ? plan_launch(weights, input, type, cus, room)
-                                                              : plan_launch(what == kPlanWeights ? weights : input, none, type, cus, room);
+        (what == kPlanBoth ? f->both : f->input) = plan_rows(what == kPlanBoth ? weights : none, input, type, cus, room);
     }
     f->rows_of[what] = n;
 }
@@ -562,11 +568,18 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
         in.out = d_x;
         in.out_stride = d_x_stride;
         in.kind = kInput;
-        if (both) {
-            launch_gradients<T>(a, w, &in, f->gradients[kPlanBoth - kPlanWeights], st);
-        } else {
-            if (weights) launch_gradients<T>(a, w, nullptr, f->gradients[0], st);
-            if (d_x) launch_gradients<T>(a, nullptr, &in, f->gradients[kPlanInput - kPlanWeights], st);
+        const RowPlan &rows = both ? f->both : f->input;
+        if (weights && !both) launch_gradients<T>(a, w, nullptr, f->weights, st);
+        if (d_x) {
+            in.M = rows.rows;
+            launch_gradients<T>(a, both ? w : nullptr, &in, rows.main, st);
+            if (rows.rows < N) {
+                a.p[0] = in;
+                a.p[0].M = N;
+                skip_rows<T, kInput>(a, rows.rows);
+                in = a.p[0];
+                launch_gradients<T>(a, nullptr, &in, rows.rest, st);
+            }
         }
     });
     return launched();
