@@ -290,10 +290,13 @@ class Dropout:
     def apply(self, x, out, residual=None, stream=None, check=True):
         """out = residual + dropout(x); the gradient of x is apply(gradient of out).  x, out, residual: [rows, cols] of fp32, bf16 or
         fp16, rows at any multiple of 4 elements from each other; out may be x or residual."""
-        assert _is_rows(x, x.shape[0], x.shape[-1], x.dtype) and _is_rows(out, x.shape[0], x.shape[1], x.dtype)
-        assert residual is None or _is_rows(residual, x.shape[0], x.shape[1], x.dtype)
-        rc = self._lib.ecrm_dropout(self.mask, x.data_ptr(), _row(x), *_optional(residual), out.data_ptr(), _row(out), _type(x),
-                                    x.shape[0], x.shape[1], _stream(stream))
+        shape, t = x.shape, x.dtype
+        assert x.is_cuda and out.is_cuda and len(shape) == 2 and out.shape == shape and out.dtype == t
+        rows, cols = shape
+        assert rows == 0 or cols < 2 or (x.stride(1) == 1 and out.stride(1) == 1)
+        assert residual is None or _is_rows(residual, rows, cols, t)
+        rc = self._lib.ecrm_dropout(self.mask, x.data_ptr(), _row(x), *_optional(residual), out.data_ptr(), _row(out), _type(x), rows, cols,
+                                    _stream(stream))
         if check and rc != ECRM_OK:
             raise EcrmError(rc, "ecrm_dropout")
         return rc

@@ -8,23 +8,27 @@
 namespace ecrm {
 
 // ---- which tiles -----------------------------------------------------------------------------------------------------------------
-// What a product takes is estimated in us from what was measured (M, N of 1024 to 4096, all CUs in step): a tile's steps of 128 bytes of
+// What a product takes is estimated in us from what was measured (M, N of 512 to 4096, all CUs in step): a tile's steps of 128 bytes of
 // K, alone on its CU and for each of several; the launch, a tile's begin and end.  16 bits: 64 x 64 0.50 and 0.17 a step, 128 x 128 0.65
-// and 0.47, 256 x 256 1.58; 32 bits: 0.62 and 0.46, 1.96 and 1.79 (256 x 256 is 7.2 and gains nothing).
-enum { kTile256 = 0, kTile128 = 1, kTile64 = 2, kTilings = 3 };
-struct TilingCost { uint32_t side, resident; double step[2], shared[2], launch, tile; };          // [0] 16 bits, [1] 32
+// and 0.47, 256 x 256 1.58.  32 bits are bound by their matrix instructions, 137 TFLOP/s with any of these and all CUs full, so that small
+// tiles, more of them to a CU, gain: 32 x 32 0.24 and 0.12, 64 x 64 0.62 and 0.46, 128 x 128 1.96 and 1.79 (777 rows, D = 260, F =
+// 684: 26 us with 64 x 64 at least, 19 so).
+enum { kTile256 = 0, kTile128 = 1, kTile64 = 2, kTile32 = 3, kTilings = 4 };
+struct TilingCost { uint32_t side, resident; double step[2], shared[2], launch, tile; };          // [0] 16 bits, [1] 32; 0: not for these
 constexpr TilingCost kCosts[kTilings] = {{256, 1, {1.58, 0}, {1.58, 0}, 3.0, 8.0}, {128, 2, {0.65, 1.96}, {0.47, 1.79}, 5.0, 1.4},
-                                         {64, 5, {0.50, 0.62}, {0.172, 0.46}, 2.5, 0.42}};
+                                         {64, 5, {0.50, 0.62}, {0.172, 0.46}, 2.5, 0.42}, {32, 8, {0, 0.24}, {0, 0.12}, 2.5, 0.3}};
+// Columns of a tile; of each projection for kGate.
+static constexpr uint32_t columns_of(uint32_t side, bool dual) { return dual && side > 32 ? side / 2u : side; }
 constexpr uint32_t kSplitCounts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
 constexpr double kJoinLaunch = 3.0, kJoinRate = 4.0e6;       // parts of the first product of a call, by a launch of their own: us; bytes a us
 constexpr double kJoinWait = 2.0, kJoinOne = 2.5e4;          // others by the workgroup that is there last
 constexpr uint32_t kSkinnyParts = 16;
 constexpr size_t kPartMost = 32u << 20;          // bytes of the parts of split products, at most
-constexpr uint32_t kCounters = kPartMost / (2u * 64u * 64u * 4u);       // tiles of two parts or more
+constexpr uint32_t kCounters = kPartMost / (2u * 32u * 32u * 4u);       // tiles of two parts or more
 
 struct Split { uint32_t splits, each; };
 // Products of one launch (the last of them with the splits of their own, where there are two sizes).
-struct Plan { uint32_t tiling; Split split[2]; double cost; };
+struct Plan { uint32_t tiling; Split split[2]; uint32_t counters; double cost; };
 // Rows up to `rows` of the results with one tiling, the others (if there are any) with another.
 struct RowPlan { uint32_t rows; Plan main, rest; };
 
@@ -32,7 +36,7 @@ struct ProductSize { uint32_t M, N, K, halves, count; bool dual, first; };      
 
 static uint64_t tiles_of(const ProductSize &z, uint32_t M, uint32_t side)
 {
-    const uint32_t columns = z.dual ? side / 2u : side;
+    const uint32_t columns = columns_of(side, z.dual);
     return (uint64_t)((M + side - 1) / side) * ((z.N + columns - 1) / columns) * z.count;
 }
 
@@ -57,8 +61,9 @@ static Plan plan_launch(const ProductSize &a, const ProductSize &b, uint32_t typ
     const uint32_t wide = type == ECRM_F32 ? 1u : 0u, elements = kRowBytes / type_bytes(type);
     const ProductSize *sizes[2] = {&a, &b};
     Plan best{};
-    for (uint32_t t = wide ? kTile128 : kTile256; t < kTilings; ++t) {
+    for (uint32_t t = 0; t < kTilings; ++t) {
         const TilingCost &c = kCosts[t];
+        if (c.step[wide] == 0.0) continue;
         uint64_t tiles[2];
         uint32_t k_tiles[2];
         for (int i = 0; i < 2; ++i) {
@@ -91,7 +96,8 @@ static Plan plan_launch(const ProductSize &a, const ProductSize &b, uint32_t typ
                 double cost = c.launch + (ua >= ub ? makespan(tiles[0] * x.splits, ua, tiles[1] * y.splits, ub, slots)
                                                    : makespan(tiles[1] * y.splits, ub, tiles[0] * x.splits, ua, slots));
                 if (a.first && x.splits > 1) cost += kJoinLaunch + 2.0 * a_bytes / kJoinRate;
-                if (!best.split[0].splits || cost < best.cost) best = Plan{t, {x, y}, cost};
+                const uint64_t counters = (x.splits > 1 ? tiles[0] : 0) + (y.splits > 1 ? tiles[1] : 0);
+                if (!best.split[0].splits || cost < best.cost) best = Plan{t, {x, y}, (uint32_t)counters, cost};
             }
         }
     }
@@ -166,6 +172,13 @@ static void launch_planned(ProductArgs &a, const Plan &plan, hipStream_t st)
             return;
         }
     }
+    if constexpr (sizeof(T) == 4) {
+        if (plan.tiling == kTile32) {
+            if constexpr (KIND == kGate) launch_tiling<T, KIND, 32, 64, 2, 2>(a, st);
+            else launch_tiling<T, KIND, 32, 32, 2, 2>(a, st);
+            return;
+        }
+    }
     if (plan.tiling == kTile128) {
         if constexpr (KIND == kGate) launch_tiling<T, KIND, 128, 128, 4, 1>(a, st);
         else launch_tiling<T, KIND, 128, 128, 2, 2>(a, st);
@@ -205,6 +218,8 @@ static void launch_gradients(ProductArgs &a, const Product *weights, const Produ
     }
     if constexpr (sizeof(T) == 2)
         if (plan.tiling == kTile256) return launch_gradients<T, 256, 256, 2, 4>(a, st);
+    if constexpr (sizeof(T) == 4)
+        if (plan.tiling == kTile32) return launch_gradients<T, 32, 32, 2, 2>(a, st);
     if (plan.tiling == kTile128) launch_gradients<T, 128, 128, 2, 2>(a, st);
     else launch_gradients<T, 64, 64, 2, 2>(a, st);
 }
@@ -229,31 +244,39 @@ static void skip_rows(ProductArgs &a, uint32_t first)
     p.M -= first;
 }
 
-// Up to 32 rows, of 32 bits up to 16, see skinny_kernel.  us forward so / by tiles, 16 and 32 rows: bf16 D = 128, F = 512 6.8 / 8.7, 8.2 /
+// Up to 32 rows, of 32 bits up to 16, are skinny_kernel's.  us forward so / by tiles, 16 and 32 rows: bf16 D = 128, F = 512 6.8 / 8.7, 8.2 /
 // 8.7; 1024, 1024 9.2 / 14.5, 11.5 / 14.6; 1024, 4096 15.1 / 19.8, 20.1 / 19.8.  fp32 8.0 / 12.6, 10.0 / 12.7; 15.2 / 21.4, 23.5 / 21.3;
 // 29.2 / 31.5, 44.3 / 31.4.
+static uint32_t skinny_waves(uint32_t K, uint32_t type)        // that have kAtOnce steps each
+{
+    const uint32_t steps = (K * type_bytes(type) + 63u) / 64u;
+    return (steps + kAtOnce - 1u) / kAtOnce;
+}
+static uint32_t skinny_parts(uint32_t N, uint32_t K, uint32_t type, uint32_t cus)
+{
+    const uint32_t blocks = (N + 15u) / 16u, fit = cus / blocks, fill = skinny_waves(K, type) / 8u;
+    const uint32_t parts = fit < fill ? fit : fill;      // no more workgroups than CUs, eight waves at least to each
+    return parts < 1u ? 1u : parts > kSkinnyParts ? kSkinnyParts : parts;
+}
+static bool is_skinny(uint32_t rows, uint32_t type) { return rows <= (type == ECRM_F32 ? 16u : 32u); }
+
 template <typename T, int KIND, int XB>
-static void launch_skinny(ProductArgs &a, uint32_t cus, hipStream_t st)
+static void launch_skinny(ProductArgs &a, uint32_t type, uint32_t cus, hipStream_t st)
 {
     const Product &p = a.p[0];
-    const uint32_t blocks = (p.N + 15u) / 16u, steps = (p.K * (uint32_t)sizeof(T) + 63u) / 64u, wanted = (steps + kAtOnce - 1u) / kAtOnce;
-    uint32_t parts = 1;
-    if (KIND == kOut && blocks < cus) {                  // no more workgroups than CUs, eight waves at least to each
-        const uint32_t fit = cus / blocks, fill = wanted / 8u;
-        parts = fit < fill ? fit : fill;
-        parts = parts < 1u ? 1u : parts > kSkinnyParts ? kSkinnyParts : parts;
-    }
-    const uint32_t share = (wanted + parts - 1u) / parts, waves = share < Skinny<XB>::kWaves ? share : Skinny<XB>::kWaves;
-    hipLaunchKernelGGL((skinny_kernel<T, KIND, XB>), dim3(blocks, parts), dim3(waves * kWave), 0, st, a);
+    const uint32_t parts = KIND == kOut ? skinny_parts(p.N, p.K, type, cus) : 1u, share = (skinny_waves(p.K, type) + parts - 1u) / parts;
+    const uint32_t waves = share < Skinny<XB>::kWaves ? share : Skinny<XB>::kWaves;
+    hipLaunchKernelGGL((skinny_kernel<T, KIND, XB>), dim3((p.N + 15u) / 16u, parts), dim3(waves * kWave), 0, st, a);
 }
 
 template <typename T, int KIND>
-static void launch_product(ProductArgs &a, const RowPlan &plan, int cus, hipStream_t st)
+static void launch_product(ProductArgs &a, const RowPlan &plan, uint32_t type, uint32_t cus, hipStream_t st)
 {
     if constexpr (KIND == kGate || KIND == kOut) {
-        if (a.p[0].M <= 16) return launch_skinny<T, KIND, 1>(a, (uint32_t)cus, st);
-        if constexpr (sizeof(T) == 2)
-            if (a.p[0].M <= 32) return launch_skinny<T, KIND, 2>(a, (uint32_t)cus, st);
+        if (is_skinny(a.p[0].M, type)) {
+            if (a.p[0].M <= 16) return launch_skinny<T, KIND, 1>(a, type, cus, st);
+            if constexpr (sizeof(T) == 2) return launch_skinny<T, KIND, 2>(a, type, cus, st);
+        }
     }
     const uint32_t M = a.p[0].M;
     a.first_row = 0;
@@ -282,7 +305,6 @@ struct ecrm_ffn {
     uint64_t pitch;                       // elements of a row of h, dg, du
     uint64_t e_pitch;                     // of a row of e
     size_t off_h, off_dg, off_du, off_e, off_arrived, off_part, part_bytes, bytes;
-    uint32_t counters;
     const void *gate_weights, *up, *down;
     uint64_t gate_stride, up_stride, down_stride;
     char *work;
@@ -342,6 +364,8 @@ Product product(const void *a, uint64_t a_stride, const void *b, uint64_t b_stri
     return p;
 }
 
+uint32_t counters_of(const RowPlan &p) { return p.main.counters > p.rest.counters ? p.main.counters : p.rest.counters; }
+
 void make_plan(ecrm_ffn *f, int what, uint32_t n)
 {
     if (f->rows_of[what] == n) return;
@@ -387,8 +411,7 @@ int ecrm_ffn_create(const ecrm_ffn_config *cfg, ecrm_ffn **out)
         f->off_du = take(cfg->max_rows * f->pitch * size);
         f->off_e = take(cfg->max_rows * f->e_pitch * size);
     }
-    f->counters = (cfg->dim + 15u) / 16u * 2u > kCounters ? (cfg->dim + 15u) / 16u * 2u : kCounters;
-    f->off_arrived = take(f->counters * 4u);
+    f->off_arrived = take(((cfg->dim + 15u) / 16u * 2u > kCounters ? (cfg->dim + 15u) / 16u * 2u : kCounters) * 4u);
     f->part_bytes = kPartMost;
     f->off_part = take(f->part_bytes);
     f->bytes = off;
@@ -448,7 +471,7 @@ int ecrm_ffn_forward(ecrm_ffn *f, const void *x, uint64_t x_stride, uint64_t n, 
     a.part = (float *)(f->work + f->off_part);
     make_plan(f, kPlanForward, N);
     a.arrived = (uint32_t *)(f->work + f->off_arrived);
-    a.clear = f->counters;
+    a.clear = is_skinny(N, type) ? (skinny_parts(D, F, type, (uint32_t)f->cus) > 1 ? (D + 15u) / 16u * 2u : 0u) : counters_of(f->out);
     a.activation = f->cfg.activation;
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
@@ -458,14 +481,14 @@ int ecrm_ffn_forward(ecrm_ffn *f, const void *x, uint64_t x_stride, uint64_t n, 
         a.p[0].out = h;
         a.p[0].out_stride = f->pitch;
         a.p[0].out2 = saved;
-        launch_product<T, kGate>(a, f->gate, f->cus, st);
+        launch_product<T, kGate>(a, f->gate, type, (uint32_t)f->cus, st);
         a.p[0] = product(h, f->pitch, f->down, f->down_stride, N, D, F);
         a.p[0].out = out;
         a.p[0].out_stride = out_stride;
         a.p[0].in = residual;
         a.p[0].in_stride = residual_stride;
         a.masked = mask ? 1u : 0u;
-        launch_product<T, kOut>(a, f->out, f->cus, st);
+        launch_product<T, kOut>(a, f->out, type, (uint32_t)f->cus, st);
     });
     return launched();
 }
@@ -539,7 +562,9 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
     a.accumulate = accumulate ? 1u : 0u;
     a.wide = weight_type == ECRM_F32 ? 1u : 0u;
     a.arrived = (uint32_t *)(f->work + f->off_arrived);
-    a.clear = f->counters;
+    a.clear = both ? counters_of(f->both) : 0u;
+    if (!both && weights) a.clear = f->weights.counters;
+    if (!both && d_x && counters_of(f->input) > a.clear) a.clear = counters_of(f->input);
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
         a.p[0] = product(e, e_stride, f->down, f->down_stride, N, F, D);
@@ -548,7 +573,7 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
         a.p[0].out2 = du;
         a.p[0].out3 = h;
         a.p[0].out_stride = f->pitch;
-        launch_product<T, kBack>(a, f->back, f->cus, st);
+        launch_product<T, kBack>(a, f->back, type, (uint32_t)f->cus, st);
         Product w[3], in;
         w[0] = product(dg, f->pitch, x, x_stride, F, D, N);
         w[0].out = d_gate;

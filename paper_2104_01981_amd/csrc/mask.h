@@ -26,6 +26,8 @@ __device__ __forceinline__ MaskKey mask_key(const MaskArgs &a)
     return MaskKey{(uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)number, (uint32_t)(number >> 32), a.border, a.factor};
 }
 
+__device__ __forceinline__ uint32_t xor3(uint32_t x, uint32_t y, uint32_t z) { return __builtin_amdgcn_bitop3_b32(x, y, z, 0x96); }
+
 // the 128 bits of columns 8 * block .. 8 * block + 7
 __device__ __forceinline__ uint4 mask_block(const MaskKey &k, uint32_t row, uint32_t block)
 {
@@ -33,7 +35,7 @@ __device__ __forceinline__ uint4 mask_block(const MaskKey &k, uint32_t row, uint
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
         const uint64_t a = (uint64_t)x * 0xD2511F53u, b = (uint64_t)z * 0xCD9E8D57u;
-        const uint32_t nx = (uint32_t)(b >> 32) ^ y ^ s0, nz = (uint32_t)(a >> 32) ^ w ^ s1;
+        const uint32_t nx = xor3((uint32_t)(b >> 32), y, s0), nz = xor3((uint32_t)(a >> 32), w, s1);
         x = nx;
         y = (uint32_t)b;
         z = nz;

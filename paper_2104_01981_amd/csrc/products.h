@@ -160,7 +160,7 @@ struct Loader {
 #pragma unroll
             for (uint32_t i = 0; i < kLoads; ++i) {
                 const uint32_t byte = (load + i) * 1024u + lane * 16u, row = byte / kBytes, chunk = byte % kBytes / 16u;
-                const uint32_t by = sizeof(T) == 2 ? (((row & 3u) | (row >> 3 & 1u) << 2) & (kBytes / 32u - 1u)) << 1 : (row >> 2 & 3u) << 2;
+                const uint32_t by = sizeof(T) == 2 ? (((row & 3u) | (row >> 3 & 1u) << 2) & (kBytes / 32u - 1u)) << 1 : (row >> 2 & 3u & (kBytes / 64u - 1u)) << 2;
                 at[i] = row * stride + (chunk ^ by) * 16u;
             }
         }
@@ -229,7 +229,7 @@ __device__ __forceinline__ void read_fragments(const char *tile, uint32_t first,
         constexpr uint32_t kBytes = ROWS * sizeof(T);
 #pragma unroll
         for (int b = 0; b < N; ++b) {
-            const char *p = tile + (s * 16u + q * 4u) * kBytes + (((first + b) ^ q) * 64u) + i * 4u;
+            const char *p = tile + (s * 16u + q * 4u) * kBytes + (((first + b) ^ (q & (kBytes / 64u - 1u))) * 64u) + i * 4u;
 #pragma unroll
             for (int j = 0; j < 4; ++j) f[b][j] = *(const uint32_t *)(p + j * (int)kBytes);
         }
