@@ -338,7 +338,7 @@ int ecrm_embed_grad_dense_dropout(ecrm_ctx *ctx, const uint64_t *keys, const voi
  *     e = drop(d),  b = e Wd,  dg = b * u * act'(g),  du = b * act(g),
  *     d_x = add + dg Wg + du Wu,  d_gate = dg^T x,  d_up = du^T x,  d_down = e^T h.
  * act: ECRM_SILU g / (1 + e^-g), ECRM_GELU g (1 + erf(g / sqrt 2)) / 2, ECRM_RELU max(g, 0) with the derivative 0 at 0.
- * Sums are formed in fp32, in an order that follows from the sizes alone; in 16-bit types h, dg, du and e are rounded to the type
+ * Sums are formed in fp32, in an order that follows from the sizes alone; in 16-bit types h, dg and du are rounded to the type
  * between the products, and so are the saved g and u.  Needs no ecrm_ctx.
  *
  * ecrm_ffn_create    checks the configuration and makes a host-side handle (destroy it with ecrm_ffn_destroy; NULL is allowed).

@@ -86,6 +86,38 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(DropArgs a)
     }
 }
 
+void launch_dropout(MaskArgs mask, const void *x, uint64_t x_stride, const void *residual, uint64_t residual_stride, void *out, uint64_t out_stride,
+                    uint32_t type, uint64_t rows, uint32_t cols, hipStream_t st)
+{
+    DropArgs a{};
+    const uint32_t size = type_bytes(type);
+    a.mask = mask;
+    a.cols = cols;
+    a.x_stride = x_stride; a.residual_stride = residual_stride; a.out_stride = out_stride;
+    const uint32_t blocks = (cols + 7u) / 8u;
+    a.blocks = make_divider(blocks);
+    auto wide_rows = [&](const void *p, uint64_t stride) { return (uintptr_t)p % 16 == 0 && stride * size % 16 == 0; };
+    const bool wide = cols % 8 == 0 && wide_rows(x, x_stride) && wide_rows(out, out_stride) && (!residual || wide_rows(residual, residual_stride));
+    const uint64_t slice = kDropUnits / blocks;
+    for (uint64_t at = 0; at < rows; at += slice) {
+        const uint64_t cnt = rows - at < slice ? rows - at : slice;
+        a.first_row = (uint32_t)at;
+        a.units = (uint32_t)(cnt * blocks);
+        a.x = (const char *)x + at * x_stride * size;
+        a.residual = residual ? (const char *)residual + at * residual_stride * size : nullptr;
+        a.out = (char *)out + at * out_stride * size;
+        const uint32_t most = 256u * 8u, wanted = (a.units + kDropThreads - 1) / kDropThreads;
+        const dim3 grid(wanted < most ? wanted : most), threads(kDropThreads);
+        with_type(type, [&](auto t) {
+            typedef decltype(t) T;
+            if (wide && residual) hipLaunchKernelGGL((dropout_kernel<T, true, true>), grid, threads, 0, st, a);
+            else if (wide) hipLaunchKernelGGL((dropout_kernel<T, true, false>), grid, threads, 0, st, a);
+            else if (residual) hipLaunchKernelGGL((dropout_kernel<T, false, true>), grid, threads, 0, st, a);
+            else hipLaunchKernelGGL((dropout_kernel<T, false, false>), grid, threads, 0, st, a);
+        });
+    }
+}
+
 bool make_mask(const ecrm_mask *mask, MaskArgs &to, double &factor)
 {
     if (!mask->state || (uintptr_t)mask->state % 8 || !(mask->p >= 0.0 && mask->p <= 1.0)) return false;
@@ -142,30 +174,6 @@ extern "C" int ecrm_dropout(const ecrm_mask *mask, const void *x, uint64_t x_str
     if (!same_or_apart(x, x_stride) || (residual && !same_or_apart(residual, residual_stride)) ||
         !strided_apart(mask->state, 1, 16, 16, out, rows, row, out_stride * size))
         return ECRM_EINVAL;
-    a.cols = cols;
-    a.x_stride = x_stride; a.residual_stride = residual_stride; a.out_stride = out_stride;
-    const uint32_t blocks = (cols + 7u) / 8u;
-    a.blocks = make_divider(blocks);
-    auto wide_rows = [&](const void *p, uint64_t stride) { return (uintptr_t)p % 16 == 0 && stride * size % 16 == 0; };
-    const bool wide = cols % 8 == 0 && wide_rows(x, x_stride) && wide_rows(out, out_stride) && (!residual || wide_rows(residual, residual_stride));
-    const uint64_t slice = kDropUnits / blocks;
-    for (uint64_t at = 0; at < rows; at += slice) {
-        const uint64_t cnt = rows - at < slice ? rows - at : slice;
-        a.first_row = (uint32_t)at;
-        a.units = (uint32_t)(cnt * blocks);
-        a.x = (const char *)x + at * x_stride * size;
-        a.residual = residual ? (const char *)residual + at * residual_stride * size : nullptr;
-        a.out = (char *)out + at * out_stride * size;
-        const uint32_t most = 256u * 8u, wanted = (a.units + kDropThreads - 1) / kDropThreads;
-        const dim3 grid(wanted < most ? wanted : most), threads(kDropThreads);
-        with_type(type, [&](auto t) {
-            typedef decltype(t) T;
-            hipStream_t st = (hipStream_t)stream;
-            if (wide && residual) hipLaunchKernelGGL((dropout_kernel<T, true, true>), grid, threads, 0, st, a);
-            else if (wide) hipLaunchKernelGGL((dropout_kernel<T, true, false>), grid, threads, 0, st, a);
-            else if (residual) hipLaunchKernelGGL((dropout_kernel<T, false, true>), grid, threads, 0, st, a);
-            else hipLaunchKernelGGL((dropout_kernel<T, false, false>), grid, threads, 0, st, a);
-        });
-    }
+    launch_dropout(a.mask, x, x_stride, residual, residual_stride, out, out_stride, type, rows, cols, (hipStream_t)stream);
     return hipGetLastError() == hipSuccess ? ECRM_OK : ECRM_EHIP;
 }

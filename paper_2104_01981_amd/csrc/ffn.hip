@@ -9,14 +9,14 @@ namespace ecrm {
 
 // ---- which tiles -----------------------------------------------------------------------------------------------------------------
 // What a product takes is estimated in us from what was measured (M, N of 512 to 4096, all CUs in step): a tile's steps of 128 bytes of
-// K, alone on its CU and for each of several; the launch, a tile's begin and end.  16 bits: 64 x 64 0.50 and 0.17 a step, 128 x 128 0.65
+// K, alone on its CU and for each of several (times `transposed` for the gradients in 16 bits); the launch, a tile's begin and end.  16 bits: 64 x 64 0.50 and 0.17 a step, 128 x 128 0.65
 // and 0.47, 256 x 256 1.58.  32 bits are bound by their matrix instructions, 137 TFLOP/s with any of these and all CUs full, so that small
 // tiles, more of them to a CU, gain: 32 x 32 0.24 and 0.12, 64 x 64 0.62 and 0.46, 128 x 128 1.96 and 1.79 (777 rows, D = 260, F =
 // 684: 26 us with 64 x 64 at least, 19 so).
 enum { kTile256 = 0, kTile128 = 1, kTile64 = 2, kTile32 = 3, kTilings = 4 };
-struct TilingCost { uint32_t side, resident; double step[2], shared[2], launch, tile; };          // [0] 16 bits, [1] 32; 0: not for these
-constexpr TilingCost kCosts[kTilings] = {{256, 1, {1.58, 0}, {1.58, 0}, 3.0, 8.0}, {128, 2, {0.65, 1.96}, {0.47, 1.79}, 5.0, 1.4},
-                                         {64, 5, {0.50, 0.62}, {0.172, 0.46}, 2.5, 0.42}, {32, 8, {0, 0.24}, {0, 0.12}, 2.5, 0.3}};
+struct TilingCost { uint32_t side, resident; double step[2], shared[2], transposed, launch, tile; };      // [0] 16 bits, [1] 32; 0: not for these
+constexpr TilingCost kCosts[kTilings] = {{256, 1, {1.58, 0}, {1.58, 0}, 1.0, 3.0, 8.0}, {128, 2, {0.65, 1.96}, {0.47, 1.79}, 1.06, 5.0, 1.4},
+                                         {64, 5, {0.50, 0.62}, {0.172, 0.46}, 1.25, 2.5, 0.42}, {32, 8, {0, 0.24}, {0, 0.12}, 1.0, 2.5, 0.3}};
 // Columns of a tile; of each projection for kGate.
 static constexpr uint32_t columns_of(uint32_t side, bool dual) { return dual && side > 32 ? side / 2u : side; }
 constexpr uint32_t kSplitCounts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
@@ -32,7 +32,7 @@ struct Plan { uint32_t tiling; Split split[2]; uint32_t counters; double cost; }
 // Rows up to `rows` of the results with one tiling, the others (if there are any) with another.
 struct RowPlan { uint32_t rows; Plan main, rest; };
 
-struct ProductSize { uint32_t M, N, K, halves, count; bool dual, first; };       // `count` of them
+struct ProductSize { uint32_t M, N, K, halves, count; bool dual, first, gradients; };       // `count` of them
 
 static uint64_t tiles_of(const ProductSize &z, uint32_t M, uint32_t side)
 {
@@ -87,7 +87,8 @@ static Plan plan_launch(const ProductSize &a, const ProductSize &b, uint32_t typ
                 if (bytes > (double)room) break;
                 const uint64_t units = tiles[0] * x.splits + tiles[1] * y.splits, there = (units + cus - 1) / cus;
                 const double together = there < c.resident ? (double)there : (double)c.resident;
-                const double step = c.shared[wide] * together > c.step[wide] ? c.shared[wide] * together : c.step[wide];
+                const double shared = c.shared[wide] * together * (a.gradients && !wide ? c.transposed : 1.0);
+                const double step = shared > c.step[wide] ? shared : c.step[wide];
                 auto unit = [&](int i, const Split &s) {
                     return c.tile * together + s.each * step + (s.splits > 1 && !sizes[i]->first ? kJoinWait + s.splits * part / kJoinOne : 0.0);
                 };
@@ -361,6 +362,7 @@ Product product(const void *a, uint64_t a_stride, const void *b, uint64_t b_stri
     p.b.p[0] = p.b.p[1] = b;
     p.b.stride[0] = p.b.stride[1] = b_stride;
     p.M = M; p.N = N; p.K = K;
+    p.scale = 1.0f;
     return p;
 }
 
@@ -371,12 +373,12 @@ void make_plan(ecrm_ffn *f, int what, uint32_t n)
     if (f->rows_of[what] == n) return;
     const uint32_t D = f->cfg.dim, F = f->cfg.hidden, type = f->cfg.type, cus = (uint32_t)f->cus;
     const size_t room = f->part_bytes;
-    const ProductSize none{}, weights{F, D, n, 1, 3, false, false}, input{n, D, F, 2, 1, false, false};
+    const ProductSize none{}, weights{F, D, n, 1, 3, false, false, true}, input{n, D, F, 2, 1, false, false, true};
     if (what == kPlanForward) {
-        f->gate = plan_rows(none, ProductSize{n, F, D, 1, 1, true, true}, type, cus, room);
-        f->out = plan_rows(none, ProductSize{n, D, F, 1, 1, false, false}, type, cus, room);
+        f->gate = plan_rows(none, ProductSize{n, F, D, 1, 1, true, true, false}, type, cus, room);
+        f->out = plan_rows(none, ProductSize{n, D, F, 1, 1, false, false, false}, type, cus, room);
     } else if (what == kPlanBack) {
-        f->back = plan_rows(none, ProductSize{n, F, D, 1, 1, false, true}, type, cus, room);
+        f->back = plan_rows(none, ProductSize{n, F, D, 1, 1, false, true, false}, type, cus, room);
     } else if (what == kPlanWeights) {
         f->weights = plan_launch(weights, none, type, cus, room);
     } else {
@@ -541,13 +543,15 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
 
     void *h = f->work + f->off_h, *dg = f->work + f->off_dg, *du = f->work + f->off_du;
     a.part = (float *)(f->work + f->off_part);
-    const void *e = d_out;
+    const void *e = d_out;                // without the factor
     uint64_t e_stride = d_out_stride;
+    float scale = 1.0f;
     if (mask) {
         e = f->work + f->off_e;
         e_stride = f->e_pitch;
-        const int rc = ecrm_dropout(mask, d_out, d_out_stride, nullptr, 0, (void *)e, e_stride, type, n, D, stream);
-        if (rc != ECRM_OK) return rc;
+        scale = a.mask.factor;
+        a.mask.factor = 1.0f;
+        launch_dropout(a.mask, d_out, d_out_stride, nullptr, 0, (void *)e, e_stride, type, n, D, st);
     }
     // where d_x takes the place of what the weights' products read, it comes behind them
     const bool both = weights && d_x && !(e == d_out && d_x == d_out);
@@ -573,6 +577,7 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
         a.p[0].out2 = du;
         a.p[0].out3 = h;
         a.p[0].out_stride = f->pitch;
+        a.p[0].scale = scale;
         launch_product<T, kBack>(a, f->back, type, (uint32_t)f->cus, st);
         Product w[3], in;
         w[0] = product(dg, f->pitch, x, x_stride, F, D, N);
@@ -581,6 +586,7 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
         w[1].out = d_up;
         w[2] = product(e, e_stride, h, f->pitch, D, F, N);
         w[2].out = d_down;
+        w[2].scale = scale;
         w[0].out_stride = w[1].out_stride = D;
         w[2].out_stride = F;
         for (Product &p : w) p.kind = kWeights;

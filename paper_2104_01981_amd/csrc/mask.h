@@ -90,6 +90,10 @@ __device__ __forceinline__ f32x4 drop4(f32x4 v, uint2 bits, const MaskKey &k) { 
 // false: a bad mask.  `factor`: that of MaskArgs in 64 bits.
 bool make_mask(const ecrm_mask *mask, MaskArgs &to, double &factor);
 
+// out = residual + the mask's factor times what it keeps of x; arguments have been checked.
+void launch_dropout(MaskArgs mask, const void *x, uint64_t x_stride, const void *residual, uint64_t residual_stride, void *out, uint64_t out_stride,
+                    uint32_t type, uint64_t rows, uint32_t cols, hipStream_t st);
+
 // Have the rows of a and of b no byte in common?  Rows of one stride may lie between each other; of unlike strides, a whole range of
 // rows lies before the other.
 bool strided_apart(const void *a, uint64_t a_rows, uint64_t a_row_bytes, uint64_t a_stride_bytes, const void *b, uint64_t b_rows,

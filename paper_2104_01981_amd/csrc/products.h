@@ -48,6 +48,7 @@ struct Product {
     const void *in;            // kOut: residual;  kInput: what is added;  kBack: saved g and u
     uint64_t in_stride;
     void *out2, *out3;         // kGate: saved g and u (or null);  kBack: du, h
+    float scale;               // kBack, kWeights: of the sums (the dropout's factor, which e comes without: that is exact in every type)
     uint32_t kind;             // kInput or kWeights, where they are worked off side by side
     uint32_t tiles_m, tiles_n;
     uint32_t splits, each;     // K tiles: cut into so many parts of at most so many
@@ -370,6 +371,7 @@ __device__ __forceinline__ void finish(const ProductArgs &a, const Product &p, c
             for (int q = 0; q < W; ++q)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
+                    v[q][i] *= p.scale;
                     float slope;
                     const float value = activation<T, decltype(act)::value>(x[q][i], slope);
                     x[q][i] = v[q][i] * value;
@@ -384,6 +386,9 @@ __device__ __forceinline__ void finish(const ProductArgs &a, const Product &p, c
             v[0] = drop4(v[0], upper ? uint2{bits.z, bits.w} : uint2{bits.x, bits.y}, mask);
             if (W == 2) v[W - 1] = drop4(v[W - 1], uint2{bits.z, bits.w}, mask);
         }
+        if (KIND == kWeights)
+#pragma unroll
+            for (int q = 0; q < W; ++q) v[q] *= p.scale;
         if (KIND == kWeights ? a.accumulate != 0u : p.in != nullptr)
 #pragma unroll
             for (int q = 0; q < W; ++q) v[q] += x[q];
@@ -398,6 +403,7 @@ __device__ __forceinline__ void write_wide(const ProductArgs &a, const Product &
 #pragma unroll
     for (uint32_t q = 0; q < (uint32_t)W; ++q) {
         if (row >= p.M || col + q * 4u >= p.N) break;
+        v[q] *= p.scale;
         if (a.accumulate) v[q] += *(const f32x4 *)(to + q * 4u);
         *(f32x4 *)(to + q * 4u) = v[q];
     }
