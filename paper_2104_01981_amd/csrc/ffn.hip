@@ -105,6 +105,23 @@ static Plan plan_launch(const ProductSize &a, const ProductSize &b, uint32_t typ
     return best;
 }
 
+// Up to 32 rows, of 32 bits up to 16, are skinny_kernel's.  us forward so / by tiles, 16 and 32 rows: bf16 D = 128, F = 512 6.8 / 8.7, 8.2 /
+// 8.7; 1024, 1024 9.2 / 14.5, 11.5 / 14.6; 1024, 4096 15.1 / 19.8, 20.1 / 19.8.  fp32 8.0 / 12.6, 10.0 / 12.7; 15.2 / 21.4, 23.5 / 21.3;
+// 29.2 / 31.5, 44.3 / 31.4.
+static uint32_t skinny_waves(uint32_t K, uint32_t type)        // that have kAtOnce steps each
+{
+    const uint32_t steps = (K * type_bytes(type) + 63u) / 64u;
+    return (steps + kAtOnce - 1u) / kAtOnce;
+}
+static uint32_t skinny_parts(uint32_t N, uint32_t K, uint32_t type, uint32_t cus)
+{
+    const uint32_t blocks = (N + 15u) / 16u, fit = cus / blocks, fill = skinny_waves(K, type) / 8u;
+    const uint32_t parts = fit < fill ? fit : fill;      // no more workgroups than CUs, eight waves at least to each
+    return parts < 1u ? 1u : parts > kSkinnyParts ? kSkinnyParts : parts;
+}
+constexpr double kSkinnyLaunch = 3.5, kSkinnyRate = 2.5e6;               // us; bytes of weights a us
+static bool is_skinny(uint32_t rows, uint32_t type) { return rows <= (type == ECRM_F32 ? 16u : 32u); }
+
 // z's products with its rows cut where that is faster, those up to the cut beside the other size's (other.count = 0: alone).
 static RowPlan plan_rows(const ProductSize &other, const ProductSize &z, uint32_t type, uint32_t cus, size_t room)
 {
@@ -112,6 +129,11 @@ static RowPlan plan_rows(const ProductSize &other, const ProductSize &z, uint32_
     auto plan = [&](uint32_t rows, bool beside) {
         ProductSize part = z;
         part.M = rows;
+        if (!z.gradients && (z.dual || !z.first) && is_skinny(rows, type)) {
+            Plan skinny{};
+            skinny.cost = kSkinnyLaunch + (double)z.N * z.K * (z.dual ? 2 : 1) * type_bytes(type) / kSkinnyRate;
+            return skinny;
+        }
         return beside && other.count ? plan_launch(other, part, type, cus, room) : plan_launch(part, none, type, cus, room);
     };
     RowPlan best{z.M, plan(z.M, true), Plan{}};
@@ -245,22 +267,6 @@ static void skip_rows(ProductArgs &a, uint32_t first)
     p.M -= first;
 }
 
-// Up to 32 rows, of 32 bits up to 16, are skinny_kernel's.  us forward so / by tiles, 16 and 32 rows: bf16 D = 128, F = 512 6.8 / 8.7, 8.2 /
-// 8.7; 1024, 1024 9.2 / 14.5, 11.5 / 14.6; 1024, 4096 15.1 / 19.8, 20.1 / 19.8.  fp32 8.0 / 12.6, 10.0 / 12.7; 15.2 / 21.4, 23.5 / 21.3;
-// 29.2 / 31.5, 44.3 / 31.4.
-static uint32_t skinny_waves(uint32_t K, uint32_t type)        // that have kAtOnce steps each
-{
-    const uint32_t steps = (K * type_bytes(type) + 63u) / 64u;
-    return (steps + kAtOnce - 1u) / kAtOnce;
-}
-static uint32_t skinny_parts(uint32_t N, uint32_t K, uint32_t type, uint32_t cus)
-{
-    const uint32_t blocks = (N + 15u) / 16u, fit = cus / blocks, fill = skinny_waves(K, type) / 8u;
-    const uint32_t parts = fit < fill ? fit : fill;      // no more workgroups than CUs, eight waves at least to each
-    return parts < 1u ? 1u : parts > kSkinnyParts ? kSkinnyParts : parts;
-}
-static bool is_skinny(uint32_t rows, uint32_t type) { return rows <= (type == ECRM_F32 ? 16u : 32u); }
-
 template <typename T, int KIND, int XB>
 static void launch_skinny(ProductArgs &a, uint32_t type, uint32_t cus, hipStream_t st)
 {
@@ -271,7 +277,7 @@ static void launch_skinny(ProductArgs &a, uint32_t type, uint32_t cus, hipStream
 }
 
 template <typename T, int KIND>
-static void launch_product(ProductArgs &a, const RowPlan &plan, uint32_t type, uint32_t cus, hipStream_t st)
+static void launch_rows(ProductArgs &a, const Plan &plan, uint32_t type, uint32_t cus, hipStream_t st)
 {
     if constexpr (KIND == kGate || KIND == kOut) {
         if (is_skinny(a.p[0].M, type)) {
@@ -279,14 +285,20 @@ static void launch_product(ProductArgs &a, const RowPlan &plan, uint32_t type, u
             if constexpr (sizeof(T) == 2) return launch_skinny<T, KIND, 2>(a, type, cus, st);
         }
     }
+    launch_planned<T, KIND>(a, plan, st);
+}
+
+template <typename T, int KIND>
+static void launch_product(ProductArgs &a, const RowPlan &plan, uint32_t type, uint32_t cus, hipStream_t st)
+{
     const uint32_t M = a.p[0].M;
     a.first_row = 0;
     a.p[0].M = plan.rows;
-    launch_planned<T, KIND>(a, plan.main, st);
+    launch_rows<T, KIND>(a, plan.main, type, cus, st);
     if (plan.rows == M) return;
     a.p[0].M = M;
     skip_rows<T, KIND>(a, plan.rows);
-    launch_planned<T, KIND>(a, plan.rest, st);
+    launch_rows<T, KIND>(a, plan.rest, type, cus, st);
 }
 
 __global__ __launch_bounds__(256) void clear_kernel(uint32_t *to, uint64_t words)
@@ -473,7 +485,9 @@ int ecrm_ffn_forward(ecrm_ffn *f, const void *x, uint64_t x_stride, uint64_t n, 
     a.part = (float *)(f->work + f->off_part);
     make_plan(f, kPlanForward, N);
     a.arrived = (uint32_t *)(f->work + f->off_arrived);
-    a.clear = is_skinny(N, type) ? (skinny_parts(D, F, type, (uint32_t)f->cus) > 1 ? (D + 15u) / 16u * 2u : 0u) : counters_of(f->out);
+    a.clear = counters_of(f->out);
+    if (is_skinny(f->out.rows < N ? N - f->out.rows : N, type) && skinny_parts(D, F, type, (uint32_t)f->cus) > 1 && a.clear < (D + 15u) / 16u * 2u)
+        a.clear = (D + 15u) / 16u * 2u;
     a.activation = f->cfg.activation;
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
