@@ -1,5 +1,6 @@
-"""Trains a next-token model whose token table is kept by the library: lookup, model, gradient by sorted tokens, global
-norm over the model's gradients and the table's, clipping, update with difference propagation -- and a server lost half way.
+"""Trains a next-token model whose token table is kept by the library: lookup with dropout, a gated feed-forward block, an output layer,
+the block's gradients, gradient by sorted tokens, global norm over the model's gradients and the table's, clipping, update with
+difference propagation -- and a server lost half way.
 
     python examples/train_tokens.py [--steps 60]
 
@@ -17,12 +18,13 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 if ROOT not in sys.path:
     sys.path.insert(0, ROOT)
 
-from paper_2104_01981_amd import Ecrm, Grads  # noqa: E402
+from paper_2104_01981_amd import Dropout, Ecrm, FeedForward, Grads  # noqa: E402
 
-VOCABULARY, DIM, K, SERVERS = 4096, 128, 4, 5
+VOCABULARY, DIM, HIDDEN, K, SERVERS = 4096, 128, 512, 4, 5
 SEQUENCES, LENGTH = 64, 129
 PAD = -1                                   # the tokens behind a sequence's end
 MAX_NORM = 1.0
+DROPPED = 0.05
 
 
 def batch(gen):
@@ -55,22 +57,34 @@ def main(steps=60, verbose=True):
     ctx.bind(E, A, PE, PA, load[0], load[1], scratch)
     ctx.encode()
 
-    # the model beside it, in 16 bits with 32-bit weights for its optimizer
-    model = torch.nn.Linear(DIM, VOCABULARY, dtype=torch.bfloat16, device="cuda")
+    # the model beside it, in 16 bits with 32-bit weights for its optimizer: the block's weights, the output layer
+    gate, up, down = (torch.randn(*shape, generator=gen, device="cuda").mul_(shape[1] ** -0.5).bfloat16()
+                      for shape in ((HIDDEN, DIM), (HIDDEN, DIM), (DIM, HIDDEN)))
+    block = FeedForward(gate, up, down, max_rows=n, training=True)
+    head = torch.nn.Linear(DIM, VOCABULARY, dtype=torch.bfloat16, device="cuda")
     with torch.no_grad():
-        model.weight.copy_(torch.randn(VOCABULARY, DIM, generator=gen, device="cuda") * 0.02)
-        model.bias.zero_()
-    weights = [p.detach().float() for p in model.parameters()]
-    squares = [torch.zeros_like(w) for w in weights]
-    for p in model.parameters():
+        head.weight.copy_(torch.randn(VOCABULARY, DIM, generator=gen, device="cuda") * 0.02)
+        head.bias.zero_()
+    for p in head.parameters():
         p.grad = torch.zeros_like(p)
+    parameters = [gate, up, down] + [p.detach() for p in head.parameters()]
+    weights = [p.float() for p in parameters]
+    squares = [torch.zeros_like(w) for w in weights]
+
+    # the masks of dropout: a seed and how many were drawn; two places of the model draw one each in a step
+    state = torch.tensor([2024, 0], device="cuda")
+    dropout = Dropout(DROPPED, state, 0), Dropout(DROPPED, state, 1)
 
     # what a step leaves: one gradient row for each distinct token; the clipped gradients in 32 bits
-    x = torch.zeros(n, DIM, dtype=torch.bfloat16, device="cuda", requires_grad=True)
+    x = torch.zeros(n, DIM, dtype=torch.bfloat16, device="cuda")
+    saved = torch.empty(n, 2 * HIDDEN, dtype=torch.bfloat16, device="cuda")
+    y = torch.zeros(n, DIM, dtype=torch.bfloat16, device="cuda", requires_grad=True)
+    y.grad = torch.zeros_like(y)
+    d_x, d_block = torch.empty_like(x), [torch.empty_like(p) for p in (gate, up, down)]
     rows, row_grads = torch.empty(n, dtype=torch.int64, device="cuda"), torch.empty(n, DIM, device="cuda")
     count, norm = torch.zeros(1, dtype=torch.int64, device="cuda"), torch.zeros(1, device="cuda")
     clipped = [torch.empty_like(w) for w in weights]
-    grads = Grads([p.grad for p in model.parameters()] + [(row_grads, count)])
+    grads = Grads(d_block + [p.grad for p in head.parameters()] + [(row_grads, count)])
     out = Grads(clipped + [row_grads])
 
     losses = []
@@ -81,21 +95,24 @@ def main(steps=60, verbose=True):
             lost = 2
             ctx.fail_server(lost)
         with torch.no_grad():
-            ctx.embed(tokens, x, scale=scale, padding=PAD, lost_server=lost)
+            ctx.embed(tokens, x, scale=scale, padding=PAD, lost_server=lost, dropout=dropout[0])
+            block.forward(x, y, residual=x, dropout=dropout[1], saved=saved)
         if lost is not None:
             ctx.recover_server(lost)
-        loss = torch.nn.functional.cross_entropy(model(x).float(), follow)
-        x.grad = None
-        for p in model.parameters():
+        loss = torch.nn.functional.cross_entropy(head(y).float(), follow)
+        y.grad.zero_()
+        for p in head.parameters():
             p.grad.zero_()
         loss.backward()
 
-        ctx.embed_grad(tokens, x.grad, rows, row_grads, count, scale=scale, padding=PAD)
+        block.backward(x, saved, y.grad, d_x, *d_block, add=y.grad, dropout=dropout[1])
+        ctx.embed_grad(tokens, d_x, rows, row_grads, count, scale=scale, padding=PAD, dropout=dropout[0])
+        state[1] += len(dropout)
         grads.norm(norm)
         grads.clip(norm, MAX_NORM, out=out)
         ctx.update(rows, row_grads, n=int(count))
         with torch.no_grad():
-            for p, w, s, g in zip(model.parameters(), weights, squares, clipped):
+            for p, w, s, g in zip(parameters, weights, squares, clipped):
                 s.addcmul_(g, g)
                 w.addcdiv_(g, s.sqrt().add_(1e-8), value=-0.05)
                 p.copy_(w)
