@@ -20,8 +20,7 @@ constexpr TilingCost kCosts[kTilings] = {{256, 1, {1.58, 0}, {1.58, 0}, 1.0, 3.0
 // Columns of a tile; of each projection for kGate.
 static constexpr uint32_t columns_of(uint32_t side, bool dual) { return dual && side > 32 ? side / 2u : side; }
 constexpr uint32_t kSplitCounts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
-constexpr double kJoinLaunch = 3.0, kJoinRate = 4.0e6;       // parts of the first product of a call, by a launch of their own: us; bytes a us
-constexpr double kJoinWait = 2.0, kJoinOne = 2.5e4;          // others by the workgroup that is there last
+constexpr double kJoinWait = 2.0, kJoinOne = 2.5e4;          // parts joined by the workgroup that is there last: us; bytes a us
 constexpr uint32_t kSkinnyParts = 16;
 constexpr size_t kPartMost = 32u << 20;          // bytes of the parts of split products, at most
 constexpr uint32_t kCounters = kPartMost / (2u * 32u * 32u * 4u);       // tiles of two parts or more
@@ -76,7 +75,7 @@ static Plan plan_launch(const ProductSize &a, const ProductSize &b, uint32_t typ
         };
         const double part = (double)c.side * c.side * 4.0;
         for (uint32_t sa : kSplitCounts) {
-            if (sa > k_tiles[0]) break;
+            if (sa > k_tiles[0] || (a.first && sa > 1)) break;           // a call's first product has no counters that are cleared before it
             const Split x = split(0, sa);
             const double a_bytes = x.splits > 1 ? part * tiles[0] * x.splits : 0.0;
             if (a_bytes > (double)room) break;
@@ -87,16 +86,17 @@ static Plan plan_launch(const ProductSize &a, const ProductSize &b, uint32_t typ
                 if (bytes > (double)room) break;
                 const uint64_t units = tiles[0] * x.splits + tiles[1] * y.splits, there = (units + cus - 1) / cus;
                 const double together = there < c.resident ? (double)there : (double)c.resident;
-                const double shared = c.shared[wide] * together * (a.gradients && !wide ? c.transposed : 1.0);
-                const double step = shared > c.step[wide] ? shared : c.step[wide];
+                // 32 x 32 of each projection are twice the work, larger tiles have both in their width
+                const double twice = a.dual && c.side == 32 ? 2.0 : 1.0;
+                const double alone = c.step[wide] * twice, shared = c.shared[wide] * twice * together * (a.gradients && !wide ? c.transposed : 1.0);
+                const double step = shared > alone ? shared : alone;
                 auto unit = [&](int i, const Split &s) {
-                    return c.tile * together + s.each * step + (s.splits > 1 && !sizes[i]->first ? kJoinWait + s.splits * part / kJoinOne : 0.0);
+                    return c.tile * together + s.each * step + (s.splits > 1 ? kJoinWait + s.splits * part / kJoinOne : 0.0);
                 };
                 const uint64_t slots = (uint64_t)(cus * together);
                 const double ua = unit(0, x), ub = b.count ? unit(1, y) : 1.0;
                 double cost = c.launch + (ua >= ub ? makespan(tiles[0] * x.splits, ua, tiles[1] * y.splits, ub, slots)
                                                    : makespan(tiles[1] * y.splits, ub, tiles[0] * x.splits, ua, slots));
-                if (a.first && x.splits > 1) cost += kJoinLaunch + 2.0 * a_bytes / kJoinRate;
                 const uint64_t counters = (x.splits > 1 ? tiles[0] : 0) + (y.splits > 1 ? tiles[1] : 0);
                 if (!best.split[0].splits || cost < best.cost) best = Plan{t, {x, y}, (uint32_t)counters, cost};
             }
@@ -176,9 +176,6 @@ static void launch_tiling(ProductArgs &a, hipStream_t st)
     typedef Tiling<T, KIND, BM, BN, WM, WN> L;
     lay_out(a, BM, L::kColumns);
     hipLaunchKernelGGL((product_kernel<T, KIND, BM, BN, WM, WN>), dim3(a.workgroups), dim3(L::kThreads), 0, st, a);
-    if constexpr (L::kFirst)
-        if (a.p[0].splits > 1)
-            hipLaunchKernelGGL((join_kernel<T, KIND, BM, BN, WM, WN>), dim3(a.p[0].tiles_m * a.p[0].tiles_n, L::MB * L::kGroups), dim3(L::kThreads), 0, st, a);
 }
 
 template <typename T, int KIND>

@@ -620,16 +620,9 @@ __device__ __forceinline__ void run_tile(const ProductArgs &a, const Product &p,
         if (t + 1u < stop) step(t + 1u, s_a1, s_b1, s_a0, s_b0);
     }
 
-    if (p.splits > 1u) {
+    if (!L::kFirst && p.splits > 1u) {
         const uint64_t size = MB * NB * L::kThreads;     // of a part, in f32x4
         f32x4 *parts = (f32x4 *)a.part + (uint64_t)(p.part + tile * p.splits) * size + tid;
-        if (L::kFirst) {                                 // joined by a launch of its own
-#pragma unroll
-            for (int i = 0; i < MB; ++i)
-#pragma unroll
-                for (int j = 0; j < NB; ++j) parts[split * size + (i * NB + j) * L::kThreads] = acc[i][j];
-            return;
-        }
 #pragma unroll
         for (int i = 0; i < MB; ++i)
 #pragma unroll
@@ -696,36 +689,6 @@ __global__ __launch_bounds__(WM * WN * kWave, 2) void gradients_kernel(ProductAr
     const Product &p = a.p[which];
     if (p.kind == kInput) run_tile<T, kInput, BM, BN, WM, WN>(a, p, blockIdx.x - p.first, s_a0, s_b0, s_a1, s_b1);
     else run_tile<T, kWeights, BM, BN, WM, WN>(a, p, blockIdx.x - p.first, s_a0, s_b0, s_a1, s_b1);
-}
-
-// Adds up what the parts of K of a call's first product gave, in order; a workgroup has a group of each of a tile's waves.
-template <typename T, int KIND, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM * WN * kWave) void join_kernel(ProductArgs a)
-{
-    typedef Tiling<T, KIND, BM, BN, WM, WN> L;
-    constexpr uint32_t NB = L::NB, MB = L::MB, W = L::kPair, N = L::kTogether * W;
-    const uint32_t tile = blockIdx.x, i = blockIdx.y / L::kGroups, g = blockIdx.y % L::kGroups;
-    uint32_t m, n;
-    const Product &p = a.p[0];
-    find_tile(p, tile, m, n);
-    const f32x4 *from = (const f32x4 *)a.part + (uint64_t)tile * p.splits * (MB * NB * L::kThreads) + (i * NB + g * N) * L::kThreads + threadIdx.x;
-    typename L::In in;
-    L::fetch(a, p, m, n, i, g, in);
-    f32x4 v[N], w[N];
-#pragma unroll
-    for (uint32_t q = 0; q < N; ++q) v[q] = w[q] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (uint32_t s = 0; s < p.splits; ++s) {
-        const f32x4 *part = from + (uint64_t)s * (MB * NB * L::kThreads);
-#pragma unroll
-        for (uint32_t q = 0; q < N; ++q) {
-            v[q] += part[q * L::kThreads];
-            if (L::kDual) w[q] += part[(q + L::kNeed) * L::kThreads];
-        }
-    }
-    MaskKey mask{};
-    if (KIND == kOut && a.masked) mask = mask_key(a.mask);
-    L::finish_group(a, p, mask, m, n, i, g, in, [&](uint32_t k, int q) { return v[k * W + q]; }, [&](uint32_t k, int q) { return w[k * W + q]; });
 }
 
 // ---- few rows --------------------------------------------------------------------------------------------------------------------

@@ -19,6 +19,9 @@ DEV = "cuda:0"
 TYPES = [torch.float32, torch.bfloat16, torch.float16]
 SIZES = [(1, 4, 4), (1, 128, 512), (2, 12, 20), (3, 8, 132), (5, 60, 64), (15, 64, 68), (16, 68, 60), (17, 132, 36), (31, 36, 260), (33, 256, 100),
          (63, 100, 256), (65, 128, 128), (128, 124, 516), (129, 260, 124), (257, 64, 1028), (300, 516, 268), (1000, 4, 512), (1025, 128, 4)]
+# every tiling of every product, of 16 and of 32 bits, with and without parts of K, and rows behind the last whole tiles
+LARGE = [(2100, 512, 1028), (4099, 260, 2052), (300, 1024, 4096), (3000, 1024, 1028), (5000, 512, 2052), (8300, 132, 1028), (16400, 1024, 260),
+         (4100, 1024, 4100)]
 
 
 def whole(n, m, t, gen, share, extra=0):
@@ -60,7 +63,7 @@ def exact_case(n, D, F, t, extra, seed):
 
 
 @pytest.mark.parametrize("t", TYPES)
-@pytest.mark.parametrize("n,D,F", SIZES + [(2100, 512, 1028), (4099, 260, 2052)])
+@pytest.mark.parametrize("n,D,F", SIZES + LARGE)
 def test_forward_exactly(n, D, F, t):
     for extra in (0, 4, 8):
         gen, x, wg, wu, wd = exact_case(n, D, F, t, extra, n + D + F)
@@ -87,7 +90,7 @@ def test_forward_exactly(n, D, F, t):
 
 
 @pytest.mark.parametrize("t", TYPES)
-@pytest.mark.parametrize("n,D,F", SIZES + [(2100, 512, 1028), (4099, 260, 2052)])
+@pytest.mark.parametrize("n,D,F", SIZES + LARGE)
 def test_backward_exactly(n, D, F, t):
     for extra, p in ((0, None), (4, 0.5), (8, None)):
         gen, x, wg, wu, wd = exact_case(n, D, F, t, extra, 3 * n + D + F)
