@@ -9,14 +9,15 @@ namespace ecrm {
 
 // ---- which tiles -----------------------------------------------------------------------------------------------------------------
 // What a product takes is estimated in us from what was measured (M, N of 512 to 4096, all CUs in step): a tile's steps of 128 bytes of
-// K, alone on its CU and for each of several (times `transposed` for the gradients in 16 bits); the launch, a tile's begin and end.  16 bits: 64 x 64 0.50 and 0.17 a step, 128 x 128 0.65
+// K, alone on its CU and for each of several (times `transposed` for the gradients in 16 bits); the launch, a tile's begin and end (`back`: kBack's,
+// which is bound by what it reads and writes).  16 bits: 64 x 64 0.50 and 0.17 a step, 128 x 128 0.65
 // and 0.47, 256 x 256 1.58.  32 bits are bound by their matrix instructions, 137 TFLOP/s with any of these and all CUs full, so that small
 // tiles, more of them to a CU, gain: 32 x 32 0.24 and 0.12, 64 x 64 0.62 and 0.46, 128 x 128 1.96 and 1.79 (777 rows, D = 260, F =
 // 684: 26 us with 64 x 64 at least, 19 so).
 enum { kTile256 = 0, kTile128 = 1, kTile64 = 2, kTile32 = 3, kTilings = 4 };
-struct TilingCost { uint32_t side, resident; double step[2], shared[2], transposed, launch, tile; };      // [0] 16 bits, [1] 32; 0: not for these
-constexpr TilingCost kCosts[kTilings] = {{256, 1, {1.58, 0}, {1.58, 0}, 1.0, 3.0, 8.0}, {128, 2, {0.65, 1.96}, {0.47, 1.79}, 1.06, 5.0, 1.4},
-                                         {64, 5, {0.50, 0.62}, {0.172, 0.46}, 1.25, 2.5, 0.42}, {32, 8, {0, 0.24}, {0, 0.12}, 1.0, 2.5, 0.3}};
+struct TilingCost { uint32_t side, resident; double step[2], shared[2], transposed, launch, tile, back; };      // [0] 16 bits, [1] 32; 0: not for these
+constexpr TilingCost kCosts[kTilings] = {{256, 1, {1.58, 0}, {1.58, 0}, 1.0, 3.0, 8.0, 20.0}, {128, 2, {0.65, 1.96}, {0.47, 1.79}, 1.06, 5.0, 1.4, 6.8},
+                                         {64, 5, {0.50, 0.62}, {0.172, 0.46}, 1.25, 2.5, 0.42, 1.6}, {32, 8, {0, 0.24}, {0, 0.12}, 1.0, 2.5, 0.3, 0.6}};
 // Columns of a tile; of each projection for kGate.
 static constexpr uint32_t columns_of(uint32_t side, bool dual) { return dual && side > 32 ? side / 2u : side; }
 constexpr uint32_t kSplitCounts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
@@ -91,7 +92,7 @@ static Plan plan_launch(const ProductSize &a, const ProductSize &b, uint32_t typ
                 const double alone = c.step[wide] * twice, shared = c.shared[wide] * twice * together * (a.gradients && !wide ? c.transposed : 1.0);
                 const double step = shared > alone ? shared : alone;
                 auto unit = [&](int i, const Split &s) {
-                    return c.tile * together + s.each * step + (s.splits > 1 ? kJoinWait + s.splits * part / kJoinOne : 0.0);
+                    return (a.first && !a.dual ? c.back : c.tile) * together + s.each * step + (s.splits > 1 ? kJoinWait + s.splits * part / kJoinOne : 0.0);
                 };
                 const uint64_t slots = (uint64_t)(cus * together);
                 const double ua = unit(0, x), ub = b.count ? unit(1, y) : 1.0;

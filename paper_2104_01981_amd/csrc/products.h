@@ -303,6 +303,11 @@ struct Piece {
     {
         return quads ? read(p, quads) : u32x4{0u, 0u, 0u, 0u};
     }
+    static __device__ __forceinline__ void write_past(T *p, uint32_t quads, u32x4 v)
+    {
+        if (quads >= (uint32_t)kQuads) __builtin_nontemporal_store((Loose)v, (Loose *)p);
+        else write(p, quads, v);
+    }
     static __device__ __forceinline__ void write(T *p, uint32_t quads, u32x4 v)
     {
         if (quads >= (uint32_t)kQuads) *(Loose *)p = v;
@@ -445,6 +450,14 @@ struct Tiling {
         row = (row & ~15u) + (lane & 7u) + k * 8u;
     }
 
+    // What another call reads is written past the caches, where whole lines are, and leaves them to the operands: g and u of 16384 x 4096, K =
+    // 1024, bf16, 282 -> 265 us (with h, which the next launch reads, 273); 8192 x 512, K = 128, in all of a forward pass 18.2 -> 16.9.
+    static __device__ __forceinline__ void write_far(T *p, uint32_t quads, u32x4 v)
+    {
+        if (kTogether == 2) Piece<T>::write_past(p, quads, v);
+        else Piece<T>::write(p, quads, v);
+    }
+
     struct In { u32x4 x[kTogether][kReads]; };
     static __device__ __forceinline__ void fetch(const ProductArgs &a, const Product &p, uint32_t m, uint32_t n, uint32_t i, uint32_t g, In &in)
     {
@@ -511,8 +524,8 @@ struct Tiling {
             Piece<T>::write((T *)p.out + at, quads, out[k][0]);
             if (KIND == kGate && p.out2) {
                 T *s = (T *)p.out2 + (uint64_t)row * 2u * p.N + col;
-                Piece<T>::write(s, quads, out[k][1]);
-                Piece<T>::write(s + p.N, quads, out[k][2]);
+                write_far(s, quads, out[k][1]);
+                write_far(s + p.N, quads, out[k][2]);
             } else if (KIND == kBack) {
                 Piece<T>::write((T *)p.out2 + at, quads, out[k][1]);
                 Piece<T>::write((T *)p.out3 + at, quads, out[k][2]);
@@ -602,8 +615,9 @@ __device__ __forceinline__ void run_tile(const ProductArgs &a, const Product &p,
                 for (int j = 0; j < NB; ++j) acc[i][j] = Fragment<T>::multiply(fb[j], fa[i], acc[i][j]);
         }
     };
-    auto step = [&](uint32_t t, char *ta, char *tb, char *next_a, char *next_b) {
-        __builtin_amdgcn_s_waitcnt(0);                   // this wave's part of the tile is there ...
+    // tile t is there, all of it
+    auto arrive = [&](uint32_t t, char *ta, char *tb) {
+        __builtin_amdgcn_s_waitcnt(0);                   // this wave's part of it ...
         __syncthreads();                                 // ... and everybody's; nobody reads the other tile any more
         const uint32_t left = K - (KIND == kInput && t >= half_tiles ? t - half_tiles : t) * L::kElements;
         if (sizeof(T) == 2 && !(L::kColumnsA && L::kColumnsB) && left < L::kElements && left % 8u) {
@@ -611,13 +625,32 @@ __device__ __forceinline__ void run_tile(const ProductArgs &a, const Product &p,
             if (!L::kColumnsB) clear_behind<BN, L::kThreads>(tb, left, tid);
             __syncthreads();
         }
-        if (t + 1u < stop) issue(t + 1u, next_a, next_b);
+    };
+    auto step = [&](uint32_t t, char *ta, char *tb, char *next_a, char *next_b) {
+        arrive(t, ta, tb);
+        issue(t + 1u, next_a, next_b);
         multiply(ta, tb);
     };
     if (begin < stop) issue(begin, s_a0, s_b0);
-    for (uint32_t t = begin; t < stop; t += 2u) {
+    for (uint32_t t = begin; t + 1u < stop; t += 2u) {
         step(t, s_a0, s_b0, s_a1, s_b1);
-        if (t + 1u < stop) step(t + 1u, s_a1, s_b1, s_a0, s_b0);
+        if (t + 2u < stop) step(t + 1u, s_a1, s_b1, s_a0, s_b0);
+    }
+    // What the first rows' results are finished with is on its way before the last multiplications, and then always that of the next: a
+    // store could change it for all the compiler knows, which would wait for one block's after the other (kBack 16384 x 4096, K = 1024:
+    // 497 us; one row of blocks ahead 303).
+    constexpr uint32_t G = L::kGroups, kAhead = KIND == kBack && MB < 8 ? MB : 1;      // as the registers allow
+    typename L::In in[kAhead + 1][G];
+    if (begin < stop) {
+        const bool first = (stop - begin) % 2u;          // the last tile lies in the first place
+        char *ta = first ? s_a0 : s_a1, *tb = first ? s_b0 : s_b1;
+        arrive(stop - 1u, ta, tb);
+#pragma unroll
+        for (uint32_t i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (uint32_t g = 0; g < G; ++g) L::fetch(a, p, m, n, i, g, in[i][g]);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(ta, tb);
     }
 
     if (!L::kFirst && p.splits > 1u) {
@@ -652,18 +685,14 @@ __device__ __forceinline__ void run_tile(const ProductArgs &a, const Product &p,
     if (KIND == kOut && a.masked) mask = mask_key(a.mask);
     // What the next rows' results are finished with is on its way: a store could change it for all the compiler knows, which would wait
     // for one block's after the other (kBack 16384 x 4096, K = 1024: 497 us; one row of blocks ahead 303).
-    constexpr uint32_t G = L::kGroups;
-    typename L::In in[2][G];
-#pragma unroll
-    for (uint32_t g = 0; g < G; ++g) L::fetch(a, p, m, n, 0u, g, in[0][g]);
 #pragma unroll
     for (uint32_t i = 0; i < MB; ++i) {
-        if (i + 1u < MB)
+        if (i + kAhead < MB)
 #pragma unroll
-            for (uint32_t g = 0; g < G; ++g) L::fetch(a, p, m, n, i + 1u, g, in[(i + 1u) % 2u][g]);
+            for (uint32_t g = 0; g < G; ++g) L::fetch(a, p, m, n, i + kAhead, g, in[(i + kAhead) % (kAhead + 1)][g]);
 #pragma unroll
         for (uint32_t g = 0; g < G; ++g)
-            L::finish_group(a, p, mask, m, n, i, g, in[i % 2u][g],
+            L::finish_group(a, p, mask, m, n, i, g, in[i % (kAhead + 1)][g],
                             [&](uint32_t k, int q) { return acc[i][(g * L::kTogether + k) * L::kPair + q]; },
                             [&](uint32_t k, int q) { return acc[i][((g * L::kTogether + k) * L::kPair + q + L::kNeed) % NB]; });
     }
