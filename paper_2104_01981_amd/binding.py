@@ -136,7 +136,7 @@ def _ptr(t):
     return C.c_void_p(t.data_ptr()) if t is not None else C.c_void_p(0)
 
 
-_raw_stream = None
+_raw_stream = _raw_device = None
 
 
 def _stream(stream):
@@ -153,6 +153,15 @@ def _stream(stream):
         else:
             _raw_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
     return _raw_stream()
+
+
+def _current_device():
+    """Index of the current device (of torch.cuda.current_device, without its checks)."""
+    global _raw_device
+    if _raw_device is None:
+        import torch
+        _raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _raw_device()
 
 
 def _stream_object(stream):
@@ -329,7 +338,8 @@ class FeedForward:
         self.dtype, self.max_rows = gate.dtype, max_rows
         assert _is_rows(gate, self.hidden, self.dim, self.dtype) and _is_rows(up, self.hidden, self.dim, self.dtype)
         assert _is_rows(down, self.dim, self.hidden, self.dtype)
-        assert gate.device == up.device == down.device and gate.device.index == torch.cuda.current_device()
+        self._device = gate.device.index
+        assert gate.device == up.device == down.device and self._device == torch.cuda.current_device()
         cfg = EcrmFfnConfig(self.dim, self.hidden, _type(gate), self.ACTIVATIONS[activation], max_rows, 1 if training else 0)
         rc = self._lib.ecrm_ffn_create(C.byref(cfg), C.byref(self._ffn))
         if rc != ECRM_OK:
@@ -351,6 +361,7 @@ class FeedForward:
     def _on(self, stream):
         """Address of a call's stream; the allocator learns that weights and workspace are used there."""
         address = _stream(stream)
+        assert _current_device() == self._device, "the block's device has to be the current one"
         if address not in self._streams:
             self._streams.add(address)
             use = _stream_object(stream)

@@ -26,6 +26,8 @@ constexpr uint32_t kSkinnyParts = 16;
 constexpr size_t kPartMost = 32u << 20;          // bytes of the parts of split products, at most
 constexpr uint32_t kCounters = kPartMost / (2u * 32u * 32u * 4u);       // tiles of two parts or more
 
+constexpr uint64_t kMostWorkgroups = 0xFFFFFFFFu / 512u;        // a launch has fewer than 2^32 threads
+
 struct Split { uint32_t splits, each; };
 // Products of one launch (the last of them with the splits of their own, where there are two sizes).
 struct Plan { uint32_t tiling; Split split[2]; uint32_t counters; double cost; };
@@ -86,6 +88,7 @@ static Plan plan_launch(const ProductSize &a, const ProductSize &b, uint32_t typ
                 const double bytes = a_bytes + (y.splits > 1 ? part * tiles[1] * y.splits : 0.0);
                 if (bytes > (double)room) break;
                 const uint64_t units = tiles[0] * x.splits + tiles[1] * y.splits, there = (units + cus - 1) / cus;
+                if (units > kMostWorkgroups) continue;
                 const double together = there < c.resident ? (double)there : (double)c.resident;
                 // 32 x 32 of each projection are twice the work, larger tiles have both in their width
                 const double twice = a.dual && c.side == 32 ? 2.0 : 1.0;
@@ -376,6 +379,8 @@ Product product(const void *a, uint64_t a_stride, const void *b, uint64_t b_stri
     return p;
 }
 
+// false: more workgroups than a launch can have, of any tiling
+bool is_planned(const RowPlan &p) { return p.main.cost > 0; }
 uint32_t counters_of(const RowPlan &p) { return p.main.counters > p.rest.counters ? p.main.counters : p.rest.counters; }
 
 void make_plan(ecrm_ffn *f, int what, uint32_t n)
@@ -482,6 +487,7 @@ int ecrm_ffn_forward(ecrm_ffn *f, const void *x, uint64_t x_stride, uint64_t n, 
     void *h = f->work + f->off_h;
     a.part = (float *)(f->work + f->off_part);
     make_plan(f, kPlanForward, N);
+    if (!is_planned(f->gate) || !is_planned(f->out)) return ECRM_EINVAL;
     a.arrived = (uint32_t *)(f->work + f->off_arrived);
     a.clear = counters_of(f->out);
     if (is_skinny(f->out.rows < N ? N - f->out.rows : N, type) && skinny_parts(D, F, type, (uint32_t)f->cus) > 1 && a.clear < (D + 15u) / 16u * 2u)
@@ -553,6 +559,17 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
     }
     if (!weights && !d_x) return ECRM_OK;
 
+    // where d_x takes the place of what the weights' products read, it comes behind them
+    const bool both = weights && d_x && (mask || d_x != d_out);
+    make_plan(f, kPlanBack, N);
+    if (both) {
+        make_plan(f, kPlanBoth, N);
+    } else {
+        if (weights) make_plan(f, kPlanWeights, N);
+        if (d_x) make_plan(f, kPlanInput, N);
+    }
+    if (!is_planned(f->back) || (d_x && !is_planned(both ? f->both : f->input)) || (weights && !both && !f->weights.split[0].splits)) return ECRM_EINVAL;
+
     void *h = f->work + f->off_h, *dg = f->work + f->off_dg, *du = f->work + f->off_du;
     a.part = (float *)(f->work + f->off_part);
     const void *e = d_out;                // without the factor
@@ -565,18 +582,9 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
         a.mask.factor = 1.0f;
         launch_dropout(a.mask, d_out, d_out_stride, nullptr, 0, (void *)e, e_stride, type, n, D, st);
     }
-    // where d_x takes the place of what the weights' products read, it comes behind them
-    const bool both = weights && d_x && !(e == d_out && d_x == d_out);
-    make_plan(f, kPlanBack, N);
-    if (both) {
-        make_plan(f, kPlanBoth, N);
-    } else {
-        if (weights) make_plan(f, kPlanWeights, N);
-        if (d_x) make_plan(f, kPlanInput, N);
-    }
     a.activation = f->cfg.activation;
     a.accumulate = accumulate ? 1u : 0u;
-    a.wide = weight_type == ECRM_F32 ? 1u : 0u;
+    a.wide = weight_type != type ? 1u : 0u;
     a.arrived = (uint32_t *)(f->work + f->off_arrived);
     a.clear = both ? counters_of(f->both) : 0u;
     if (!both && weights) a.clear = f->weights.counters;

@@ -110,13 +110,32 @@ __device__ __forceinline__ const char *scalar(const char *p)
     return (const char *)((uint64_t)scalar((uint32_t)((uint64_t)p >> 32)) << 32 | scalar((uint32_t)(uint64_t)p));
 }
 
-// 64 lanes' 16 bytes each from a buffer (zeros behind its end) to the 1 KB of LDS at `to` + `behind`.  Written out because the compiler, which does not
-// tell the tiles' two halves apart where fragments are read transposed, waits for the load before the next such read (kInput with
-// K = 4096: 980 TFLOP/s that way, 1310 so).  Nothing but a wait for all loads and a barrier may come before the tile is read.
-__device__ __forceinline__ void load_to_lds(u32x4 buffer, uint32_t at, uint32_t from, uint32_t to, uint32_t behind)
+// 64 lanes' 16 bytes each from a buffer (zeros behind its end) to the 1 KB of LDS at `to` + BEHIND.  Written out because the compiler,
+// which does not tell the tiles' two halves apart where fragments are read transposed, waits for the load before the next such read
+// (kInput with K = 4096: 980 TFLOP/s that way, 1310 so).  It does not count these loads either: before the tile is read there have to be
+// a wait for all of them and a barrier.  Nor does it keep the distances that it keeps for a load of its own: M0 is written two instructions
+// before its use, and scalar registers that a vector instruction may have written last (readfirstlane) five at least, in the
+// first of several loads, which have them in common.
+template <uint32_t BEHIND>
+__device__ __forceinline__ void load_to_lds(u32x4 buffer, uint32_t at, uint32_t from, uint32_t to)
 {
-    asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds"
-                 :: "s"(to), "i"(behind), "v"(at), "s"(buffer), "s"(from) : "memory", "scc");
+    if (BEHIND == 0)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                     :: "s"(to), "v"(at), "s"(buffer), "s"(from) : "memory", "m0");
+    else
+        asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds"
+                     :: "s"(to), "i"(BEHIND), "v"(at), "s"(buffer), "s"(from) : "memory", "scc", "m0");
+}
+// f(Constant<0>()), f(Constant<1>()) .. f(Constant<N - 1>())
+template <uint32_t V>
+struct Constant { static constexpr uint32_t value = V; };
+template <uint32_t N, uint32_t I = 0, typename F>
+__device__ __forceinline__ void for_each(F f)
+{
+    if constexpr (I < N) {
+        f(Constant<I>());
+        for_each<N, I + 1>(f);
+    }
 }
 __device__ __forceinline__ u32x4 buffer_of(const char *base, uint32_t bytes)
 {
@@ -176,25 +195,23 @@ struct Loader {
             const u32x4 buffer = buffer_of(base, end);
             const uint32_t from = scalar(k0 * (uint32_t)sizeof(T));
             if (left >= kElements) {
-#pragma unroll
-                for (uint32_t i = 0; i < kLoads; ++i) load_to_lds(buffer, at[i], from, to, i * 1024u);
+                for_each<kLoads>([&](auto i) { load_to_lds<decltype(i)::value * 1024u>(buffer, at[decltype(i)::value], from, to); });
             } else {
-#pragma unroll
-                for (uint32_t i = 0; i < kLoads; ++i) {
-                    const uint32_t chunk = (lane % 8u) ^ ((lane / 16u) | ((load + i) & 1u) << 2);
-                    load_to_lds(buffer, chunk * (16u / (uint32_t)sizeof(T)) >= left ? kOutside : at[i], from, to, i * 1024u);
-                }
+                for_each<kLoads>([&](auto i) {
+                    const uint32_t chunk = (lane % 8u) ^ ((lane / 16u) | ((load + decltype(i)::value) & 1u) << 2);
+                    const bool outside = chunk * (16u / (uint32_t)sizeof(T)) >= left;
+                    load_to_lds<decltype(i)::value * 1024u>(buffer, outside ? kOutside : at[decltype(i)::value], from, to);
+                });
             }
         } else {
             const uint32_t rows = min(left, kElements);
             const u32x4 buffer = buffer_of(scalar(base + (uint64_t)k0 * stride), scalar(end ? (rows - 1u) * stride + end : 0u));
-#pragma unroll
-            for (uint32_t i = 0; i < kLoads; ++i) load_to_lds(buffer, at[i], 0u, to, i * 1024u);
+            for_each<kLoads>([&](auto i) { load_to_lds<decltype(i)::value * 1024u>(buffer, at[decltype(i)::value], 0u, to); });
         }
     }
 };
 
-// K ends in the middle of a chunk of 16 bits a element, `left` elements from the tile's begin: what is behind is cleared in all rows.
+// K ends in the middle of a 16-byte chunk, `left` 16-bit elements from the tile's begin: what is behind it in the chunk is cleared in all rows.
 template <int ROWS, int THREADS>
 __device__ __forceinline__ void clear_behind(char *tile, uint32_t left, uint32_t tid)
 {
@@ -277,8 +294,6 @@ __device__ __forceinline__ float activation(float g, float &slope)
     return g > 0.f ? g : g != g ? g : 0.f;
 }
 
-template <uint32_t V>
-struct Constant { static constexpr uint32_t value = V; };
 // f(Constant<activation>()): one branch for all that f does
 template <typename F>
 __device__ __forceinline__ void with_activation(uint32_t kind, F f)
@@ -499,8 +514,10 @@ struct Tiling {
                 v[q] = of(k, q);
                 w[q] = of_up(k, q);
             }
-            if (KIND == kWeights && a.wide) write_wide<kPair>(a, p, row, col, v);
-            if (KIND == kWeights && a.wide) continue;
+            if (KIND == kWeights && a.wide) {
+                write_wide<kPair>(a, p, row, col, v);
+                continue;
+            }
             f32x4 x[kPair], y[kPair];
             if (kIn >= 1) Piece<T>::widen(in.x[k][0], x);
             if (kIn >= 2) Piece<T>::widen(in.x[k][1], y);
@@ -683,8 +700,6 @@ __device__ __forceinline__ void run_tile(const ProductArgs &a, const Product &p,
     }
     MaskKey mask{};
     if (KIND == kOut && a.masked) mask = mask_key(a.mask);
-    // What the next rows' results are finished with is on its way: a store could change it for all the compiler knows, which would wait
-    // for one block's after the other (kBack 16384 x 4096, K = 1024: 497 us; one row of blocks ahead 303).
 #pragma unroll
     for (uint32_t i = 0; i < MB; ++i) {
         if (i + kAhead < MB)

@@ -25,20 +25,26 @@ LARGE = [(2100, 512, 1028), (4099, 260, 2052), (300, 1024, 4096), (3000, 1024, 1
 
 
 def whole(n, m, t, gen, share, extra=0):
-    """Numbers -1, 0, 1 inside wider rows of NaN, a row of it behind."""
+    """Numbers -1, 0, 1 inside wider rows of NaN, a row of it behind; from a multiple of four elements on, not always of 16 bytes."""
     wide = torch.full((n + 1, m + extra), float("nan"), dtype=t, device=DEV)
     x = torch.randint(-1, 2, (n, m), generator=gen, device=DEV) * (torch.rand(n, m, generator=gen, device=DEV) < share)
-    wide[:n, :m] = x.to(t)
-    return wide[:n, :m]
+    wide[:n, extra:] = x.to(t)
+    return wide[:n, extra:]
 
 
 def inside(n, m, t, extra):
     wide = torch.full((n + 1, m + extra), -7.0, dtype=t, device=DEV)
-    return wide[:n, :m], wide
+    return wide[:n, extra:], wide
 
 
 def untouched(wide, n, m):
-    return bool((wide[n] == -7.0).all()) and bool((wide[:, m:] == -7.0).all())
+    return bool((wide[n] == -7.0).all()) and bool((wide[:, :wide.shape[1] - m] == -7.0).all())
+
+
+def behind(n, m, t, extra, fill):
+    """Contiguous, `extra` elements from the begin of its memory."""
+    flat = torch.full((n * m + extra + 8,), fill, dtype=t, device=DEV)
+    return flat[extra:extra + n * m].view(n, m), flat
 
 
 def relu_reference(x, wg, wu, wd):
@@ -73,7 +79,7 @@ def test_forward_exactly(n, D, F, t):
         r = whole(n, D, t, gen, 0.5, extra)
         for residual, p in ((None, None), (r, None), (r, 0.5)):
             out, around = inside(n, D, t, extra)
-            saved, saved_around = inside(n, 2 * F, t, 0)
+            saved, saved_around = behind(n, 2 * F, t, extra, -7.0)
             want = y
             if p is not None:                             # the factor is 2
                 want = want * factors(p, 77, 5 + n, n, D)
@@ -83,7 +89,8 @@ def test_forward_exactly(n, D, F, t):
             block.forward(x, out, residual=residual, dropout=drop, saved=saved)
             assert torch.equal(out, want.to(t)), (extra, p, int((out != want.to(t)).sum()))
             assert torch.equal(saved, torch.cat([g, u], 1).to(t))
-            assert untouched(around, n, D) and untouched(saved_around, n, 2 * F)
+            assert untouched(around, n, D)
+            assert bool((saved_around[:extra] == -7.0).all()) and bool((saved_around[extra + n * 2 * F:] == -7.0).all())
             again, _ = inside(n, D, t, 0)
             poisoned(block).forward(x, again, residual=residual, dropout=drop)
             assert torch.equal(again, out)
@@ -95,7 +102,8 @@ def test_backward_exactly(n, D, F, t):
     for extra, p in ((0, None), (4, 0.5), (8, None)):
         gen, x, wg, wu, wd = exact_case(n, D, F, t, extra, 3 * n + D + F)
         g, u, h, _ = relu_reference(x, wg, wu, wd)
-        saved = torch.cat([g, u], 1).to(t)
+        saved, _ = behind(n, 2 * F, t, extra, float("nan"))
+        saved.copy_(torch.cat([g, u], 1))
         d = whole(n, D, t, gen, min(1.0, 6.0 / D), extra)
         drop = Dropout(p, state(78, 6), n) if p is not None else None
         e = d.double() * factors(p, 78, 6 + n, n, D) if p is not None else d.double()
@@ -107,11 +115,16 @@ def test_backward_exactly(n, D, F, t):
         block = poisoned(FeedForward(wg, wu, wd, max_rows=n, activation="relu", training=True))
         for add in (None, d):
             d_x, around = inside(n, D, t, extra)
-            grads = [torch.full(s, 7.0, dtype=t, device=DEV) for s in ((F, D), (F, D), (D, F))]
+            grads, grads_around = zip(*[behind(*s, t, extra, -7.0) for s in ((F, D), (F, D), (D, F))])
             block.backward(x, saved, d, d_x, *grads, add=add, dropout=drop)
             assert torch.equal(d_x, (want_x + add.double() if add is not None else want_x).to(t)) and untouched(around, n, D)
-            for got, w in zip(grads, want):
+            for got, w, flat in zip(grads, want, grads_around):
                 assert torch.equal(got, w.to(t))
+                assert bool((flat[:extra] == -7.0).all()) and bool((flat[extra + D * F:] == -7.0).all())
+        # in the type, added to what is there
+        poisoned(block).backward(x, saved, d, None, *grads, dropout=drop, accumulate=True)
+        for got, w in zip(grads, want):
+            assert torch.equal(got, (w.to(t).double() + w).to(t))
         # in 32 bits, added to what is there; the input's gradient alone; the weights' alone; in the place of the output's gradient
         wide = [torch.full(s, 3.0, device=DEV) for s in ((F, D), (F, D), (D, F))]
         poisoned(block).backward(x, saved, d, None, *wide, dropout=drop, accumulate=True)
@@ -280,6 +293,33 @@ def test_rows_do_not_depend_on_their_neighbours():
         block.forward(y, bad)
         keep = [i for i in range(n) if i not in (5, 77, 199)]
         assert torch.equal(out[keep], bad[keep]) and bool(torch.isnan(bad[5]).all())
+
+
+def test_rows_far_apart():
+    """The largest stride: 2100 rows lie more than 4 GiB apart.  All of a call's rows side by side in one buffer."""
+    n, D, F, t = 2100, 64, 68, torch.bfloat16
+    gen, a, wg, wu, wd = exact_case(n, D, F, t, 0, 12)
+    wide = torch.full((n, 1 << 20), -7.0, dtype=t, device=DEV)
+    x, r, out, d, d_x = (wide[:, i * D:(i + 1) * D] for i in range(5))
+    x.copy_(a)
+    r.copy_(whole(n, D, t, gen, 0.5))
+    d.copy_(whole(n, D, t, gen, 0.1))
+    g, u, h, y = relu_reference(x, wg, wu, wd)
+    block, saved = FeedForward(wg, wu, wd, max_rows=n, activation="relu", training=True), torch.empty(n, 2 * F, dtype=t, device=DEV)
+    drop, m = Dropout(0.5, state(79, 8)), factors(0.5, 79, 8, n, D)
+    block.forward(x, out, residual=r, dropout=drop, saved=saved)
+    assert torch.equal(out, (y * m + r.double()).to(t)) and torch.equal(x, a)
+    grads = [torch.empty_like(w) for w in (wg, wu, wd)]
+    block.backward(x, saved, d, d_x, *grads, add=d, dropout=drop)
+    e = d.double() * m
+    b = e @ wd.double()
+    dg, du = b * u * (g > 0), b * g.clamp(min=0)
+    assert torch.equal(d_x, (dg @ wg.double() + du @ wu.double() + d.double()).to(t))
+    for got, w in zip(grads, (dg.t() @ x.double(), du.t() @ x.double(), e.t() @ h)):
+        assert torch.equal(got, w.to(t))
+    drop.apply(x, d_x, residual=r)
+    assert torch.equal(d_x, (x.double() * m + r.double()).to(t))
+    assert bool((wide[:, 5 * D:] == -7.0).all())
 
 
 def test_in_place():
