@@ -355,8 +355,8 @@ int ecrm_embed_grad_dense_dropout(ecrm_ctx *ctx, const uint64_t *keys, const voi
  *
  * Rows: device memory aligned to four elements, strides multiples of 4, at least D (F for Wd), at most 2^20.  n <= max_rows, else
  * EBATCH.  out is x or residual (of the same stride) or overlaps neither; d_x is add or d_out (of the same stride) or overlaps no input;
- * what is written overlaps no other input, no weight, no workspace, no state and nothing else that is written.  What of this the pointers show is
- * refused with EINVAL.  Calls only enqueue. */
+ * what is written overlaps no other input, no weight, no state and nothing else that is written, and nothing lies in the workspace.  What of
+ * this the pointers show is refused with EINVAL.  Calls only enqueue; calls on one handle come from one thread at a time. */
 enum { ECRM_SILU = 0, ECRM_GELU = 1, ECRM_RELU = 2 };
 typedef struct {
     uint32_t dim, hidden; /* D, F: multiples of 4, 4 .. 65536 */

@@ -354,6 +354,9 @@ bool apart(uint32_t a_size, const Rows &a, uint32_t b_size, const Rows &b)
     return strided_apart(a.p, a.p ? a.rows : 0, a.cols * a_size, a.stride * a_size, b.p, b.p ? b.rows : 0, b.cols * b_size, b.stride * b_size);
 }
 
+// Is what is read clear of the workspace, which is written?
+bool clear_of_work(const ecrm_ffn *f, const Rows &r) { return apart(type_bytes(f->cfg.type), r, 1, Rows{f->work, 1, f->bytes, f->bytes}); }
+
 // Is what is written clear of the weights, the workspace and the mask's state?
 bool clear_of_own(const ecrm_ffn *f, const ecrm_mask *mask, uint32_t size, const Rows &w)
 {
@@ -480,7 +483,7 @@ int ecrm_ffn_forward(ecrm_ffn *f, const void *x, uint64_t x_stride, uint64_t n, 
     if (saved && (uintptr_t)saved % (4 * size)) return ECRM_EINVAL;
     auto in_place = [&](const Rows &r) { return r.p == out && r.stride == out_stride; };
     if ((!in_place(rx) && !apart(size, rx, size, ro)) || (residual && !in_place(rr) && !apart(size, rr, size, ro))) return ECRM_EINVAL;
-    if (!clear_of_own(f, mask, size, ro)) return ECRM_EINVAL;
+    if (!clear_of_own(f, mask, size, ro) || !clear_of_work(f, rx) || !clear_of_work(f, rr)) return ECRM_EINVAL;
     if (saved && (!apart(size, rs, size, rx) || !apart(size, rs, size, rr) || !apart(size, rs, size, ro) || !clear_of_own(f, mask, size, rs)))
         return ECRM_EINVAL;
     hipStream_t st = (hipStream_t)stream;
@@ -547,6 +550,8 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
         rdx{d_x, n, D, d_x_stride};
     if (!rows_fit(f, rx) || !rows_fit(f, ro) || (d_x && !rows_fit(f, rdx)) || (ra.p && !rows_fit(f, ra))) return ECRM_EINVAL;
     if (!saved || (uintptr_t)saved % (4 * size)) return ECRM_EINVAL;
+    for (const Rows *r : {&rx, &rs, &ro, &ra})
+        if (!clear_of_work(f, *r)) return ECRM_EINVAL;
     if (weights)
         for (const Rows *w : {&rg, &ru, &rd})
             for (const Rows *r : {&rx, &rs, &ro, &ra, &rdx})

@@ -626,10 +626,13 @@ __device__ __forceinline__ void run_tile(const ProductArgs &a, const Product &p,
             u32x4 fa[MB], fb[NB];
             read_fragments<T, L::kColumnsA, BM, false, MB>(ta, wm * MB, s, fa);
             read_fragments<T, L::kColumnsB, BN, L::kPair == 2, NB>(tb, wn * NB, s, fb);
+            // before the other wave's reads (1 to 2 % with a's rows along K, nothing or less with weight gradients)
+            if (!L::kColumnsA) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int i = 0; i < MB; ++i)
 #pragma unroll
                 for (int j = 0; j < NB; ++j) acc[i][j] = Fragment<T>::multiply(fb[j], fa[i], acc[i][j]);
+            if (!L::kColumnsA) __builtin_amdgcn_s_setprio(0);
         }
     };
     // tile t is there, all of it

@@ -429,6 +429,8 @@ def test_refusals():
     assert code(lambda: block.forward(x, wd[:n, :D])) == ECRM_EINVAL                  # a weight
     own = block.workspace[:n * D * 2].view(t).view(n, D)
     assert code(lambda: block.forward(x, own)) == ECRM_EINVAL
+    assert code(lambda: block.forward(own, out)) == ECRM_EINVAL
+    assert code(lambda: block.forward(x, out, residual=own)) == ECRM_EINVAL
     assert code(lambda: block.forward(x[:4], out[:4], saved=x.flatten()[:4 * 2 * F].view(4, 2 * F))) == ECRM_EINVAL
     with pytest.raises(EcrmError):
         FeedForward(wg, wu, wd, max_rows=n, workspace=torch.empty(1024, dtype=torch.uint8, device=DEV))
