@@ -11,7 +11,7 @@
 // kSortHere tokens, 6.8 us for 64), two (up to kOneBlock, 11 us for 600), three (up to kRankMost), five (up to 2^16; four for the dense
 // form, which counts no rows), then two for each digit of the sort, or three, and three or four behind it: five to nine up to 2^18
 // tokens, six to sixteen beyond (twelve for rows of 19 to 27 bits).  Of 2^16 tokens of text with 256 floats in bf16, 42 us, the sums
-// take 16, the sort 20 and the join 4.
+// take 16, the sort 20 and the join 4; with dropout (mask.h), which the sums draw again, the sums take 20, of 2^20 tokens 177.
 #include "mask.h"
 
 namespace ecrm {
@@ -363,7 +363,7 @@ __global__ __launch_bounds__(kSumThreads) void sum_runs_kernel(SumArgs a)
                     row[q] = s_idx[min(i0 + q, hi - 1u)];
                     col[q] = c;
                 }
-                mask_quads<U>(mask, row, col, a.units.d % 2u == 0 && a.quads % 2u == 0, bits);
+                mask_quads<U>(mask, row, col, a.units.d % 2u == 0 && a.quads % 2u == 0, U, bits);
             }
 #pragma unroll
             for (uint32_t q = 0; q < U; ++q) {

@@ -16,6 +16,11 @@
 //
 // The results' 16 x 16 blocks are held transposed (b is the first operand of the instruction): a lane has four consecutive columns of
 // a row.  Of 16-bit results two blocks make a pair, the columns dealt out to them by fours, so that a lane has eight: 16 bytes to an access.
+//
+// What bounds the loop: 256 x 256 tiles, one workgroup of eight waves to a CU, move 64 KB from the caches for 8.4 MFLOP.  16384 x 4096, K =
+// 4096, bf16: 415 to 440 us, 1250 to 1320 TFLOP/s; with all rows in one place, so that nothing but L1 is asked, 385 (1430), a
+// bf16 product of 8192^3 by the library 1460: the clock under this load is what is left.  LDS is read a fifth of the time, without
+// conflicts.  Fragments read ahead of the barrier changed nothing (1 %), K rotated by tile, so that tiles ask unlike channels, cost 10 %.
 #pragma once
 
 #include "mask.h"
