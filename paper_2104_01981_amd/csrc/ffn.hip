@@ -6,307 +6,12 @@
 // with 0.27 GB of g and u written on the way), backward 900 to 925 (910); the same products alone take the library 515 and 1215 us.  kBack is bound by
 // memory instead: two elements in and three out for each of h, 245 us, 105 of them multiplications.  D = 128, F = 512, 8192
 // rows: memory, 16 us forward, of which g, u and h take 6; 34 backward.  A few rows: the weights, 25 MB for five rows in 11 us.
-#include "products.h"
+#include "ffn_plan.h"
 
 #include <new>
 #include <string.h>
 
 namespace ecrm {
-
-// ---- which tiles -----------------------------------------------------------------------------------------------------------------
-// What a product takes is estimated in us from what was measured (M, N of 512 to 4096, all CUs in step): a tile's steps of 128 bytes of
-// K, alone on its CU and for each of several (times `transposed` for the gradients in 16 bits); the launch, a tile's begin and end (`back`: kBack's,
-// which is bound by what it reads and writes).  16 bits: 64 x 64 0.50 and 0.17 a step, 128 x 128 0.65
-// and 0.47, 256 x 256 1.58.  32 bits are bound by their matrix instructions, 137 TFLOP/s with any of these and all CUs full, so that small
-// tiles, more of them to a CU, gain: 32 x 32 0.24 and 0.12, 64 x 64 0.62 and 0.46, 128 x 128 1.96 and 1.79 (777 rows, D = 260, F =
-// 684: 26 us with 64 x 64 at least, 19 so).
-enum { kTile256 = 0, kTile128 = 1, kTile64 = 2, kTile32 = 3, kTilings = 4 };
-struct TilingCost { uint32_t side, resident; double step[2], shared[2], transposed, launch, tile, back; };      // [0] 16 bits, [1] 32; 0: not for these
-constexpr TilingCost kCosts[kTilings] = {{256, 1, {1.58, 0}, {1.58, 0}, 1.0, 3.0, 8.0, 20.0}, {128, 2, {0.65, 1.96}, {0.47, 1.79}, 1.06, 5.0, 1.4, 6.8},
-                                         {64, 5, {0.50, 0.62}, {0.172, 0.46}, 1.25, 2.5, 0.42, 1.6}, {32, 8, {0, 0.24}, {0, 0.12}, 1.0, 2.5, 0.3, 0.6}};
-// Columns of a tile; of each projection for kGate.
-static constexpr uint32_t columns_of(uint32_t side, bool dual) { return dual && side > 32 ? side / 2u : side; }
-constexpr uint32_t kSplitCounts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
-constexpr double kJoinWait = 2.0, kJoinOne = 2.5e4;          // parts joined by the workgroup that is there last: us; bytes a us
-constexpr uint32_t kSkinnyParts = 16;
-constexpr size_t kPartMost = 32u << 20;          // bytes of the parts of split products, at most
-constexpr uint32_t kCounters = kPartMost / (2u * 32u * 32u * 4u);       // tiles of two parts or more
-
-constexpr uint64_t kMostWorkgroups = 0xFFFFFFFFu / 512u;        // a launch has fewer than 2^32 threads
-
-struct Split { uint32_t splits, each; };
-// Products of one launch (the last of them with the splits of their own, where there are two sizes).
-struct Plan { uint32_t tiling; Split split[2]; uint32_t counters; double cost; };
-// Rows up to `rows` of the results with one tiling, the others (if there are any) with another.
-struct RowPlan { uint32_t rows; Plan main, rest; };
-
-struct ProductSize { uint32_t M, N, K, halves, count; bool dual, first, gradients; };       // `count` of them
-
-static uint64_t tiles_of(const ProductSize &z, uint32_t M, uint32_t side)
-{
-    const uint32_t columns = columns_of(side, z.dual);
-    return (uint64_t)((M + side - 1) / side) * ((z.N + columns - 1) / columns) * z.count;
-}
-
-// What a launch of A tiles that take ta and then B that take tb, so many at a time, takes.
-static double makespan(uint64_t A, double ta, uint64_t B, double tb, uint64_t slots)
-{
-    // the places that have one of the first kind more than the others, and those others
-    uint64_t n[2] = {A % slots, slots - A % slots};
-    double at[2] = {(double)(A / slots + 1) * ta, (double)(A / slots) * ta}, end = n[0] ? at[0] : at[1];
-    while (B) {
-        const int g = n[0] && at[0] <= at[1] ? 0 : 1;
-        at[g] += tb;
-        if (at[g] > end) end = at[g];
-        B -= B < n[g] ? B : n[g];
-    }
-    return end;
-}
-
-// The sizes' products side by side (b.count = 0: a alone).
-static Plan plan_launch(const ProductSize &a, const ProductSize &b, uint32_t type, uint32_t cus, size_t room)
-{
-    const uint32_t wide = type == ECRM_F32 ? 1u : 0u, elements = kRowBytes / type_bytes(type);
-    const ProductSize *sizes[2] = {&a, &b};
-    Plan best{};
-    for (uint32_t t = 0; t < kTilings; ++t) {
-        const TilingCost &c = kCosts[t];
-        if (c.step[wide] == 0.0) continue;
-        uint64_t tiles[2];
-        uint32_t k_tiles[2];
-        for (int i = 0; i < 2; ++i) {
-            tiles[i] = sizes[i]->count ? tiles_of(*sizes[i], sizes[i]->M, c.side) : 0;
-            k_tiles[i] = (sizes[i]->K + elements - 1) / elements * sizes[i]->halves;
-        }
-        auto split = [&](int i, uint32_t splits) {
-            const uint32_t each = (k_tiles[i] + splits - 1) / splits;
-            return Split{(k_tiles[i] + each - 1) / each, each};
-        };
-        const double part = (double)c.side * c.side * 4.0;
-        for (uint32_t sa : kSplitCounts) {
-            if (sa > k_tiles[0] || (a.first && sa > 1)) break;           // a call's first product has no counters that are cleared before it
-            const Split x = split(0, sa);
-            const double a_bytes = x.splits > 1 ? part * tiles[0] * x.splits : 0.0;
-            if (a_bytes > (double)room) break;
-            for (uint32_t sb : kSplitCounts) {
-                if (b.count ? sb > k_tiles[1] : sb > 1) break;
-                const Split y = b.count ? split(1, sb) : Split{1, 0};
-                const double bytes = a_bytes + (y.splits > 1 ? part * tiles[1] * y.splits : 0.0);
-                if (bytes > (double)room) break;
-                const uint64_t units = tiles[0] * x.splits + tiles[1] * y.splits, there = (units + cus - 1) / cus;
-                if (units > kMostWorkgroups) continue;
-                const double together = there < c.resident ? (double)there : (double)c.resident;
-                // 32 x 32 of each projection are twice the work, larger tiles have both in their width
-                const double twice = a.dual && c.side == 32 ? 2.0 : 1.0;
-                const double alone = c.step[wide] * twice, shared = c.shared[wide] * twice * together * (a.gradients && !wide ? c.transposed : 1.0);
-                const double step = shared > alone ? shared : alone;
-                auto unit = [&](int i, const Split &s) {
-                    return (a.first && !a.dual ? c.back : c.tile) * together + s.each * step + (s.splits > 1 ? kJoinWait + s.splits * part / kJoinOne : 0.0);
-                };
-                const uint64_t slots = (uint64_t)(cus * together);
-                const double ua = unit(0, x), ub = b.count ? unit(1, y) : 1.0;
-                double cost = c.launch + (ua >= ub ? makespan(tiles[0] * x.splits, ua, tiles[1] * y.splits, ub, slots)
-                                                   : makespan(tiles[1] * y.splits, ub, tiles[0] * x.splits, ua, slots));
-                const uint64_t counters = (x.splits > 1 ? tiles[0] : 0) + (y.splits > 1 ? tiles[1] : 0);
-                if (!best.split[0].splits || cost < best.cost) best = Plan{t, {x, y}, (uint32_t)counters, cost};
-            }
-        }
-    }
-    return best;
-}
-
-// Up to 32 rows, of 32 bits up to 16, are skinny_kernel's.  us forward so / by tiles, 16 and 32 rows: bf16 D = 128, F = 512 6.8 / 8.7, 8.2 /
-// 8.7; 1024, 1024 9.2 / 14.5, 11.5 / 14.6; 1024, 4096 15.1 / 19.8, 20.1 / 19.8.  fp32 8.0 / 12.6, 10.0 / 12.7; 15.2 / 21.4, 23.5 / 21.3;
-// 29.2 / 31.5, 44.3 / 31.4.
-static uint32_t skinny_waves(uint32_t K, uint32_t type)        // that have kAtOnce steps each
-{
-    const uint32_t steps = (K * type_bytes(type) + 63u) / 64u;
-    return (steps + kAtOnce - 1u) / kAtOnce;
-}
-static uint32_t skinny_parts(uint32_t N, uint32_t K, uint32_t type, uint32_t cus)
-{
-    const uint32_t blocks = (N + 15u) / 16u, fit = cus / blocks, fill = skinny_waves(K, type) / 8u;
-    const uint32_t parts = fit < fill ? fit : fill;      // no more workgroups than CUs, eight waves at least to each
-    return parts < 1u ? 1u : parts > kSkinnyParts ? kSkinnyParts : parts;
-}
-constexpr double kSkinnyLaunch = 3.5, kSkinnyRate = 2.5e6;               // us; bytes of weights a us
-static bool is_skinny(uint32_t rows, uint32_t type) { return rows <= (type == ECRM_F32 ? 16u : 32u); }
-
-// z's products with its rows cut where that is faster, those up to the cut beside the other size's (other.count = 0: alone).
-static RowPlan plan_rows(const ProductSize &other, const ProductSize &z, uint32_t type, uint32_t cus, size_t room)
-{
-    const ProductSize none{};
-    auto plan = [&](uint32_t rows, bool beside) {
-        ProductSize part = z;
-        part.M = rows;
-        if (!z.gradients && (z.dual || !z.first) && is_skinny(rows, type)) {
-            Plan skinny{};
-            skinny.cost = kSkinnyLaunch + (double)z.N * z.K * (z.dual ? 2 : 1) * type_bytes(type) / kSkinnyRate;
-            return skinny;
-        }
-        return beside && other.count ? plan_launch(other, part, type, cus, room) : plan_launch(part, none, type, cus, room);
-    };
-    RowPlan best{z.M, plan(z.M, true), Plan{}};
-    for (uint32_t side : {256u, 128u, 64u}) {
-        // as many rows of tiles as fill the CUs to the last, or as are whole
-        const uint64_t across = tiles_of(z, side, side), all = z.M / side, rounds = all * across / cus;
-        for (uint64_t down : {rounds * cus / across, all}) {
-            const uint32_t rows = (uint32_t)(down * side);
-            if (!rows || rows >= z.M) continue;
-            const Plan main = plan(rows, true), rest = plan(z.M - rows, false);
-            if (main.cost + rest.cost < best.main.cost + best.rest.cost) best = RowPlan{rows, main, rest};
-        }
-    }
-    return best;
-}
-
-// Gives the products of a launch their tiles, parts and workgroups, in order.
-static void lay_out(ProductArgs &a, uint32_t rows, uint32_t columns)
-{
-    a.workgroups = 0;
-    uint32_t part = 0, counter = 0;
-    for (uint32_t i = 0; i < a.products; ++i) {
-        Product &p = a.p[i];
-        p.tiles_m = (p.M + rows - 1) / rows;
-        p.tiles_n = (p.N + columns - 1) / columns;
-        const uint32_t tiles = p.tiles_m * p.tiles_n;
-        p.first = a.workgroups;
-        a.workgroups += tiles * p.splits;
-        if (p.splits == 1) continue;
-        p.part = part;
-        p.counter = counter;
-        part += tiles * p.splits;
-        counter += tiles;
-    }
-}
-
-template <typename T, int KIND, int BM, int BN, int WM, int WN>
-static void launch_tiling(ProductArgs &a, hipStream_t st)
-{
-    typedef Tiling<T, KIND, BM, BN, WM, WN> L;
-    lay_out(a, BM, L::kColumns);
-    hipLaunchKernelGGL((product_kernel<T, KIND, BM, BN, WM, WN>), dim3(a.workgroups), dim3(L::kThreads), 0, st, a);
-}
-
-template <typename T, int KIND>
-static void launch_planned(ProductArgs &a, const Plan &plan, hipStream_t st)
-{
-    a.products = 1;
-    a.p[0].splits = plan.split[0].splits;
-    a.p[0].each = plan.split[0].each;
-    // both projections of kGate: 64 columns of each to a wave (32 of 64 x 64), whole lines of the results
-    if constexpr (sizeof(T) == 2) {
-        if (plan.tiling == kTile256) {
-            if constexpr (KIND == kGate) launch_tiling<T, KIND, 256, 256, 4, 2>(a, st);
-            else launch_tiling<T, KIND, 256, 256, 2, 4>(a, st);
-            return;
-        }
-    }
-    if constexpr (sizeof(T) == 4) {
-        if (plan.tiling == kTile32) {
-            if constexpr (KIND == kGate) launch_tiling<T, KIND, 32, 64, 2, 2>(a, st);
-            else launch_tiling<T, KIND, 32, 32, 2, 2>(a, st);
-            return;
-        }
-    }
-    if (plan.tiling == kTile128) {
-        if constexpr (KIND == kGate) launch_tiling<T, KIND, 128, 128, 4, 1>(a, st);
-        else launch_tiling<T, KIND, 128, 128, 2, 2>(a, st);
-    } else {
-        if constexpr (KIND == kGate) launch_tiling<T, KIND, 64, 64, 4, 1>(a, st);
-        else launch_tiling<T, KIND, 64, 64, 2, 2>(a, st);
-    }
-}
-
-template <typename T, int BM, int BN, int WM, int WN>
-static void launch_gradients(ProductArgs &a, hipStream_t st)
-{
-    lay_out(a, BM, BN);
-    hipLaunchKernelGGL((gradients_kernel<T, BM, BN, WM, WN>), dim3(a.workgroups), dim3(WM * WN * kWave), 0, st, a);
-}
-
-// The weights' products, those of x, or both.
-template <typename T>
-static void launch_gradients(ProductArgs &a, const Product *weights, const Product *input, const Plan &plan, hipStream_t st)
-{
-    a.products = 0;
-    auto take = [&](const Product *p, uint32_t count, const Split &s) {
-        for (uint32_t i = 0; i < count; ++i) {
-            Product &to = a.p[a.products++];
-            to = p[i];
-            to.splits = s.splits;
-            to.each = s.each;
-        }
-    };
-    // longest first
-    if (weights && input && plan.split[0].each < plan.split[1].each) {
-        take(input, 1, plan.split[1]);
-        take(weights, 3, plan.split[0]);
-    } else {
-        if (weights) take(weights, 3, plan.split[0]);
-        if (input) take(input, 1, plan.split[weights ? 1 : 0]);
-    }
-    if constexpr (sizeof(T) == 2)
-        if (plan.tiling == kTile256) return launch_gradients<T, 256, 256, 2, 4>(a, st);
-    if constexpr (sizeof(T) == 4)
-        if (plan.tiling == kTile32) return launch_gradients<T, 32, 32, 2, 2>(a, st);
-    if (plan.tiling == kTile128) launch_gradients<T, 128, 128, 2, 2>(a, st);
-    else launch_gradients<T, 64, 64, 2, 2>(a, st);
-}
-
-// The product's rows from `first` on.
-template <typename T, int KIND>
-static void skip_rows(ProductArgs &a, uint32_t first)
-{
-    Product &p = a.p[0];
-    auto on = [&](const void *q, uint64_t stride) { return q ? (void *)((T *)q + first * stride) : nullptr; };
-    for (int i = 0; i < 2; ++i) p.a.p[i] = on(p.a.p[i], p.a.stride[i]);
-    p.out = on(p.out, p.out_stride);
-    if (KIND == kGate) p.out2 = on(p.out2, 2ull * p.N);
-    if (KIND == kBack) {
-        p.in = on(p.in, 2ull * p.N);
-        p.out2 = on(p.out2, p.out_stride);
-        p.out3 = on(p.out3, p.out_stride);
-    } else {
-        p.in = on(p.in, p.in_stride);
-    }
-    a.first_row = first;
-    p.M -= first;
-}
-
-template <typename T, int KIND, int XB>
-static void launch_skinny(ProductArgs &a, uint32_t type, uint32_t cus, hipStream_t st)
-{
-    const Product &p = a.p[0];
-    const uint32_t parts = KIND == kOut ? skinny_parts(p.N, p.K, type, cus) : 1u, share = (skinny_waves(p.K, type) + parts - 1u) / parts;
-    const uint32_t waves = share < Skinny<XB>::kWaves ? share : Skinny<XB>::kWaves;
-    hipLaunchKernelGGL((skinny_kernel<T, KIND, XB>), dim3((p.N + 15u) / 16u, parts), dim3(waves * kWave), 0, st, a);
-}
-
-template <typename T, int KIND>
-static void launch_rows(ProductArgs &a, const Plan &plan, uint32_t type, uint32_t cus, hipStream_t st)
-{
-    if constexpr (KIND == kGate || KIND == kOut) {
-        if (is_skinny(a.p[0].M, type)) {
-            if (a.p[0].M <= 16) return launch_skinny<T, KIND, 1>(a, type, cus, st);
-            if constexpr (sizeof(T) == 2) return launch_skinny<T, KIND, 2>(a, type, cus, st);
-        }
-    }
-    launch_planned<T, KIND>(a, plan, st);
-}
-
-template <typename T, int KIND>
-static void launch_product(ProductArgs &a, const RowPlan &plan, uint32_t type, uint32_t cus, hipStream_t st)
-{
-    const uint32_t M = a.p[0].M;
-    a.first_row = 0;
-    a.p[0].M = plan.rows;
-    launch_rows<T, KIND>(a, plan.main, type, cus, st);
-    if (plan.rows == M) return;
-    a.p[0].M = M;
-    skip_rows<T, KIND>(a, plan.rows);
-    launch_rows<T, KIND>(a, plan.rest, type, cus, st);
-}
 
 __global__ __launch_bounds__(256) void clear_kernel(uint32_t *to, uint64_t words)
 {
@@ -331,8 +36,7 @@ struct ecrm_ffn {
     int cus;
     // plans, kept while the number of rows stays, since making them takes some us
     uint64_t rows_of[kPlans];
-    RowPlan gate, out, back, input, both;
-    Plan weights;
+    RowPlan gate, out, back, input, both, weights;
 };
 
 namespace {
@@ -404,7 +108,7 @@ void make_plan(ecrm_ffn *f, int what, uint32_t n)
     } else if (what == kPlanBack) {
         f->back = plan_rows(none, ProductSize{n, F, D, 1, 1, false, true, false}, type, cus, room);
     } else if (what == kPlanWeights) {
-        f->weights = plan_launch(weights, none, type, cus, room);
+        f->weights = RowPlan{F, plan_launch(weights, none, type, cus, room), Plan{}};
     } else {
         (what == kPlanBoth ? f->both : f->input) = plan_rows(what == kPlanBoth ? weights : none, input, type, cus, room);
     }
@@ -510,14 +214,14 @@ int ecrm_ffn_forward(ecrm_ffn *f, const void *x, uint64_t x_stride, uint64_t n, 
         a.p[0].out = h;
         a.p[0].out_stride = f->pitch;
         a.p[0].out2 = saved;
-        launch_product<T, kGate>(a, f->gate, type, (uint32_t)f->cus, st);
+        BlockLaunch<T>::gate(a, f->gate, (uint32_t)f->cus, st);
         a.p[0] = product(h, f->pitch, f->down, f->down_stride, N, D, F);
         a.p[0].out = out;
         a.p[0].out_stride = out_stride;
         a.p[0].in = residual;
         a.p[0].in_stride = residual_stride;
         a.masked = mask ? 1u : 0u;
-        launch_product<T, kOut>(a, f->out, type, (uint32_t)f->cus, st);
+        BlockLaunch<T>::out(a, f->out, (uint32_t)f->cus, st);
     });
     return launched();
 }
@@ -579,7 +283,7 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
         if (weights) make_plan(f, kPlanWeights, N);
         if (d_x) make_plan(f, kPlanInput, N);
     }
-    if (!is_planned(f->back) || (d_x && !is_planned(both ? f->both : f->input)) || (weights && !both && !f->weights.split[0].splits)) return ECRM_EINVAL;
+    if (!is_planned(f->back) || (d_x && !is_planned(both ? f->both : f->input)) || (weights && !both && !is_planned(f->weights))) return ECRM_EINVAL;
 
     void *h = f->work + f->off_h, *dg = f->work + f->off_dg, *du = f->work + f->off_du;
     a.part = (float *)(f->work + f->off_part);
@@ -598,7 +302,7 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
     a.wide = weight_type != type ? 1u : 0u;
     a.arrived = (uint32_t *)(f->work + f->off_arrived);
     a.clear = both ? counters_of(f->both) : 0u;
-    if (!both && weights) a.clear = f->weights.counters;
+    if (!both && weights) a.clear = counters_of(f->weights);
     if (!both && d_x && counters_of(f->input) > a.clear) a.clear = counters_of(f->input);
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
@@ -609,7 +313,7 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
         a.p[0].out3 = h;
         a.p[0].out_stride = f->pitch;
         a.p[0].scale = scale;
-        launch_product<T, kBack>(a, f->back, type, (uint32_t)f->cus, st);
+        BlockLaunch<T>::back(a, f->back, (uint32_t)f->cus, st);
         Product w[3], in;
         w[0] = product(dg, f->pitch, x, x_stride, F, D, N);
         w[0].out = d_gate;
@@ -630,19 +334,8 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
         in.out = d_x;
         in.out_stride = d_x_stride;
         in.kind = kInput;
-        const RowPlan &rows = both ? f->both : f->input;
-        if (weights && !both) launch_gradients<T>(a, w, nullptr, f->weights, st);
-        if (d_x) {
-            in.M = rows.rows;
-            launch_gradients<T>(a, both ? w : nullptr, &in, rows.main, st);
-            if (rows.rows < N) {
-                a.p[0] = in;
-                a.p[0].M = N;
-                skip_rows<T, kInput>(a, rows.rows);
-                in = a.p[0];
-                launch_gradients<T>(a, nullptr, &in, rows.rest, st);
-            }
-        }
+        if (weights && !both) BlockLaunch<T>::gradients(a, w, nullptr, f->weights, st);
+        if (d_x) BlockLaunch<T>::gradients(a, both ? w : nullptr, &in, both ? f->both : f->input, st);
     });
     return launched();
 }
