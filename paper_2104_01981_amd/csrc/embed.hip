@@ -98,7 +98,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(EmbedArgs a)
         f32x4 e[U];
         size_t to[U];
         uint32_t row[U], col[U];
-        uint2 bits[U];
+        uint2 bits[U] = {};
 #pragma unroll
         for (uint32_t q = 0; q < U; ++q) {
             const uint32_t u = min(u0 + q * kWave + lane, total - 1u), r = a.d4.div(u), c = (u - r * a.d4.d) * 4u;
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(EmbedArgs a)
             if (what.x != kNoKey) e[q] = *(const f32x4 *)(a.E + (size_t)what.x * D + c) * a.scale;
         }
         if (DROP) {                                      // lanes 2i and 2i + 1 have quads 2j and 2j + 1 if a row has an even number
-            mask_quads<U>(mask, row, col, a.d4.d % 2u == 0, (total - u0 + kWave - 1u) / kWave, bits);
+            mask_quads<U, true>(mask, row, col, a.d4.d % 2u == 0, bits, (total - u0 + kWave - 1u) / kWave);
 #pragma unroll
             for (uint32_t q = 0; q < U; ++q) e[q] = drop4(e[q], bits[q], mask);
         }

@@ -363,7 +363,7 @@ __global__ __launch_bounds__(kSumThreads) void sum_runs_kernel(SumArgs a)
                     row[q] = s_idx[min(i0 + q, hi - 1u)];
                     col[q] = c;
                 }
-                mask_quads<U>(mask, row, col, a.units.d % 2u == 0 && a.quads % 2u == 0, U, bits);
+                mask_quads<U>(mask, row, col, a.units.d % 2u == 0 && a.quads % 2u == 0, bits);
             }
 #pragma unroll
             for (uint32_t q = 0; q < U; ++q) {

@@ -55,25 +55,22 @@ __device__ __forceinline__ uint2 mask_quad(const MaskKey &k, uint32_t row, uint3
 
 // The bits of N places in lanes' quads, all of them by turns where both lanes of a pair (2i, 2i + 1) have the halves of one block
 // each time (`paired`, the same for the wave; both lanes of a pair get here together): a lane draws every other one and hands its
-// neighbour the half that it has no use for.  Only the first `used` places count (the same for the wave).
-template <int N>
-__device__ __forceinline__ void mask_quads(const MaskKey &k, const uint32_t (&row)[N], const uint32_t (&c)[N], bool paired, uint32_t used,
-                                           uint2 (&bits)[N])
+// neighbour the half that it has no use for.  FEW: only the first `used` places count (the same for the wave).
+template <int N, bool FEW = false>
+__device__ __forceinline__ void mask_quads(const MaskKey &k, const uint32_t (&row)[N], const uint32_t (&c)[N], bool paired, uint2 (&bits)[N],
+                                           uint32_t used = N)
 {
     static_assert(N % 2 == 0, "places are taken in twos");
     if (!paired) {
 #pragma unroll
-        for (int q = 0; q < N; ++q) {
-            bits[q] = uint2{0u, 0u};
-            if ((uint32_t)q < used) bits[q] = mask_quad(k, row[q], c[q]);
-        }
+        for (int q = 0; q < N; ++q)
+            if (!FEW || (uint32_t)q < used) bits[q] = mask_quad(k, row[q], c[q]);
         return;
     }
     const bool odd = threadIdx.x & 1u;
 #pragma unroll
     for (int q = 0; q < N; q += 2) {
-        bits[q] = bits[q + 1] = uint2{0u, 0u};
-        if ((uint32_t)q >= used) continue;
+        if (FEW && (uint32_t)q >= used) break;
         const uint4 b = mask_block(k, odd ? row[q + 1] : row[q], (odd ? c[q + 1] : c[q]) / 8u);
         const int s0 = (int)(odd ? b.x : b.z), s1 = (int)(odd ? b.y : b.w);
         constexpr int kSwap = 0xB1;                      // lanes 1, 0, 3, 2 of each four
