@@ -312,7 +312,7 @@ int ecrm_grads_clip(ecrm_grads *grads, const ecrm_grads *out, const float *norm,
  *
  * ecrm_dropout          out = residual + drop(x), formed in fp32, rounded once; residual = NULL: out = drop(x), and, of the gradient of
  *                       that, the gradient of x.  rows x cols elements of `type`; cols a multiple of 4, up to 2^24; up to 2^32
- *                       rows, as far from each other as ecrm_embed allows.  out is x or residual (of the same stride), or overlaps neither, nor state.
+ *                       rows, at least cols apart (a multiple of 4), all of them within 2^48 elements.  out is x or residual (of the same stride), or overlaps neither, nor state.
  * ecrm_embed_dropout    ecrm_embed with out = drop(scale * entry), row i of the mask for out[i]; n <= 2^32.
  * ecrm_embed_grad_dropout, ecrm_embed_grad_dense_dropout
  *                       the gradients of that: what was dropped of a row of d_out counts for nothing, and sums are multiplied by c, too,

@@ -165,7 +165,7 @@ extern "C" int ecrm_dropout(const ecrm_mask *mask, const void *x, uint64_t x_str
     const uint32_t size = type_bytes(type);
     const uint64_t row = (uint64_t)cols * size;
     auto ok = [&](const void *p, uint64_t stride) {
-        return p && (uintptr_t)p % (4 * size) == 0 && stride >= cols && stride % 4 == 0 && (rows == 1 || stride <= 1ull << 48);
+        return p && (uintptr_t)p % (4 * size) == 0 && stride >= cols && stride % 4 == 0 && (rows == 1 || stride <= (1ull << 48) / (rows - 1));
     };
     if (rows == 1) x_stride = residual_stride = out_stride = cols;          // of one row it says nothing
     if (!ok(x, x_stride) || !ok(out, out_stride) || (residual && !ok(residual, residual_stride))) return ECRM_EINVAL;

@@ -57,6 +57,12 @@ def test_dropout_refuses(lib, bad):
                             a["rows"], a["cols"], None) == EINVAL
 
 
+def test_dropout_refuses_rows_that_no_memory_holds(lib):
+    """As far apart as one row after another may be, but 2^20 of them: the last one's address passes 64 bits and comes round."""
+    for rows, stride in ((1 << 20, 1 << 48), (1 << 32, 1 << 32), (3, (1 << 47) + 4)):
+        assert lib.ecrm_dropout(_mask(), 8192, stride, None, 0, 65536, stride, F32, rows, 16, None) == EINVAL, (rows, stride)
+
+
 def test_dropout_of_nothing(lib):
     assert lib.ecrm_dropout(_mask(), None, 0, None, 0, None, 0, F32, 0, 16, None) == 0
 
