@@ -293,17 +293,19 @@ class Dropout:
     def __init__(self, p, state, offset=0):
         assert _is_words(state) and state.numel() == 2
         self._lib = load_library()
-        self.state = state
+        self.state, self._device = state, state.get_device()
         self.mask = EcrmMask(state.data_ptr(), offset & 0xFFFFFFFFFFFFFFFF, p)
 
     def apply(self, x, out, residual=None, stream=None, check=True):
         """out = residual + dropout(x); the gradient of x is apply(gradient of out).  x, out, residual: [rows, cols] of fp32, bf16 or
         fp16, rows at any multiple of 4 elements from each other; out may be x or residual."""
         shape, t = x.shape, x.dtype
-        assert x.is_cuda and out.is_cuda and len(shape) == 2 and out.shape == shape and out.dtype == t
+        device = self._device
+        assert len(shape) == 2 and out.shape == shape and out.dtype == t
+        assert x.get_device() == out.get_device() == device == _current_device(), "all on the current device"
         rows, cols = shape
         assert rows == 0 or cols < 2 or (x.stride(1) == 1 and out.stride(1) == 1)
-        assert residual is None or _is_rows(residual, rows, cols, t)
+        assert residual is None or _is_rows(residual, rows, cols, t, device)
         rc = self._lib.ecrm_dropout(self.mask, x.data_ptr(), _row(x), *_optional(residual), out.data_ptr(), _row(out), _type(x), rows, cols,
                                     _stream(stream))
         if check and rc != ECRM_OK:
@@ -311,9 +313,9 @@ class Dropout:
         return rc
 
 
-def _is_rows(t, rows, cols, dtype):
-    """A matrix in device memory whose rows have their elements side by side?"""
-    return (t.is_cuda and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols and t.dtype == dtype
+def _is_rows(t, rows, cols, dtype, device):
+    """A matrix in that device's memory whose rows have their elements side by side?"""
+    return (t.get_device() == device and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols and t.dtype == dtype
             and (rows == 0 or cols < 2 or t.stride(1) == 1))
 
 
@@ -336,10 +338,9 @@ class FeedForward:
         self._ffn = C.c_void_p(0)
         self.hidden, self.dim = gate.shape
         self.dtype, self.max_rows = gate.dtype, max_rows
-        assert _is_rows(gate, self.hidden, self.dim, self.dtype) and _is_rows(up, self.hidden, self.dim, self.dtype)
-        assert _is_rows(down, self.dim, self.hidden, self.dtype)
-        self._device = gate.device.index
-        assert gate.device == up.device == down.device and self._device == torch.cuda.current_device()
+        self._device = device = torch.cuda.current_device()
+        assert _is_rows(gate, self.hidden, self.dim, self.dtype, device) and _is_rows(up, self.hidden, self.dim, self.dtype, device)
+        assert _is_rows(down, self.dim, self.hidden, self.dtype, device)
         cfg = EcrmFfnConfig(self.dim, self.hidden, _type(gate), self.ACTIVATIONS[activation], max_rows, 1 if training else 0)
         rc = self._lib.ecrm_ffn_create(C.byref(cfg), C.byref(self._ffn))
         if rc != ECRM_OK:
@@ -383,10 +384,11 @@ class FeedForward:
     def forward(self, x, out, residual=None, dropout=None, saved=None, stream=None, check=True):
         """out = residual + dropout(block(x)); x, out, residual: [n, dim], rows at any multiple of 4 elements from each other; out may be
         x or residual.  saved [n, 2 * hidden]: what the backward pass needs."""
-        n, t = x.shape[0], self.dtype
-        assert _is_rows(x, n, self.dim, t) and _is_rows(out, n, self.dim, t)
-        assert residual is None or _is_rows(residual, n, self.dim, t)
-        assert saved is None or (_is_rows(saved, n, 2 * self.hidden, t) and saved.is_contiguous())
+        n, t, device = x.shape[0], self.dtype, self._device
+        assert _is_rows(x, n, self.dim, t, device) and _is_rows(out, n, self.dim, t, device)
+        assert residual is None or _is_rows(residual, n, self.dim, t, device)
+        assert saved is None or (_is_rows(saved, n, 2 * self.hidden, t, device) and saved.is_contiguous())
+        assert dropout is None or dropout._device == device
         rc = self._lib.ecrm_ffn_forward(self._ffn, x.data_ptr(), _row(x), n, *_optional(residual), dropout.mask if dropout else None,
                                         out.data_ptr(), _row(out), saved.data_ptr() if saved is not None else None, self._on(stream))
         if check and rc != ECRM_OK:
@@ -397,16 +399,17 @@ class FeedForward:
                  stream=None, check=True):
         """x, saved, dropout: the forward call's.  d_x = add + gradient of x (add: d_out where the residual was x); d_x may be add or d_out.
         d_gate, d_up, d_down: contiguous, of the block's type or fp32, all or none; accumulate: added to."""
-        n, t = x.shape[0], self.dtype
-        assert _is_rows(x, n, self.dim, t) and _is_rows(d_out, n, self.dim, t)
-        assert _is_rows(saved, n, 2 * self.hidden, t) and saved.is_contiguous()
-        assert d_x is None or _is_rows(d_x, n, self.dim, t)
-        assert add is None or _is_rows(add, n, self.dim, t)
+        n, t, device = x.shape[0], self.dtype, self._device
+        assert _is_rows(x, n, self.dim, t, device) and _is_rows(d_out, n, self.dim, t, device)
+        assert _is_rows(saved, n, 2 * self.hidden, t, device) and saved.is_contiguous()
+        assert d_x is None or _is_rows(d_x, n, self.dim, t, device)
+        assert add is None or _is_rows(add, n, self.dim, t, device)
         weights = [w for w in (d_gate, d_up, d_down) if w is not None]
-        assert all(w.is_cuda and w.is_contiguous() and w.dtype == weights[0].dtype for w in weights)
+        assert all(w.get_device() == device and w.is_contiguous() and w.dtype == weights[0].dtype for w in weights)
         assert d_gate is None or tuple(d_gate.shape) == (self.hidden, self.dim)
         assert d_up is None or tuple(d_up.shape) == (self.hidden, self.dim)
         assert d_down is None or tuple(d_down.shape) == (self.dim, self.hidden)
+        assert dropout is None or dropout._device == device
         rc = self._lib.ecrm_ffn_backward(self._ffn, x.data_ptr(), _row(x), saved.data_ptr(), d_out.data_ptr(), _row(d_out), n,
                                          dropout.mask if dropout else None, *_optional(add), *_optional(d_x),
                                          *[w.data_ptr() if w is not None else None for w in (d_gate, d_up, d_down)],
@@ -574,6 +577,7 @@ class Ecrm:
             rc = self._lib.ecrm_embed(self._ctx, keys.data_ptr(), n, _key(padding), scale, lost, out.data_ptr(), _type(out), _row(out),
                                       _stream(stream))
         else:
+            assert dropout._device == out.get_device()
             rc = self._lib.ecrm_embed_dropout(self._ctx, keys.data_ptr(), n, _key(padding), scale, lost, dropout.mask, out.data_ptr(),
                                               _type(out), _row(out), _stream(stream))
         if check and rc != ECRM_OK:
@@ -600,6 +604,7 @@ class Ecrm:
         if dropout is None:
             rc = self._lib.ecrm_embed_grad(*batch, *out)
         else:
+            assert dropout._device == d_out.get_device()
             rc = self._lib.ecrm_embed_grad_dropout(*batch, dropout.mask, *out)
         if check and rc != ECRM_OK:
             raise EcrmError(rc, "ecrm_embed_grad" if dropout is None else "ecrm_embed_grad_dropout")
@@ -615,6 +620,7 @@ class Ecrm:
         if dropout is None:
             rc = self._lib.ecrm_embed_grad_dense(*batch, *to)
         else:
+            assert dropout._device == d_out.get_device()
             rc = self._lib.ecrm_embed_grad_dense_dropout(*batch, dropout.mask, *to)
         if check and rc != ECRM_OK:
             raise EcrmError(rc, "ecrm_embed_grad_dense" if dropout is None else "ecrm_embed_grad_dense_dropout")

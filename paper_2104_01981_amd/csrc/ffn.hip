@@ -67,6 +67,12 @@ bool apart(uint32_t a_size, const Rows &a, uint32_t b_size, const Rows &b)
 // Is what is read clear of the workspace, which is written?
 bool clear_of_work(const ecrm_ffn *f, const Rows &r) { return apart(type_bytes(f->cfg.type), r, 1, Rows{f->work, 1, f->bytes, f->bytes}); }
 
+bool mask_fits(const ecrm_ffn *f, const ecrm_mask *mask, MaskArgs &to)
+{
+    double factor;
+    return make_mask(mask, to, factor) && apart(1, Rows{mask->state, 1, 16, 16}, 1, Rows{f->work, 1, f->bytes, f->bytes});
+}
+
 // Is what is written clear of the weights, the workspace and the mask's state?
 bool clear_of_own(const ecrm_ffn *f, const ecrm_mask *mask, uint32_t size, const Rows &w)
 {
@@ -183,8 +189,7 @@ int ecrm_ffn_forward(ecrm_ffn *f, const void *x, uint64_t x_stride, uint64_t n, 
     if (n > f->cfg.max_rows) return ECRM_EBATCH;
     ProductArgs a;
     memset(&a, 0, sizeof(a));
-    double factor;
-    if (mask && !make_mask(mask, a.mask, factor)) return ECRM_EINVAL;
+    if (mask && !mask_fits(f, mask, a.mask)) return ECRM_EINVAL;
     if (!n) return ECRM_OK;
     const uint32_t D = f->cfg.dim, F = f->cfg.hidden, N = (uint32_t)n, type = f->cfg.type, size = type_bytes(type);
     if (n == 1) x_stride = residual_stride = out_stride = D;             // of one row it says nothing
@@ -236,8 +241,7 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
     if (n > f->cfg.max_rows) return ECRM_EBATCH;
     ProductArgs a;
     memset(&a, 0, sizeof(a));
-    double factor;
-    if (mask && !make_mask(mask, a.mask, factor)) return ECRM_EINVAL;
+    if (mask && !mask_fits(f, mask, a.mask)) return ECRM_EINVAL;
     const uint32_t D = f->cfg.dim, F = f->cfg.hidden, N = (uint32_t)n, type = f->cfg.type, size = type_bytes(type);
     const bool weights = d_gate || d_up || d_down;
     const uint32_t weight_size = type_bytes(weight_type);

@@ -449,3 +449,42 @@ def test_refusals():
     assert code(lambda: train.backward(x, saved, d, x)) == ECRM_EINVAL                # the place of x
     assert code(lambda: train.backward(x, saved, d, saved[:, :D])) == ECRM_EINVAL
     train.backward(x, saved, d)                                                       # nothing is wanted
+
+
+def test_the_mask_state_lies_outside_the_workspace():
+    n, D, F, t = 20, 64, 128, torch.bfloat16
+    gen, x, wg, wu, wd = model(n, D, F, t, 12)
+    block = FeedForward(wg, wu, wd, max_rows=n, training=True)
+    out, saved = torch.empty_like(x), torch.empty(n, 2 * F, dtype=t, device=DEV)
+    words = block.workspace[:256].view(torch.int64)
+    for inside in (words[:2], words[16:18]):
+        with pytest.raises(EcrmError) as e:
+            block.forward(x, out, dropout=Dropout(0.5, inside), saved=saved)
+        assert e.value.code == ECRM_EINVAL
+        with pytest.raises(EcrmError) as e:
+            block.backward(x, saved, x, out, dropout=Dropout(0.5, inside))
+        assert e.value.code == ECRM_EINVAL
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """The block, or the mask, taken for one of device 1."""
+    n, D, F, t = 4, 64, 128, torch.bfloat16
+    gen, x, wg, wu, wd = model(n, D, F, t, 13)
+    out, saved = torch.empty_like(x), torch.empty(n, 2 * F, dtype=t, device=DEV)
+    block, drop = FeedForward(wg, wu, wd, max_rows=n, training=True), Dropout(0.5, state())
+    drop._device = 1
+    for call in (lambda: block.forward(x, out, dropout=drop), lambda: block.backward(x, saved, x, out, dropout=drop), lambda: drop.apply(x, out)):
+        with pytest.raises(AssertionError):
+            call()
+    block._device = 1
+    for call in (lambda: block.forward(x, out), lambda: block.backward(x, saved, x, out)):
+        with pytest.raises(AssertionError):
+            call()
+    block._device = 0
+    for call in (lambda: block.forward(x.cpu(), out), lambda: block.forward(x, out.cpu()), lambda: FeedForward(wg, wu.cpu(), wd, max_rows=n)):
+        with pytest.raises(AssertionError):
+            call()
+    monkeypatch.setattr("paper_2104_01981_amd.binding._raw_device", lambda: 1)
+    for call in (lambda: block.forward(x, out), lambda: Dropout(0.5, state()).apply(x, out)):
+        with pytest.raises(AssertionError):
+            call()
