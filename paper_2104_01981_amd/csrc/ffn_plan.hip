@@ -4,7 +4,11 @@
 namespace ecrm {
 
 constexpr uint32_t kSplitCounts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
-constexpr double kJoinWait = 2.0, kJoinOne = 2.5e4;          // parts joined by the workgroup that is there last: us; bytes a us
+// Parts joined by the workgroup that is there last: us; bytes of parts a us, of one tile's and, in 16 bits, of all.  Without the last, bf16,
+// backward of 8192 rows, D = 512, F = 2048 174 us instead of 144, of 4096, 256 x 1024 42.6 instead of 36.6, forward of 2000 of these 21.2
+// instead of 18.4; it costs forward of 4096, 1024 x 4096 3 % and backward of 16384, 260 x 684 9 %.  In 32 bits, whose tiles take longer,
+// it would cost forward of 600 rows, 260 x 684 18.6 -> 20.6 and gain nothing.
+constexpr double kJoinWait = 2.0, kJoinOne = 2.5e4, kJoinAll = 1e7;
 constexpr uint64_t kMostWorkgroups = 0xFFFFFFFFu / 512u;        // a launch has fewer than 2^32 threads
 
 constexpr double kSkinnyLaunch = 3.5, kSkinnyRate = 2.5e6;               // us; bytes of weights a us
@@ -72,8 +76,8 @@ Plan plan_launch(const ProductSize &a, const ProductSize &b, uint32_t type, uint
                 };
                 const uint64_t slots = (uint64_t)(cus * together);
                 const double ua = unit(0, x), ub = b.count ? unit(1, y) : 1.0;
-                double cost = c.launch + (ua >= ub ? makespan(tiles[0] * x.splits, ua, tiles[1] * y.splits, ub, slots)
-                                                   : makespan(tiles[1] * y.splits, ub, tiles[0] * x.splits, ua, slots));
+                double cost = c.launch + (wide ? 0.0 : bytes / kJoinAll) + (ua >= ub ? makespan(tiles[0] * x.splits, ua, tiles[1] * y.splits, ub, slots)
+                                                                                       : makespan(tiles[1] * y.splits, ub, tiles[0] * x.splits, ua, slots));
                 const uint64_t counters = (x.splits > 1 ? tiles[0] : 0) + (y.splits > 1 ? tiles[1] : 0);
                 if (!best.split[0].splits || cost < best.cost) best = Plan{t, {x, y}, (uint32_t)counters, cost};
             }
