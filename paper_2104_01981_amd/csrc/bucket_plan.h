@@ -3,13 +3,7 @@
 // a test can ask the very same functions.
 #pragma once
 
-#include <stdint.h>
-
-#ifdef __HIP__
-#define ECRM_HD __host__ __device__ __forceinline__
-#else
-#define ECRM_HD inline
-#endif
+#include "host_device.h"
 
 namespace ecrm {
 

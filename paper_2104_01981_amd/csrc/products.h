@@ -9,7 +9,7 @@
 //   columns: LDS holds [K][BM]; 16-bit fragments are read transposed (ds_read_b64_tr_b16: the 16 lanes that read 4 x 16 elements get
 //            a column of four each), their 32-byte chunks exchanged by K % 4 and K / 8 % 2; 32-bit ones are read word by word, 64-byte
 //            chunks exchanged by K / 4 % 4.
-// The buffer descriptors end with the operand, rows or K: what lies behind comes back as zeros.  Rows along K need two more
+// The buffer descriptors end with the operand, rows or K: what lies behind comes back as zeros (load_range.h).  Rows along K need two more
 // precautions where K ends inside a tile, because the next row follows: lanes whose chunk lies behind K read out of range, and the
 // upper half of a chunk that K ends in the middle of (K % 8 == 4, 16 bits) is cleared in LDS.  Both operands, since
 // zero times what is not finite is not zero.
@@ -23,6 +23,7 @@
 // conflicts.  Fragments read ahead of the barrier changed nothing (1 %), K rotated by tile, so that tiles ask unlike channels, cost 10 %.
 #pragma once
 
+#include "load_range.h"
 #include "mask.h"
 
 namespace ecrm {
@@ -104,7 +105,6 @@ struct Fragment<float> {
 };
 
 constexpr uint32_t kRowBytes = 128;              // of K, in a tile
-constexpr uint32_t kOutside = 0x7FFFFFFFu;       // an offset behind any operand's end
 
 // A value that is the same for the wave, in scalar registers: what a division gives lies in vector registers, and a load whose descriptor
 // or LDS address does would be made lane by lane.
@@ -170,8 +170,7 @@ struct Loader {
         stride = (uint32_t)(elements * sizeof(T));
         if (!COLUMNS) {
             base = scalar((const char *)p + (uint64_t)first * stride);
-            const uint32_t rows = count > first ? min(count - first, (uint32_t)ROWS) : 0u;
-            end = scalar(rows ? (rows - 1u) * stride + K * (uint32_t)sizeof(T) : 0u);
+            end = scalar(rows_end(count, first, (uint32_t)ROWS, stride, K * (uint32_t)sizeof(T)));
 #pragma unroll
             for (uint32_t i = 0; i < kLoads; ++i) {
                 const uint32_t j = load + i, chunk = (lane % 8u) ^ ((lane / 16u) | (j & 1u) << 2);
@@ -198,7 +197,7 @@ struct Loader {
         const uint32_t to = scalar((uint32_t)(uintptr_t)(lds_t *)tile + load * 1024u);
         if (!COLUMNS) {
             const u32x4 buffer = buffer_of(base, end);
-            const uint32_t from = scalar(k0 * (uint32_t)sizeof(T));
+            const uint32_t from = scalar(rows_from(end, k0 * (uint32_t)sizeof(T)));
             if (left >= kElements) {
                 for_each<kLoads>([&](auto i) { load_to_lds<decltype(i)::value * 1024u>(buffer, at[decltype(i)::value], from, to); });
             } else {
@@ -209,8 +208,7 @@ struct Loader {
                 });
             }
         } else {
-            const uint32_t rows = min(left, kElements);
-            const u32x4 buffer = buffer_of(scalar(base + (uint64_t)k0 * stride), scalar(end ? (rows - 1u) * stride + end : 0u));
+            const u32x4 buffer = buffer_of(scalar(base + (uint64_t)k0 * stride), scalar(columns_end(min(left, kElements), stride, end)));
             for_each<kLoads>([&](auto i) { load_to_lds<decltype(i)::value * 1024u>(buffer, at[decltype(i)::value], 0u, to); });
         }
     }
