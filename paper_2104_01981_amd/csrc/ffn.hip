@@ -6,7 +6,7 @@
 // with 0.27 GB of g and u written on the way), backward 905 to 955 (910 to 860); the same products alone take the library 515 and 1215 us.  kBack is bound by
 // memory instead: two elements in and three out for each of h, 245 us, 105 of them multiplications.  D = 128, F = 512, 8192
 // rows: memory, 16 us forward, of which g, u and h take 6; 33 backward.  A few rows: the weights, 25 MB for five rows in 11 us.
-#include "ffn_plan.h"
+#include "ffn_block.h"
 
 #include <new>
 #include <string.h>
@@ -22,8 +22,6 @@ __global__ __launch_bounds__(256) void clear_kernel(uint32_t *to, uint64_t words
 
 using namespace ecrm;
 
-enum { kPlanForward, kPlanBack, kPlanWeights, kPlanInput, kPlanBoth, kPlans };
-
 // ---- C ABI -----------------------------------------------------------------------------------------------------------------------
 struct ecrm_ffn {
     ecrm_ffn_config cfg;
@@ -36,7 +34,7 @@ struct ecrm_ffn {
     int cus;
     // plans, kept while the number of rows stays, since making them takes some us
     uint64_t rows_of[kPlans];
-    RowPlan gate, out, back, input, both, weights;
+    BlockPlans plans;
 };
 
 namespace {
@@ -98,26 +96,10 @@ Product product(const void *a, uint64_t a_stride, const void *b, uint64_t b_stri
     return p;
 }
 
-// false: more workgroups than a launch can have, of any tiling
-bool is_planned(const RowPlan &p) { return p.main.cost > 0; }
-uint32_t counters_of(const RowPlan &p) { return p.main.counters > p.rest.counters ? p.main.counters : p.rest.counters; }
-
 void make_plan(ecrm_ffn *f, int what, uint32_t n)
 {
     if (f->rows_of[what] == n) return;
-    const uint32_t D = f->cfg.dim, F = f->cfg.hidden, type = f->cfg.type, cus = (uint32_t)f->cus;
-    const size_t room = f->part_bytes;
-    const ProductSize none{}, weights{F, D, n, 1, 3, false, false, true}, input{n, D, F, 2, 1, false, false, true};
-    if (what == kPlanForward) {
-        f->gate = plan_rows(none, ProductSize{n, F, D, 1, 1, true, true, false}, type, cus, room);
-        f->out = plan_rows(none, ProductSize{n, D, F, 1, 1, false, false, false}, type, cus, room);
-    } else if (what == kPlanBack) {
-        f->back = plan_rows(none, ProductSize{n, F, D, 1, 1, false, true, false}, type, cus, room);
-    } else if (what == kPlanWeights) {
-        f->weights = RowPlan{F, plan_launch(weights, none, type, cus, room), Plan{}};
-    } else {
-        (what == kPlanBoth ? f->both : f->input) = plan_rows(what == kPlanBoth ? weights : none, input, type, cus, room);
-    }
+    plan_block(f->plans, what, n, f->cfg.dim, f->cfg.hidden, f->cfg.type, (uint32_t)f->cus, f->part_bytes);
     f->rows_of[what] = n;
 }
 
@@ -205,10 +187,11 @@ int ecrm_ffn_forward(ecrm_ffn *f, const void *x, uint64_t x_stride, uint64_t n, 
     void *h = f->work + f->off_h;
     a.part = (float *)(f->work + f->off_part);
     make_plan(f, kPlanForward, N);
-    if (!is_planned(f->gate) || !is_planned(f->out)) return ECRM_EINVAL;
+    if (!is_planned(f->plans.gate) || !is_planned(f->plans.out)) return ECRM_EINVAL;
     a.arrived = (uint32_t *)(f->work + f->off_arrived);
-    a.clear = counters_of(f->out);
-    if (is_skinny(f->out.rows < N ? N - f->out.rows : N, type) && skinny_parts(D, F, type, (uint32_t)f->cus) > 1 && a.clear < (D + 15u) / 16u * 2u)
+    a.clear = counters_of(f->plans.out);
+    if (is_skinny(f->plans.out.rows < N ? N - f->plans.out.rows : N, type) && skinny_parts(D, F, type, (uint32_t)f->cus) > 1 &&
+        a.clear < (D + 15u) / 16u * 2u)
         a.clear = (D + 15u) / 16u * 2u;
     a.activation = f->cfg.activation;
     with_type(type, [&](auto t) {
@@ -219,14 +202,14 @@ int ecrm_ffn_forward(ecrm_ffn *f, const void *x, uint64_t x_stride, uint64_t n, 
         a.p[0].out = h;
         a.p[0].out_stride = f->pitch;
         a.p[0].out2 = saved;
-        BlockLaunch<T>::gate(a, f->gate, (uint32_t)f->cus, st);
+        BlockLaunch<T>::gate(a, f->plans.gate, (uint32_t)f->cus, st);
         a.p[0] = product(h, f->pitch, f->down, f->down_stride, N, D, F);
         a.p[0].out = out;
         a.p[0].out_stride = out_stride;
         a.p[0].in = residual;
         a.p[0].in_stride = residual_stride;
         a.masked = mask ? 1u : 0u;
-        BlockLaunch<T>::out(a, f->out, (uint32_t)f->cus, st);
+        BlockLaunch<T>::out(a, f->plans.out, (uint32_t)f->cus, st);
     });
     return launched();
 }
@@ -287,7 +270,9 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
         if (weights) make_plan(f, kPlanWeights, N);
         if (d_x) make_plan(f, kPlanInput, N);
     }
-    if (!is_planned(f->back) || (d_x && !is_planned(both ? f->both : f->input)) || (weights && !both && !is_planned(f->weights))) return ECRM_EINVAL;
+    if (!is_planned(f->plans.back) || (d_x && !is_planned(both ? f->plans.both : f->plans.input)) ||
+        (weights && !both && !is_planned(f->plans.weights)))
+        return ECRM_EINVAL;
 
     void *h = f->work + f->off_h, *dg = f->work + f->off_dg, *du = f->work + f->off_du;
     a.part = (float *)(f->work + f->off_part);
@@ -305,9 +290,9 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
     a.accumulate = accumulate ? 1u : 0u;
     a.wide = weight_type != type ? 1u : 0u;
     a.arrived = (uint32_t *)(f->work + f->off_arrived);
-    a.clear = both ? counters_of(f->both) : 0u;
-    if (!both && weights) a.clear = counters_of(f->weights);
-    if (!both && d_x && counters_of(f->input) > a.clear) a.clear = counters_of(f->input);
+    a.clear = both ? counters_of(f->plans.both) : 0u;
+    if (!both && weights) a.clear = counters_of(f->plans.weights);
+    if (!both && d_x && counters_of(f->plans.input) > a.clear) a.clear = counters_of(f->plans.input);
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
         a.p[0] = product(e, e_stride, f->down, f->down_stride, N, F, D);
@@ -317,7 +302,7 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
         a.p[0].out3 = h;
         a.p[0].out_stride = f->pitch;
         a.p[0].scale = scale;
-        BlockLaunch<T>::back(a, f->back, (uint32_t)f->cus, st);
+        BlockLaunch<T>::back(a, f->plans.back, (uint32_t)f->cus, st);
         Product w[3], in;
         w[0] = product(dg, f->pitch, x, x_stride, F, D, N);
         w[0].out = d_gate;
@@ -338,8 +323,8 @@ int ecrm_ffn_backward(ecrm_ffn *f, const void *x, uint64_t x_stride, const void 
         in.out = d_x;
         in.out_stride = d_x_stride;
         in.kind = kInput;
-        if (weights && !both) BlockLaunch<T>::gradients(a, w, nullptr, f->weights, st);
-        if (d_x) BlockLaunch<T>::gradients(a, both ? w : nullptr, &in, both ? f->both : f->input, st);
+        if (weights && !both) BlockLaunch<T>::gradients(a, w, nullptr, f->plans.weights, st);
+        if (d_x) BlockLaunch<T>::gradients(a, both ? w : nullptr, &in, both ? f->plans.both : f->plans.input, st);
     });
     return launched();
 }

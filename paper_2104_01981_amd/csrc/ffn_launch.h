@@ -1,7 +1,7 @@
-// Launches of the feed-forward block's products as planned, for a type (ffn_plan.h).
+// Launches of the feed-forward block's products as planned, for a type (ffn_block.h).
 #pragma once
 
-#include "ffn_plan.h"
+#include "ffn_block.h"
 
 namespace ecrm {
 

@@ -1,9 +1,15 @@
-// Which tiles the products of the feed-forward block take, and their launches (ffn.hip).
+// Which tiles the products of the feed-forward block take (products.h, ffn.hip), and what of that the kernels have to know.  Host code that
+// compiles without HIP, so that tests can ask it.
 #pragma once
 
-#include "products.h"
+#include <stddef.h>
+
+#include "element.h"
 
 namespace ecrm {
+
+constexpr uint32_t kRowBytes = 128;              // of K, in a tile
+constexpr uint32_t kAtOnce = 4;                  // steps of 64 bytes of K that a wave of few rows' products has in flight
 
 // ---- which tiles -----------------------------------------------------------------------------------------------------------------
 // What a product takes is estimated in us from what was measured (M, N of 512 to 4096, all CUs in step): a tile's steps of 128 bytes of
@@ -49,14 +55,14 @@ inline bool is_skinny(uint32_t rows, uint32_t type) { return rows <= (type == EC
 Plan plan_launch(const ProductSize &a, const ProductSize &b, uint32_t type, uint32_t cus, size_t room);
 RowPlan plan_rows(const ProductSize &other, const ProductSize &z, uint32_t type, uint32_t cus, size_t room);
 
-// The launches of one type: a source of its own for each (ffn_bf16.hip and so on), since compiling them takes most of the build.
-template <typename T>
-struct BlockLaunch {
-    static void gate(ProductArgs &a, const RowPlan &plan, uint32_t cus, hipStream_t st);
-    static void out(ProductArgs &a, const RowPlan &plan, uint32_t cus, hipStream_t st);
-    static void back(ProductArgs &a, const RowPlan &plan, uint32_t cus, hipStream_t st);
-    // the products of the weights, those of x, or both (one or the other may be null), x's rows as planned
-    static void gradients(ProductArgs &a, const Product *weights, const Product *input, const RowPlan &plan, hipStream_t st);
-};
+// What of a block is planned at a time: the launches of a forward pass (gate and out); of a backward pass the gradient of h, and those of the
+// weights alone, of x alone, or of both side by side.
+enum { kPlanForward, kPlanBack, kPlanWeights, kPlanInput, kPlanBoth, kPlans };
+struct BlockPlans { RowPlan gate, out, back, weights, input, both; };
+void plan_block(BlockPlans &plans, int what, uint32_t rows, uint32_t dim, uint32_t hidden, uint32_t type, uint32_t cus, size_t room);
+
+// false: more workgroups than a launch can have, of any tiling
+inline bool is_planned(const RowPlan &p) { return p.main.cost > 0; }
+inline uint32_t counters_of(const RowPlan &p) { return p.main.counters > p.rest.counters ? p.main.counters : p.rest.counters; }
 
 }  // namespace ecrm

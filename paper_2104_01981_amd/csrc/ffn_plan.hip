@@ -1,5 +1,7 @@
-// Plans of the feed-forward block's products: see ffn_plan.h.  Host code only.
+// Plans of the feed-forward block's products: see ffn_plan.h.  Host code only, without HIP.
 #include "ffn_plan.h"
+
+#include <initializer_list>
 
 namespace ecrm {
 
@@ -112,6 +114,23 @@ RowPlan plan_rows(const ProductSize &other, const ProductSize &z, uint32_t type,
         }
     }
     return best;
+}
+
+void plan_block(BlockPlans &plans, int what, uint32_t rows, uint32_t dim, uint32_t hidden, uint32_t type, uint32_t cus, size_t room)
+{
+    const ProductSize none{}, weights{hidden, dim, rows, 1, 3, false, false, true}, input{rows, dim, hidden, 2, 1, false, false, true};
+    if (what == kPlanForward) {
+        plans.gate = plan_rows(none, ProductSize{rows, hidden, dim, 1, 1, true, true, false}, type, cus, room);
+        plans.out = plan_rows(none, ProductSize{rows, dim, hidden, 1, 1, false, false, false}, type, cus, room);
+    } else if (what == kPlanBack) {
+        plans.back = plan_rows(none, ProductSize{rows, hidden, dim, 1, 1, false, true, false}, type, cus, room);
+    } else if (what == kPlanWeights) {
+        plans.weights = RowPlan{hidden, plan_launch(weights, none, type, cus, room), Plan{}};
+    } else if (what == kPlanInput) {
+        plans.input = plan_rows(none, input, type, cus, room);
+    } else {
+        plans.both = plan_rows(weights, input, type, cus, room);
+    }
 }
 
 }  // namespace ecrm

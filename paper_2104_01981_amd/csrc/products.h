@@ -23,6 +23,7 @@
 // conflicts.  Fragments read ahead of the barrier changed nothing (1 %), K rotated by tile, so that tiles ask unlike channels, cost 10 %.
 #pragma once
 
+#include "ffn_plan.h"
 #include "load_range.h"
 #include "mask.h"
 
@@ -104,7 +105,6 @@ struct Fragment<float> {
     }
 };
 
-constexpr uint32_t kRowBytes = 128;              // of K, in a tile
 
 // A value that is the same for the wave, in scalar registers: what a division gives lies in vector registers, and a load whose descriptor
 // or LDS address does would be made lane by lane.
@@ -750,7 +750,6 @@ __global__ __launch_bounds__(WM * WN * kWave, 2) void gradients_kernel(ProductAr
 // both projections) and all of K or, where there are few columns and a long K, a part of it; its waves share that, every one with up to
 // kAtOnce steps of 64 bytes of 16 rows of weights in flight, straight into the registers of the matrix instructions, whose second operand
 // are the rows.  The waves' sums are added up in LDS, in order; those of several workgroups by the one that is there last, in order, too.
-constexpr uint32_t kAtOnce = 4;
 template <int XB>
 struct Skinny { static constexpr uint32_t kWaves = XB == 1 ? 16 : 8; };          // as the registers allow
 

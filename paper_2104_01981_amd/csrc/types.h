@@ -2,6 +2,7 @@
 #pragma once
 
 #include "ecrm_internal.h"
+#include "element.h"
 
 namespace ecrm {
 
@@ -19,8 +20,6 @@ __device__ __forceinline__ typename Quad<T>::type round4(f32x4 v)       // to ne
 {
     return __builtin_convertvector(v, typename Quad<T>::type);
 }
-
-__host__ __device__ __forceinline__ uint32_t type_bytes(uint32_t type) { return type == ECRM_F32 ? 4u : 2u; }
 
 // f(T()) for the element type
 template <typename F>

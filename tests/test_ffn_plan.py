@@ -1,0 +1,87 @@
+"""Plans of the feed-forward block's products, on the host: parts of K cover it and stay inside the workspace, counters inside theirs, rows
+are taken once, launches stay as small as they have to be."""
+import math
+import random
+
+import pytest
+
+import ffn_plan as fp
+
+F32, BF16, F16 = 0, 1, 2
+
+
+def sizes(count, seed):
+    """Rows, columns, hidden columns over the range that a block may have, those that memory holds."""
+    rng = random.Random(seed)
+
+    def some(lo, hi):
+        return int(math.exp(rng.uniform(math.log(lo), math.log(hi + 1))))
+
+    found = []
+    while len(found) < count:
+        n, D, F = some(1, 1 << 26), 4 * some(1, 1 << 14), 4 * some(1, 1 << 14)
+        if n * (D + F) < 1 << 36 and D * F < 1 << 31:
+            found.append((n, D, F))
+    return found
+
+
+def launches(n, D, F, type, p):
+    """Of each launch that is planned by tiles: name, plan, its products as (rows, columns, K tiles, how many, parts)."""
+    elements = fp.constants()["row_bytes"] // (4 if type == F32 else 2)
+
+    def k_tiles(K):
+        return -(-K // elements)
+
+    for name in fp.NAMES:
+        rows, main, rest = p[name]
+        whole = F if name == "weights" else n
+        assert 0 < rows <= whole and (name != "weights" or rows == whole)
+        for plan, m, first in ((main, rows, True), (rest, whole - rows, False)):
+            if m == 0:
+                continue
+            assert plan.planned
+            if name in ("gate", "out") and fp.is_skinny(m, type):
+                continue
+            products = []
+            if name == "weights" or (name == "both" and first):
+                products.append((F, D, k_tiles(n), 3, plan.splits[0]))
+            if name == "gate":
+                products.append((m, F, k_tiles(D), 1, plan.splits[0]))
+            if name == "back":
+                products.append((m, F, k_tiles(D), 1, plan.splits[0]))
+            if name == "out":
+                products.append((m, D, k_tiles(F), 1, plan.splits[0]))
+            if name in ("input", "both"):
+                products.append((m, D, 2 * k_tiles(F), 1, plan.splits[1 if products else 0]))
+            yield name, plan, products
+
+
+@pytest.mark.parametrize("cus", [256, 304, 80])
+@pytest.mark.parametrize("type", [F32, BF16, F16])
+def test_plans_hold_over_the_range(type, cus):
+    c = fp.constants()
+    for n, D, F in sizes(1000, cus + type):
+        p = fp.plans(n, D, F, type, cus)
+        for name, plan, products in launches(n, D, F, type, p):
+            what = (n, D, F, name, plan)
+            side = fp.side(plan.tiling)
+            assert side != (256 if type == F32 else 32), what
+            parts = counters = workgroups = 0
+            for M, N, K, count, (splits, each) in products:
+                assert splits >= 1 and splits * each >= K > (splits - 1) * each, what          # all of K, and no part without any
+                tiles = -(-M // side) * -(-N // fp.columns(side, name == "gate")) * count
+                workgroups += tiles * splits
+                if splits > 1:
+                    assert name not in ("gate", "back"), what
+                    parts += tiles * splits * side * side * 4
+                    counters += tiles
+            assert parts <= c["part_most"] and counters == plan.counters <= c["counters"], what
+            assert workgroups * 512 < 1 << 32, what
+        # few rows' parts: a place for each of 64 lanes' four sums, of up to two blocks of rows
+        parts, blocks = fp.skinny_parts(D, F, type, cus), -(-D // 16)
+        assert 1 <= parts <= c["skinny_parts"] and (parts == 1 or (parts * blocks <= cus and parts * blocks * 2 * 1024 <= c["part_most"]))
+
+
+def test_types_of_16_bits_have_the_same_plans():
+    for size in sizes(300, 9):
+        assert fp.plans(*size, BF16) == fp.plans(*size, F16)
