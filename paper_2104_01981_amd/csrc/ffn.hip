@@ -130,7 +130,7 @@ int ecrm_ffn_create(const ecrm_ffn_config *cfg, ecrm_ffn **out)
         f->off_e = take(cfg->max_rows * f->e_pitch * size);
     }
     f->off_arrived = take(((cfg->dim + 15u) / 16u * 2u > kCounters ? (cfg->dim + 15u) / 16u * 2u : kCounters) * 4u);
-    f->part_bytes = kPartMost;
+    f->part_bytes = parts_room(cfg->dim, cfg->hidden, cfg->max_rows, cfg->type, cfg->training != 0);
     f->off_part = take(f->part_bytes);
     f->bytes = off;
     *out = f;

@@ -60,6 +60,8 @@ RowPlan plan_rows(const ProductSize &other, const ProductSize &z, uint32_t type,
 enum { kPlanForward, kPlanBack, kPlanWeights, kPlanInput, kPlanBoth, kPlans };
 struct BlockPlans { RowPlan gate, out, back, weights, input, both; };
 void plan_block(BlockPlans &plans, int what, uint32_t rows, uint32_t dim, uint32_t hidden, uint32_t type, uint32_t cus, size_t room);
+// Bytes of parts, kPartMost at most, that no plan of a block of up to max_rows rows is the worse for, whatever the number of CUs.
+size_t parts_room(uint32_t dim, uint32_t hidden, uint64_t max_rows, uint32_t type, bool training);
 
 // false: more workgroups than a launch can have, of any tiling
 inline bool is_planned(const RowPlan &p) { return p.main.cost > 0; }

@@ -5,7 +5,7 @@
 
 namespace ecrm {
 
-constexpr uint32_t kSplitCounts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+constexpr uint32_t kSplitCounts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}, kMostParts = 64;
 // Parts joined by the workgroup that is there last: us; bytes of parts a us, of one tile's and, in 16 bits, of all.  Without the last, bf16,
 // backward of 8192 rows, D = 512, F = 2048 174 us instead of 144, of 4096, 256 x 1024 42.6 instead of 36.6, forward of 2000 of these 21.2
 // instead of 18.4; it costs forward of 4096, 1024 x 4096 3 % and backward of 16384, 260 x 684 9 %.  In 32 bits, whose tiles take longer,
@@ -131,6 +131,31 @@ void plan_block(BlockPlans &plans, int what, uint32_t rows, uint32_t dim, uint32
     } else {
         plans.both = plan_rows(weights, input, type, cus, room);
     }
+}
+
+size_t parts_room(uint32_t dim, uint32_t hidden, uint64_t max_rows, uint32_t type, bool training)
+{
+    const uint32_t rows = (uint32_t)max_rows, wide = type == ECRM_F32 ? 1u : 0u, elements = kRowBytes / type_bytes(type);
+    uint64_t most = 0;
+    for (uint32_t t = 0; t < kTilings; ++t) {
+        const TilingCost &c = kCosts[t];
+        if (c.step[wide] == 0.0) continue;
+        // all tiles in as many parts as there may be
+        auto parts = [&](const ProductSize &z) {
+            const uint64_t k_tiles = (uint64_t)((z.K + elements - 1) / elements) * z.halves, cut = k_tiles < kMostParts ? k_tiles : kMostParts;
+            return cut > 1 ? tiles_of(z, z.M, c.side) * cut * c.side * c.side * 4u : 0u;
+        };
+        const uint64_t out = is_skinny(rows, type) ? 0 : parts(ProductSize{rows, dim, hidden, 1, 1, false, false, false});
+        const uint64_t gradients = training ? parts(ProductSize{hidden, dim, rows, 1, 3, false, false, true}) +
+                                                  parts(ProductSize{rows, dim, hidden, 2, 1, false, false, true}) : 0;
+        most = out > most ? out : most;
+        most = gradients > most ? gradients : most;
+    }
+    // few rows: 1 KB for each of up to two blocks of 16 rows and of 16 columns
+    const uint32_t waves = skinny_waves(hidden, type) / 8u;
+    const uint64_t few = waves > 1 ? (uint64_t)((dim + 15u) / 16u) * (waves < kSkinnyParts ? waves : kSkinnyParts) * 2048u : 0;
+    most = few > most ? few : most;
+    return most < kPartMost ? (size_t)most : kPartMost;
 }
 
 }  // namespace ecrm

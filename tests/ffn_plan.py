@@ -28,6 +28,10 @@ uint32_t plan_side(uint32_t tiling) { return kCosts[tiling].side; }
 uint32_t plan_columns(uint32_t side, uint32_t dual) { return columns_of(side, dual != 0); }
 uint32_t plan_is_skinny(uint32_t rows, uint32_t type) { return is_skinny(rows, type); }
 uint32_t plan_skinny_parts(uint32_t N, uint32_t K, uint32_t type, uint32_t cus) { return skinny_parts(N, K, type, cus); }
+uint64_t plan_room(uint32_t dim, uint32_t hidden, uint64_t max_rows, uint32_t type, uint32_t training)
+{
+    return parts_room(dim, hidden, max_rows, type, training != 0);
+}
 // gate, out, back, weights, input, both: of each the rows of the first part, its plan, and the others' plan
 void plan_all(uint32_t rows, uint32_t dim, uint32_t hidden, uint32_t type, uint32_t cus, uint64_t room, uint32_t *to)
 {
@@ -59,6 +63,7 @@ def lib():
             subprocess.check_call(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-I", CSRC, "-I", os.path.join(ROOT, "include"), src, "-o", out])
             _lib = C.CDLL(out)
             _lib.plan_all.argtypes = [C.c_uint32] * 5 + [C.c_uint64, C.POINTER(C.c_uint32)]
+            _lib.plan_room.argtypes, _lib.plan_room.restype = [C.c_uint32, C.c_uint32, C.c_uint64, C.c_uint32, C.c_uint32], C.c_uint64
     return _lib
 
 
@@ -80,6 +85,10 @@ def is_skinny(rows, type):
 
 def skinny_parts(N, K, type, cus=CUS):
     return int(lib().plan_skinny_parts(N, K, type, cus))
+
+
+def room(dim, hidden, max_rows, type, training):
+    return int(lib().plan_room(dim, hidden, max_rows, type, 1 if training else 0))
 
 
 def plans(n, dim, hidden, type, cus=CUS, room=None):

@@ -1,11 +1,14 @@
 """Plans of the feed-forward block's products, on the host: parts of K cover it and stay inside the workspace, counters inside theirs, rows
 are taken once, launches stay as small as they have to be."""
+import ctypes as C
 import math
+import os
 import random
 
 import pytest
 
 import ffn_plan as fp
+from paper_2104_01981_amd import binding, build
 
 F32, BF16, F16 = 0, 1, 2
 
@@ -80,6 +83,47 @@ def test_plans_hold_over_the_range(type, cus):
         # few rows' parts: a place for each of 64 lanes' four sums, of up to two blocks of rows
         parts, blocks = fp.skinny_parts(D, F, type, cus), -(-D // 16)
         assert 1 <= parts <= c["skinny_parts"] and (parts == 1 or (parts * blocks <= cus and parts * blocks * 2 * 1024 <= c["part_most"]))
+
+
+@pytest.mark.parametrize("cus", [256, 304])
+@pytest.mark.parametrize("type", [F32, BF16])
+def test_the_workspace_has_room_for_the_same_plans(type, cus):
+    """With what a block's workspace has for parts, calls of fewer rows, too, are planned as with all there may be."""
+    rng = random.Random(cus)
+    for n, D, F in sizes(600, 3 * cus + type) + [(m, D, F) for m in (1, 16, 17, 32, 33, 64, 100) for D, F in ((4, 4), (64, 132), (1024, 4096))]:
+        for training in (False, True):
+            room = fp.room(D, F, n, type, training)
+            assert room <= fp.constants()["part_most"]
+            for rows in {n, rng.randint(1, n), min(n, 32)}:
+                free, held = fp.plans(rows, D, F, type, cus), fp.plans(rows, D, F, type, cus, room)
+                for name in fp.NAMES if training else ("gate", "out"):
+                    assert free[name] == held[name], (n, D, F, rows, name)
+                blocks, parts = -(-D // 16), fp.skinny_parts(D, F, type, cus)
+                if parts > 1 and fp.is_skinny(min(rows, 16), type):
+                    assert blocks * (2 if type != F32 else 1) * parts * 1024 <= room, (n, D, F)
+
+
+def test_small_blocks_have_small_workspaces():
+    """Parts of products take memory only where there can be any: bytes of the whole workspace, of blocks that need no more of it."""
+    if not os.path.exists(binding.library_path()):
+        build.build()
+    lib = binding.load_library()
+
+    def size(**kw):
+        ffn = C.c_void_p(0)
+        assert lib.ecrm_ffn_create(C.byref(binding.EcrmFfnConfig(**kw)), C.byref(ffn)) == 0
+        held = lib.ecrm_ffn_bytes(ffn)
+        lib.ecrm_ffn_destroy(ffn)
+        return held
+
+    counters, h = 4 * fp.constants()["counters"], 1024
+    assert size(dim=4, hidden=4, type=BF16, activation=0, max_rows=1, training=0) <= h + counters
+    # a decoding step's rows: a long K of few rows in 16 parts at most, 2 KB for 16 columns
+    assert size(dim=1024, hidden=4096, type=BF16, activation=0, max_rows=32, training=0) <= 32 * (8192 + 512) + counters + 64 * 16 * 2048
+    assert size(dim=128, hidden=512, type=F32, activation=0, max_rows=16, training=0) <= 16 * (2048 + 512) + counters + 8 * 16 * 2048
+    # 256 x 256 tiles of one product with two K tiles are the most a tiny block's gradients can have
+    assert size(dim=4, hidden=4, type=BF16, activation=0, max_rows=1, training=1) <= 4 * h + counters + 2 * 256 * 256 * 4
+    assert size(dim=4096, hidden=16384, type=BF16, activation=0, max_rows=8192, training=1) >= fp.constants()["part_most"]
 
 
 def test_types_of_16_bits_have_the_same_plans():
