@@ -288,13 +288,22 @@ class Grads:
 
 class Dropout:
     """The masks of one place of a model (ecrm_mask): probability, device tensor of two 64-bit integers -- a seed and the number of masks
-    drawn before, which the program adds to, once a step -- and the place's offset among those of a step.  The state is kept alive."""
+    drawn before, which the program adds to, once a step -- and the place's offset among those of a step.  The state is kept alive; it and
+    the object may be dropped while calls are still to run, on whatever streams; a graph that draws from it needs it kept."""
 
     def __init__(self, p, state, offset=0):
         assert _is_words(state) and state.numel() == 2
         self._lib = load_library()
         self.state, self._device = state, state.get_device()
         self.mask = EcrmMask(state.data_ptr(), offset & 0xFFFFFFFFFFFFFFFF, p)
+        self._streams = set()
+
+    def _on(self, address, stream):
+        """The mask, for a call on that stream: the allocator learns that the state is read there."""
+        if address not in self._streams:
+            self._streams.add(address)
+            self.state.record_stream(_stream_object(stream))
+        return self.mask
 
     def apply(self, x, out, residual=None, stream=None, check=True):
         """out = residual + dropout(x); the gradient of x is apply(gradient of out).  x, out, residual: [rows, cols] of fp32, bf16 or
@@ -306,8 +315,11 @@ class Dropout:
         rows, cols = shape
         assert rows == 0 or cols < 2 or (x.stride(1) == 1 and out.stride(1) == 1)
         assert residual is None or _is_rows(residual, rows, cols, t, device)
-        rc = self._lib.ecrm_dropout(self.mask, x.data_ptr(), _row(x), *_optional(residual), out.data_ptr(), _row(out), _type(x), rows, cols,
-                                    _stream(stream))
+        address = _stream(stream)
+        if address not in self._streams:                 # as _on, without a call
+            self._on(address, stream)
+        rc = self._lib.ecrm_dropout(self.mask, x.data_ptr(), _row(x), *_optional(residual), out.data_ptr(), _row(out), _type(x),
+                                    rows, cols, address)
         if check and rc != ECRM_OK:
             raise EcrmError(rc, "ecrm_dropout")
         return rc
@@ -389,8 +401,10 @@ class FeedForward:
         assert residual is None or _is_rows(residual, n, self.dim, t, device)
         assert saved is None or (_is_rows(saved, n, 2 * self.hidden, t, device) and saved.is_contiguous())
         assert dropout is None or dropout._device == device
-        rc = self._lib.ecrm_ffn_forward(self._ffn, x.data_ptr(), _row(x), n, *_optional(residual), dropout.mask if dropout else None,
-                                        out.data_ptr(), _row(out), saved.data_ptr() if saved is not None else None, self._on(stream))
+        address = self._on(stream)
+        rc = self._lib.ecrm_ffn_forward(self._ffn, x.data_ptr(), _row(x), n, *_optional(residual),
+                                        dropout._on(address, stream) if dropout else None, out.data_ptr(), _row(out),
+                                        saved.data_ptr() if saved is not None else None, address)
         if check and rc != ECRM_OK:
             raise EcrmError(rc, "ecrm_ffn_forward")
         return rc
@@ -410,10 +424,11 @@ class FeedForward:
         assert d_up is None or tuple(d_up.shape) == (self.hidden, self.dim)
         assert d_down is None or tuple(d_down.shape) == (self.dim, self.hidden)
         assert dropout is None or dropout._device == device
+        address = self._on(stream)
         rc = self._lib.ecrm_ffn_backward(self._ffn, x.data_ptr(), _row(x), saved.data_ptr(), d_out.data_ptr(), _row(d_out), n,
-                                         dropout.mask if dropout else None, *_optional(add), *_optional(d_x),
+                                         dropout._on(address, stream) if dropout else None, *_optional(add), *_optional(d_x),
                                          *[w.data_ptr() if w is not None else None for w in (d_gate, d_up, d_down)],
-                                         _type(weights[0]) if weights else 0, 1 if accumulate else 0, self._on(stream))
+                                         _type(weights[0]) if weights else 0, 1 if accumulate else 0, address)
         if check and rc != ECRM_OK:
             raise EcrmError(rc, "ecrm_ffn_backward")
         return rc
@@ -578,8 +593,9 @@ class Ecrm:
                                       _stream(stream))
         else:
             assert dropout._device == out.get_device()
-            rc = self._lib.ecrm_embed_dropout(self._ctx, keys.data_ptr(), n, _key(padding), scale, lost, dropout.mask, out.data_ptr(),
-                                              _type(out), _row(out), _stream(stream))
+            address = _stream(stream)
+            rc = self._lib.ecrm_embed_dropout(self._ctx, keys.data_ptr(), n, _key(padding), scale, lost, dropout._on(address, stream),
+                                              out.data_ptr(), _type(out), _row(out), address)
         if check and rc != ECRM_OK:
             raise EcrmError(rc, "ecrm_embed" if dropout is None else "ecrm_embed_dropout")
         return rc
@@ -600,12 +616,13 @@ class Ecrm:
         assert out_grads.is_cuda and out_grads.dtype == torch.float32 and out_grads.is_contiguous()
         assert out_grads.numel() >= n * self.cfg.dim and _is_words(count) and count.numel() == 1
         batch = (self._ctx, keys.data_ptr(), d_out.data_ptr(), _type(d_out), _row(d_out), n, _key(padding), scale)
-        out = (out_keys.data_ptr(), out_grads.data_ptr(), count.data_ptr(), _stream(stream))
+        address = _stream(stream)
+        out = (out_keys.data_ptr(), out_grads.data_ptr(), count.data_ptr(), address)
         if dropout is None:
             rc = self._lib.ecrm_embed_grad(*batch, *out)
         else:
             assert dropout._device == d_out.get_device()
-            rc = self._lib.ecrm_embed_grad_dropout(*batch, dropout.mask, *out)
+            rc = self._lib.ecrm_embed_grad_dropout(*batch, dropout._on(address, stream), *out)
         if check and rc != ECRM_OK:
             raise EcrmError(rc, "ecrm_embed_grad" if dropout is None else "ecrm_embed_grad_dropout")
         return rc
@@ -616,12 +633,13 @@ class Ecrm:
         n = self._check_grad(keys, d_out)
         assert out.is_cuda and out.dtype == torch.float32 and out.is_contiguous() and tuple(out.shape) == (self.cfg.rows, self.cfg.dim)
         batch = (self._ctx, keys.data_ptr(), d_out.data_ptr(), _type(d_out), _row(d_out), n, _key(padding), scale)
-        to = (out.data_ptr(), 1 if accumulate else 0, _stream(stream))
+        address = _stream(stream)
+        to = (out.data_ptr(), 1 if accumulate else 0, address)
         if dropout is None:
             rc = self._lib.ecrm_embed_grad_dense(*batch, *to)
         else:
             assert dropout._device == d_out.get_device()
-            rc = self._lib.ecrm_embed_grad_dense_dropout(*batch, dropout.mask, *to)
+            rc = self._lib.ecrm_embed_grad_dense_dropout(*batch, dropout._on(address, stream), *to)
         if check and rc != ECRM_OK:
             raise EcrmError(rc, "ecrm_embed_grad_dense" if dropout is None else "ecrm_embed_grad_dense_dropout")
         return rc
