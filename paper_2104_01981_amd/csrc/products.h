@@ -38,8 +38,7 @@ enum {
     kOut = 1,       // the block's output: dropout, residual
     kBack = 2,      // gradient of h; dg, du and h again
     kInput = 3,     // gradient of x, added to something
-    kWeights = 4,   // weight gradients
-    kKinds = 5
+    kWeights = 4    // weight gradients
 };
 
 struct Operand {
