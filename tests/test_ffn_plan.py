@@ -126,6 +126,21 @@ def test_small_blocks_have_small_workspaces():
     assert size(dim=4096, hidden=16384, type=BF16, activation=0, max_rows=8192, training=1) >= fp.constants()["part_most"]
 
 
+def test_the_sizes_of_the_gpu_tests_take_every_kind_of_launch():
+    """Whatever kind of launch a block of some size has -- product, tile, rows up to the last whole tiles or those behind, parts of K -- the
+    exact tests have a size that has it, too, in 16 and in 32 bits.  (Of a million sizes none had another kind.)"""
+    import test_gpu_feed_forward as ff
+    import test_gpu_feed_forward_plans as more
+    taken, rng, asked = {k for size in ff.SIZES + ff.LARGE + more.PLANNED for t in (F32, BF16) for k in fp.kinds(*size, t)}, random.Random(4), 0
+    while asked < 15000:
+        n, D, F = (int(math.exp(rng.uniform(0, math.log(m)))) * (1 if i == 0 else 4) for i, m in enumerate((1 << 17, 1 << 11, 1 << 12)))
+        if n * (D + F) > 3 << 26 or n * D * F > 1 << 38:
+            continue
+        asked += 1
+        for t in (F32, BF16):
+            assert not fp.kinds(n, D, F, t) - taken, (n, D, F)
+
+
 def test_types_of_16_bits_have_the_same_plans():
     for size in sizes(300, 9):
         assert fp.plans(*size, BF16) == fp.plans(*size, F16)

@@ -19,7 +19,8 @@ DEV = "cuda:0"
 TYPES = [torch.float32, torch.bfloat16, torch.float16]
 SIZES = [(1, 4, 4), (1, 128, 512), (2, 12, 20), (3, 8, 132), (5, 60, 64), (15, 64, 68), (16, 68, 60), (17, 132, 36), (31, 36, 260), (33, 256, 100),
          (63, 100, 256), (65, 128, 128), (128, 124, 516), (129, 260, 124), (257, 64, 1028), (300, 516, 268), (1000, 4, 512), (1025, 128, 4)]
-# every tiling of every product, of 16 and of 32 bits, with and without parts of K, and rows behind the last whole tiles
+# every tiling of every product, of 16 and of 32 bits; of their kinds of launches -- cut along K or not, rows behind the last whole tiles -- 91 of
+# 131, the others at the sizes of test_gpu_feed_forward_plans.py
 LARGE = [(2100, 512, 1028), (4099, 260, 2052), (300, 1024, 4096), (3000, 1024, 1028), (5000, 512, 2052), (8300, 132, 1028), (16400, 1024, 260),
          (4100, 1024, 4100), (95597, 84, 92), (685, 1900, 860), (652, 6152, 364), (58412, 1152, 4), (370, 7080, 108), (26758, 36, 1272),
          (163, 7060, 1756), (5180, 1268, 956), (2932, 1208, 1664)]
