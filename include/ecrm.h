@@ -312,7 +312,9 @@ int ecrm_grads_clip(ecrm_grads *grads, const ecrm_grads *out, const float *norm,
  *
  * ecrm_dropout          out = residual + drop(x), formed in fp32, rounded once; residual = NULL: out = drop(x), and, of the gradient of
  *                       that, the gradient of x.  rows x cols elements of `type`; cols a multiple of 4, up to 2^24; up to 2^32
- *                       rows, at least cols apart (a multiple of 4), all of them within 2^48 elements.  out is x or residual (of the same stride), or overlaps neither, nor state.
+ *                       rows, at least cols apart (a multiple of 4), all of them within 2^48 elements.  out is x or residual (of the same
+ *                       stride), or overlaps neither, nor state; several rows at unlike strides overlap if the ranges from the first's begin to
+ *                       the last's end do.
  * ecrm_embed_dropout    ecrm_embed with out = drop(scale * entry), row i of the mask for out[i]; n <= 2^32.
  * ecrm_embed_grad_dropout, ecrm_embed_grad_dense_dropout
  *                       the gradients of that: what was dropped of a row of d_out counts for nothing, and sums are multiplied by c, too,
@@ -338,11 +340,16 @@ int ecrm_embed_grad_dense_dropout(ecrm_ctx *ctx, const uint64_t *keys, const voi
  *     e = drop(d),  b = e Wd,  dg = b * u * act'(g),  du = b * act(g),
  *     d_x = add + dg Wg + du Wu,  d_gate = dg^T x,  d_up = du^T x,  d_down = e^T h.
  * act: ECRM_SILU g / (1 + e^-g), ECRM_GELU g (1 + erf(g / sqrt 2)) / 2, ECRM_RELU max(g, 0) with the derivative 0 at 0.
- * Sums are formed in fp32, in an order that follows from the sizes alone; in 16-bit types h, dg and du are rounded to the type
- * between the products, and so are the saved g and u.  Needs no ecrm_ctx.
+ * Sums are formed in fp32; in 16-bit types h, dg and du are rounded to the type between the products, and so are the saved g and u.  The
+ * order of a sum follows from the sizes (n among them), the type, the number of the device's compute units, and, backward, from whether the
+ * weights' gradients and d_x are formed side by side: where both are wanted, unless d_x takes d_out's place without a mask.  So the same call
+ * gives the same bits, and weight gradients of a call that wants no d_x may differ from those of one that does by roundings of their sums.
+ * Needs no ecrm_ctx.
  *
  * ecrm_ffn_create    checks the configuration and makes a host-side handle (destroy it with ecrm_ffn_destroy; NULL is allowed).
- * ecrm_ffn_bytes     size of the workspace that ecrm_ffn_bind needs.
+ * ecrm_ffn_bytes     size of the workspace that ecrm_ffn_bind needs: about [max_rows][F] elements, training three of these and [max_rows][D],
+ *                    and up to 32 MiB for parts of sums.  A handle of the same type that is no larger in dim, hidden and max_rows, and trains
+ *                    only if this one does, needs no more.
  * ecrm_ffn_bind      hands over weights and workspace (256-byte aligned, else ESCRATCH) and learns the device: call it outside a
  *                    stream capture.  The workspace holds nothing from one call for the next: handles may share one.  Calls that use one
  *                    and overlap in time race; order them, and the streams they are on, as for a context.
@@ -355,8 +362,9 @@ int ecrm_embed_grad_dense_dropout(ecrm_ctx *ctx, const uint64_t *keys, const voi
  *
  * Rows: device memory aligned to four elements, strides multiples of 4, at least D (F for Wd), at most 2^20.  n <= max_rows, else
  * EBATCH.  out is x or residual (of the same stride) or overlaps neither; d_x is add or d_out (of the same stride) or overlaps no input;
- * what is written overlaps no other input, no weight, no state and nothing else that is written, and nothing lies in the workspace.  What of
- * this the pointers show is refused with EINVAL.  Calls only enqueue; calls on one handle come from one thread at a time. */
+ * what is written overlaps no other input, no weight, no state and nothing else that is written (rows at unlike strides: as for ecrm_dropout),
+ * and nothing lies in the workspace.  What of this the pointers show is refused with EINVAL.  Calls only enqueue; calls on one handle come
+ * from one thread at a time. */
 enum { ECRM_SILU = 0, ECRM_GELU = 1, ECRM_RELU = 2 };
 typedef struct {
     uint32_t dim, hidden; /* D, F: multiples of 4, 4 .. 65536 */

@@ -103,19 +103,31 @@ def test_the_workspace_has_room_for_the_same_plans(type, cus):
                     assert blocks * (2 if type != F32 else 1) * parts * 1024 <= room, (n, D, F)
 
 
-def test_small_blocks_have_small_workspaces():
-    """Parts of products take memory only where there can be any: bytes of the whole workspace, of blocks that need no more of it."""
+def workspace_size(**kw):
     if not os.path.exists(binding.library_path()):
         build.build()
-    lib = binding.load_library()
+    lib, ffn = binding.load_library(), C.c_void_p(0)
+    assert lib.ecrm_ffn_create(C.byref(binding.EcrmFfnConfig(**kw)), C.byref(ffn)) == 0
+    held = lib.ecrm_ffn_bytes(ffn)
+    lib.ecrm_ffn_destroy(ffn)
+    return held
 
-    def size(**kw):
-        ffn = C.c_void_p(0)
-        assert lib.ecrm_ffn_create(C.byref(binding.EcrmFfnConfig(**kw)), C.byref(ffn)) == 0
-        held = lib.ecrm_ffn_bytes(ffn)
-        lib.ecrm_ffn_destroy(ffn)
-        return held
 
+def test_a_larger_block_has_a_workspace_for_a_smaller_one():
+    rng = random.Random(7)
+    for n, D, F in sizes(2000, 11):
+        D, F = min(D, 65536), min(F, 65536)
+        t, training = rng.randint(0, 2), rng.randint(0, 1)
+        smaller = dict(dim=4 * rng.randint(1, D // 4), hidden=4 * rng.randint(1, F // 4), max_rows=rng.randint(1, n), training=rng.randint(0, training))
+        larger = dict(dim=D, hidden=F, max_rows=n, training=training)
+        for key in rng.sample(list(smaller), rng.randint(0, 3)):                   # as large in some
+            smaller[key] = larger[key]
+        assert workspace_size(type=t, activation=0, **smaller) <= workspace_size(type=t, activation=1, **larger), (t, smaller, larger)
+
+
+def test_small_blocks_have_small_workspaces():
+    """Parts of products take memory only where there can be any: bytes of the whole workspace, of blocks that need no more of it."""
+    size = workspace_size
     counters, h = 4 * fp.constants()["counters"], 1024
     assert size(dim=4, hidden=4, type=BF16, activation=0, max_rows=1, training=0) <= h + counters
     # a decoding step's rows: a long K of few rows in 16 parts at most, 2 KB for 16 columns
