@@ -3,7 +3,7 @@
 // (one), the gradients of the three weights and of x side by side (one).  g and u are saved, not computed again: two products in six.
 //
 // What bounds it.  Large batches: the matrix cores, 16 411 rows with D = 1024 and F = 4096 in bf16 forward 405 to 440 us (1020 to 940 TFLOP/s,
-// with 0.27 GB of g and u written on the way), backward 905 to 955 (910 to 860); the same products alone take the library 515 and 1215 us.  kBack is bound by
+// with 0.27 GB of g and u written on the way), backward 900 to 955 (920 to 860); the same products alone take the library 515 and 1215 us.  kBack is bound by
 // memory instead: two elements in and three out for each of h, 245 us, 105 of them multiplications.  D = 128, F = 512, 8192
 // rows: memory, 16 us forward, of which g, u and h take 6; 33 backward.  A few rows: the weights, 25 MB for five rows in 11 us.
 #include "ffn_block.h"
