@@ -340,7 +340,8 @@ class FeedForward:
     """A gated feed-forward block (ecrm_ffn_<name>) with the weights gate, up [hidden, dim] and down [dim, hidden], which are kept alive
     and have to stay where they are.  activation: "silu", "gelu" or "relu".  Its workspace, for calls of up to max_rows rows and, with
     training, the backward pass, may be another block's (workspace=other.workspace) if no two calls on them overlap in time; one of the same
-    type that is no smaller in dim, hidden and max_rows, and trains if this one does, has a workspace that is large enough.  The block may be dropped while calls are still to run, on whatever streams; a graph that uses it needs it kept."""
+    type that is no smaller in dim, hidden and max_rows, and trains if this one does, has a workspace that is large enough.  The block
+    may be dropped while calls are still to run, on whatever streams; a graph that uses it needs it kept."""
 
     ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
 
